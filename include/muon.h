@@ -263,6 +263,101 @@ typedef struct {
 int muon_adamw_step(const muon_adamw_param* params, int32_t n, const muon_adamw_hparams* hp, void* hip_stream);
 
 /*
+ * The losses of a language model's head, from its last hidden states H [tokens, width] and the head's weight W [vocab, width], with the
+ * gradients of both; the logits are never kept whole.  With z = H W^T:
+ *
+ *   muon_cross_entropy   loss_t = lse_t - z_t,y(t),  lse_t = log sum_v exp(z_tv)
+ *                        d z_tv = scale_t (p_tv - [v = y_t]),  p_tv = exp(z_tv - lse_t)
+ *   muon_distill         the teacher's entries (index_tj, s_tj), j < top: q_t = softmax_j(s_tj / tau); z' = z / tau
+ *                        loss_t = tau^2 sum_j q_tj (log q_tj - z'_t,index(j) + lse_t),  lse_t = log sum_v exp(z'_tv)
+ *                        d z_tv = scale_t tau (p'_tv - sum of q_tj over the j with index_tj = v),  p' = exp(z' - lse)
+ *   both                 d_hidden = dz W  [tokens, width],  d_weight = dz^T H  [vocab, width]
+ *
+ * scale_t is the gradient of the training loss with respect to loss_t (1/count for a mean), given before the call; loss is unscaled.
+ * A token without target (a negative target; every index negative, or every teacher's logit of the others -inf) has loss 0; so has a token
+ * with scale 0 no gradient: its hidden state, whatever it holds, does not reach d_weight, and its row of d_hidden is zero.  An entry with a
+ * negative index is no entry, whatever its logit.  An index that occurs twice counts twice.  An index of vocab or more makes the token's
+ * loss NaN and gives no gradient.
+ *
+ * Types: H, W and their gradients all bf16 or all fp32.  Products of bf16 accumulate in fp32; dz is rounded to bf16 once, the gradients
+ * once more (probabilities wait in f16, 2^-11 relative, those below 2^-29 of the largest in their block of the vocabulary 2^-40 of
+ * it); products of fp32 run on three bf16 planes per operand (about 2^-23).  Statistics, losses and the target's entries of dz are
+ * computed in fp32 and double.  Results do not depend on anything but the arguments: no atomics, fixed orders of summation.
+ *
+ * Tokens are processed in pieces, as many at a time as the workspace holds: per token of a piece vocab elements of 2 bytes (fp32: 10) where
+ * gradients are asked for.  Asynchronous on hip_stream; nothing is allocated.
+ */
+typedef struct {
+  const void* hidden;       /* device; [tokens, width], rows hidden_stride apart                        */
+  const void* weight;       /* device; [vocab, width], rows weight_stride apart                         */
+  int64_t hidden_stride;    /* elements, >= width                                                       */
+  int64_t weight_stride;
+  int64_t tokens;           /* 0 .. 2^30; 0: d_weight is set to zero                                    */
+  int64_t vocab;            /* 1 .. 2^30                                                                */
+  int64_t width;            /* 1 .. 2^20                                                                */
+  int32_t dtype;            /* MUON_F32 or MUON_BF16: hidden, weight, d_hidden, d_weight                */
+  int32_t reserved;         /* must be 0                                                                */
+} muon_head;
+
+enum { MUON_HEAD_D_HIDDEN = 1, MUON_HEAD_D_WEIGHT = 2 };
+
+/*
+ * Bytes of workspace (256-byte aligned device memory) for a call with this head.  top: entries per token (1 for muon_cross_entropy, up to
+ * 4096); gradients: which of MUON_HEAD_D_HIDDEN | MUON_HEAD_D_WEIGHT will be asked for.  max_bytes: the most that may be answered, in
+ * exchange for smaller pieces (the smallest workspace there is may be larger); 0: pieces of up to 8192 tokens.  The pointers in *head are
+ * read for their alignment only and may be null.  A call takes any workspace of at least the smallest size, and larger pieces in a
+ * larger one.
+ */
+int muon_head_workspace_bytes(const muon_head* head, int32_t top, int32_t gradients, size_t max_bytes, size_t* out);
+
+/*
+ * targets: [tokens] of targets_bytes (4 or 8) each.  token_scale: [tokens] or null (all 1).  loss: [tokens]; lse: [tokens] or null.
+ * d_hidden, d_weight: dense, overwritten, or null where not wanted.
+ */
+int muon_cross_entropy(const muon_head* head, const void* targets, int32_t targets_bytes, const float* token_scale, float* loss, float* lse,
+                       void* d_hidden, void* d_weight, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* index, teacher_logits: dense [tokens, top], of index_bytes (4 or 8) and teacher_dtype; temperature: tau > 0. */
+int muon_distill(const muon_head* head, const void* index, int32_t index_bytes, const void* teacher_logits, int32_t teacher_dtype, int32_t top,
+                 double temperature, const float* token_scale, float* loss, float* lse, void* d_hidden, void* d_weight, void* workspace,
+                 size_t workspace_bytes, void* hip_stream);
+
+/*
+ * A mixture's tokens to their experts and back.  muon_expert_sort ranks the tokens' pairs (token t, choice j) by expert, pairs of one expert
+ * in their own order:
+ *   position[t, j]  the pair's row in that order, -1 where its expert is not in [0, experts): such a pair is dropped
+ *   source[r]       the pair t * top + j of row r, -1 behind the last row
+ *   offsets[e]      first row of expert e; offsets[experts]: number of rows (device memory; the rows' buffers have tokens * top rows)
+ * The rows' kernels go by position and offsets[experts]; a position outside the rows counts as dropped:
+ *   dispatch           rows[position[t, j]] = x[t]; rows behind the last pair's are set to zero
+ *   combine            out[t] = sum_j weights[t, j] rows[position[t, j]] over the pairs that are not dropped; weights null: all 1, which
+ *                      is the gradient of dispatch
+ *   combine_backward   d_rows[position[t, j]] = weights[t, j] d_out[t], zero behind the last pair's;
+ *                      d_weights[t, j] = <d_out[t], rows[position[t, j]]>, 0 for a dropped pair
+ * Rows, x, out and their gradients are all bf16 or all fp32 (dtype) and dense but for x and d_out, whose rows lie a stride (elements) apart;
+ * weights and d_weights are dense fp32.  Sums are taken in fp32 in a fixed order and rounded once.  Everything is enqueued on hip_stream;
+ * nothing is allocated.  1 <= experts <= 4096, 1 <= top <= 64, tokens * top < 2^31 - 2^16; no tokens: nothing but offsets is written.
+ */
+typedef struct {
+  const int32_t* position;  /* device; [tokens, top]                                                   */
+  const int32_t* offsets;   /* device; [experts + 1]                                                   */
+  int64_t tokens;
+  int32_t top;              /* choices per token                                                        */
+  int32_t experts;
+} muon_routing;
+
+/* Bytes of workspace (4-byte aligned device memory) of a sort; 0 for few pairs. */
+int muon_expert_sort_bytes(int64_t tokens, int32_t top, int32_t experts, size_t* out);
+/* expert: dense [tokens, top] of expert_bytes (4 or 8) each. */
+int muon_expert_sort(const void* expert, int32_t expert_bytes, int64_t tokens, int32_t top, int32_t experts, int32_t* position, int32_t* source,
+                     int32_t* offsets, void* workspace, size_t workspace_bytes, void* hip_stream);
+int muon_expert_dispatch(const muon_routing* routing, const void* x, int64_t x_stride, int64_t width, int32_t dtype, void* rows, void* hip_stream);
+int muon_expert_combine(const muon_routing* routing, const void* rows, const float* weights, int64_t width, int32_t dtype, void* out,
+                        void* hip_stream);
+int muon_expert_combine_backward(const muon_routing* routing, const void* d_out, int64_t d_out_stride, const void* rows, const float* weights,
+                                 int64_t width, int32_t dtype, void* d_rows, float* d_weights, void* hip_stream);
+
+/*
  * Measurement aid (not part of the optimizer path; Section 2.1's Newton-Schulz products are what it prices):
  * runs the bf16 matrix-core instruction and register blocking of the Newton-Schulz GEMMs with operands that never
  * leave registers, one 256-thread block per compute unit, and reports the sustained rate.  That rate bounds every

@@ -29,6 +29,8 @@ EXPORTS = (
     "muon_plan_describe", "muon_plan_chunks", "muon_destroy", "muon_status_string", "muon_last_hip_error",
     "muon_profile_enable", "muon_profile_read", "muon_adamw_step", "muon_probe_mfma_rate",
     "muon_plan_only", "muon_plan_tiles", "muon_step_static",
+    "muon_head_workspace_bytes", "muon_cross_entropy", "muon_distill",
+    "muon_expert_sort_bytes", "muon_expert_sort", "muon_expert_dispatch", "muon_expert_combine", "muon_expert_combine_backward",
 )
 PROF_NAMES = ("momentum_norm_cast", "norm_finalize", "gram", "poly", "apply_poly", "weight_update", "update_rms")
 
@@ -55,6 +57,18 @@ class muon_adamw_param(C.Structure):
 class muon_adamw_hparams(C.Structure):
     _fields_ = [("lr", C.c_double), ("weight_decay", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
                 ("eps", C.c_double), ("step", C.c_int64)]
+
+
+class muon_head(C.Structure):
+    _fields_ = [("hidden", C.c_void_p), ("weight", C.c_void_p), ("hidden_stride", C.c_int64), ("weight_stride", C.c_int64),
+                ("tokens", C.c_int64), ("vocab", C.c_int64), ("width", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+MUON_HEAD_D_HIDDEN, MUON_HEAD_D_WEIGHT = 1, 2
+
+
+class muon_routing(C.Structure):
+    _fields_ = [("position", C.c_void_p), ("offsets", C.c_void_p), ("tokens", C.c_int64), ("top", C.c_int32), ("experts", C.c_int32)]
 
 
 class MuonError(RuntimeError):
@@ -122,6 +136,26 @@ def lib() -> C.CDLL:
     L.muon_plan_only.restype = C.c_int
     L.muon_plan_tiles.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, P(C.c_int32), C.c_int32]
     L.muon_plan_tiles.restype = C.c_int
+    L.muon_head_workspace_bytes.argtypes = [P(muon_head), C.c_int32, C.c_int32, C.c_size_t, P(C.c_size_t)]
+    L.muon_head_workspace_bytes.restype = C.c_int
+    L.muon_cross_entropy.argtypes = [P(muon_head), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_size_t, C.c_void_p]
+    L.muon_cross_entropy.restype = C.c_int
+    L.muon_distill.argtypes = [P(muon_head), C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_double, C.c_void_p, C.c_void_p,
+                               C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    L.muon_distill.restype = C.c_int
+    L.muon_expert_sort_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32, P(C.c_size_t)]
+    L.muon_expert_sort_bytes.restype = C.c_int
+    L.muon_expert_sort.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                   C.c_size_t, C.c_void_p]
+    L.muon_expert_sort.restype = C.c_int
+    L.muon_expert_dispatch.argtypes = [P(muon_routing), C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p]
+    L.muon_expert_dispatch.restype = C.c_int
+    L.muon_expert_combine.argtypes = [P(muon_routing), C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p]
+    L.muon_expert_combine.restype = C.c_int
+    L.muon_expert_combine_backward.argtypes = [P(muon_routing), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
+                                               C.c_void_p, C.c_void_p]
+    L.muon_expert_combine_backward.restype = C.c_int
     _LIB = L
     return L
 
@@ -317,6 +351,51 @@ def muon_adamw_step(tensors, *, lr: float, weight_decay: float, beta1: float = 0
         pack(arr, offset, p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), n, dtype_code(p.dtype), dtype_code(g.dtype))
         offset += size
     _check(lib().muon_adamw_step(arr, len(tensors), C.byref(hp), C.c_void_p(stream_ptr)), "muon_adamw_step")
+
+
+def muon_head_workspace_bytes(head: muon_head, top: int, gradients: int, max_bytes: int = 0) -> int:
+    out = C.c_size_t(0)
+    _check(lib().muon_head_workspace_bytes(C.byref(head), top, gradients, max_bytes, C.byref(out)), "muon_head_workspace_bytes")
+    return int(out.value)
+
+
+def muon_cross_entropy(head: muon_head, targets_ptr: int, targets_bytes: int, scale_ptr: int, loss_ptr: int, lse_ptr: int,
+                       d_hidden_ptr: int, d_weight_ptr: int, workspace_ptr: int, workspace_bytes: int, stream_ptr: int = 0) -> None:
+    _check(lib().muon_cross_entropy(C.byref(head), targets_ptr, targets_bytes, scale_ptr, loss_ptr, lse_ptr, d_hidden_ptr, d_weight_ptr,
+                                    workspace_ptr, workspace_bytes, stream_ptr), "muon_cross_entropy")
+
+
+def muon_distill(head: muon_head, index_ptr: int, index_bytes: int, logits_ptr: int, logits_dtype: int, top: int, temperature: float,
+                 scale_ptr: int, loss_ptr: int, lse_ptr: int, d_hidden_ptr: int, d_weight_ptr: int, workspace_ptr: int,
+                 workspace_bytes: int, stream_ptr: int = 0) -> None:
+    _check(lib().muon_distill(C.byref(head), index_ptr, index_bytes, logits_ptr, logits_dtype, top, temperature, scale_ptr, loss_ptr,
+                              lse_ptr, d_hidden_ptr, d_weight_ptr, workspace_ptr, workspace_bytes, stream_ptr), "muon_distill")
+
+
+def muon_expert_sort_bytes(tokens: int, top: int, experts: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().muon_expert_sort_bytes(tokens, top, experts, C.byref(out)), "muon_expert_sort_bytes")
+    return int(out.value)
+
+
+def muon_expert_sort(expert_ptr: int, expert_bytes: int, tokens: int, top: int, experts: int, position_ptr: int, source_ptr: int,
+                     offsets_ptr: int, workspace_ptr: int, workspace_bytes: int, stream_ptr: int = 0) -> None:
+    _check(lib().muon_expert_sort(expert_ptr, expert_bytes, tokens, top, experts, position_ptr, source_ptr, offsets_ptr, workspace_ptr,
+                                  workspace_bytes, stream_ptr), "muon_expert_sort")
+
+
+def muon_expert_dispatch(routing: muon_routing, x_ptr: int, x_stride: int, width: int, dtype: int, rows_ptr: int, stream_ptr: int = 0) -> None:
+    _check(lib().muon_expert_dispatch(C.byref(routing), x_ptr, x_stride, width, dtype, rows_ptr, stream_ptr), "muon_expert_dispatch")
+
+
+def muon_expert_combine(routing: muon_routing, rows_ptr: int, weights_ptr: int, width: int, dtype: int, out_ptr: int, stream_ptr: int = 0) -> None:
+    _check(lib().muon_expert_combine(C.byref(routing), rows_ptr, weights_ptr, width, dtype, out_ptr, stream_ptr), "muon_expert_combine")
+
+
+def muon_expert_combine_backward(routing: muon_routing, d_out_ptr: int, d_out_stride: int, rows_ptr: int, weights_ptr: int, width: int,
+                                 dtype: int, d_rows_ptr: int, d_weights_ptr: int, stream_ptr: int = 0) -> None:
+    _check(lib().muon_expert_combine_backward(C.byref(routing), d_out_ptr, d_out_stride, rows_ptr, weights_ptr, width, dtype, d_rows_ptr,
+                                              d_weights_ptr, stream_ptr), "muon_expert_combine_backward")
 
 
 def muon_destroy(ctx) -> None:

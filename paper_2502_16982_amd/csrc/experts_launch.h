@@ -1,0 +1,34 @@
+// Host-callable launchers of the experts' sort, dispatch and combine (internal to the library).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace muon {
+
+constexpr int kMaxExperts = 4096, kMaxExpertTop = 64;
+constexpr int64_t kMaxExpertPairs = (1ll << 31) - (1 << 16);      // positions are 32-bit, and so is the last block's end
+// Pairs per block of the sort: one block for all of few, never more than kSortBlocks of them.
+constexpr int kSortChunk = 2048, kSortBlocks = 256;
+inline int64_t sort_chunk(int64_t pairs) {
+  const int64_t even = (pairs + kSortBlocks - 1) / kSortBlocks;
+  return even <= kSortChunk ? kSortChunk : (even + 255) / 256 * 256;
+}
+inline int sort_blocks(int64_t pairs) { return pairs <= kSortChunk ? 1 : (int)((pairs + sort_chunk(pairs) - 1) / sort_chunk(pairs)); }
+
+hipError_t launch_expert_sort(const void* expert, int index64, int64_t pairs, int experts, int* position, int* source, int* offsets,
+                              int* counts, hipStream_t s);
+// The tokens' way to their rows and back.  `count`: device address of the number of rows that belong to a pair.
+struct ExpertRows {
+  const int* position;      // [tokens, top]
+  const int* count;
+  long long tokens, width;
+  int top;
+  int f32;
+};
+hipError_t launch_expert_dispatch(const ExpertRows& r, const void* x, long long x_stride, void* rows, hipStream_t s);
+hipError_t launch_expert_combine(const ExpertRows& r, const void* rows, const float* weights, void* out, hipStream_t s);
+hipError_t launch_expert_combine_backward(const ExpertRows& r, const void* d_out, long long d_out_stride, const void* rows,
+                                          const float* weights, void* d_rows, float* d_weights, hipStream_t s);
+
+}  // namespace muon

@@ -1,0 +1,90 @@
+#include "head_plan.h"
+
+#include <algorithm>
+
+namespace muon {
+namespace {
+
+constexpr int64_t up(int64_t v, int64_t grain) { return (v + grain - 1) / grain * grain; }
+
+void plan_piece(const HeadShape& s, int64_t piece, HeadPlan* p) {
+  p->piece = piece;
+  p->pieces = std::max<int64_t>(1, (s.tokens + piece - 1) / piece);
+  const bool gradients = s.d_hidden || s.d_weight;
+  const int64_t sizes[2] = {piece, s.tokens - (p->pieces - 1) * piece};
+  int64_t blocks = 0, partial = 0;
+  for (int i = 0; i < 2; ++i) {
+    p->logits[i] = head_product(s.vocab, sizes[i], p->width_k, p->pairs, false);
+    p->hidden[i] = head_product(s.width, sizes[i], s.vocab, p->pairs, true);
+    p->weight[i] = head_product(s.width, s.vocab, sizes[i], p->pairs, true);
+    blocks = std::max(blocks, head_blocks(p->logits[i]));
+    if (s.d_hidden && p->hidden[i].splits > 1) partial = std::max(partial, p->hidden[i].splits * sizes[i] * s.width * 4);
+    if (s.d_weight && p->weight[i].splits > 1) partial = std::max(partial, p->weight[i].splits * s.vocab * s.width * 4);
+  }
+  size_t at = 0;
+  auto take = [&](bool wanted, int64_t bytes) {
+    const size_t here = at;
+    if (wanted) at += (size_t)up(bytes, 256);
+    return here;
+  };
+  const int64_t row = p->planes * p->width_k * 2;
+  p->packed_weight = take(p->pack_weight, s.vocab * row);
+  p->sum = take(s.d_weight && p->pieces > 1, s.vocab * s.width * 4);
+  p->packed_hidden = take(p->pack_hidden, piece * row);
+  p->masked_hidden = take(s.d_weight, piece * row);
+  p->stats = take(true, blocks * piece * 8);
+  p->entry = take(true, piece * s.top * 4);
+  p->value = take(gradients, piece * s.top * 4);
+  p->scale = take(true, piece * 4);
+  p->lse = take(true, piece * 4);
+  p->prob = take(gradients, piece * p->vocab_pitch * (s.f32 ? 4 : 2));
+  p->grad = s.f32 ? take(gradients, 3 * piece * p->vocab_pitch * 2) : p->prob;      // bf16: in place of the probabilities
+  p->partial = take(partial > 0, partial);
+  p->total = std::max<size_t>(at, 256);
+}
+
+}  // namespace
+
+HeadProduct head_product(int64_t m, int64_t n, int64_t k, int pairs, bool may_split) {
+  constexpr int64_t kUnits = 256;
+  HeadProduct p{};
+  p.m = m;
+  p.n = n;
+  p.k = k;
+  p.tile = 128;
+  p.tiles_m = (int)((m + p.tile - 1) / p.tile);
+  p.tiles_n = (int)((n + p.tile - 1) / p.tile);
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, slabs = std::max<int64_t>(1, (k + kHeadSlab - 1) / kHeadSlab * pairs);
+  int64_t splits = 1;
+  // A split's partial result is written and read back in fp32: only where the tiles leave compute units idle, and with at least
+  // eight slabs each.
+  if (may_split && tiles < kUnits) splits = std::max<int64_t>(1, std::min(2 * kUnits / std::max<int64_t>(1, tiles), slabs / 8));
+  p.slabs_per_split = (int)((slabs + splits - 1) / splits);
+  p.splits = (int)((slabs + p.slabs_per_split - 1) / p.slabs_per_split);
+  return p;
+}
+
+bool head_plan(const HeadShape& s, size_t max_bytes, HeadPlan* p) {
+  *p = HeadPlan{};
+  p->planes = s.f32 ? 3 : 1;
+  p->pairs = s.f32 ? 6 : 1;
+  p->width_k = up(s.width, 8);
+  p->vocab_pitch = up(s.vocab, 256);
+  // fp32 operands are split into planes; bf16 rows that do not come in whole aligned chunks of 16 bytes are copied
+  const bool ragged = s.f32 || s.width % 8 != 0;
+  p->pack_hidden = ragged || s.hidden_stride % 8 != 0 || s.hidden_stride > kHeadMaxPitch || !s.hidden_aligned;
+  p->pack_weight = ragged || s.weight_stride % 8 != 0 || s.weight_stride > kHeadMaxPitch || !s.weight_aligned;
+  // Equal pieces of whole tiles, ever more of them until the workspace fits: what a query answers is one of these, so that a call
+  // that is given as many bytes finds it (or an earlier one).
+  const int64_t all = std::max<int64_t>(1, s.tokens);
+  for (int64_t pieces = max_bytes == 0 ? (all + kHeadPieceTokens - 1) / kHeadPieceTokens : 1;;) {
+    const int64_t piece = std::min(all, up((all + pieces - 1) / pieces, 256));
+    plan_piece(s, piece, p);
+    if (max_bytes == 0 || p->total <= max_bytes) return true;
+    const int64_t smaller = (piece - 1) / 256 * 256;
+    if (smaller == 0) return false;
+    pieces = (all + smaller - 1) / smaller;
+  }
+}
+
+}  // namespace muon

@@ -1,0 +1,59 @@
+// How a call of the head's losses is cut up: tokens in pieces, the workspace's sections, tiles and splits of the three products
+// (plain C++, no HIP include).
+#pragma once
+#include <cstddef>
+#include <cstdint>
+
+namespace muon {
+
+constexpr int64_t kHeadMaxTokens = 1ll << 30, kHeadMaxVocab = 1ll << 30, kHeadMaxWidth = 1ll << 20;
+constexpr int kHeadMaxTop = 4096;
+// Rows further apart than this are copied first: a tile's offsets stay below 2^32 bytes.
+constexpr int64_t kHeadMaxPitch = 1ll << 22;
+// Tokens of a piece where the caller sets no limit to the workspace.
+constexpr int64_t kHeadPieceTokens = 8192;
+
+struct HeadShape {
+  int64_t tokens, vocab, width;
+  int64_t hidden_stride, weight_stride;     // elements
+  bool f32;
+  bool hidden_aligned, weight_aligned;      // to 16 bytes
+  int top;                                  // sparse entries of a token's target
+  bool d_hidden, d_weight;
+};
+
+// One of the three products as it is launched: T = L R^T in tiles of tile x tile, the slabs of K in `splits` equal runs.
+struct HeadProduct {
+  int64_t m, n, k;          // rows of L, rows of R
+  int tile;
+  int tiles_m, tiles_n;
+  int splits;
+  int slabs_per_split;      // of kHeadSlab elements of K, over all pairs of planes
+};
+
+constexpr int kHeadSlab = 64;
+
+// Vocabulary entries that one pair (maximum, sum) of the logits' product stands for, and such pairs per token.
+inline int head_grain(const HeadProduct& logits) { return logits.tile / 2; }
+inline int64_t head_blocks(const HeadProduct& logits) { return 2ll * logits.tiles_m; }
+
+struct HeadPlan {
+  int planes;               // bf16 planes that an operand is the sum of: 1, or 3 for fp32
+  int pairs;                // pairs of planes that are multiplied: 1 or 6
+  int64_t width_k;          // columns of packed operands; K of the logits' product
+  int64_t vocab_pitch;      // row pitch of the probabilities and of the logits' gradient
+  int64_t piece, pieces;    // tokens per piece
+  bool pack_hidden, pack_weight;
+  HeadProduct logits[2], hidden[2], weight[2];      // of a whole piece; of the last one
+  // byte offsets of the workspace's sections
+  size_t packed_weight, packed_hidden, masked_hidden, stats, entry, value, scale, lse, prob, grad, partial, sum;
+  size_t total;
+};
+
+// The product of an m x k by a k x n operand for a device of 256 compute units.
+HeadProduct head_product(int64_t m, int64_t n, int64_t k, int pairs, bool may_split);
+// The plan with the largest pieces whose workspace is at most max_bytes (0: pieces of kHeadPieceTokens), or, where none is, the one with
+// the smallest; for a call, which gives the bytes that there are, false where they do not suffice.
+bool head_plan(const HeadShape& shape, size_t max_bytes, HeadPlan* out);
+
+}  // namespace muon

@@ -1,0 +1,467 @@
+// Softmax losses of a language model's head from hidden states H [T, D] and the head's weight W [V, D], logits never kept whole.
+//
+//   z = H W^T / tau     lse_t = log sum_v exp z_tv     dz_tv = g_t tau (p_tv - q_tv),  p = exp(z - lse)     dH = dz W     dW = dz^T H
+//
+// q is the target: one entry of 1 (cross entropy) or the softmax of a teacher's few best logits.  The logits' product runs over tiles of
+// vocabulary x tokens whose epilogue leaves, per block of the vocabulary and token, the maximum and the sum of exp(z - maximum), and, for
+// the gradient, exp(z - maximum) in f16.  Joining the blocks gives lse and loss; one pass scales the probabilities to dz in bf16, in
+// place, and writes the target's few entries from logits computed in fp32 (p - q there cancels); two more products give the gradients.
+#include <hip/hip_runtime.h>
+
+#include "head_gemm.h"
+
+namespace muon {
+namespace {
+
+using namespace head;
+
+// ---- loads of rows of any alignment ----
+struct Row8 {
+  float v[8];
+};
+// Elements [c, c + 8) of a row of `width` elements, zero behind its end.  vec: the row starts at a multiple of 16 bytes.
+template <bool F32>
+__device__ __forceinline__ Row8 load_row8(const void* base, long long row_at, long long c, long long width, bool vec) {
+  Row8 r;
+  if constexpr (F32) {
+    const float* p = static_cast<const float*>(base) + row_at + c;
+    if (vec && c + 8 <= width) {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.v[e] = a[e], r.v[4 + e] = b[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r.v[e] = c + e < width ? p[e] : 0.f;
+    }
+  } else {
+    const u16* p = static_cast<const u16*>(base) + row_at + c;
+    if (vec && c + 8 <= width) {
+      const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) r.v[2 * e] = bf16_lo(a[e]), r.v[2 * e + 1] = bf16_hi(a[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r.v[e] = c + e < width ? bf16_value(p[e]) : 0.f;
+    }
+  }
+  return r;
+}
+template <bool F32>
+__device__ __forceinline__ bool row_is_aligned(const void* base, long long row_at) {
+  return ((reinterpret_cast<uintptr_t>(base) + (F32 ? 4 : 2) * row_at) & 15) == 0;
+}
+// Eight fp32 values as operand planes: each plane what the ones before it left, rounded to bf16.
+template <bool F32>
+__device__ __forceinline__ void store_planes8(const Row8& r, u16* dst, long long plane) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = r.v[e];
+#pragma unroll
+  for (int q = 0; q < (F32 ? 3 : 1); ++q) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+      v[2 * e] -= bf16_lo(w[e]);
+      v[2 * e + 1] -= bf16_hi(w[e]);
+    }
+    *reinterpret_cast<u32x4*>(dst + q * plane) = w;
+  }
+}
+
+template <bool F32>
+__global__ __launch_bounds__(256) void head_pack_kernel(const void* __restrict__ src, long long stride, long long n, long long width,
+                                                        u16* __restrict__ dst, long long ld, long long plane) {
+  const long long chunks = ld / 8;
+  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n * chunks; i += gridDim.x * 256ll) {
+    const long long row = i / chunks, c = (i - row * chunks) * 8;
+    store_planes8<F32>(load_row8<F32>(src, row * stride, c, width, row_is_aligned<F32>(src, row * stride)), dst + row * ld + c, plane);
+  }
+}
+
+// ---- targets ----
+__device__ __forceinline__ long long index_at(const HeadTarget& t, long long i) {
+  return t.index64 ? static_cast<const long long*>(t.index)[i] : (long long)static_cast<const int*>(t.index)[i];
+}
+__device__ __forceinline__ float teacher_at(const HeadTarget& t, long long i) {
+  return t.inv_tau * (t.logits_bf16 ? bf16_value(static_cast<const u16*>(t.logits)[i]) : static_cast<const float*>(t.logits)[i]);
+}
+// Entry i is one: an index of the vocabulary whose teacher's logit is not -inf.
+__device__ __forceinline__ bool entry_there(const HeadTarget& t, long long i, long long vocab) {
+  const long long v = index_at(t, i);
+  return v >= 0 && v < vocab && !(t.logits && teacher_at(t, i) == -INFINITY);
+}
+struct TokenState {
+  bool some, beyond;        // has entries; has an index beyond the vocabulary
+};
+// By a whole wave.
+__device__ __forceinline__ TokenState token_state(const HeadTarget& t, long long token, long long vocab) {
+  bool some = false, beyond = false;
+  for (int j = threadIdx.x & 63; j < t.top; j += 64) {
+    some |= entry_there(t, token * t.top + j, vocab);
+    beyond |= index_at(t, token * t.top + j) >= vocab;
+  }
+  return {__any(some) != 0, __any(beyond) != 0};
+}
+__device__ __forceinline__ float token_scale(const HeadTarget& t, long long token, TokenState state) {
+  const float g = t.token_scale ? t.token_scale[token] : 1.f;
+  return state.some && !state.beyond ? g : 0.f;
+}
+
+// One block per token.  Each wave takes every fourth entry: a dot product of two rows in fp32.
+template <bool F32>
+__global__ __launch_bounds__(256) void head_entries_kernel(HeadTarget t, const void* __restrict__ hidden, long long hidden_stride,
+                                                           const void* __restrict__ weight, long long weight_stride, long long vocab,
+                                                           long long width, float* __restrict__ entry, u16* __restrict__ masked, long long ld,
+                                                           long long plane) {
+  const long long token = blockIdx.x, at = token * hidden_stride;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const bool hvec = row_is_aligned<F32>(hidden, at);
+  for (int j = wave; j < t.top; j += 4) {
+    const long long v = index_at(t, token * t.top + j);
+    float sum = 0.f;
+    if (v >= 0 && v < vocab) {
+      const bool wvec = row_is_aligned<F32>(weight, v * weight_stride);
+      for (long long c = lane * 8; c < width; c += 512) {
+        const Row8 a = load_row8<F32>(hidden, at, c, width, hvec), b = load_row8<F32>(weight, v * weight_stride, c, width, wvec);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum = fmaf(a.v[e], b.v[e], sum);
+      }
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    }
+    if (lane == 0) entry[token * t.top + j] = t.inv_tau * sum;
+  }
+  if (masked) {
+    const bool kept = token_scale(t, token, token_state(t, token, vocab)) != 0.f;
+    for (long long c = threadIdx.x * 8; c < ld; c += 2048) {
+      Row8 r{};
+      if (kept) r = load_row8<F32>(hidden, at, c, width, hvec);
+      store_planes8<F32>(r, masked + token * ld + c, plane);
+    }
+  }
+}
+
+// ---- logits ----
+template <bool PROB, bool F32>
+__global__ __launch_bounds__(256) void head_logits_kernel(HeadOperand weight, HeadOperand hidden, HeadTiles g, float inv_tau,
+                                                          float2* __restrict__ stats, long long stats_pitch, void* __restrict__ prob,
+                                                          long long prob_pitch) {
+  __shared__ __align__(16) u16 lds[Tile128::kLds / 2];
+  const long long row0 = (long long)(blockIdx.x % g.tiles_m) * 128, col0 = (long long)(blockIdx.x / g.tiles_m) * 128;
+  Tile128 tile;
+  tile.run<false, false>(weight, hidden, row0, col0, g.k, 0, g.slabs_per_split, lds);
+  const int fr = tile.lane & 31, fh = tile.lane >> 5;
+  const long long v0 = row0 + tile.wm * 64;
+  const bool whole = v0 + 64 <= weight.rows;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const long long token = col0 + tile.wn * 64 + 32 * j + fr;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        float z = inv_tau * tile.acc[i][j][v];
+        if (!whole && v0 + 32 * i + 8 * (v / 4) + 4 * fh + v % 4 >= weight.rows) z = -INFINITY;
+        tile.acc[i][j][v] = z;
+        top = fmaxf(top, z);
+      }
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    const float shift = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e] = __builtin_amdgcn_exp2f((tile.acc[i][j][4 * q + e] - shift) * kLog2e);
+          sum += x[e];
+        }
+        if (PROB && token < hidden.rows) {
+          const long long at = token * prob_pitch + v0 + 32 * i + 8 * q + 4 * fh;
+          if constexpr (F32) {
+            f32x4 z;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = tile.acc[i][j][4 * q + e];
+            *reinterpret_cast<f32x4*>(static_cast<float*>(prob) + at) = z;
+          } else {
+            const u32x2 p = {pack_f16(kProbScale * x[0], kProbScale * x[1]), pack_f16(kProbScale * x[2], kProbScale * x[3])};
+            *reinterpret_cast<u32x2*>(static_cast<u16*>(prob) + at) = p;
+          }
+        }
+      }
+    sum += __shfl_xor(sum, 32, 64);
+    if (fh == 0 && token < hidden.rows) stats[v0 / 64 * stats_pitch + token] = make_float2(top, sum);
+  }
+}
+
+// ---- join ----
+// Sixteen tokens per block; their blocks of the vocabulary over sixteen threads each, then their entries over a wave each.
+__global__ __launch_bounds__(256) void head_join_kernel(HeadTarget t, const float2* __restrict__ stats, long long stats_pitch,
+                                                        long long blocks, const float* __restrict__ entry, long long tokens,
+                                                        long long vocab, float* __restrict__ loss, float* __restrict__ lse,
+                                                        float* __restrict__ value, float* __restrict__ scale) {
+  __shared__ float tops[16][17];
+  __shared__ double sums[16][17];
+  __shared__ double joined[16];
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+  const long long token = blockIdx.x * 16ll + x, read = token < tokens ? token : tokens - 1;
+  float top = -INFINITY;
+  for (long long b = y; b < blocks; b += 16) top = fmaxf(top, stats[b * stats_pitch + read].x);
+  tops[y][x] = top;
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 16; ++u) top = fmaxf(top, tops[u][x]);
+  const float shift = top == -INFINITY ? 0.f : top;
+  double sum = 0.0;
+  for (long long b = y; b < blocks; b += 16) {
+    const float2 v = stats[b * stats_pitch + read];
+    if (v.y != 0.f) sum += (double)(v.y * __builtin_amdgcn_exp2f((v.x - shift) * kLog2e));
+  }
+  sums[y][x] = sum;
+  __syncthreads();
+  if (y == 0) {
+    sum = 0.0;
+#pragma unroll
+    for (int u = 0; u < 16; ++u) sum += sums[u][x];
+    joined[x] = (double)shift + log(sum);
+    if (token < tokens) lse[token] = (float)joined[x];
+  }
+  __syncthreads();
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  for (int u = wave; u < 16; u += 4) {
+    const long long tk = blockIdx.x * 16ll + u;
+    if (tk >= tokens) break;
+    const TokenState state = token_state(t, tk, vocab);
+    const float g = token_scale(t, tk, state);
+    const double l = joined[u];
+    double sum_loss = 0.0;
+    if (!t.logits) {
+      if (lane == 0) {
+        const double z = (double)entry[tk];
+        sum_loss = state.some ? l - z : 0.0;
+        if (value) value[tk] = g == 0.f ? 0.f : (float)((double)g * expm1(z - l));
+      }
+    } else if (state.some) {
+      float best = -INFINITY;
+      for (int j = lane; j < t.top; j += 64)
+        if (entry_there(t, tk * t.top + j, vocab)) best = fmaxf(best, teacher_at(t, tk * t.top + j));
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) best = fmaxf(best, __shfl_xor(best, off, 64));
+      double mass = 0.0;
+      for (int j = lane; j < t.top; j += 64)
+        if (entry_there(t, tk * t.top + j, vocab)) mass += exp((double)teacher_at(t, tk * t.top + j) - (double)best);
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) mass += __shfl_xor(mass, off, 64);
+      const double norm = (double)best + log(mass);
+      for (int j0 = 0; j0 < t.top; j0 += 64) {
+        const int j = j0 + lane;
+        const bool there = j < t.top && entry_there(t, tk * t.top + j, vocab);
+        const long long v = there ? index_at(t, tk * t.top + j) : -1;
+        const double z = there ? (double)entry[tk * t.top + j] : 0.0;
+        const double logq = there ? (double)teacher_at(t, tk * t.top + j) - norm : 0.0;
+        if (there) sum_loss += exp(logq) * (logq - z + l);
+        if (value) {
+          double q = 0.0;                        // of every entry with this index
+          for (int k0 = 0; k0 < t.top; k0 += 64) {
+            const int k = k0 + lane;
+            const bool kt = k < t.top && entry_there(t, tk * t.top + k, vocab);
+            const long long vk = kt ? index_at(t, tk * t.top + k) : -2;
+            const double qk = kt ? exp((double)teacher_at(t, tk * t.top + k) - norm) : 0.0;
+            const int n = t.top - k0 < 64 ? t.top - k0 : 64;
+            for (int w = 0; w < n; ++w) {
+              const long long vw = __shfl(vk, w, 64);
+              const double qw = __shfl(qk, w, 64);
+              if (vw == v) q += qw;
+            }
+          }
+          if (j < t.top) value[tk * t.top + j] = there && g != 0.f ? (float)((double)g * (double)t.tau * (exp(z - l) - q)) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) sum_loss += __shfl_xor(sum_loss, off, 64);
+    } else if (value) {
+      for (int j = lane; j < t.top; j += 64) value[tk * t.top + j] = 0.f;
+    }
+    if (lane == 0) {
+      loss[tk] = state.beyond ? __builtin_nanf("") : (float)((double)t.tau * (double)t.tau * sum_loss);
+      if (scale) scale[tk] = t.tau * g;
+    }
+  }
+}
+
+// ---- dz ----
+constexpr int kGradSpan = 4096;                  // vocabulary entries per block
+template <bool F32>
+__global__ __launch_bounds__(256) void head_grad_kernel(HeadTarget t, const float2* __restrict__ stats, long long stats_pitch, int grain_bits,
+                                                        const float* __restrict__ lse, const float* __restrict__ value,
+                                                        const float* __restrict__ scale, long long vocab, int spans,
+                                                        const void* prob, long long pitch, u16* grad, long long plane) {
+  const long long token = blockIdx.x / spans, v0 = (long long)(blockIdx.x % spans) * kGradSpan;
+  const float g = scale[token], l = lse[token];
+  const long long row = token * pitch;
+  for (long long v = v0 + threadIdx.x * 8; v < v0 + kGradSpan && v < pitch; v += 2048) {
+    Row8 r{};
+    if (g != 0.f && v < vocab) {
+      if constexpr (F32) {
+        const float* z = static_cast<const float*>(prob) + row + v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.v[e] = v + e < vocab ? g * __builtin_amdgcn_exp2f((z[e] - l) * kLog2e) : 0.f;
+      } else {
+        const u32x4 p = *reinterpret_cast<const u32x4*>(static_cast<const u16*>(prob) + row + v);
+        const float top = stats[(v >> grain_bits) * stats_pitch + token].x;
+        const float f = g * (__builtin_amdgcn_exp2f((top - l) * kLog2e) * (1.f / kProbScale));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const unsigned pair = p[e / 2];        // (a bit cast of the vector's element itself would take its first)
+          const f16x2 two = __builtin_bit_cast(f16x2, pair);
+          r.v[e] = v + e < vocab ? f * (float)two[e & 1] : 0.f;
+        }
+      }
+    }
+    store_planes8<F32>(r, grad + row + v, plane);
+  }
+  if (g == 0.f) return;
+  __syncthreads();                               // the entries go over what this block wrote
+  for (int j = threadIdx.x; j < t.top; j += 256) {
+    const long long i = token * t.top + j;
+    const long long v = index_at(t, i);
+    if (v < v0 || v >= v0 + kGradSpan || !entry_there(t, i, vocab)) continue;
+    float x = value[i];
+#pragma unroll
+    for (int q = 0; q < (F32 ? 3 : 1); ++q) {
+      const u16 b = bf16_bits(x);
+      grad[q * plane + row + v] = b;
+      x -= bf16_value(b);
+    }
+  }
+}
+
+// ---- gradients ----
+__device__ __forceinline__ void store_out(const HeadOut& o, long long at, float x) {
+  if (o.f32) static_cast<float*>(o.out)[at] = x;
+  else static_cast<u16*>(o.out)[at] = bf16_bits(x);
+}
+__device__ __forceinline__ void finish_out(const HeadOut& o, long long at, float x) {
+  if (o.add) x += o.sum[at];
+  if (o.keep) o.sum[at] = x;
+  else store_out(o, at, x);
+}
+
+template <bool RKM>
+__global__ __launch_bounds__(256) void head_product_kernel(HeadOperand l, HeadOperand r, HeadTiles g, HeadOut out) {
+  __shared__ __align__(16) u16 lds[Tile128::kLds / 2];
+  const int split = blockIdx.x % g.splits, at = blockIdx.x / g.splits;
+  const long long row0 = (long long)(at % g.tiles_m) * 128, col0 = (long long)(at / g.tiles_m) * 128;
+  const int slabs = (int)((g.k + kHeadSlab - 1) / kHeadSlab) * g.pairs;
+  const int first = split * g.slabs_per_split, last = first + g.slabs_per_split < slabs ? first + g.slabs_per_split : slabs;
+  Tile128 tile;
+  tile.run<true, RKM>(l, r, row0, col0, g.k, first, last, lds);
+  const int fr = tile.lane & 31, fh = tile.lane >> 5;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const long long n = col0 + tile.wn * 64 + 32 * j + fr;
+    if (n >= r.rows) continue;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const long long m = row0 + tile.wm * 64 + 32 * i + 8 * (v / 4) + 4 * fh + v % 4;
+        if (m >= l.rows) continue;
+        if (g.splits > 1) out.partial[((long long)split * r.rows + n) * l.rows + m] = tile.acc[i][j][v];
+        else finish_out(out, n * l.rows + m, tile.acc[i][j][v]);
+      }
+  }
+}
+
+__global__ __launch_bounds__(256) void head_sum_splits_kernel(HeadOut out, int splits, long long count) {
+  const long long at = blockIdx.x * 256ll + threadIdx.x;
+  if (at >= count) return;
+  float x = 0.f;
+  for (int u = 0; u < splits; ++u) x += out.partial[u * count + at];
+  finish_out(out, at, x);
+}
+
+__global__ __launch_bounds__(256) void fill_zero_kernel(u16* p, size_t n) {
+  for (size_t i = blockIdx.x * 256ull + threadIdx.x; i < n; i += gridDim.x * 256ull) p[i] = 0;
+}
+
+HeadTiles tiles_of(const HeadProduct& g, int pairs) {
+  return {g.k, pairs, g.tiles_m, g.tiles_n, g.splits, g.slabs_per_split};
+}
+unsigned blocks_for(long long threads) {
+  const long long b = (threads + 255) / 256;
+  return (unsigned)(b < (1ll << 20) ? b : (1ll << 20));
+}
+
+}  // namespace
+
+hipError_t launch_head_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float inv_tau,
+                              float2* stats, long long stats_pitch, void* prob, long long prob_pitch, int prob_f32, hipStream_t s) {
+  const dim3 grid((unsigned)((long long)g.tiles_m * g.tiles_n));
+  auto go = [&](auto kernel) {
+    kernel<<<grid, 256, 0, s>>>(weight, hidden, tiles_of(g, pairs), inv_tau, stats, stats_pitch, prob, prob_pitch);
+    return hipGetLastError();
+  };
+  if (!prob) return go(head_logits_kernel<false, false>);
+  return prob_f32 ? go(head_logits_kernel<true, true>) : go(head_logits_kernel<true, false>);
+}
+
+hipError_t launch_head_product(const HeadOperand& l, const HeadOperand& r, int r_kmajor, const HeadProduct& g, int pairs,
+                               const HeadOut& out, hipStream_t s) {
+  const dim3 grid((unsigned)((long long)g.tiles_m * g.tiles_n * g.splits));
+  if (r_kmajor) head_product_kernel<true><<<grid, 256, 0, s>>>(l, r, tiles_of(g, pairs), out);
+  else head_product_kernel<false><<<grid, 256, 0, s>>>(l, r, tiles_of(g, pairs), out);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_pack(const void* src, long long stride, int f32, long long n, long long width, u16* dst, long long ld,
+                            long long plane, hipStream_t s) {
+  const unsigned blocks = blocks_for(n * (ld / 8));
+  if (f32) head_pack_kernel<true><<<blocks, 256, 0, s>>>(src, stride, n, width, dst, ld, plane);
+  else head_pack_kernel<false><<<blocks, 256, 0, s>>>(src, stride, n, width, dst, ld, plane);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_entries(const HeadTarget& t, const void* hidden, long long hidden_stride, const void* weight,
+                               long long weight_stride, int f32, long long tokens, long long vocab, long long width, float* entry,
+                               u16* masked, long long ld, long long plane, hipStream_t s) {
+  auto go = [&](auto kernel) {
+    kernel<<<(unsigned)tokens, 256, 0, s>>>(t, hidden, hidden_stride, weight, weight_stride, vocab, width, entry, masked, ld, plane);
+    return hipGetLastError();
+  };
+  return f32 ? go(head_entries_kernel<true>) : go(head_entries_kernel<false>);
+}
+
+hipError_t launch_head_join(const HeadTarget& t, const float2* stats, long long stats_pitch, long long blocks, const float* entry,
+                            long long tokens, long long vocab, float* loss, float* lse, float* value, float* scale, hipStream_t s) {
+  head_join_kernel<<<(unsigned)((tokens + 15) / 16), 256, 0, s>>>(t, stats, stats_pitch, blocks, entry, tokens, vocab, loss, lse, value,
+                                                                 scale);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_grad(const HeadTarget& t, const float2* stats, long long stats_pitch, int grain, const float* lse,
+                            const float* value, const float* scale, long long tokens, long long vocab, const void* prob, long long pitch,
+                            int f32, u16* grad, long long plane, hipStream_t s) {
+  const int spans = (int)((pitch + kGradSpan - 1) / kGradSpan);
+  auto go = [&](auto kernel) {
+    kernel<<<(unsigned)(tokens * spans), 256, 0, s>>>(t, stats, stats_pitch, __builtin_ctz(grain), lse, value, scale, vocab, spans, prob, pitch, grad, plane);
+    return hipGetLastError();
+  };
+  return f32 ? go(head_grad_kernel<true>) : go(head_grad_kernel<false>);
+}
+
+hipError_t launch_head_sum_splits(const HeadOut& out, int splits, long long count, hipStream_t s) {
+  head_sum_splits_kernel<<<(unsigned)((count + 255) / 256), 256, 0, s>>>(out, splits, count);
+  return hipGetLastError();
+}
+
+hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t s) {
+  fill_zero_kernel<<<blocks_for((long long)(bytes / 2)), 256, 0, s>>>(static_cast<u16*>(p), bytes / 2);
+  return hipGetLastError();
+}
+
+}  // namespace muon

@@ -9,10 +9,10 @@
 #include <cmath>
 #include <cstdlib>
 #include <cstring>
-#include <new>
 #include <vector>
 
 #include "../../include/muon.h"
+#include "api_guard.h"
 #include "muon_launch.h"
 #include "muon_plan.h"
 
@@ -22,28 +22,6 @@ namespace {
 
 thread_local int g_last_hip_error = 0;
 
-inline int hip_fail(hipError_t e) {
-  g_last_hip_error = (int)e;
-  return MUON_E_HIP;
-}
-#define MUON_HIP(expr)                          \
-  do {                                          \
-    hipError_t e__ = (expr);                    \
-    if (e__ != hipSuccess) return hip_fail(e__); \
-  } while (0)
-
-// Every entry point runs its body through this: nothing may unwind through the C ABI.
-template <typename F>
-int guarded(F&& body) noexcept {
-  try {
-    return body();
-  } catch (const std::bad_alloc&) {
-    return MUON_E_NO_MEMORY;
-  } catch (...) {
-    return MUON_E_INVALID_ARG;
-  }
-}
-
 // Scratch of muon_step_static, the entry point for callers that cannot allocate device memory: the tables and
 // Newton-Schulz temporaries that muon_step keeps in the caller's workspace live in this array instead.  Every device
 // the library runs on holds its own copy, at its own address, until the process ends.  In host code the name is only
@@ -52,6 +30,11 @@ constexpr size_t kStaticScratchBytes = MUON_STATIC_MAX_BYTES;
 static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 
 }  // namespace
+
+int muon::hip_fail(hipError_t e) {
+  g_last_hip_error = (int)e;
+  return MUON_E_HIP;
+}
 
 namespace {
 
