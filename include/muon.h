@@ -293,7 +293,7 @@ typedef struct {
   int64_t hidden_stride;    /* elements, >= width                                                       */
   int64_t weight_stride;
   int64_t tokens;           /* 0 .. 2^30; 0: d_weight is set to zero                                    */
-  int64_t vocab;            /* 1 .. 2^30                                                                */
+  int64_t vocab;            /* 1 .. 2^21                                                                */
   int64_t width;            /* 1 .. 2^20                                                                */
   int32_t dtype;            /* MUON_F32 or MUON_BF16: hidden, weight, d_hidden, d_weight                */
   int32_t reserved;         /* must be 0                                                                */

@@ -51,7 +51,8 @@ HeadProduct head_product(int64_t m, int64_t n, int64_t k, int pairs, bool may_sp
   p.m = m;
   p.n = n;
   p.k = k;
-  p.tile = 128;
+  const int64_t wide = ((m + 255) / 256) * ((n + 255) / 256);
+  p.tile = wide >= kUnits ? 256 : 128;
   p.tiles_m = (int)((m + p.tile - 1) / p.tile);
   p.tiles_n = (int)((n + p.tile - 1) / p.tile);
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, slabs = std::max<int64_t>(1, (k + kHeadSlab - 1) / kHeadSlab * pairs);

@@ -6,10 +6,10 @@
 
 namespace muon {
 
-constexpr int64_t kHeadMaxTokens = 1ll << 30, kHeadMaxVocab = 1ll << 30, kHeadMaxWidth = 1ll << 20;
+constexpr int64_t kHeadMaxTokens = 1ll << 30, kHeadMaxVocab = 1ll << 21, kHeadMaxWidth = 1ll << 20;
 constexpr int kHeadMaxTop = 4096;
-// Rows further apart than this are copied first: a tile's offsets stay below 2^32 bytes.
-constexpr int64_t kHeadMaxPitch = 1ll << 22;
+// Rows further apart than this are copied first: offsets in a tile of 256 rows stay below 2^30 bytes.
+constexpr int64_t kHeadMaxPitch = 1ll << 21;
 // Tokens of a piece where the caller sets no limit to the workspace.
 constexpr int64_t kHeadPieceTokens = 8192;
 

@@ -8,6 +8,8 @@
 // place, and writes the target's few entries from logits computed in fp32 (p - q there cancels); two more products give the gradients.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
+
 #include "head_gemm.h"
 
 namespace muon {
@@ -143,23 +145,27 @@ __global__ __launch_bounds__(256) void head_entries_kernel(HeadTarget t, const v
 }
 
 // ---- logits ----
-template <bool PROB, bool F32>
-__global__ __launch_bounds__(256) void head_logits_kernel(HeadOperand weight, HeadOperand hidden, HeadTiles g, float inv_tau,
-                                                          float2* __restrict__ stats, long long stats_pitch, void* __restrict__ prob,
-                                                          long long prob_pitch) {
-  __shared__ __align__(16) u16 lds[Tile128::kLds / 2];
-  const long long row0 = (long long)(blockIdx.x % g.tiles_m) * 128, col0 = (long long)(blockIdx.x / g.tiles_m) * 128;
-  Tile128 tile;
-  tile.run<false, false>(weight, hidden, row0, col0, g.k, 0, g.slabs_per_split, lds);
+// A wave's part of a tile is WM (64 or 128) vocabulary entries, the block that one pair of statistics stands for; a lane holds half of
+// such a block for each of its tokens.
+template <int B, bool PROB, bool F32>
+__global__ __launch_bounds__(256, B == 256 ? 1 : 2) void head_logits_kernel(HeadOperand weight, HeadOperand hidden, HeadTiles g, float inv_tau,
+                                                                            float2* __restrict__ stats, long long stats_pitch,
+                                                                            void* __restrict__ prob, long long prob_pitch) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  using T = Tile<B, B, false, false>;
+  const TileAt at = tile_at(g);
+  const long long row0 = (long long)at.m * B, col0 = (long long)at.n * B;
+  T tile;
+  tile.run(weight, hidden, row0, col0, g.k, 0, g.slabs_per_split, smem);
   const int fr = tile.lane & 31, fh = tile.lane >> 5;
-  const long long v0 = row0 + tile.wm * 64;
-  const bool whole = v0 + 64 <= weight.rows;
+  const long long v0 = row0 + tile.wm * T::WM;
+  const bool whole = v0 + T::WM <= weight.rows;
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const long long token = col0 + tile.wn * 64 + 32 * j + fr;
+  for (int j = 0; j < T::FN; ++j) {
+    const long long token = col0 + tile.wn * T::WN + 32 * j + fr;
     float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < T::FM; ++i)
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         float z = inv_tau * tile.acc[i][j][v];
@@ -171,7 +177,7 @@ __global__ __launch_bounds__(256) void head_logits_kernel(HeadOperand weight, He
     const float shift = top == -INFINITY ? 0.f : top;
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < T::FM; ++i)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         float x[4];
@@ -180,21 +186,25 @@ __global__ __launch_bounds__(256) void head_logits_kernel(HeadOperand weight, He
           x[e] = __builtin_amdgcn_exp2f((tile.acc[i][j][4 * q + e] - shift) * kLog2e);
           sum += x[e];
         }
-        if (PROB && token < hidden.rows) {
-          const long long at = token * prob_pitch + v0 + 32 * i + 8 * q + 4 * fh;
-          if constexpr (F32) {
+        if constexpr (PROB && F32) {
+          if (token < hidden.rows) {
             f32x4 z;
 #pragma unroll
             for (int e = 0; e < 4; ++e) z[e] = tile.acc[i][j][4 * q + e];
-            *reinterpret_cast<f32x4*>(static_cast<float*>(prob) + at) = z;
-          } else {
-            const u32x2 p = {pack_f16(kProbScale * x[0], kProbScale * x[1]), pack_f16(kProbScale * x[2], kProbScale * x[3])};
-            *reinterpret_cast<u32x2*>(static_cast<u16*>(prob) + at) = p;
+            *reinterpret_cast<f32x4*>(static_cast<float*>(prob) + token * prob_pitch + v0 + 32 * i + 8 * q + 4 * fh) = z;
           }
+        } else if constexpr (PROB) {
+          tile.put(smem, i, j, q, u32x2{pack_f16(kProbScale * x[0], kProbScale * x[1]), pack_f16(kProbScale * x[2], kProbScale * x[3])});
         }
       }
     sum += __shfl_xor(sum, 32, 64);
-    if (fh == 0 && token < hidden.rows) stats[v0 / 64 * stats_pitch + token] = make_float2(top, sum);
+    if (fh == 0 && token < hidden.rows) stats[v0 / T::WM * stats_pitch + token] = make_float2(top, sum);
+  }
+  if constexpr (PROB && !F32) {
+    __syncthreads();
+    tile.image_out(smem, [&](int c, int r, u32x4 v) {
+      if (col0 + c < hidden.rows) *reinterpret_cast<u32x4*>(static_cast<u16*>(prob) + (col0 + c) * prob_pitch + row0 + r) = v;
+    });
   }
 }
 
@@ -351,30 +361,95 @@ __device__ __forceinline__ void finish_out(const HeadOut& o, long long at, float
   else store_out(o, at, x);
 }
 
-template <bool RKM>
-__global__ __launch_bounds__(256) void head_product_kernel(HeadOperand l, HeadOperand r, HeadTiles g, HeadOut out) {
-  __shared__ __align__(16) u16 lds[Tile128::kLds / 2];
-  const int split = blockIdx.x % g.splits, at = blockIdx.x / g.splits;
-  const long long row0 = (long long)(at % g.tiles_m) * 128, col0 = (long long)(at / g.tiles_m) * 128;
-  const int slabs = (int)((g.k + kHeadSlab - 1) / kHeadSlab) * g.pairs;
-  const int first = split * g.slabs_per_split, last = first + g.slabs_per_split < slabs ? first + g.slabs_per_split : slabs;
-  Tile128 tile;
-  tile.run<true, RKM>(l, r, row0, col0, g.k, first, last, lds);
-  const int fr = tile.lane & 31, fh = tile.lane >> 5;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const long long n = col0 + tile.wn * 64 + 32 * j + fr;
-    if (n >= r.rows) continue;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const long long m = row0 + tile.wm * 64 + 32 * i + 8 * (v / 4) + 4 * fh + v % 4;
-        if (m >= l.rows) continue;
-        if (g.splits > 1) out.partial[((long long)split * r.rows + n) * l.rows + m] = tile.acc[i][j][v];
-        else finish_out(out, n * l.rows + m, tile.acc[i][j][v]);
+// Global memory takes 16 (8) bytes at any address of an element.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+
+// fp32 results, parts of a sum, or both: four elements per lane and store.
+template <typename T>
+__device__ __forceinline__ void store_parts(const T& tile, const HeadOperand& l, const HeadOperand& r, const HeadTiles& g, const HeadOut& out, int split,
+                                            long long row0, long long col0) {
+      const int fr = tile.lane & 31, fh = tile.lane >> 5;
+      // fp32 destination, or none: then it is the bf16 result
+      float* to = g.splits > 1 ? out.partial + (long long)split * r.rows * l.rows : out.keep ? out.sum : out.f32 ? static_cast<float*>(out.out) : nullptr;
+      const float* add = g.splits > 1 || !out.add ? nullptr : out.sum;
+  #pragma unroll
+      for (int j = 0; j < T::FN; ++j) {
+        const long long n = col0 + tile.wn * T::WN + 32 * j + fr;
+  #pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+  #pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const long long m = row0 + tile.wm * T::WM + 32 * i + 8 * q + 4 * fh, p = n * l.rows + m;
+            if (n >= r.rows || m >= l.rows) continue;
+            f32x4 x;
+  #pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = tile.acc[i][j][4 * q + e];
+            if (m + 4 <= l.rows) {
+              if (add) x += *reinterpret_cast<const f32x4_any*>(add + p);
+              if (to) *reinterpret_cast<f32x4_any*>(to + p) = x;
+              else *reinterpret_cast<u32x2_any*>(static_cast<u16*>(out.out) + p) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+            } else {
+  #pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if (m + e >= l.rows) continue;
+                const float y = add ? x[e] + add[p + e] : x[e];
+                if (to) to[p + e] = y;
+                else static_cast<u16*>(out.out)[p + e] = bf16_bits(y);
+              }
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-  }
+}
+
+// bf16 results in whole, through the image in LDS.
+template <typename T>
+__device__ __forceinline__ void store_whole(const T& tile, const HeadOperand& l, const HeadOperand& r, const HeadOut& out, long long row0,
+                                            long long col0, unsigned char* smem) {
+  #pragma unroll
+      for (int j = 0; j < T::FN; ++j)
+  #pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+  #pragma unroll
+          for (int q = 0; q < 4; ++q)
+            tile.put(smem, i, j, q, u32x2{pack_bf16(tile.acc[i][j][4 * q], tile.acc[i][j][4 * q + 1]), pack_bf16(tile.acc[i][j][4 * q + 2], tile.acc[i][j][4 * q + 3])});
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      __syncthreads();
+      tile.image_out(smem, [&](int c, int m, u32x4 v) {
+        const long long n = col0 + c;
+        if (n >= r.rows || row0 + m >= l.rows) return;
+        u16* to = static_cast<u16*>(out.out) + n * l.rows + row0 + m;
+        if (row0 + m + 8 <= l.rows) {
+          *reinterpret_cast<u32x4_any*>(to) = v;
+        } else {
+  #pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (row0 + m + e < l.rows) to[e] = (u16)(v[e / 2] >> (16 * (e & 1)));
+        }
+      });
+}
+
+template <int B, bool RKM, bool IMAGE>
+__device__ __forceinline__ void product_tile(const HeadOperand& l, const HeadOperand& r, const HeadTiles& g, const HeadOut& out, unsigned char* smem) {
+  using T = Tile<B, B, true, RKM>;
+  const TileAt at = tile_at(g);
+  const long long row0 = (long long)at.m * B, col0 = (long long)at.n * B;
+  const int slabs = (int)((g.k + kHeadSlab - 1) / kHeadSlab) * g.pairs;
+  const int first = at.split * g.slabs_per_split, last = first + g.slabs_per_split < slabs ? first + g.slabs_per_split : slabs;
+  T tile;
+  tile.run(l, r, row0, col0, g.k, first, last, smem);
+  if constexpr (IMAGE) store_whole(tile, l, r, out, row0, col0, smem);
+  else store_parts(tile, l, r, g, out, at.split, row0, col0);
+}
+
+template <int B, bool RKM, bool IMAGE>
+__global__ __launch_bounds__(256, B == 256 ? 1 : 2) void head_product_kernel(HeadOperand l, HeadOperand r, HeadTiles g, HeadOut out) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  product_tile<B, RKM, IMAGE>(l, r, g, out, smem);
 }
 
 __global__ __launch_bounds__(256) void head_sum_splits_kernel(HeadOut out, int splits, long long count) {
@@ -399,23 +474,63 @@ unsigned blocks_for(long long threads) {
 
 }  // namespace
 
+// More than 64 KB of LDS has to be asked for, once per kernel and device (two threads that get here together ask twice).
+hipError_t allow_lds(std::atomic<uint64_t>& done, const void* kernel, int bytes) {
+  int dev = 0;
+  if (hipError_t e = hipGetDevice(&dev)) return e;
+  const uint64_t bit = dev < 64 ? uint64_t{1} << dev : 0;
+  if (done.load(std::memory_order_acquire) & bit) return hipSuccess;
+  if (hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes)) return e;
+  done.fetch_or(bit, std::memory_order_release);
+  return hipSuccess;
+}
+
+template <int B, bool PROB, bool F32>
+hipError_t logits_of(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float inv_tau, float2* stats,
+                     long long stats_pitch, void* prob, long long prob_pitch, hipStream_t s) {
+  constexpr int lds = Tile<B, B, false, false>::kLds;
+  static std::atomic<uint64_t> done{0};
+  if (hipError_t e = allow_lds(done, reinterpret_cast<const void*>(&head_logits_kernel<B, PROB, F32>), lds)) return e;
+  head_logits_kernel<B, PROB, F32><<<(unsigned)((long long)g.tiles_m * g.tiles_n), 256, lds, s>>>(weight, hidden, tiles_of(g, pairs), inv_tau, stats, stats_pitch, prob,
+                                                                     prob_pitch);
+  return hipGetLastError();
+}
+
 hipError_t launch_head_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float inv_tau,
                               float2* stats, long long stats_pitch, void* prob, long long prob_pitch, int prob_f32, hipStream_t s) {
-  const dim3 grid((unsigned)((long long)g.tiles_m * g.tiles_n));
-  auto go = [&](auto kernel) {
-    kernel<<<grid, 256, 0, s>>>(weight, hidden, tiles_of(g, pairs), inv_tau, stats, stats_pitch, prob, prob_pitch);
-    return hipGetLastError();
+  auto go = [&](auto b) {
+    constexpr int B = decltype(b)::value;
+    if (!prob) return logits_of<B, false, false>(weight, hidden, g, pairs, inv_tau, stats, stats_pitch, prob, prob_pitch, s);
+    if (prob_f32) return logits_of<B, true, true>(weight, hidden, g, pairs, inv_tau, stats, stats_pitch, prob, prob_pitch, s);
+    return logits_of<B, true, false>(weight, hidden, g, pairs, inv_tau, stats, stats_pitch, prob, prob_pitch, s);
   };
-  if (!prob) return go(head_logits_kernel<false, false>);
-  return prob_f32 ? go(head_logits_kernel<true, true>) : go(head_logits_kernel<true, false>);
+  return g.tile == 256 ? go(std::integral_constant<int, 256>{}) : go(std::integral_constant<int, 128>{});
+}
+
+template <int B, bool RKM, bool IMAGE>
+hipError_t product_of(const HeadOperand& l, const HeadOperand& r, const HeadProduct& g, int pairs, const HeadOut& out, hipStream_t s) {
+  constexpr int lds = Tile<B, B, true, RKM>::kLds;
+  static std::atomic<uint64_t> done{0};
+  if (hipError_t e = allow_lds(done, reinterpret_cast<const void*>(&head_product_kernel<B, RKM, IMAGE>), lds)) return e;
+  head_product_kernel<B, RKM, IMAGE><<<(unsigned)((long long)g.tiles_m * g.tiles_n * g.splits), 256, lds, s>>>(l, r, tiles_of(g, pairs), out);
+  return hipGetLastError();
 }
 
 hipError_t launch_head_product(const HeadOperand& l, const HeadOperand& r, int r_kmajor, const HeadProduct& g, int pairs,
                                const HeadOut& out, hipStream_t s) {
-  const dim3 grid((unsigned)((long long)g.tiles_m * g.tiles_n * g.splits));
-  if (r_kmajor) head_product_kernel<true><<<grid, 256, 0, s>>>(l, r, tiles_of(g, pairs), out);
-  else head_product_kernel<false><<<grid, 256, 0, s>>>(l, r, tiles_of(g, pairs), out);
-  return hipGetLastError();
+  const bool image = g.splits == 1 && !out.f32 && !out.add && !out.keep;
+#define MUON_HEAD_CASE(B, KM, IMAGE) \
+  if (g.tile == B && (r_kmajor != 0) == KM && image == IMAGE) return product_of<B, KM, IMAGE>(l, r, g, pairs, out, s)
+  MUON_HEAD_CASE(256, false, true);
+  MUON_HEAD_CASE(256, false, false);
+  MUON_HEAD_CASE(256, true, true);
+  MUON_HEAD_CASE(256, true, false);
+  MUON_HEAD_CASE(128, false, true);
+  MUON_HEAD_CASE(128, false, false);
+  MUON_HEAD_CASE(128, true, true);
+  MUON_HEAD_CASE(128, true, false);
+#undef MUON_HEAD_CASE
+  return hipErrorInvalidValue;
 }
 
 hipError_t launch_head_pack(const void* src, long long stride, int f32, long long n, long long width, u16* dst, long long ld,
