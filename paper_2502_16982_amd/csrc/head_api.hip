@@ -52,6 +52,13 @@ int run_head(const muon_head* h, const HeadTarget& target, const HeadOutputs& ou
   auto u16_at = [&](size_t at) { return reinterpret_cast<uint16_t*>(ws + at); };
   auto f32_at = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
   const bool gradients = shape.d_hidden || shape.d_weight;
+  const float unit = (float)(1.44269504088896340736 * (double)target.inv_tau);
+  // dz goes through the products over the largest scale: where all are alike the target's entries stay near -1, which bf16 holds exactly
+  const float* peak = nullptr;
+  if (gradients && target.token_scale) {
+    peak = f32_at(p.peak);
+    MUON_HIP(launch_head_peak(target.token_scale, shape.tokens, f32_at(p.peak), s));
+  }
 
   HeadOperand weight{static_cast<const uint16_t*>(h->weight), h->weight_stride, 0, shape.vocab};
   if (p.pack_weight) {
@@ -77,24 +84,24 @@ int run_head(const muon_head* h, const HeadTarget& target, const HeadOutputs& ou
     MUON_HIP(launch_head_entries(t, rows, h->hidden_stride, h->weight, h->weight_stride, shape.f32, n, shape.vocab, shape.width,
                                  f32_at(p.entry), masked, p.width_k, masked_plane, s));
     float2* stats = reinterpret_cast<float2*>(ws + p.stats);
-    MUON_HIP(launch_head_logits(weight, hidden, p.logits[last], p.pairs, target.inv_tau, stats, p.piece, gradients ? ws + p.prob : nullptr,
+    MUON_HIP(launch_head_logits(weight, hidden, p.logits[last], p.pairs, unit, stats, p.piece, gradients ? ws + p.prob : nullptr,
                                 p.vocab_pitch, shape.f32, s));
-    float* lse = out.lse ? out.lse + t0 : f32_at(p.lse);
-    MUON_HIP(launch_head_join(t, stats, p.piece, head_blocks(p.logits[last]), f32_at(p.entry), n, shape.vocab, out.loss + t0, lse,
-                              gradients ? f32_at(p.value) : nullptr, gradients ? f32_at(p.scale) : nullptr, s));
+    float2* log2sum = reinterpret_cast<float2*>(ws + p.lse);
+    MUON_HIP(launch_head_join(t, unit, peak, stats, p.piece, p.blocks, f32_at(p.entry), n, shape.vocab, out.loss + t0,
+                              out.lse ? out.lse + t0 : nullptr, gradients ? f32_at(p.value) : nullptr, f32_at(p.scale), log2sum, s));
     if (!gradients) continue;
     const int64_t grad_plane = p.piece * p.vocab_pitch;
-    MUON_HIP(launch_head_grad(t, stats, p.piece, head_grain(p.logits[last]), lse, f32_at(p.value), f32_at(p.scale), n, shape.vocab,
-                              ws + p.prob, p.vocab_pitch, shape.f32, u16_at(p.grad), grad_plane, s));
+    MUON_HIP(launch_head_grad(t, unit, stats, p.piece, log2sum, f32_at(p.value), f32_at(p.scale), n, shape.vocab, ws + p.prob,
+                              p.vocab_pitch, shape.f32, u16_at(p.grad), grad_plane, s));
     if (shape.d_hidden) {
-      const HeadOut o{static_cast<unsigned char*>(out.d_hidden) + elem * t0 * shape.width, shape.f32, f32_at(p.partial), nullptr, 0, 0};
+      const HeadOut o{static_cast<unsigned char*>(out.d_hidden) + elem * t0 * shape.width, shape.f32, f32_at(p.partial), nullptr, 0, 0, target.tau, peak};
       const HeadOperand l{weight.p, weight.ld, weight.plane, shape.width}, r{u16_at(p.grad), p.vocab_pitch, grad_plane, n};
       const HeadProduct& g = p.hidden[last];
       MUON_HIP(launch_head_product(l, r, 0, g, p.pairs, o, s));
       if (g.splits > 1) MUON_HIP(launch_head_sum_splits(o, g.splits, n * shape.width, s));
     }
     if (shape.d_weight) {
-      const HeadOut o{out.d_weight, shape.f32, f32_at(p.partial), f32_at(p.sum), piece > 0, !last};
+      const HeadOut o{out.d_weight, shape.f32, f32_at(p.partial), f32_at(p.sum), piece > 0, !last, target.tau, peak};
       const HeadOperand l{masked, p.width_k, masked_plane, shape.width}, r{u16_at(p.grad), p.vocab_pitch, grad_plane, shape.vocab};
       const HeadProduct& g = p.weight[last];
       MUON_HIP(launch_head_product(l, r, 1, g, p.pairs, o, s));

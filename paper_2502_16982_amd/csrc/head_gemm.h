@@ -33,13 +33,13 @@ __device__ __forceinline__ float bf16_value(u16 v) { return __uint_as_float((uns
 __device__ __forceinline__ u16 bf16_bits(float x) { return (u16)(pack_bf16(x, 0.f) & 0xffffu); }
 
 constexpr float kLog2e = 1.44269504088896340736f;
-// 2^15: the largest probability relative to its block's maximum lies high in f16's range, so that 2^-12 of relative precision holds
-// down to 2^-29 of the maximum.
-constexpr float kProbScale = 32768.f;
+// The largest power of a block is 2^15, high in f16's range: 2^-11 of relative precision holds down to 2^-29 of it.
+constexpr float kProbTop = 15.f;
 
-// The planes of the pair with that number, (0,0) (0,1) (1,0) (1,1) (0,2) (2,0): what is left out is below 2^-24.
-__device__ __forceinline__ int pair_left(int pair) { return pair == 2 || pair == 3 ? 1 : pair == 5 ? 2 : 0; }
-__device__ __forceinline__ int pair_right(int pair) { return pair == 1 || pair == 3 ? 1 : pair == 4 ? 2 : 0; }
+// The planes of the pair with that number: (0,0) alone, or (0,2) (2,0) (1,1) (0,1) (1,0) (0,0), the smallest first, so that they do not
+// add their roundings to the large sum; what is left out is below 2^-24.
+__device__ __forceinline__ int pair_left(int pairs, int pair) { return pairs == 1 ? 0 : (0x021010 >> 4 * (5 - pair)) & 15; }
+__device__ __forceinline__ int pair_right(int pairs, int pair) { return pairs == 1 ? 0 : (0x201100 >> 4 * (5 - pair)) & 15; }
 
 typedef const __attribute__((address_space(1))) void* gptr;
 typedef __attribute__((address_space(3))) void* lptr;
@@ -57,17 +57,24 @@ __device__ __forceinline__ void static_for(F&& f) {
 // eight columns row by row: the 32 tiles that run together on a die share four panels of L and eight of R in its L2.
 struct TileAt {
   int m, n, split;
+  int quarter;              // -1: the whole tile
 };
 __device__ __forceinline__ TileAt tile_at(const HeadTiles& g) {
-  const int tiles = g.tiles_m * g.tiles_n, all = tiles * g.splits, b = blockIdx.x;
-  const int die = b & 7, per = all >> 3, rest = all & 7;
-  int t = die * per + (die < rest ? die : rest) + (b >> 3);
-  const int split = t / tiles;
-  t -= split * tiles;
+  const int all = g.whole * g.splits, b = blockIdx.x;
+  int t, split = 0, quarter = -1;
+  if (b < all) {
+    const int die = b & 7, per = all >> 3, rest = all & 7;
+    t = die * per + (die < rest ? die : rest) + (b >> 3);
+    split = t / g.whole;
+    t -= split * g.whole;
+  } else {                  // (splits = 1)
+    t = g.whole + (b - all) / 4;
+    quarter = (b - all) % 4;
+  }
   constexpr int kBand = 8;
   const int band = t / (kBand * g.tiles_m), wide = g.tiles_n - band * kBand < kBand ? g.tiles_n - band * kBand : kBand;
   t -= band * kBand * g.tiles_m;
-  return {t / wide, band * kBand + t % wide, split};
+  return {t / wide, band * kBand + t % wide, split, quarter};
 }
 
 // Fragments of F rows of 32 for one k-step of 16, as LDS reads deliver them.
@@ -213,8 +220,8 @@ struct Tile {
   f32x16 acc[FM][FN];
   int lane, wave, wm, wn;
 
-  __device__ __forceinline__ void run(const HeadOperand& lo, const HeadOperand& ro, long long row0, long long col0, long long k, int first, int last,
-                                      unsigned char* smem) {
+  __device__ __forceinline__ void run(const HeadOperand& lo, const HeadOperand& ro, long long row0, long long col0, long long k, int pairs, int first,
+                                      int last, unsigned char* smem) {
     lane = threadIdx.x & 63;
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     wm = wave >> 1;
@@ -236,8 +243,8 @@ struct Tile {
     typename L::Source ls;
     typename R::Source rs;
     auto take_next = [&]() {
-      ls = l.source(pair_left(next_pair), next_kt, k);
-      rs = r.source(pair_right(next_pair), next_kt, k);
+      ls = l.source(pair_left(pairs, next_pair), next_kt, k);
+      rs = r.source(pair_right(pairs, next_pair), next_kt, k);
       if (++next_kt == per_pair) next_kt = 0, ++next_pair;
     };
     constexpr int LOADS = L::LOADS + R::LOADS;

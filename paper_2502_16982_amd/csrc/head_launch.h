@@ -20,24 +20,27 @@ struct HeadOperand {
 struct HeadTiles {
   long long k;
   int pairs;
-  int tiles_m, tiles_n;
+  int tiles_m, tiles_n, whole;
   int splits, slabs_per_split;
 };
 
 // Where a gradient's tiles go.  out: n rows of m elements, dense.  partial (splits > 1): [split][n][m] in fp32.  sum: fp32 [n][m],
-// the pieces of tokens before (add) and with this one (keep).
+// the pieces of tokens before (add) and with this one (keep).  Results are times `scale` and *peak (null: 1).
 struct HeadOut {
   void* out;
   int f32;
   float* partial;
   float* sum;
   int add, keep;
+  float scale;
+  const float* peak;
 };
 
-// logits: L = weight, R = hidden.  Per block of `grain` vocabulary entries and token the maximum and the sum of exp(z - maximum); with
-// `prob` what the gradient needs: f16 2^15 exp(z - maximum), or, fp32, the logits themselves.
-hipError_t launch_head_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float inv_tau,
-                              float2* stats, long long stats_pitch, void* prob, long long prob_pitch, int prob_f32, hipStream_t s);
+// logits: L = weight, R = hidden, in units of log 2: y = unit z, unit = log2(e) / tau.  Per block of kHeadGrain vocabulary entries and token
+// the pair (bias, sum of 2^(y + bias)), the largest of these powers being 2^15; with `prob` what the gradient needs: these powers in f16,
+// or, fp32, z.
+hipError_t launch_head_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, float2* stats,
+                              long long stats_pitch, void* prob, long long prob_pitch, int prob_f32, hipStream_t s);
 // out = L R^T with L K-major; R plain or K-major.
 hipError_t launch_head_product(const HeadOperand& l, const HeadOperand& r, int r_kmajor, const HeadProduct& g, int pairs,
                                const HeadOut& out, hipStream_t s);
@@ -60,11 +63,15 @@ struct HeadTarget {
 hipError_t launch_head_entries(const HeadTarget& t, const void* hidden, long long hidden_stride, const void* weight,
                                long long weight_stride, int f32, long long tokens, long long vocab, long long width, float* entry,
                                uint16_t* masked, long long ld, long long plane, hipStream_t s);
-// Joins the pairs (maximum, sum): lse and loss per token; with `value`, the gradients at the entries and the scale of the others.
-hipError_t launch_head_join(const HeadTarget& t, const float2* stats, long long stats_pitch, long long blocks, const float* entry,
-                            long long tokens, long long vocab, float* loss, float* lse, float* value, float* scale, hipStream_t s);
+// *peak = the largest finite |token_scale|, or 1.
+hipError_t launch_head_peak(const float* token_scale, long long tokens, float* peak, hipStream_t s);
+// Joins the pairs: loss and, if wanted, lse per token; with `value`, the gradients at the entries over tau and *peak, the scale of the others, and
+// log2 of the sum of 2^y in two floats.
+hipError_t launch_head_join(const HeadTarget& t, float unit, const float* peak, const float2* stats, long long stats_pitch, long long blocks,
+                            const float* entry, long long tokens, long long vocab, float* loss, float* lse, float* value, float* scale,
+                            float2* log2sum, hipStream_t s);
 // The logits' gradient in bf16 (in place of the probabilities) or three planes.
-hipError_t launch_head_grad(const HeadTarget& t, const float2* stats, long long stats_pitch, int grain, const float* lse,
+hipError_t launch_head_grad(const HeadTarget& t, float unit, const float2* stats, long long stats_pitch, const float2* log2sum,
                             const float* value, const float* scale, long long tokens, long long vocab, const void* prob, long long pitch,
                             int f32, uint16_t* grad, long long plane, hipStream_t s);
 // Sums the splits of a product.

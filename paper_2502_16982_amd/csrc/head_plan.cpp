@@ -12,12 +12,11 @@ void plan_piece(const HeadShape& s, int64_t piece, HeadPlan* p) {
   p->pieces = std::max<int64_t>(1, (s.tokens + piece - 1) / piece);
   const bool gradients = s.d_hidden || s.d_weight;
   const int64_t sizes[2] = {piece, s.tokens - (p->pieces - 1) * piece};
-  int64_t blocks = 0, partial = 0;
+  int64_t partial = 0;
   for (int i = 0; i < 2; ++i) {
     p->logits[i] = head_product(s.vocab, sizes[i], p->width_k, p->pairs, false);
     p->hidden[i] = head_product(s.width, sizes[i], s.vocab, p->pairs, true);
     p->weight[i] = head_product(s.width, s.vocab, sizes[i], p->pairs, true);
-    blocks = std::max(blocks, head_blocks(p->logits[i]));
     if (s.d_hidden && p->hidden[i].splits > 1) partial = std::max(partial, p->hidden[i].splits * sizes[i] * s.width * 4);
     if (s.d_weight && p->weight[i].splits > 1) partial = std::max(partial, p->weight[i].splits * s.vocab * s.width * 4);
   }
@@ -32,11 +31,12 @@ void plan_piece(const HeadShape& s, int64_t piece, HeadPlan* p) {
   p->sum = take(s.d_weight && p->pieces > 1, s.vocab * s.width * 4);
   p->packed_hidden = take(p->pack_hidden, piece * row);
   p->masked_hidden = take(s.d_weight, piece * row);
-  p->stats = take(true, blocks * piece * 8);
+  p->stats = take(true, p->blocks * piece * 8);
   p->entry = take(true, piece * s.top * 4);
   p->value = take(gradients, piece * s.top * 4);
   p->scale = take(true, piece * 4);
-  p->lse = take(true, piece * 4);
+  p->lse = take(true, piece * 8);
+  p->peak = take(gradients, 4);
   p->prob = take(gradients, piece * p->vocab_pitch * (s.f32 ? 4 : 2));
   p->grad = s.f32 ? take(gradients, 3 * piece * p->vocab_pitch * 2) : p->prob;      // bf16: in place of the probabilities
   p->partial = take(partial > 0, partial);
@@ -45,21 +45,51 @@ void plan_piece(const HeadShape& s, int64_t piece, HeadPlan* p) {
 
 }  // namespace
 
+namespace {
+
+constexpr int64_t kUnits = 256;                  // compute units
+// What a launch takes, in us, from the time of a slab of 64 of K (both sides measured at K of 1000 slabs and of 64): a 256-wide tile per
+// compute unit 1.78; two 128-wide ones 1.17; one alone 0.65; and 6 to start and to store.
+double time_wide(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (1.78 * slabs + 6); }
+double time_narrow(int64_t blocks, double slabs) {
+  const int64_t rest = blocks % (2 * kUnits);
+  return (double)(blocks / (2 * kUnits)) * (1.17 * slabs + 6) + (rest == 0 ? 0 : (rest <= kUnits ? 0.65 : 1.17) * slabs + 6);
+}
+double time_lone(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (0.65 * slabs + 6); }
+
+}  // namespace
+
+// The fastest by the times above of: tiles of 256, with what the last round holds in tiles of 128 where that is quicker; tiles of 128;
+// either with K in up to 64 runs of at least eight slabs, whose fp32 results are written and read once more (at 5 bytes per ps, and a launch).
 HeadProduct head_product(int64_t m, int64_t n, int64_t k, int pairs, bool may_split) {
-  constexpr int64_t kUnits = 256;
   HeadProduct p{};
   p.m = m;
   p.n = n;
   p.k = k;
-  const int64_t wide = ((m + 255) / 256) * ((n + 255) / 256);
-  p.tile = wide >= kUnits ? 256 : 128;
+  auto tiles = [&](int64_t tile) { return ((m + tile - 1) / tile) * ((n + tile - 1) / tile); };
+  const int64_t wide = tiles(256), narrow = tiles(128), slabs = std::max<int64_t>(1, (k + kHeadSlab - 1) / kHeadSlab * pairs);
+  double best = 0;
+  int64_t splits = 1;
+  auto offer = [&](double us, int tile, int64_t whole, int64_t s) {
+    if (p.tile && us >= best) return;
+    best = us;
+    p.tile = tile;
+    p.whole = (int)whole;
+    splits = s;
+  };
+  offer(time_narrow(narrow, (double)slabs), 128, narrow, 1);
+  offer(time_wide(wide, (double)slabs), 256, wide, 1);
+  const int64_t rest = wide % kUnits;
+  if (wide > kUnits && rest) offer(time_wide(wide - rest, (double)slabs) + time_lone(4 * rest, (double)slabs), 256, wide - rest, 1);
+  if (may_split) {
+    for (int64_t s = 2; s <= 64 && slabs / s >= 8; ++s) {
+      const double each = (double)((slabs + s - 1) / s), join = 4 + (double)(s * m * n) * 8e-6 / 5;
+      if (narrow * s <= 2 * kUnits) offer(time_narrow(narrow * s, each) + join, 128, narrow, s);
+      if (wide * s <= 2 * kUnits) offer(time_wide(wide * s, each) + join, 256, wide, s);
+    }
+  }
   p.tiles_m = (int)((m + p.tile - 1) / p.tile);
   p.tiles_n = (int)((n + p.tile - 1) / p.tile);
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, slabs = std::max<int64_t>(1, (k + kHeadSlab - 1) / kHeadSlab * pairs);
-  int64_t splits = 1;
-  // A split's partial result is written and read back in fp32: only where the tiles leave compute units idle, and with at least
-  // eight slabs each.
-  if (may_split && tiles < kUnits) splits = std::max<int64_t>(1, std::min(2 * kUnits / std::max<int64_t>(1, tiles), slabs / 8));
   p.slabs_per_split = (int)((slabs + splits - 1) / splits);
   p.splits = (int)((slabs + p.slabs_per_split - 1) / p.slabs_per_split);
   return p;
@@ -71,6 +101,7 @@ bool head_plan(const HeadShape& s, size_t max_bytes, HeadPlan* p) {
   p->pairs = s.f32 ? 6 : 1;
   p->width_k = up(s.width, 8);
   p->vocab_pitch = up(s.vocab, 256);
+  p->blocks = up(s.vocab, kHeadGrain) / kHeadGrain;
   // fp32 operands are split into planes; bf16 rows that do not come in whole aligned chunks of 16 bytes are copied
   const bool ragged = s.f32 || s.width % 8 != 0;
   p->pack_hidden = ragged || s.hidden_stride % 8 != 0 || s.hidden_stride > kHeadMaxPitch || !s.hidden_aligned;

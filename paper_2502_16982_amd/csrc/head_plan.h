@@ -22,20 +22,22 @@ struct HeadShape {
   bool d_hidden, d_weight;
 };
 
-// One of the three products as it is launched: T = L R^T in tiles of tile x tile, the slabs of K in `splits` equal runs.
+// One of the three products as it is launched: T = L R^T in tiles of tile x tile, the slabs of K in `splits` equal runs.  Of the tiles of
+// 256 the first `whole` run as they are and the others, too few for the chip, as four of 128 each.
 struct HeadProduct {
   int64_t m, n, k;          // rows of L, rows of R
   int tile;
   int tiles_m, tiles_n;
+  int whole;
   int splits;
   int slabs_per_split;      // of kHeadSlab elements of K, over all pairs of planes
+  int64_t blocks() const { return ((int64_t)whole + 4 * ((int64_t)tiles_m * tiles_n - whole)) * splits; }
 };
 
 constexpr int kHeadSlab = 64;
 
-// Vocabulary entries that one pair (maximum, sum) of the logits' product stands for, and such pairs per token.
-inline int head_grain(const HeadProduct& logits) { return logits.tile / 2; }
-inline int64_t head_blocks(const HeadProduct& logits) { return 2ll * logits.tiles_m; }
+// Vocabulary entries that one pair of statistics of the logits' product stands for.
+constexpr int kHeadGrain = 128;
 
 struct HeadPlan {
   int planes;               // bf16 planes that an operand is the sum of: 1, or 3 for fp32
@@ -44,9 +46,10 @@ struct HeadPlan {
   int64_t vocab_pitch;      // row pitch of the probabilities and of the logits' gradient
   int64_t piece, pieces;    // tokens per piece
   bool pack_hidden, pack_weight;
+  int64_t blocks;           // pairs of statistics per token
   HeadProduct logits[2], hidden[2], weight[2];      // of a whole piece; of the last one
   // byte offsets of the workspace's sections
-  size_t packed_weight, packed_hidden, masked_hidden, stats, entry, value, scale, lse, prob, grad, partial, sum;
+  size_t packed_weight, packed_hidden, masked_hidden, stats, entry, value, scale, lse, peak, prob, grad, partial, sum;
   size_t total;
 };
 

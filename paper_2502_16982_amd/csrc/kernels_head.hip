@@ -145,173 +145,268 @@ __global__ __launch_bounds__(256) void head_entries_kernel(HeadTarget t, const v
 }
 
 // ---- logits ----
-// A wave's part of a tile is WM (64 or 128) vocabulary entries, the block that one pair of statistics stands for; a lane holds half of
-// such a block for each of its tokens.
+// A block of statistics is 128 vocabulary entries: the rows of one wave in a tile of 256, of two in a tile of 128, which compare notes in
+// LDS.  A lane holds half of a wave's rows for each of its tokens.  Powers of two throughout: 2^(unit z + bias) is one multiply-add and one
+// exponential, and as every power of a block carries the very bias that is stored, rounding the bias costs nothing.
 template <int B, bool PROB, bool F32>
-__global__ __launch_bounds__(256, B == 256 ? 1 : 2) void head_logits_kernel(HeadOperand weight, HeadOperand hidden, HeadTiles g, float inv_tau,
-                                                                            float2* __restrict__ stats, long long stats_pitch,
-                                                                            void* __restrict__ prob, long long prob_pitch) {
-  extern __shared__ __align__(16) unsigned char smem[];
+__device__ __forceinline__ void logits_tile(const HeadOperand& weight, const HeadOperand& hidden, const HeadTiles& g, float unit, float2* stats,
+                                            long long stats_pitch, void* prob, long long prob_pitch, long long row0, long long col0,
+                                            unsigned char* smem) {
   using T = Tile<B, B, false, false>;
-  const TileAt at = tile_at(g);
-  const long long row0 = (long long)at.m * B, col0 = (long long)at.n * B;
   T tile;
-  tile.run(weight, hidden, row0, col0, g.k, 0, g.slabs_per_split, smem);
+  tile.run(weight, hidden, row0, col0, g.k, g.pairs, 0, g.slabs_per_split, smem);
   const int fr = tile.lane & 31, fh = tile.lane >> 5;
   const long long v0 = row0 + tile.wm * T::WM;
-  const bool whole = v0 + T::WM <= weight.rows;
+  // rows of the wave's that there are; MASKED: not all of them
+  const int there = (int)(weight.rows - v0 < T::WM ? weight.rows - v0 : T::WM);
+  auto row = [&](int i, int v) { return 32 * i + 8 * (v / 4) + 4 * fh + v % 4; };
+  float top[T::FN];
+  auto find_top = [&](auto masked) {
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+      top[j] = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (!decltype(masked)::value || row(i, v) < there) top[j] = fmaxf(top[j], tile.acc[i][j][v]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      top[j] = fmaxf(top[j], __shfl_xor(top[j], 32, 64));
+    }
+  };
+  if (there == T::WM) find_top(std::false_type{});
+  else find_top(std::true_type{});
+  float* notes = reinterpret_cast<float*>(smem + T::kStage);          // behind the image
+  if constexpr (B == 128) {
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) notes[tile.wm * 128 + tile.wn * 64 + 32 * j + fr] = top[j];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) top[j] = fmaxf(top[j], notes[(tile.wm ^ 1) * 128 + tile.wn * 64 + 32 * j + fr]);
+  }
+  float sums[T::FN];
+  auto take_powers = [&](auto masked) {
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+      const float bias = kProbTop - (top[j] == -INFINITY ? 0.f : unit * top[j]);
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[e] = __builtin_amdgcn_exp2f(fmaf(unit, tile.acc[i][j][4 * q + e], bias));
+            if (decltype(masked)::value && row(i, 4 * q + e) >= there) x[e] = 0.f;
+            sum += x[e];
+          }
+          if constexpr (PROB && !F32) {
+            tile.put(smem, i, j, q, u32x2{pack_f16(x[0], x[1]), pack_f16(x[2], x[3])});
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      sums[j] = sum + __shfl_xor(sum, 32, 64);
+      if constexpr (B == 128) notes[256 + tile.wm * 128 + tile.wn * 64 + 32 * j + fr] = sums[j];
+      top[j] = bias;
+    }
+  };
+  if (there == T::WM) take_powers(std::false_type{});
+  else take_powers(std::true_type{});
+  if constexpr (PROB && F32) {
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+      const long long token = col0 + tile.wn * T::WN + 32 * j + fr;
+      float* z = static_cast<float*>(prob) + token * prob_pitch + v0 + 4 * fh;
+      if (token >= hidden.rows) continue;
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          f32x4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = tile.acc[i][j][4 * q + e];
+          *reinterpret_cast<f32x4*>(z + 32 * i + 8 * q) = x;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+  }
+  if constexpr (B == 128 || (PROB && !F32)) __syncthreads();
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
-    const long long token = col0 + tile.wn * T::WN + 32 * j + fr;
-    float top = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < T::FM; ++i)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        float z = inv_tau * tile.acc[i][j][v];
-        if (!whole && v0 + 32 * i + 8 * (v / 4) + 4 * fh + v % 4 >= weight.rows) z = -INFINITY;
-        tile.acc[i][j][v] = z;
-        top = fmaxf(top, z);
-      }
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float shift = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < T::FM; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[e] = __builtin_amdgcn_exp2f((tile.acc[i][j][4 * q + e] - shift) * kLog2e);
-          sum += x[e];
-        }
-        if constexpr (PROB && F32) {
-          if (token < hidden.rows) {
-            f32x4 z;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] = tile.acc[i][j][4 * q + e];
-            *reinterpret_cast<f32x4*>(static_cast<float*>(prob) + token * prob_pitch + v0 + 32 * i + 8 * q + 4 * fh) = z;
-          }
-        } else if constexpr (PROB) {
-          tile.put(smem, i, j, q, u32x2{pack_f16(kProbScale * x[0], kProbScale * x[1]), pack_f16(kProbScale * x[2], kProbScale * x[3])});
-        }
-      }
-    sum += __shfl_xor(sum, 32, 64);
-    if (fh == 0 && token < hidden.rows) stats[v0 / T::WM * stats_pitch + token] = make_float2(top, sum);
+    const int c = tile.wn * T::WN + 32 * j + fr;
+    if constexpr (B == 128) sums[j] += notes[256 + (tile.wm ^ 1) * 128 + c];
+    if (fh == 0 && (B == 256 || tile.wm == 0) && v0 < weight.rows && col0 + c < hidden.rows)
+      stats[v0 / kHeadGrain * stats_pitch + col0 + c] = make_float2(top[j], sums[j]);
   }
   if constexpr (PROB && !F32) {
-    __syncthreads();
     tile.image_out(smem, [&](int c, int r, u32x4 v) {
       if (col0 + c < hidden.rows) *reinterpret_cast<u32x4*>(static_cast<u16*>(prob) + (col0 + c) * prob_pitch + row0 + r) = v;
     });
   }
 }
 
+template <int B, bool PROB, bool F32>
+__global__ __launch_bounds__(256, B == 256 ? 1 : 2) void head_logits_kernel(HeadOperand weight, HeadOperand hidden, HeadTiles g, float unit,
+                                                                            float2* __restrict__ stats, long long stats_pitch,
+                                                                            void* __restrict__ prob, long long prob_pitch) {
+#if defined(__HIP_DEVICE_COMPILE__)            // (the host's pass knows no buffer descriptors)
+  extern __shared__ __align__(16) unsigned char smem[];
+  const TileAt at = tile_at(g);
+  long long row0 = (long long)at.m * B, col0 = (long long)at.n * B;
+  if (B == 128 || at.quarter < 0) {
+    logits_tile<B, PROB, F32>(weight, hidden, g, unit, stats, stats_pitch, prob, prob_pitch, row0, col0, smem);
+  } else if constexpr (B == 256) {
+    row0 += 128 * (at.quarter >> 1);
+    col0 += 128 * (at.quarter & 1);
+    if (row0 < weight.rows && col0 < hidden.rows)
+      logits_tile<128, PROB, F32>(weight, hidden, g, unit, stats, stats_pitch, prob, prob_pitch, row0, col0, smem);
+  }
+#endif
+}
+
 // ---- join ----
-// Sixteen tokens per block; their blocks of the vocabulary over sixteen threads each, then their entries over a wave each.
-__global__ __launch_bounds__(256) void head_join_kernel(HeadTarget t, const float2* __restrict__ stats, long long stats_pitch,
-                                                        long long blocks, const float* __restrict__ entry, long long tokens,
-                                                        long long vocab, float* __restrict__ loss, float* __restrict__ lse,
-                                                        float* __restrict__ value, float* __restrict__ scale) {
-  __shared__ float tops[16][17];
-  __shared__ double sums[16][17];
+__global__ __launch_bounds__(1024) void head_peak_kernel(const float* __restrict__ token_scale, long long tokens, float* __restrict__ peak) {
+  __shared__ float waves[16];
+  float top = 0.f;
+  for (long long i = threadIdx.x; i < tokens; i += 1024) {
+    const float g = fabsf(token_scale[i]);
+    if (g < INFINITY) top = fmaxf(top, g);
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+  if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 16; ++w) top = fmaxf(top, waves[w]);
+    *peak = top > 0.f ? top : 1.f;
+  }
+}
+
+// Sixteen tokens per block (a line of statistics), their blocks of the vocabulary over 64 threads each, eight loads at a time; then a wave
+// per token for its entries.
+__global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float unit, const float* __restrict__ peak, const float2* __restrict__ stats,
+                                                         long long stats_pitch, long long blocks, const float* __restrict__ entry,
+                                                         long long tokens, long long vocab, float* __restrict__ loss, float* __restrict__ lse,
+                                                         float* __restrict__ value, float* __restrict__ scale, float2* __restrict__ log2sum) {
+  __shared__ float tops[64][17];
+  __shared__ float sums[64][17];
   __shared__ double joined[16];
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
   const long long token = blockIdx.x * 16ll + x, read = token < tokens ? token : tokens - 1;
-  float top = -INFINITY;
-  for (long long b = y; b < blocks; b += 16) top = fmaxf(top, stats[b * stats_pitch + read].x);
-  tops[y][x] = top;
-  __syncthreads();
+  float top = -INFINITY, sum = 0.f;              // the sum is sum * 2^top
+  for (long long b0 = y; b0 < blocks; b0 += 64 * 8) {
+    float2 v[8];
 #pragma unroll
-  for (int u = 0; u < 16; ++u) top = fmaxf(top, tops[u][x]);
-  const float shift = top == -INFINITY ? 0.f : top;
-  double sum = 0.0;
-  for (long long b = y; b < blocks; b += 16) {
-    const float2 v = stats[b * stats_pitch + read];
-    if (v.y != 0.f) sum += (double)(v.y * __builtin_amdgcn_exp2f((v.x - shift) * kLog2e));
+    for (int u = 0; u < 8; ++u) v[u] = b0 + 64 * u < blocks ? stats[(b0 + 64 * u) * stats_pitch + read] : make_float2(0.f, 0.f);
+    float here = top;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (v[u].y != 0.f) here = fmaxf(here, -v[u].x);
+    const float shift = here == -INFINITY ? 0.f : here;
+    sum *= __builtin_amdgcn_exp2f(top - shift);
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (v[u].y != 0.f) sum += v[u].y * __builtin_amdgcn_exp2f(-v[u].x - shift);
+    top = here;
   }
+  tops[y][x] = top;
   sums[y][x] = sum;
   __syncthreads();
-  if (y == 0) {
-    sum = 0.0;
-#pragma unroll
-    for (int u = 0; u < 16; ++u) sum += sums[u][x];
-    joined[x] = (double)shift + log(sum);
-    if (token < tokens) lse[token] = (float)joined[x];
-  }
-  __syncthreads();
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int u = wave; u < 16; u += 4) {
-    const long long tk = blockIdx.x * 16ll + u;
-    if (tk >= tokens) break;
-    const TokenState state = token_state(t, tk, vocab);
-    const float g = token_scale(t, tk, state);
-    const double l = joined[u];
-    double sum_loss = 0.0;
-    if (!t.logits) {
-      if (lane == 0) {
-        const double z = (double)entry[tk];
-        sum_loss = state.some ? l - z : 0.0;
-        if (value) value[tk] = g == 0.f ? 0.f : (float)((double)g * expm1(z - l));
-      }
-    } else if (state.some) {
-      float best = -INFINITY;
-      for (int j = lane; j < t.top; j += 64)
-        if (entry_there(t, tk * t.top + j, vocab)) best = fmaxf(best, teacher_at(t, tk * t.top + j));
+  {                                              // wave w: token w, lane: its thread's share
+    const float mine = tops[lane][wave];
+    float all = mine;
 #pragma unroll
-      for (int off = 32; off > 0; off >>= 1) best = fmaxf(best, __shfl_xor(best, off, 64));
-      double mass = 0.0;
-      for (int j = lane; j < t.top; j += 64)
-        if (entry_there(t, tk * t.top + j, vocab)) mass += exp((double)teacher_at(t, tk * t.top + j) - (double)best);
+    for (int off = 32; off > 0; off >>= 1) all = fmaxf(all, __shfl_xor(all, off, 64));
+    const float shift = all == -INFINITY ? 0.f : all;
+    double part = (double)(sums[lane][wave] * __builtin_amdgcn_exp2f(mine - shift));
 #pragma unroll
-      for (int off = 32; off > 0; off >>= 1) mass += __shfl_xor(mass, off, 64);
-      const double norm = (double)best + log(mass);
-      for (int j0 = 0; j0 < t.top; j0 += 64) {
-        const int j = j0 + lane;
-        const bool there = j < t.top && entry_there(t, tk * t.top + j, vocab);
-        const long long v = there ? index_at(t, tk * t.top + j) : -1;
-        const double z = there ? (double)entry[tk * t.top + j] : 0.0;
-        const double logq = there ? (double)teacher_at(t, tk * t.top + j) - norm : 0.0;
-        if (there) sum_loss += exp(logq) * (logq - z + l);
-        if (value) {
-          double q = 0.0;                        // of every entry with this index
-          for (int k0 = 0; k0 < t.top; k0 += 64) {
-            const int k = k0 + lane;
-            const bool kt = k < t.top && entry_there(t, tk * t.top + k, vocab);
-            const long long vk = kt ? index_at(t, tk * t.top + k) : -2;
-            const double qk = kt ? exp((double)teacher_at(t, tk * t.top + k) - norm) : 0.0;
-            const int n = t.top - k0 < 64 ? t.top - k0 : 64;
-            for (int w = 0; w < n; ++w) {
-              const long long vw = __shfl(vk, w, 64);
-              const double qw = __shfl(qk, w, 64);
-              if (vw == v) q += qw;
-            }
-          }
-          if (j < t.top) value[tk * t.top + j] = there && g != 0.f ? (float)((double)g * (double)t.tau * (exp(z - l) - q)) : 0.f;
-        }
-      }
-#pragma unroll
-      for (int off = 32; off > 0; off >>= 1) sum_loss += __shfl_xor(sum_loss, off, 64);
-    } else if (value) {
-      for (int j = lane; j < t.top; j += 64) value[tk * t.top + j] = 0.f;
-    }
-    if (lane == 0) {
-      loss[tk] = state.beyond ? __builtin_nanf("") : (float)((double)t.tau * (double)t.tau * sum_loss);
-      if (scale) scale[tk] = t.tau * g;
+    for (int off = 32; off > 0; off >>= 1) part += __shfl_xor(part, off, 64);
+    if (lane == 0) joined[wave] = (double)shift + log2(part);
+  }
+  const long long tk = blockIdx.x * 16ll + wave;
+  if (tk >= tokens) return;
+  // (the wave's own LDS write, read back by the same wave)
+  __builtin_amdgcn_wave_barrier();
+  const double y2 = joined[wave], l = y2 * ((double)t.inv_tau / (double)unit);       // log2 and natural log of the sum
+  const TokenState state = token_state(t, tk, vocab);
+  const float g = token_scale(t, tk, state), r = g == 0.f ? 0.f : peak ? g / *peak : g;
+  if (lane == 0) {
+    if (lse) lse[tk] = (float)l;
+    if (value) {
+      scale[tk] = r;
+      const float hi = (float)y2;
+      log2sum[tk] = make_float2(hi, (float)(y2 - (double)hi));
     }
   }
+  double sum_loss = 0.0;
+  if (!t.logits) {
+    const double z = (double)entry[tk];
+    if (lane == 0) {
+      sum_loss = state.some ? l - z : 0.0;
+      if (value) value[tk] = r == 0.f ? 0.f : (float)((double)r * expm1(z - l));
+    }
+  } else if (state.some) {
+    float best = -INFINITY;
+    for (int j = lane; j < t.top; j += 64)
+      if (entry_there(t, tk * t.top + j, vocab)) best = fmaxf(best, teacher_at(t, tk * t.top + j));
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) best = fmaxf(best, __shfl_xor(best, off, 64));
+    double mass = 0.0;
+    for (int j = lane; j < t.top; j += 64)
+      if (entry_there(t, tk * t.top + j, vocab)) mass += exp((double)teacher_at(t, tk * t.top + j) - (double)best);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) mass += __shfl_xor(mass, off, 64);
+    const double norm = (double)best + log(mass);
+    for (int j0 = 0; j0 < t.top; j0 += 64) {
+      const int j = j0 + lane;
+      const bool there = j < t.top && entry_there(t, tk * t.top + j, vocab);
+      const int v = there ? (int)index_at(t, tk * t.top + j) : -1;
+      const double z = there ? (double)entry[tk * t.top + j] : 0.0;
+      const double logq = there ? (double)teacher_at(t, tk * t.top + j) - norm : 0.0;
+      const double own = there ? exp(logq) : 0.0;
+      if (there) sum_loss += own * (logq - z + l);
+      if (value) {
+        double q = 0.0;                          // of every entry with this index
+        for (int k0 = 0; k0 < t.top; k0 += 64) {
+          const int k = k0 + lane;
+          int vk = v;
+          double qk = own;
+          if (k0 != j0) {
+            const bool kt = k < t.top && entry_there(t, tk * t.top + k, vocab);
+            vk = kt ? (int)index_at(t, tk * t.top + k) : -1;
+            qk = kt ? exp((double)teacher_at(t, tk * t.top + k) - norm) : 0.0;
+          }
+          const int n = t.top - k0 < 64 ? t.top - k0 : 64;
+          for (int w = 0; w < n; ++w) {
+            const int vw = __shfl(vk, w, 64);
+            const double qw = __shfl(qk, w, 64);
+            if (vw == v) q += qw;
+          }
+        }
+        if (j < t.top) value[tk * t.top + j] = there && r != 0.f ? (float)((double)r * (exp(z - l) - q)) : 0.f;
+      }
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum_loss += __shfl_xor(sum_loss, off, 64);
+  } else if (value) {
+    for (int j = lane; j < t.top; j += 64) value[tk * t.top + j] = 0.f;
+  }
+  if (lane == 0) loss[tk] = state.beyond ? __builtin_nanf("") : (float)((double)t.tau * (double)t.tau * sum_loss);
 }
 
 // ---- dz ----
 constexpr int kGradSpan = 4096;                  // vocabulary entries per block
 template <bool F32>
-__global__ __launch_bounds__(256) void head_grad_kernel(HeadTarget t, const float2* __restrict__ stats, long long stats_pitch, int grain_bits,
-                                                        const float* __restrict__ lse, const float* __restrict__ value,
+__global__ __launch_bounds__(256) void head_grad_kernel(HeadTarget t, float unit, const float2* __restrict__ stats, long long stats_pitch,
+                                                        const float2* __restrict__ log2sum, const float* __restrict__ value,
                                                         const float* __restrict__ scale, long long vocab, int spans,
                                                         const void* prob, long long pitch, u16* grad, long long plane) {
   const long long token = blockIdx.x / spans, v0 = (long long)(blockIdx.x % spans) * kGradSpan;
-  const float g = scale[token], l = lse[token];
+  const float g = scale[token];
+  const float2 l = log2sum[token];
   const long long row = token * pitch;
   for (long long v = v0 + threadIdx.x * 8; v < v0 + kGradSpan && v < pitch; v += 2048) {
     Row8 r{};
@@ -319,11 +414,10 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadTarget t, const floa
       if constexpr (F32) {
         const float* z = static_cast<const float*>(prob) + row + v;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r.v[e] = v + e < vocab ? g * __builtin_amdgcn_exp2f((z[e] - l) * kLog2e) : 0.f;
+        for (int e = 0; e < 8; ++e) r.v[e] = v + e < vocab ? g * __builtin_amdgcn_exp2f(fmaf(unit, z[e], -l.x) - l.y) : 0.f;
       } else {
         const u32x4 p = *reinterpret_cast<const u32x4*>(static_cast<const u16*>(prob) + row + v);
-        const float top = stats[(v >> grain_bits) * stats_pitch + token].x;
-        const float f = g * (__builtin_amdgcn_exp2f((top - l) * kLog2e) * (1.f / kProbScale));
+        const float f = g * __builtin_amdgcn_exp2f(-stats[v / kHeadGrain * stats_pitch + token].x - l.x - l.y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const unsigned pair = p[e / 2];        // (a bit cast of the vector's element itself would take its first)
@@ -368,96 +462,127 @@ typedef f32x4 f32x4_any __attribute__((aligned(4)));
 
 // fp32 results, parts of a sum, or both: four elements per lane and store.
 template <typename T>
-__device__ __forceinline__ void store_parts(const T& tile, const HeadOperand& l, const HeadOperand& r, const HeadTiles& g, const HeadOut& out, int split,
-                                            long long row0, long long col0) {
-      const int fr = tile.lane & 31, fh = tile.lane >> 5;
-      // fp32 destination, or none: then it is the bf16 result
-      float* to = g.splits > 1 ? out.partial + (long long)split * r.rows * l.rows : out.keep ? out.sum : out.f32 ? static_cast<float*>(out.out) : nullptr;
-      const float* add = g.splits > 1 || !out.add ? nullptr : out.sum;
-  #pragma unroll
-      for (int j = 0; j < T::FN; ++j) {
-        const long long n = col0 + tile.wn * T::WN + 32 * j + fr;
-  #pragma unroll
-        for (int i = 0; i < T::FM; ++i) {
-  #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const long long m = row0 + tile.wm * T::WM + 32 * i + 8 * q + 4 * fh, p = n * l.rows + m;
-            if (n >= r.rows || m >= l.rows) continue;
-            f32x4 x;
-  #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = tile.acc[i][j][4 * q + e];
-            if (m + 4 <= l.rows) {
-              if (add) x += *reinterpret_cast<const f32x4_any*>(add + p);
-              if (to) *reinterpret_cast<f32x4_any*>(to + p) = x;
-              else *reinterpret_cast<u32x2_any*>(static_cast<u16*>(out.out) + p) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-            } else {
-  #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if (m + e >= l.rows) continue;
-                const float y = add ? x[e] + add[p + e] : x[e];
-                if (to) to[p + e] = y;
-                else static_cast<u16*>(out.out)[p + e] = bf16_bits(y);
-              }
-            }
+__device__ __forceinline__ void store_parts(const T& tile, const HeadOperand& l, const HeadOperand& r, const HeadTiles& g, const HeadOut& out, float scale,
+                                            int split, long long row0, long long col0) {
+  const int fr = tile.lane & 31, fh = tile.lane >> 5;
+  // fp32 destination, or none: then it is the bf16 result
+  float* to = g.splits > 1 ? out.partial + (long long)split * r.rows * l.rows : out.keep ? out.sum : out.f32 ? static_cast<float*>(out.out) : nullptr;
+  const float* add = g.splits > 1 || !out.add ? nullptr : out.sum;
+#pragma unroll
+  for (int j = 0; j < T::FN; ++j) {
+    const long long n = col0 + tile.wn * T::WN + 32 * j + fr;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const long long m = row0 + tile.wm * T::WM + 32 * i + 8 * q + 4 * fh, p = n * l.rows + m;
+        if (n >= r.rows || m >= l.rows) continue;
+        f32x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = scale * tile.acc[i][j][4 * q + e];
+        if (m + 4 <= l.rows) {
+          if (add) x += *reinterpret_cast<const f32x4_any*>(add + p);
+          if (to) *reinterpret_cast<f32x4_any*>(to + p) = x;
+          else *reinterpret_cast<u32x2_any*>(static_cast<u16*>(out.out) + p) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (m + e >= l.rows) continue;
+            const float y = add ? x[e] + add[p + e] : x[e];
+            if (to) to[p + e] = y;
+            else static_cast<u16*>(out.out)[p + e] = bf16_bits(y);
           }
-          __builtin_amdgcn_sched_barrier(0);
         }
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
 }
 
 // bf16 results in whole, through the image in LDS.
 template <typename T>
-__device__ __forceinline__ void store_whole(const T& tile, const HeadOperand& l, const HeadOperand& r, const HeadOut& out, long long row0,
-                                            long long col0, unsigned char* smem) {
-  #pragma unroll
-      for (int j = 0; j < T::FN; ++j)
-  #pragma unroll
-        for (int i = 0; i < T::FM; ++i) {
-  #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            tile.put(smem, i, j, q, u32x2{pack_bf16(tile.acc[i][j][4 * q], tile.acc[i][j][4 * q + 1]), pack_bf16(tile.acc[i][j][4 * q + 2], tile.acc[i][j][4 * q + 3])});
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      __syncthreads();
-      tile.image_out(smem, [&](int c, int m, u32x4 v) {
-        const long long n = col0 + c;
-        if (n >= r.rows || row0 + m >= l.rows) return;
-        u16* to = static_cast<u16*>(out.out) + n * l.rows + row0 + m;
-        if (row0 + m + 8 <= l.rows) {
-          *reinterpret_cast<u32x4_any*>(to) = v;
-        } else {
-  #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (row0 + m + e < l.rows) to[e] = (u16)(v[e / 2] >> (16 * (e & 1)));
-        }
-      });
+__device__ __forceinline__ void store_whole(const T& tile, const HeadOperand& l, const HeadOperand& r, const HeadOut& out, float scale,
+                                            long long row0, long long col0, unsigned char* smem) {
+#pragma unroll
+  for (int j = 0; j < T::FN; ++j)
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = scale * tile.acc[i][j][4 * q + e];
+        tile.put(smem, i, j, q, u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])});
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  __syncthreads();
+  tile.image_out(smem, [&](int c, int m, u32x4 v) {
+    const long long n = col0 + c;
+    if (n >= r.rows || row0 + m >= l.rows) return;
+    u16* to = static_cast<u16*>(out.out) + n * l.rows + row0 + m;
+    if (row0 + m + 8 <= l.rows) {
+      *reinterpret_cast<u32x4_any*>(to) = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (row0 + m + e < l.rows) to[e] = (u16)(v[e / 2] >> (16 * (e & 1)));
+    }
+  });
 }
 
 template <int B, bool RKM, bool IMAGE>
-__device__ __forceinline__ void product_tile(const HeadOperand& l, const HeadOperand& r, const HeadTiles& g, const HeadOut& out, unsigned char* smem) {
+__device__ __forceinline__ void product_tile(const HeadOperand& l, const HeadOperand& r, const HeadTiles& g, const HeadOut& out, int split,
+                                             long long row0, long long col0, unsigned char* smem) {
   using T = Tile<B, B, true, RKM>;
-  const TileAt at = tile_at(g);
-  const long long row0 = (long long)at.m * B, col0 = (long long)at.n * B;
   const int slabs = (int)((g.k + kHeadSlab - 1) / kHeadSlab) * g.pairs;
-  const int first = at.split * g.slabs_per_split, last = first + g.slabs_per_split < slabs ? first + g.slabs_per_split : slabs;
+  const int first = split * g.slabs_per_split, last = first + g.slabs_per_split < slabs ? first + g.slabs_per_split : slabs;
   T tile;
-  tile.run(l, r, row0, col0, g.k, first, last, smem);
-  if constexpr (IMAGE) store_whole(tile, l, r, out, row0, col0, smem);
-  else store_parts(tile, l, r, g, out, at.split, row0, col0);
+  tile.run(l, r, row0, col0, g.k, g.pairs, first, last, smem);
+  const float scale = out.scale * (out.peak ? *out.peak : 1.f);
+  if constexpr (IMAGE) store_whole(tile, l, r, out, scale, row0, col0, smem);
+  else store_parts(tile, l, r, g, out, scale, split, row0, col0);
 }
 
 template <int B, bool RKM, bool IMAGE>
 __global__ __launch_bounds__(256, B == 256 ? 1 : 2) void head_product_kernel(HeadOperand l, HeadOperand r, HeadTiles g, HeadOut out) {
+#if defined(__HIP_DEVICE_COMPILE__)            // (the host's pass knows no buffer descriptors)
   extern __shared__ __align__(16) unsigned char smem[];
-  product_tile<B, RKM, IMAGE>(l, r, g, out, smem);
+  const TileAt at = tile_at(g);
+  long long row0 = (long long)at.m * B, col0 = (long long)at.n * B;
+  if (B == 128 || at.quarter < 0) {
+    product_tile<B, RKM, IMAGE>(l, r, g, out, at.split, row0, col0, smem);
+  } else if constexpr (B == 256) {
+    row0 += 128 * (at.quarter >> 1);
+    col0 += 128 * (at.quarter & 1);
+    if (row0 < l.rows && col0 < r.rows) product_tile<128, RKM, IMAGE>(l, r, g, out, at.split, row0, col0, smem);
+  }
+#endif
 }
 
+// 256 elements per block, four per thread; the splits over the block's waves, joined in LDS.
 __global__ __launch_bounds__(256) void head_sum_splits_kernel(HeadOut out, int splits, long long count) {
-  const long long at = blockIdx.x * 256ll + threadIdx.x;
-  if (at >= count) return;
-  float x = 0.f;
-  for (int u = 0; u < splits; ++u) x += out.partial[u * count + at];
-  finish_out(out, at, x);
+  __shared__ f32x4 parts[3][64];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const long long at = blockIdx.x * 256ll + 4 * lane;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  if (at + 4 <= count) {
+#pragma unroll 4
+    for (int u = wave; u < splits; u += 4) x += *reinterpret_cast<const f32x4_any*>(out.partial + u * count + at);
+  } else {
+    for (int u = wave; u < splits; u += 4)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (at + e < count) x[e] += out.partial[u * count + at + e];
+  }
+  if (wave > 0) parts[wave - 1][lane] = x;
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) x += parts[w][lane];
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (at + e < count) finish_out(out, at + e, x[e]);
 }
 
 __global__ __launch_bounds__(256) void fill_zero_kernel(u16* p, size_t n) {
@@ -465,7 +590,7 @@ __global__ __launch_bounds__(256) void fill_zero_kernel(u16* p, size_t n) {
 }
 
 HeadTiles tiles_of(const HeadProduct& g, int pairs) {
-  return {g.k, pairs, g.tiles_m, g.tiles_n, g.splits, g.slabs_per_split};
+  return {g.k, pairs, g.tiles_m, g.tiles_n, g.whole, g.splits, g.slabs_per_split};
 }
 unsigned blocks_for(long long threads) {
   const long long b = (threads + 255) / 256;
@@ -486,23 +611,23 @@ hipError_t allow_lds(std::atomic<uint64_t>& done, const void* kernel, int bytes)
 }
 
 template <int B, bool PROB, bool F32>
-hipError_t logits_of(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float inv_tau, float2* stats,
+hipError_t logits_of(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, float2* stats,
                      long long stats_pitch, void* prob, long long prob_pitch, hipStream_t s) {
   constexpr int lds = Tile<B, B, false, false>::kLds;
   static std::atomic<uint64_t> done{0};
   if (hipError_t e = allow_lds(done, reinterpret_cast<const void*>(&head_logits_kernel<B, PROB, F32>), lds)) return e;
-  head_logits_kernel<B, PROB, F32><<<(unsigned)((long long)g.tiles_m * g.tiles_n), 256, lds, s>>>(weight, hidden, tiles_of(g, pairs), inv_tau, stats, stats_pitch, prob,
+  head_logits_kernel<B, PROB, F32><<<(unsigned)g.blocks(), 256, lds, s>>>(weight, hidden, tiles_of(g, pairs), unit, stats, stats_pitch, prob,
                                                                      prob_pitch);
   return hipGetLastError();
 }
 
-hipError_t launch_head_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float inv_tau,
+hipError_t launch_head_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit,
                               float2* stats, long long stats_pitch, void* prob, long long prob_pitch, int prob_f32, hipStream_t s) {
   auto go = [&](auto b) {
     constexpr int B = decltype(b)::value;
-    if (!prob) return logits_of<B, false, false>(weight, hidden, g, pairs, inv_tau, stats, stats_pitch, prob, prob_pitch, s);
-    if (prob_f32) return logits_of<B, true, true>(weight, hidden, g, pairs, inv_tau, stats, stats_pitch, prob, prob_pitch, s);
-    return logits_of<B, true, false>(weight, hidden, g, pairs, inv_tau, stats, stats_pitch, prob, prob_pitch, s);
+    if (!prob) return logits_of<B, false, false>(weight, hidden, g, pairs, unit, stats, stats_pitch, prob, prob_pitch, s);
+    if (prob_f32) return logits_of<B, true, true>(weight, hidden, g, pairs, unit, stats, stats_pitch, prob, prob_pitch, s);
+    return logits_of<B, true, false>(weight, hidden, g, pairs, unit, stats, stats_pitch, prob, prob_pitch, s);
   };
   return g.tile == 256 ? go(std::integral_constant<int, 256>{}) : go(std::integral_constant<int, 128>{});
 }
@@ -512,7 +637,7 @@ hipError_t product_of(const HeadOperand& l, const HeadOperand& r, const HeadProd
   constexpr int lds = Tile<B, B, true, RKM>::kLds;
   static std::atomic<uint64_t> done{0};
   if (hipError_t e = allow_lds(done, reinterpret_cast<const void*>(&head_product_kernel<B, RKM, IMAGE>), lds)) return e;
-  head_product_kernel<B, RKM, IMAGE><<<(unsigned)((long long)g.tiles_m * g.tiles_n * g.splits), 256, lds, s>>>(l, r, tiles_of(g, pairs), out);
+  head_product_kernel<B, RKM, IMAGE><<<(unsigned)g.blocks(), 256, lds, s>>>(l, r, tiles_of(g, pairs), out);
   return hipGetLastError();
 }
 
@@ -551,19 +676,25 @@ hipError_t launch_head_entries(const HeadTarget& t, const void* hidden, long lon
   return f32 ? go(head_entries_kernel<true>) : go(head_entries_kernel<false>);
 }
 
-hipError_t launch_head_join(const HeadTarget& t, const float2* stats, long long stats_pitch, long long blocks, const float* entry,
-                            long long tokens, long long vocab, float* loss, float* lse, float* value, float* scale, hipStream_t s) {
-  head_join_kernel<<<(unsigned)((tokens + 15) / 16), 256, 0, s>>>(t, stats, stats_pitch, blocks, entry, tokens, vocab, loss, lse, value,
-                                                                 scale);
+hipError_t launch_head_peak(const float* token_scale, long long tokens, float* peak, hipStream_t s) {
+  head_peak_kernel<<<1, 1024, 0, s>>>(token_scale, tokens, peak);
   return hipGetLastError();
 }
 
-hipError_t launch_head_grad(const HeadTarget& t, const float2* stats, long long stats_pitch, int grain, const float* lse,
+hipError_t launch_head_join(const HeadTarget& t, float unit, const float* peak, const float2* stats, long long stats_pitch, long long blocks,
+                            const float* entry, long long tokens, long long vocab, float* loss, float* lse, float* value, float* scale,
+                            float2* log2sum, hipStream_t s) {
+  head_join_kernel<<<(unsigned)((tokens + 15) / 16), 1024, 0, s>>>(t, unit, peak, stats, stats_pitch, blocks, entry, tokens, vocab, loss, lse,
+                                                                  value, scale, log2sum);
+  return hipGetLastError();
+}
+
+hipError_t launch_head_grad(const HeadTarget& t, float unit, const float2* stats, long long stats_pitch, const float2* log2sum,
                             const float* value, const float* scale, long long tokens, long long vocab, const void* prob, long long pitch,
                             int f32, u16* grad, long long plane, hipStream_t s) {
   const int spans = (int)((pitch + kGradSpan - 1) / kGradSpan);
   auto go = [&](auto kernel) {
-    kernel<<<(unsigned)(tokens * spans), 256, 0, s>>>(t, stats, stats_pitch, __builtin_ctz(grain), lse, value, scale, vocab, spans, prob, pitch, grad, plane);
+    kernel<<<(unsigned)(tokens * spans), 256, 0, s>>>(t, unit, stats, stats_pitch, log2sum, value, scale, vocab, spans, prob, pitch, grad, plane);
     return hipGetLastError();
   };
   return f32 ? go(head_grad_kernel<true>) : go(head_grad_kernel<false>);
