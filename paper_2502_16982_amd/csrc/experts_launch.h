@@ -8,13 +8,14 @@ namespace muon {
 
 constexpr int kMaxExperts = 4096, kMaxExpertTop = 64;
 constexpr int64_t kMaxExpertPairs = (1ll << 31) - (1 << 16);      // positions are 32-bit, and so is the last block's end
-// Pairs per block of the sort: one block for all of few, never more than kSortBlocks of them.
-constexpr int kSortChunk = 2048, kSortBlocks = 256;
+// Pairs per block of the sort: one block for few, otherwise 512 and never more than kSortBlocks blocks.
+constexpr int kSortAlone = 2048, kSortChunk = 512, kSortBlocks = 256;
 inline int64_t sort_chunk(int64_t pairs) {
+  if (pairs <= kSortAlone) return kSortAlone;
   const int64_t even = (pairs + kSortBlocks - 1) / kSortBlocks;
   return even <= kSortChunk ? kSortChunk : (even + 255) / 256 * 256;
 }
-inline int sort_blocks(int64_t pairs) { return pairs <= kSortChunk ? 1 : (int)((pairs + sort_chunk(pairs) - 1) / sort_chunk(pairs)); }
+inline int sort_blocks(int64_t pairs) { return pairs <= kSortAlone ? 1 : (int)((pairs + sort_chunk(pairs) - 1) / sort_chunk(pairs)); }
 
 hipError_t launch_expert_sort(const void* expert, int index64, int64_t pairs, int experts, int* position, int* source, int* offsets,
                               int* counts, hipStream_t s);

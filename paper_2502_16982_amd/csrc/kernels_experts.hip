@@ -229,6 +229,7 @@ __global__ __launch_bounds__(256) void expert_dispatch_kernel(ExpertRows r, cons
 template <int BYTES, bool F32>
 __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows r, const void* __restrict__ rows_, const float* __restrict__ weights,
                                                              void* __restrict__ out_, long long pieces, int lanes) {
+  constexpr int ROWS = 8;
   using P = Piece<BYTES, F32>;
   using Raw = typename P::Raw;
   const Raw* rows = static_cast<const Raw*>(rows_);
@@ -239,17 +240,20 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows r, const
     float sum[P::N];
 #pragma unroll
     for (int e = 0; e < P::N; ++e) sum[e] = 0.f;
-    for (int j0 = 0; j0 < r.top; j0 += 4) {
-      Raw v[4];
-      float w[4];
+    for (int j0 = 0; j0 < r.top; j0 += ROWS) {   // ROWS rows on their way at a time
+      long long row[ROWS];
+      float w[ROWS];
+      Raw v[ROWS];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const long long i = token * r.top + j0 + u, row = j0 + u < r.top ? row_of(r, i) : -1;
-        w[u] = row < 0 ? 0.f : weights ? weights[i] : 1.f;
-        v[u] = row < 0 ? Raw{} : rows[row * pieces + c];
+      for (int u = 0; u < ROWS; ++u) {
+        const long long i = token * r.top + j0 + u;
+        row[u] = j0 + u < r.top ? row_of(r, i) : -1;
+        w[u] = row[u] < 0 ? 0.f : weights ? weights[i] : 1.f;
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < ROWS; ++u) v[u] = row[u] < 0 ? Raw{} : rows[row[u] * pieces + c];
+#pragma unroll
+      for (int u = 0; u < ROWS; ++u) {
         float f[P::N];
         P::unpack(v[u], f);
 #pragma unroll

@@ -17,18 +17,22 @@ namespace {
 
 using namespace head;
 
-// ---- loads of rows of any alignment ----
+// Global memory takes 16 (8) bytes at any address of an element.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+
 struct Row8 {
   float v[8];
 };
-// Elements [c, c + 8) of a row of `width` elements, zero behind its end.  vec: the row starts at a multiple of 16 bytes.
+// Elements [c, c + 8) of a row of `width` elements, zero behind its end.
 template <bool F32>
-__device__ __forceinline__ Row8 load_row8(const void* base, long long row_at, long long c, long long width, bool vec) {
+__device__ __forceinline__ Row8 load_row8(const void* base, long long row_at, long long c, long long width) {
   Row8 r;
   if constexpr (F32) {
     const float* p = static_cast<const float*>(base) + row_at + c;
-    if (vec && c + 8 <= width) {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+    if (c + 8 <= width) {
+      const f32x4 a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) r.v[e] = a[e], r.v[4 + e] = b[e];
     } else {
@@ -37,8 +41,8 @@ __device__ __forceinline__ Row8 load_row8(const void* base, long long row_at, lo
     }
   } else {
     const u16* p = static_cast<const u16*>(base) + row_at + c;
-    if (vec && c + 8 <= width) {
-      const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+    if (c + 8 <= width) {
+      const u32x4 a = *reinterpret_cast<const u32x4_any*>(p);
 #pragma unroll
       for (int e = 0; e < 4; ++e) r.v[2 * e] = bf16_lo(a[e]), r.v[2 * e + 1] = bf16_hi(a[e]);
     } else {
@@ -47,10 +51,6 @@ __device__ __forceinline__ Row8 load_row8(const void* base, long long row_at, lo
     }
   }
   return r;
-}
-template <bool F32>
-__device__ __forceinline__ bool row_is_aligned(const void* base, long long row_at) {
-  return ((reinterpret_cast<uintptr_t>(base) + (F32 ? 4 : 2) * row_at) & 15) == 0;
 }
 // Eight fp32 values as operand planes: each plane what the ones before it left, rounded to bf16.
 template <bool F32>
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void head_pack_kernel(const void* __restrict__
   const long long chunks = ld / 8;
   for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n * chunks; i += gridDim.x * 256ll) {
     const long long row = i / chunks, c = (i - row * chunks) * 8;
-    store_planes8<F32>(load_row8<F32>(src, row * stride, c, width, row_is_aligned<F32>(src, row * stride)), dst + row * ld + c, plane);
+    store_planes8<F32>(load_row8<F32>(src, row * stride, c, width), dst + row * ld + c, plane);
   }
 }
 
@@ -118,14 +118,12 @@ __global__ __launch_bounds__(256) void head_entries_kernel(HeadTarget t, const v
                                                            long long plane) {
   const long long token = blockIdx.x, at = token * hidden_stride;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const bool hvec = row_is_aligned<F32>(hidden, at);
   for (int j = wave; j < t.top; j += 4) {
     const long long v = index_at(t, token * t.top + j);
     float sum = 0.f;
     if (v >= 0 && v < vocab) {
-      const bool wvec = row_is_aligned<F32>(weight, v * weight_stride);
       for (long long c = lane * 8; c < width; c += 512) {
-        const Row8 a = load_row8<F32>(hidden, at, c, width, hvec), b = load_row8<F32>(weight, v * weight_stride, c, width, wvec);
+        const Row8 a = load_row8<F32>(hidden, at, c, width), b = load_row8<F32>(weight, v * weight_stride, c, width);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum = fmaf(a.v[e], b.v[e], sum);
       }
@@ -138,7 +136,7 @@ __global__ __launch_bounds__(256) void head_entries_kernel(HeadTarget t, const v
     const bool kept = token_scale(t, token, token_state(t, token, vocab)) != 0.f;
     for (long long c = threadIdx.x * 8; c < ld; c += 2048) {
       Row8 r{};
-      if (kept) r = load_row8<F32>(hidden, at, c, width, hvec);
+      if (kept) r = load_row8<F32>(hidden, at, c, width);
       store_planes8<F32>(r, masked + token * ld + c, plane);
     }
   }
@@ -454,11 +452,6 @@ __device__ __forceinline__ void finish_out(const HeadOut& o, long long at, float
   if (o.keep) o.sum[at] = x;
   else store_out(o, at, x);
 }
-
-// Global memory takes 16 (8) bytes at any address of an element.
-typedef u32x4 u32x4_any __attribute__((aligned(2)));
-typedef u32x2 u32x2_any __attribute__((aligned(2)));
-typedef f32x4 f32x4_any __attribute__((aligned(4)));
 
 // fp32 results, parts of a sum, or both: four elements per lane and store.
 template <typename T>

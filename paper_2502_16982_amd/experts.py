@@ -10,6 +10,7 @@ from typing import NamedTuple, Optional, Tuple
 import torch
 
 from . import binding
+from ._device import on, stream_handle
 from .binding import MuonError
 
 
@@ -21,16 +22,11 @@ class Routing(NamedTuple):
     offsets: torch.Tensor
 
 
-def _device(tensors: dict) -> torch.device:
-    devices = {name: t.device for name, t in tensors.items() if t is not None}
-    device = next(iter(devices.values()))
-    if device.type != "cuda" or any(d != device for d in devices.values()):
-        raise MuonError(-1, f"tensors of one GPU, not {devices}")
+def _device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> torch.device:
+    device = first.device
+    if device.type != "cuda" or any(t is not None and t.device != device for t in others):
+        raise MuonError(-1, f"tensors of one GPU, not {[str(t.device) for t in (first, *others) if t is not None]}")
     return device
-
-
-def _stream(device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
 
 
 def _routing(routing: Routing) -> "binding.muon_routing":
@@ -74,26 +70,27 @@ def sort_by_expert(expert: torch.Tensor, experts: int) -> Routing:
         raise MuonError(-1, f"expert: contiguous [tokens, top], not {tuple(expert.shape)}")
     if expert.dtype not in (torch.int32, torch.int64):
         raise MuonError(-2, f"expert: int32 or int64, not {expert.dtype}")
-    device = _device({"expert": expert})
+    device = _device(expert)
     tokens, top = expert.shape
     need = binding.muon_expert_sort_bytes(tokens, top, experts)
-    with torch.cuda.device(device):
+    with on(device):
         # one allocation for what is written; the workspace goes back to the stream it was used on
-        ints = torch.empty(2 * tokens * top + experts + 1, dtype=torch.int32, device=device)
-        position, source, offsets = ints.split([tokens * top, tokens * top, experts + 1])
+        pairs = tokens * top
+        ints = torch.empty(2 * pairs + experts + 1, dtype=torch.int32, device=device)
+        position, source, offsets = ints[:pairs].view(tokens, top), ints[pairs:2 * pairs], ints[2 * pairs:]
         workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
         binding.muon_expert_sort(expert.data_ptr(), expert.element_size(), tokens, top, experts, position.data_ptr(), source.data_ptr(),
-                                 offsets.data_ptr(), 0 if workspace is None else workspace.data_ptr(), need, _stream(device))
-    return Routing(position.view(tokens, top), source, offsets)
+                                 offsets.data_ptr(), 0 if workspace is None else workspace.data_ptr(), need, stream_handle(device))
+    return Routing(position, source, offsets)
 
 
 def dispatch(x: torch.Tensor, routing: Routing) -> torch.Tensor:
     """Rows [tokens * top, width] of ``x`` [tokens, width] in the experts' order; zero behind the last pair's."""
-    r, device = _routing(routing), _device({"x": x, "position": routing.position, "offsets": routing.offsets})
+    r, device = _routing(routing), _device(x, routing.position, routing.offsets)
     stride, width = _tokens("x", x, r.tokens)
-    with torch.cuda.device(device):
+    with on(device):
         rows = torch.empty(r.tokens * r.top, width, dtype=x.dtype, device=device)
-        binding.muon_expert_dispatch(r, x.data_ptr(), stride, width, binding.dtype_code(x.dtype), rows.data_ptr(), _stream(device))
+        binding.muon_expert_dispatch(r, x.data_ptr(), stride, width, binding.dtype_code(x.dtype), rows.data_ptr(), stream_handle(device))
     return rows
 
 
@@ -105,26 +102,26 @@ def dispatch_backward(d_rows: torch.Tensor, routing: Routing) -> torch.Tensor:
 def combine(rows: torch.Tensor, weights: Optional[torch.Tensor], routing: Routing) -> torch.Tensor:
     """[tokens, width]: the sum of each token's rows, times ``weights`` [tokens, top] in fp32 (None: all 1)."""
     r = _routing(routing)
-    device = _device({"rows": rows, "weights": weights, "position": routing.position, "offsets": routing.offsets})
+    device = _device(rows, weights, routing.position, routing.offsets)
     width, at = _rows("rows", rows, routing.position), 0 if weights is None else _weights(weights, routing.position)
-    with torch.cuda.device(device):
+    with on(device):
         out = torch.empty(r.tokens, width, dtype=rows.dtype, device=device)
-        binding.muon_expert_combine(r, rows.data_ptr(), at, width, binding.dtype_code(rows.dtype), out.data_ptr(), _stream(device))
+        binding.muon_expert_combine(r, rows.data_ptr(), at, width, binding.dtype_code(rows.dtype), out.data_ptr(), stream_handle(device))
     return out
 
 
 def combine_backward(d_out: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor, routing: Routing) -> Tuple[torch.Tensor, torch.Tensor]:
     """(d_rows, d_weights) of ``combine(rows, weights, routing)`` for its result's gradient."""
     r = _routing(routing)
-    device = _device({"d_out": d_out, "rows": rows, "weights": weights, "position": routing.position, "offsets": routing.offsets})
+    device = _device(d_out, rows, weights, routing.position, routing.offsets)
     width, at = _rows("rows", rows, routing.position), _weights(weights, routing.position)
     stride, d_width = _tokens("d_out", d_out, r.tokens)
     if d_width != width:
         raise MuonError(-1, f"d_out: [{r.tokens}, {width}], not {tuple(d_out.shape)}")
     if d_out.dtype != rows.dtype:
         raise MuonError(-2, f"d_out and rows of one dtype, not {d_out.dtype} and {rows.dtype}")
-    with torch.cuda.device(device):
+    with on(device):
         d_rows, d_weights = torch.empty_like(rows), torch.empty_like(weights)
         binding.muon_expert_combine_backward(r, d_out.data_ptr(), stride, rows.data_ptr(), at, width, binding.dtype_code(rows.dtype),
-                                             d_rows.data_ptr(), d_weights.data_ptr(), _stream(device))
+                                             d_rows.data_ptr(), d_weights.data_ptr(), stream_handle(device))
     return d_rows, d_weights

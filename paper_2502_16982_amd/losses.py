@@ -10,6 +10,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding
+from ._device import on, stream_handle
 from .binding import MuonError
 
 
@@ -51,12 +52,12 @@ class LossHead:
     def _fit(self, head: "binding.muon_head", top: int, gradients: int) -> None:
         """A workspace that holds the call; what there is stays where it suffices."""
         need = binding.muon_head_workspace_bytes(head, top, gradients, self.max_workspace_bytes)
-        stream = torch.cuda.current_stream(self.device)
+        stream = stream_handle(self.device)
         if self.workspace is None or self.workspace.numel() < need:
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
             self._stream = stream
         elif stream != self._stream:                       # the memory outlives what this stream does with it
-            self.workspace.record_stream(stream)
+            self.workspace.record_stream(torch.cuda.current_stream(self.device))
 
     def _head(self, hidden: torch.Tensor, weight: torch.Tensor) -> "binding.muon_head":
         if hidden.dim() != 2 or weight.dim() != 2 or hidden.shape[1] != weight.shape[1]:
@@ -109,11 +110,11 @@ class LossHead:
         if targets.shape != (hidden.shape[0],) or not targets.is_contiguous():
             raise MuonError(-1, f"targets: contiguous [{hidden.shape[0]}], not {tuple(targets.shape)}")
         size, scale = _index_bytes(targets, "targets"), self._scale(token_scale, hidden.shape[0])
-        with torch.cuda.device(self.device):
+        with on(self.device):
             out, which = self._outputs(hidden, weight, gradients)
             self._fit(head, 1, which)
             binding.muon_cross_entropy(head, targets.data_ptr(), size, scale, *self._pointers(out), self.workspace.data_ptr(),
-                                       self.workspace.numel(), torch.cuda.current_stream(self.device).cuda_stream)
+                                       self.workspace.numel(), stream_handle(self.device))
         return out
 
     def distill(self, hidden: torch.Tensor, weight: torch.Tensor, teacher_index: torch.Tensor, teacher_logits: torch.Tensor,
@@ -129,10 +130,10 @@ class LossHead:
         if not (teacher_index.is_contiguous() and teacher_logits.is_contiguous()):
             raise MuonError(-1, "teacher_index and teacher_logits must be contiguous")
         size, scale, top = _index_bytes(teacher_index, "teacher_index"), self._scale(token_scale, hidden.shape[0]), teacher_index.shape[1]
-        with torch.cuda.device(self.device):
+        with on(self.device):
             out, which = self._outputs(hidden, weight, gradients)
             self._fit(head, top, which)
             binding.muon_distill(head, teacher_index.data_ptr(), size, teacher_logits.data_ptr(), binding.dtype_code(teacher_logits.dtype),
                                  top, temperature, scale, *self._pointers(out), self.workspace.data_ptr(), self.workspace.numel(),
-                                 torch.cuda.current_stream(self.device).cuda_stream)
+                                 stream_handle(self.device))
         return out
