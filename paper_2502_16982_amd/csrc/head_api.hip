@@ -54,10 +54,10 @@ int run_head(const muon_head* h, const HeadTarget& target, const HeadOutputs& ou
   const bool gradients = shape.d_hidden || shape.d_weight;
   const float unit = (float)(1.44269504088896340736 * (double)target.inv_tau);
   // dz goes through the products over the largest scale: where all are alike the target's entries stay near -1, which bf16 holds exactly
-  const float* peak = nullptr;
+  float* peak = nullptr;
   if (gradients && target.token_scale) {
     peak = f32_at(p.peak);
-    MUON_HIP(launch_head_peak(target.token_scale, shape.tokens, f32_at(p.peak), s));
+    MUON_HIP(launch_head_peak(target.token_scale, shape.tokens, peak, s));
   }
 
   HeadOperand weight{static_cast<const uint16_t*>(h->weight), h->weight_stride, 0, shape.vocab};
@@ -87,7 +87,7 @@ int run_head(const muon_head* h, const HeadTarget& target, const HeadOutputs& ou
     MUON_HIP(launch_head_logits(weight, hidden, p.logits[last], p.pairs, unit, stats, p.piece, gradients ? ws + p.prob : nullptr,
                                 p.vocab_pitch, shape.f32, s));
     float2* log2sum = reinterpret_cast<float2*>(ws + p.lse);
-    MUON_HIP(launch_head_join(t, unit, peak, stats, p.piece, p.blocks, f32_at(p.entry), n, shape.vocab, out.loss + t0,
+    MUON_HIP(launch_head_join(t, unit, target.token_scale, shape.tokens, peak, stats, p.piece, p.blocks, f32_at(p.entry), n, shape.vocab, out.loss + t0,
                               out.lse ? out.lse + t0 : nullptr, gradients ? f32_at(p.value) : nullptr, f32_at(p.scale), log2sum, s));
     if (!gradients) continue;
     const int64_t grad_plane = p.piece * p.vocab_pitch;

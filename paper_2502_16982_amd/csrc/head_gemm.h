@@ -164,28 +164,29 @@ struct Side {
       for (int kk = 0; kk < 4; ++kk) read[kk] = lds + (place * W + fr) * 128 + (((2 * kk + fh) ^ ((fr >> 1) & 7)) * 16);
     }
   }
-  // Slab number kt of plane p.  k: K.
-  struct Source {
-    __amdgpu_buffer_rsrc_t r;
-    unsigned offset;
-  };
-  __device__ __forceinline__ Source source(int p, int kt, long long k) const {
-    const u16* at = base + p * plane + kt * slab;
-    const long long left = k - (long long)kt * kHeadSlab;             // > 0
-    int bytes;
-    unsigned off = offset;
-    if constexpr (KM) {
-      bytes = (int)(unsigned)(((left < kHeadSlab ? left : kHeadSlab) - 1) * ld * 2 + tail);
-      if (tail == 0) bytes = 0;
-    } else {
-      const long long there = (long long)rows_bytes - (long long)kt * (kHeadSlab * 2);
-      bytes = there < 0 ? 0 : (int)(unsigned)there;
-      if (chunk * 8 >= left) off = 0x80000000u;                       // behind K: out of the descriptor's range
-    }
-    return {__builtin_amdgcn_make_buffer_rsrc(const_cast<u16*>(at), 0, bytes, 0x00020000), off};
+  // The slab that is loaded next: its descriptor's base and size, the lane's offset in it.
+  const u16* at;
+  int bytes;
+  unsigned here;
+  __device__ __forceinline__ void clip(int left) {                    // left: elements of K from this slab on, fewer than a slab
+    if constexpr (KM) bytes = (int)((unsigned)(left - 1) * (unsigned)(ld * 2) + tail);
+    else here = chunk * 8 >= left ? 0x80000000u : offset;             // behind K: out of the descriptor's range
   }
-  __device__ __forceinline__ void load(const Source& s, int n, unsigned char* lds, int wave) const {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(s.r, (lptr)(lds + wave * 1024 + n * NW * 1024), 16, s.offset + n * step, 0, 0, 0);
+  __device__ __forceinline__ void start(int p, int kt, long long k) {
+    at = base + p * plane + kt * slab;
+    here = offset;
+    if constexpr (KM) bytes = (int)((unsigned)(kHeadSlab - 1) * (unsigned)(ld * 2) + tail);
+    else bytes = (int)(rows_bytes - (unsigned)kt * (kHeadSlab * 2));
+    if (k - (long long)kt * kHeadSlab < kHeadSlab) clip((int)(k - (long long)kt * kHeadSlab));
+  }
+  __device__ __forceinline__ void advance(int left) {
+    at += slab;
+    if constexpr (!KM) bytes -= kHeadSlab * 2;
+    if (left < kHeadSlab) clip(left);
+  }
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t source() const { return __builtin_amdgcn_make_buffer_rsrc(const_cast<u16*>(at), 0, bytes, 0x00020000); }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, int n, unsigned char* lds, int wave) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lptr)(lds + wave * 1024 + n * NW * 1024), 16, here + n * step, 0, 0, 0);
   }
   // Read number n of k-step KK from the stage that lies `stage` bytes behind the first.
   template <int KK, int N>
@@ -203,18 +204,27 @@ __device__ __forceinline__ void wait_lds() {
   asm volatile("s_waitcnt lgkmcnt(%0)" : : "n"(N) : "memory");
 }
 
+// At most N loads of this wave on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
 // A BM x BN tile of T = L R^T by four waves in 2 x 2: acc[i][j] of a wave holds, in lane (r, h), column 32 j + r and rows
-// 32 i + 8 q + 4 h + e.  Two stages of LDS, 64 of K each.  The loop is skewed by one k-step of 16 so that no product waits for LDS: in
+// 32 i + 8 q + 4 h + e.  A ring of S stages of LDS, 64 of K each.  Two stages (what fills the chip): the loop is skewed by one k-step of 16 so that no product waits for LDS: in
 // iteration kt (slab kt in stage `cur`, its first fragments in registers)
 //   A  products of k-step 3 of slab kt - 1 | reads of k-step 1
 //   B  products of k-step 0                | reads of k-steps 2, 3; then: my reads of `cur` and my loads of slab kt + 1 are done; barrier
 //   C  products of k-steps 1, 2            | loads of slab kt + 2 into `cur`, reads of k-step 0 of slab kt + 1
+// Four stages (a tile of 128 that has a compute unit to itself, whose phases would be too short to hide LDS and whose slabs would be waited
+// for): all fragments of slab kt + 1 are read behind the first half of the products of slab kt, with two to three slabs on their way.
 // One instruction of each kind between two products, never in bursts; the order is held by scheduling fences.  LDS reads are written in
 // assembly (the compiler puts a wait for all loads in front of its own transposing read) and waited for by hand.
-template <int BM_, int BN_, bool LKM, bool RKM>
+template <int BM_, int BN_, bool LKM, bool RKM, int S = 2>
 struct Tile {
   static constexpr int BM = BM_, BN = BN_, WM = BM / 2, WN = BN / 2, FM = WM / 32, FN = WN / 32;
-  static constexpr int kStage = (BM + BN) * 128, kLds = 2 * kStage;
+  static constexpr int kStage = (BM + BN) * 128, kLds = S * kStage;
   using L = Side<BM, WM, FM, LKM>;
   using R = Side<BN, WN, FN, RKM>;
   f32x16 acc[FM][FN];
@@ -238,109 +248,189 @@ struct Tile {
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
 
+    // A slab after the other; the descriptors move along with the loop, what K's end and the next pair of planes take is done where it occurs.
     const int per_pair = (int)((k + kHeadSlab - 1) / kHeadSlab);
-    int next_pair = first / per_pair, next_kt = first - next_pair * per_pair;      // of the slab that is loaded next
-    typename L::Source ls;
-    typename R::Source rs;
+    int pair = first / per_pair, ahead = (int)(k - (long long)(first - pair * per_pair) * kHeadSlab);       // of K from the next slab on
+    l.start(pair_left(pairs, pair), first - pair * per_pair, k);
+    r.start(pair_right(pairs, pair), first - pair * per_pair, k);
     auto take_next = [&]() {
-      ls = l.source(pair_left(pairs, next_pair), next_kt, k);
-      rs = r.source(pair_right(pairs, next_pair), next_kt, k);
-      if (++next_kt == per_pair) next_kt = 0, ++next_pair;
+      ahead -= kHeadSlab;
+      if (ahead > 0) {
+        l.advance(ahead);
+        r.advance(ahead);
+      } else {
+        ++pair;
+        ahead = (int)k;
+        l.start(pair_left(pairs, pair), 0, k);
+        r.start(pair_right(pairs, pair), 0, k);
+      }
     };
     constexpr int LOADS = L::LOADS + R::LOADS;
     auto load_one = [&](int stage, int n) {
-      if (n < L::LOADS) l.load(ls, n, smem + stage * kStage, wave);
-      else r.load(rs, n - L::LOADS, smem + stage * kStage + BM * 128, wave);
+      if (n < L::LOADS) l.load(l.source(), n, smem + stage * kStage, wave);
+      else r.load(r.source(), n - L::LOADS, smem + stage * kStage + BM * 128, wave);
     };
     const int count = last - first;
-    take_next();
+    static_for<0, S>([&](auto n_tag) {
+      constexpr int n = decltype(n_tag)::value;
+      if (n < count) {
+        if constexpr (n > 0) take_next();
 #pragma unroll
-    for (int n = 0; n < LOADS; ++n) load_one(0, n);
-    if (count > 1) {
-      take_next();
-#pragma unroll
-      for (int n = 0; n < LOADS; ++n) load_one(1, n);
-    }
-    __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));             // vmcnt(0)
+        for (int u = 0; u < LOADS; ++u) load_one(n, u);
+      }
+    });
+    if (count >= S) wait_loads<(S - 1) * LOADS>();                    // slab 0 has landed
+    else wait_loads<0>();
     __syncthreads();
 
-    Frag<LKM, FM> a[4];
-    Frag<RKM, FN> b[4];
     constexpr int READS = L::READS + R::READS, MT = FM * FN;
-    auto read = [&](int stage, auto kk, auto n) {
-      constexpr int KK = decltype(kk)::value, N = decltype(n)::value;
-      if constexpr (N < L::READS) l.template fetch<KK, N>(a[KK], stage * kStage);
-      else r.template fetch<KK, N - L::READS>(b[KK], stage * kStage);
-    };
-    auto multiply = [&](int kk, int t) {
-      acc[t / FN][t % FN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[kk].at(t / FN), b[kk].at(t % FN), acc[t / FN][t % FN], 0, 0, 0);
-    };
     using std::integral_constant;
-    a[3].zero();                                                      // the first pass of phase A multiplies zeros
-    b[3].zero();
-    static_for<0, READS>([&](auto n) { read(0, integral_constant<int, 0>{}, n); });
+    if constexpr (S == 2) {
+      Frag<LKM, FM> a[4];
+      Frag<RKM, FN> b[4];
+      auto read = [&](int stage, auto kk, auto n) {
+        constexpr int KK = decltype(kk)::value, N = decltype(n)::value;
+        if constexpr (N < L::READS) l.template fetch<KK, N>(a[KK], stage * kStage);
+        else r.template fetch<KK, N - L::READS>(b[KK], stage * kStage);
+      };
+      auto multiply = [&](int kk, int t) {
+        acc[t / FN][t % FN] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[kk].at(t / FN), b[kk].at(t % FN), acc[t / FN][t % FN], 0, 0, 0);
+      };
+      a[3].zero();                                                      // the first pass of phase A multiplies zeros
+      b[3].zero();
+      static_for<0, READS>([&](auto n) { read(0, integral_constant<int, 0>{}, n); });
 
-    int cur = 0;
-    auto iteration = [&](auto refill_tag, auto sync_tag) {
-      constexpr bool REFILL = decltype(refill_tag)::value, SYNC = decltype(sync_tag)::value;
-      static_for<0, MT>([&](auto t_tag) {                             // A
-        constexpr int t = decltype(t_tag)::value;
-        multiply(3, t);
-        static_for<t * READS / MT, (t + 1) * READS / MT>([&](auto n) { read(cur, integral_constant<int, 1>{}, n); });
+      int cur = 0;
+      auto iteration = [&](auto refill_tag, auto sync_tag) {
+        constexpr bool REFILL = decltype(refill_tag)::value, SYNC = decltype(sync_tag)::value;
+        static_for<0, MT>([&](auto t_tag) {                             // A
+          constexpr int t = decltype(t_tag)::value;
+          multiply(3, t);
+          static_for<t * READS / MT, (t + 1) * READS / MT>([&](auto n) { read(cur, integral_constant<int, 1>{}, n); });
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        wait_lds<(READS < 15 ? READS : 15)>();  // B: k-step 0 is in, k-step 1 may be on its way
+        a[0].tie();
+        b[0].tie();
         __builtin_amdgcn_sched_barrier(0);
-      });
-      wait_lds<(READS < 15 ? READS : 15)>();  // B: k-step 0 is in, k-step 1 may be on its way
-      a[0].tie();
-      b[0].tie();
-      __builtin_amdgcn_sched_barrier(0);
-      constexpr int LEAD = MT >= 8 ? 2 : 0, GROUPS = MT >= 8 ? 8 : 4;
-      static_for<0, MT>([&](auto t_tag) {
-        constexpr int t = decltype(t_tag)::value;
-        constexpr int g = t - LEAD;
-        if constexpr (g >= 0 && g < GROUPS) {
-          static_for<g * 2 * READS / GROUPS, (g + 1) * 2 * READS / GROUPS>([&](auto n) {
-            constexpr int N = decltype(n)::value;
-            read(cur, integral_constant<int, 2 + N / READS>{}, integral_constant<int, N % READS>{});
-          });
-        }
-        multiply(0, t);
-        __builtin_amdgcn_sched_barrier(0);
-      });
-      wait_lds<0>();
+        constexpr int LEAD = MT >= 8 ? 2 : 0, GROUPS = MT >= 8 ? 8 : 4;
+        static_for<0, MT>([&](auto t_tag) {
+          constexpr int t = decltype(t_tag)::value;
+          constexpr int g = t - LEAD;
+          if constexpr (g >= 0 && g < GROUPS) {
+            static_for<g * 2 * READS / GROUPS, (g + 1) * 2 * READS / GROUPS>([&](auto n) {
+              constexpr int N = decltype(n)::value;
+              read(cur, integral_constant<int, 2 + N / READS>{}, integral_constant<int, N % READS>{});
+            });
+          }
+          multiply(0, t);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        wait_lds<0>();
 #pragma unroll
-      for (int kk = 1; kk < 4; ++kk) {
-        a[kk].tie();
-        b[kk].tie();
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (SYNC) {
-        __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));         // my loads of slab kt + 1 have landed
-        __builtin_amdgcn_s_barrier();                                 // everybody's; and nobody reads stage `cur` any more
-      }
-      if constexpr (REFILL) take_next();
-      constexpr int NC = 2 * MT;
-      static_for<0, NC>([&](auto t_tag) {                             // C
-        constexpr int t = decltype(t_tag)::value;
-        multiply(1 + t / MT, t % MT);
-        if constexpr (REFILL) {
-#pragma unroll
-          for (int n = t * LOADS / NC; n < (t + 1) * LOADS / NC; ++n) load_one(cur, n);
+        for (int kk = 1; kk < 4; ++kk) {
+          a[kk].tie();
+          b[kk].tie();
         }
-        if constexpr (SYNC)
-          static_for<t * READS / NC, (t + 1) * READS / NC>([&](auto n) { read(cur ^ 1, integral_constant<int, 0>{}, n); });
         __builtin_amdgcn_sched_barrier(0);
-      });
-      cur ^= 1;
-    };
-    int left = count;
-    while (left > 2) {
-      iteration(std::true_type{}, std::true_type{});
-      --left;
+        if constexpr (SYNC) {
+          wait_loads<0>();                                              // my loads of slab kt + 1 have landed
+          __builtin_amdgcn_s_barrier();                                 // everybody's; and nobody reads stage `cur` any more
+        }
+        constexpr int NC = 2 * MT;
+        static_for<0, NC>([&](auto t_tag) {                             // C
+          constexpr int t = decltype(t_tag)::value;
+          multiply(1 + t / MT, t % MT);
+          if constexpr (REFILL && t == 0) take_next();                // (in the shadow of a product)
+          if constexpr (REFILL) {
+#pragma unroll
+            for (int n = t * LOADS / NC; n < (t + 1) * LOADS / NC; ++n) load_one(cur, n);
+          }
+          if constexpr (SYNC)
+            static_for<t * READS / NC, (t + 1) * READS / NC>([&](auto n) { read(cur ^ 1, integral_constant<int, 0>{}, n); });
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        cur ^= 1;
+      };
+      int left = count;
+      while (left > 2) {
+        iteration(std::true_type{}, std::true_type{});
+        --left;
+      }
+      if (left > 1) iteration(std::false_type{}, std::true_type{});
+      iteration(std::false_type{}, std::false_type{});
+#pragma unroll
+      for (int t = 0; t < MT; ++t) multiply(3, t);
+    } else {
+      static_assert(S == 2 || (S == 4 && FM == 2 && FN == 2), "rings");
+      Frag<LKM, FM> a[2][4];                                            // of two slabs: one multiplied, one read
+      Frag<RKM, FN> b[2][4];
+      constexpr int NR = 4 * READS, NM = 4 * MT;
+      auto read = [&](int stage, auto set, auto n) {
+        constexpr int SET = decltype(set)::value, KK = decltype(n)::value / READS, N = decltype(n)::value % READS;
+        if constexpr (N < L::READS) l.template fetch<KK, N>(a[SET][KK], stage * kStage);
+        else r.template fetch<KK, N - L::READS>(b[SET][KK], stage * kStage);
+      };
+      // BEHIND: slabs after the next one that are on their way; < 0: there is no next one
+      int cur = 0;
+      auto slab = [&](auto set_tag, auto refill_tag, auto behind_tag) {
+        constexpr int SET = decltype(set_tag)::value, BEHIND = decltype(behind_tag)::value;
+        constexpr bool REFILL = decltype(refill_tag)::value, MORE = BEHIND >= 0;
+        wait_lds<0>();
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          a[SET][kk].tie();
+          b[SET][kk].tie();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const int next = (cur + 1) & 3;
+        if constexpr (MORE) {
+          wait_loads<BEHIND * LOADS>();                                 // my loads of the next slab have landed
+          __builtin_amdgcn_s_barrier();                                 // everybody's; and everybody has read this one
+        }
+          static_for<0, NM>([&](auto t_tag) {
+          constexpr int t = decltype(t_tag)::value, kk = t / MT, i = t % MT / FN, j = t % FN;
+          if constexpr (MORE && t < NM / 2)
+            static_for<t * NR / (NM / 2), (t + 1) * NR / (NM / 2)>([&](auto n) { read(next, integral_constant<int, SET ^ 1>{}, n); });
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[SET][kk].at(i), b[SET][kk].at(j), acc[i][j], 0, 0, 0);
+          if constexpr (REFILL && t == 0) take_next();
+          if constexpr (REFILL) {
+#pragma unroll
+            for (int n = t * LOADS / NM; n < (t + 1) * LOADS / NM; ++n) load_one(cur, n);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        cur = next;
+      };
+      using I0 = integral_constant<int, 0>;
+      using I1 = integral_constant<int, 1>;
+      using I2 = integral_constant<int, 2>;
+      int left = count;                                                 // the slab that is next to be multiplied sits in set (left - 1) % 2
+      if (left > 4 || (left & 1)) {
+        if (left & 1) {
+          static_for<0, NR>([&](auto n) { read(0, I0{}, n); });
+        } else {
+          static_for<0, NR>([&](auto n) { read(0, I1{}, n); });
+          slab(I1{}, std::true_type{}, I2{});
+          --left;
+        }
+        while (left > 5) {
+          slab(I0{}, std::true_type{}, I2{});
+          slab(I1{}, std::true_type{}, I2{});
+          left -= 2;
+        }
+        if (left == 5) {
+          slab(I0{}, std::true_type{}, I2{});
+          --left;
+        }
+      } else {
+        static_for<0, NR>([&](auto n) { read(0, I1{}, n); });
+      }
+      if (left >= 4) slab(I1{}, std::false_type{}, I2{});
+      if (left >= 3) slab(I0{}, std::false_type{}, I1{});
+      if (left >= 2) slab(I1{}, std::false_type{}, I0{});
+      slab(I0{}, std::false_type{}, integral_constant<int, -1>{});
     }
-    if (left > 1) iteration(std::false_type{}, std::true_type{});
-    iteration(std::false_type{}, std::false_type{});
-#pragma unroll
-    for (int t = 0; t < MT; ++t) multiply(3, t);
     __syncthreads();                                                  // LDS is the epilogue's
   }
 

@@ -49,13 +49,10 @@ namespace {
 
 constexpr int64_t kUnits = 256;                  // compute units
 // What a launch takes, in us, from the time of a slab of 64 of K (both sides measured at K of 1000 slabs and of 64): a 256-wide tile per
-// compute unit 1.78; two 128-wide ones 1.17; one alone 0.65; and 6 to start and to store.
-double time_wide(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (1.78 * slabs + 6); }
-double time_narrow(int64_t blocks, double slabs) {
-  const int64_t rest = blocks % (2 * kUnits);
-  return (double)(blocks / (2 * kUnits)) * (1.17 * slabs + 6) + (rest == 0 ? 0 : (rest <= kUnits ? 0.65 : 1.17) * slabs + 6);
-}
-double time_lone(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (0.65 * slabs + 6); }
+// compute unit 1.75; two 128-wide ones 1.17; one alone, on the longer ring, 0.58; and 6 to start and to store.
+double time_wide(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (1.75 * slabs + 6); }
+double time_narrow(int64_t blocks, double slabs) { return (double)((blocks + 2 * kUnits - 1) / (2 * kUnits)) * (1.17 * slabs + 6); }
+double time_alone(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (0.58 * slabs + 6); }
 
 }  // namespace
 
@@ -70,22 +67,25 @@ HeadProduct head_product(int64_t m, int64_t n, int64_t k, int pairs, bool may_sp
   const int64_t wide = tiles(256), narrow = tiles(128), slabs = std::max<int64_t>(1, (k + kHeadSlab - 1) / kHeadSlab * pairs);
   double best = 0;
   int64_t splits = 1;
-  auto offer = [&](double us, int tile, int64_t whole, int64_t s) {
+  auto offer = [&](double us, int tile, bool alone, int64_t whole, int64_t s) {
     if (p.tile && us >= best) return;
     best = us;
     p.tile = tile;
+    p.alone = alone;
     p.whole = (int)whole;
     splits = s;
   };
-  offer(time_narrow(narrow, (double)slabs), 128, narrow, 1);
-  offer(time_wide(wide, (double)slabs), 256, wide, 1);
+  if (narrow <= kUnits) offer(time_alone(narrow, (double)slabs), 128, true, narrow, 1);
+  offer(time_narrow(narrow, (double)slabs), 128, false, narrow, 1);
+  offer(time_wide(wide, (double)slabs), 256, false, wide, 1);
   const int64_t rest = wide % kUnits;
-  if (wide > kUnits && rest) offer(time_wide(wide - rest, (double)slabs) + time_lone(4 * rest, (double)slabs), 256, wide - rest, 1);
+  if (wide > kUnits && rest) offer(time_wide(wide - rest, (double)slabs) + time_alone(4 * rest, (double)slabs), 256, false, wide - rest, 1);
   if (may_split) {
     for (int64_t s = 2; s <= 64 && slabs / s >= 8; ++s) {
       const double each = (double)((slabs + s - 1) / s), join = 4 + (double)(s * m * n) * 8e-6 / 5;
-      if (narrow * s <= 2 * kUnits) offer(time_narrow(narrow * s, each) + join, 128, narrow, s);
-      if (wide * s <= 2 * kUnits) offer(time_wide(wide * s, each) + join, 256, wide, s);
+      if (narrow * s <= kUnits) offer(time_alone(narrow * s, each) + join, 128, true, narrow, s);
+      if (narrow * s <= 2 * kUnits) offer(time_narrow(narrow * s, each) + join, 128, false, narrow, s);
+      if (wide * s <= 2 * kUnits) offer(time_wide(wide * s, each) + join, 256, false, wide, s);
     }
   }
   p.tiles_m = (int)((m + p.tile - 1) / p.tile);

@@ -27,6 +27,7 @@ struct HeadShape {
 struct HeadProduct {
   int64_t m, n, k;          // rows of L, rows of R
   int tile;
+  bool alone;               // tiles of 128, a compute unit each
   int tiles_m, tiles_n;
   int whole;
   int splits;

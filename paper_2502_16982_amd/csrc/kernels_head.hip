@@ -146,11 +146,11 @@ __global__ __launch_bounds__(256) void head_entries_kernel(HeadTarget t, const v
 // A block of statistics is 128 vocabulary entries: the rows of one wave in a tile of 256, of two in a tile of 128, which compare notes in
 // LDS.  A lane holds half of a wave's rows for each of its tokens.  Powers of two throughout: 2^(unit z + bias) is one multiply-add and one
 // exponential, and as every power of a block carries the very bias that is stored, rounding the bias costs nothing.
-template <int B, bool PROB, bool F32>
+template <int B, int S, bool PROB, bool F32>
 __device__ __forceinline__ void logits_tile(const HeadOperand& weight, const HeadOperand& hidden, const HeadTiles& g, float unit, float2* stats,
                                             long long stats_pitch, void* prob, long long prob_pitch, long long row0, long long col0,
                                             unsigned char* smem) {
-  using T = Tile<B, B, false, false>;
+  using T = Tile<B, B, false, false, S>;
   T tile;
   tile.run(weight, hidden, row0, col0, g.k, g.pairs, 0, g.slabs_per_split, smem);
   const int fr = tile.lane & 31, fh = tile.lane >> 5;
@@ -245,8 +245,9 @@ __device__ __forceinline__ void logits_tile(const HeadOperand& weight, const Hea
   }
 }
 
-template <int B, bool PROB, bool F32>
-__global__ __launch_bounds__(256, B == 256 ? 1 : 2) void head_logits_kernel(HeadOperand weight, HeadOperand hidden, HeadTiles g, float unit,
+// B x B tiles on a ring of S stages: 256 on two (with quarters on four), 128 on two, two blocks to a compute unit, or 128 on four.
+template <int B, int S, bool PROB, bool F32>
+__global__ __launch_bounds__(256, B == 128 && S == 2 ? 2 : 1) void head_logits_kernel(HeadOperand weight, HeadOperand hidden, HeadTiles g, float unit,
                                                                             float2* __restrict__ stats, long long stats_pitch,
                                                                             void* __restrict__ prob, long long prob_pitch) {
 #if defined(__HIP_DEVICE_COMPILE__)            // (the host's pass knows no buffer descriptors)
@@ -254,12 +255,12 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : 2) void head_logits_kernel(Head
   const TileAt at = tile_at(g);
   long long row0 = (long long)at.m * B, col0 = (long long)at.n * B;
   if (B == 128 || at.quarter < 0) {
-    logits_tile<B, PROB, F32>(weight, hidden, g, unit, stats, stats_pitch, prob, prob_pitch, row0, col0, smem);
+    logits_tile<B, S, PROB, F32>(weight, hidden, g, unit, stats, stats_pitch, prob, prob_pitch, row0, col0, smem);
   } else if constexpr (B == 256) {
     row0 += 128 * (at.quarter >> 1);
     col0 += 128 * (at.quarter & 1);
     if (row0 < weight.rows && col0 < hidden.rows)
-      logits_tile<128, PROB, F32>(weight, hidden, g, unit, stats, stats_pitch, prob, prob_pitch, row0, col0, smem);
+      logits_tile<128, 4, PROB, F32>(weight, hidden, g, unit, stats, stats_pitch, prob, prob_pitch, row0, col0, smem);
   }
 #endif
 }
@@ -282,15 +283,47 @@ __global__ __launch_bounds__(1024) void head_peak_kernel(const float* __restrict
   }
 }
 
+// Where there are no more tokens than this, every block of the join looks through all scales itself: a launch less.
+constexpr long long kPeakInJoin = 16384;
+
 // Sixteen tokens per block (a line of statistics), their blocks of the vocabulary over 64 threads each, eight loads at a time; then a wave
-// per token for its entries.
-__global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float unit, const float* __restrict__ peak, const float2* __restrict__ stats,
-                                                         long long stats_pitch, long long blocks, const float* __restrict__ entry,
-                                                         long long tokens, long long vocab, float* __restrict__ loss, float* __restrict__ lse,
-                                                         float* __restrict__ value, float* __restrict__ scale, float2* __restrict__ log2sum) {
+// per token for its entries, of which the first 64 are loaded at the start.
+__global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float unit, const float* __restrict__ all_scales, long long all_tokens,
+                                                         float* __restrict__ peak, const float2* __restrict__ stats, long long stats_pitch,
+                                                         long long blocks, const float* __restrict__ entry, long long tokens, long long vocab,
+                                                         float* __restrict__ loss, float* __restrict__ lse, float* __restrict__ value,
+                                                         float* __restrict__ scale, float2* __restrict__ log2sum) {
   __shared__ float tops[64][17];
   __shared__ float sums[64][17];
-  __shared__ double joined[16];
+  __shared__ float peaks[16];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const long long tk = blockIdx.x * 16ll + wave;
+  // this wave's token: entry `lane` of its target
+  struct Entry {
+    int v;                                       // -1: none
+    float s, z;
+  };
+  auto load_entry = [&](int j, bool* beyond) -> Entry {
+    Entry e{-1, -INFINITY, 0.f};
+    if (tk >= tokens || j >= t.top) return e;
+    const long long i = tk * t.top + j, v = index_at(t, i);
+    if (v >= vocab) *beyond = true;
+    if (v < 0 || v >= vocab) return e;
+    e.s = t.logits ? teacher_at(t, i) : 0.f;
+    e.z = entry[i];
+    if (!(e.s == -INFINITY)) e.v = (int)v;
+    return e;
+  };
+  bool beyond = false;
+  const Entry mine = load_entry(lane, &beyond);
+  float g = tk < tokens && t.token_scale ? t.token_scale[tk] : 1.f;
+  float most = 0.f;
+  if (all_scales)
+    for (long long i = threadIdx.x; i < all_tokens; i += 1024) {
+      const float x = fabsf(all_scales[i]);
+      if (x < INFINITY) most = fmaxf(most, x);
+    }
+
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
   const long long token = blockIdx.x * 16ll + x, read = token < tokens ? token : tokens - 1;
   float top = -INFINITY, sum = 0.f;              // the sum is sum * 2^top
@@ -311,26 +344,40 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
   }
   tops[y][x] = top;
   sums[y][x] = sum;
-  __syncthreads();
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  {                                              // wave w: token w, lane: its thread's share
-    const float mine = tops[lane][wave];
-    float all = mine;
+  if (all_scales) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) all = fmaxf(all, __shfl_xor(all, off, 64));
-    const float shift = all == -INFINITY ? 0.f : all;
-    double part = (double)(sums[lane][wave] * __builtin_amdgcn_exp2f(mine - shift));
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) part += __shfl_xor(part, off, 64);
-    if (lane == 0) joined[wave] = (double)shift + log2(part);
+    for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
+    if (lane == 0) peaks[wave] = most;
   }
-  const long long tk = blockIdx.x * 16ll + wave;
+  __syncthreads();
+  float largest = 1.f;
+  if (all_scales) {
+    most = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) most = fmaxf(most, peaks[w]);
+    largest = most > 0.f ? most : 1.f;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *peak = largest;
+  } else if (peak) {
+    largest = *peak;
+  }
   if (tk >= tokens) return;
-  // (the wave's own LDS write, read back by the same wave)
-  __builtin_amdgcn_wave_barrier();
-  const double y2 = joined[wave], l = y2 * ((double)t.inv_tau / (double)unit);       // log2 and natural log of the sum
-  const TokenState state = token_state(t, tk, vocab);
-  const float g = token_scale(t, tk, state), r = g == 0.f ? 0.f : peak ? g / *peak : g;
+  // wave w: token w, lane: its thread's share
+  const float share = tops[lane][wave];
+  float all = share;
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) all = fmaxf(all, __shfl_xor(all, off, 64));
+  const float shift = all == -INFINITY ? 0.f : all;
+  double part = (double)(sums[lane][wave] * __builtin_amdgcn_exp2f(share - shift));
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) part += __shfl_xor(part, off, 64);
+  const double y2 = (double)shift + log2(part), l = y2 * ((double)t.inv_tau / (double)unit);       // log2 and natural log of the sum
+
+  bool some = mine.v >= 0;
+  for (int j = lane + 64; j < t.top; j += 64) some |= load_entry(j, &beyond).v >= 0;
+  some = __any(some) != 0;
+  beyond = __any(beyond) != 0;
+  if (!some || beyond) g = 0.f;
+  const float r = g == 0.f ? 0.f : g / largest;
   if (lane == 0) {
     if (lse) lse[tk] = (float)l;
     if (value) {
@@ -341,47 +388,49 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
   }
   double sum_loss = 0.0;
   if (!t.logits) {
-    const double z = (double)entry[tk];
+    const double z = (double)mine.z;
     if (lane == 0) {
-      sum_loss = state.some ? l - z : 0.0;
+      sum_loss = some ? l - z : 0.0;
       if (value) value[tk] = r == 0.f ? 0.f : (float)((double)r * expm1(z - l));
     }
-  } else if (state.some) {
-    float best = -INFINITY;
-    for (int j = lane; j < t.top; j += 64)
-      if (entry_there(t, tk * t.top + j, vocab)) best = fmaxf(best, teacher_at(t, tk * t.top + j));
+  } else if (some) {
+    bool ignored = false;
+    float best = mine.v >= 0 ? mine.s : -INFINITY;
+    for (int j = lane + 64; j < t.top; j += 64) {
+      const Entry e = load_entry(j, &ignored);
+      if (e.v >= 0) best = fmaxf(best, e.s);
+    }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) best = fmaxf(best, __shfl_xor(best, off, 64));
-    double mass = 0.0;
-    for (int j = lane; j < t.top; j += 64)
-      if (entry_there(t, tk * t.top + j, vocab)) mass += exp((double)teacher_at(t, tk * t.top + j) - (double)best);
+    double mass = mine.v >= 0 ? exp((double)mine.s - (double)best) : 0.0;
+    for (int j = lane + 64; j < t.top; j += 64) {
+      const Entry e = load_entry(j, &ignored);
+      if (e.v >= 0) mass += exp((double)e.s - (double)best);
+    }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) mass += __shfl_xor(mass, off, 64);
     const double norm = (double)best + log(mass);
     for (int j0 = 0; j0 < t.top; j0 += 64) {
       const int j = j0 + lane;
-      const bool there = j < t.top && entry_there(t, tk * t.top + j, vocab);
-      const int v = there ? (int)index_at(t, tk * t.top + j) : -1;
-      const double z = there ? (double)entry[tk * t.top + j] : 0.0;
-      const double logq = there ? (double)teacher_at(t, tk * t.top + j) - norm : 0.0;
-      const double own = there ? exp(logq) : 0.0;
+      const Entry e = j0 == 0 ? mine : load_entry(j, &ignored);
+      const bool there = e.v >= 0;
+      const double z = (double)e.z, logq = there ? (double)e.s - norm : 0.0, own = there ? exp(logq) : 0.0;
       if (there) sum_loss += own * (logq - z + l);
       if (value) {
         double q = 0.0;                          // of every entry with this index
         for (int k0 = 0; k0 < t.top; k0 += 64) {
-          const int k = k0 + lane;
-          int vk = v;
+          int vk = e.v;
           double qk = own;
           if (k0 != j0) {
-            const bool kt = k < t.top && entry_there(t, tk * t.top + k, vocab);
-            vk = kt ? (int)index_at(t, tk * t.top + k) : -1;
-            qk = kt ? exp((double)teacher_at(t, tk * t.top + k) - norm) : 0.0;
+            const Entry o = k0 == 0 ? mine : load_entry(k0 + lane, &ignored);
+            vk = o.v;
+            qk = o.v >= 0 ? exp((double)o.s - norm) : 0.0;
           }
           const int n = t.top - k0 < 64 ? t.top - k0 : 64;
           for (int w = 0; w < n; ++w) {
             const int vw = __shfl(vk, w, 64);
             const double qw = __shfl(qk, w, 64);
-            if (vw == v) q += qw;
+            if (vw == e.v) q += qw;
           }
         }
         if (j < t.top) value[tk * t.top + j] = there && r != 0.f ? (float)((double)r * (exp(z - l) - q)) : 0.f;
@@ -392,7 +441,7 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
   } else if (value) {
     for (int j = lane; j < t.top; j += 64) value[tk * t.top + j] = 0.f;
   }
-  if (lane == 0) loss[tk] = state.beyond ? __builtin_nanf("") : (float)((double)t.tau * (double)t.tau * sum_loss);
+  if (lane == 0) loss[tk] = beyond ? __builtin_nanf("") : (float)((double)t.tau * (double)t.tau * sum_loss);
 }
 
 // ---- dz ----
@@ -524,10 +573,10 @@ __device__ __forceinline__ void store_whole(const T& tile, const HeadOperand& l,
   });
 }
 
-template <int B, bool RKM, bool IMAGE>
+template <int B, int S, bool RKM, bool IMAGE>
 __device__ __forceinline__ void product_tile(const HeadOperand& l, const HeadOperand& r, const HeadTiles& g, const HeadOut& out, int split,
                                              long long row0, long long col0, unsigned char* smem) {
-  using T = Tile<B, B, true, RKM>;
+  using T = Tile<B, B, true, RKM, S>;
   const int slabs = (int)((g.k + kHeadSlab - 1) / kHeadSlab) * g.pairs;
   const int first = split * g.slabs_per_split, last = first + g.slabs_per_split < slabs ? first + g.slabs_per_split : slabs;
   T tile;
@@ -537,18 +586,18 @@ __device__ __forceinline__ void product_tile(const HeadOperand& l, const HeadOpe
   else store_parts(tile, l, r, g, out, scale, split, row0, col0);
 }
 
-template <int B, bool RKM, bool IMAGE>
-__global__ __launch_bounds__(256, B == 256 ? 1 : 2) void head_product_kernel(HeadOperand l, HeadOperand r, HeadTiles g, HeadOut out) {
+template <int B, int S, bool RKM, bool IMAGE>
+__global__ __launch_bounds__(256, B == 128 && S == 2 ? 2 : 1) void head_product_kernel(HeadOperand l, HeadOperand r, HeadTiles g, HeadOut out) {
 #if defined(__HIP_DEVICE_COMPILE__)            // (the host's pass knows no buffer descriptors)
   extern __shared__ __align__(16) unsigned char smem[];
   const TileAt at = tile_at(g);
   long long row0 = (long long)at.m * B, col0 = (long long)at.n * B;
   if (B == 128 || at.quarter < 0) {
-    product_tile<B, RKM, IMAGE>(l, r, g, out, at.split, row0, col0, smem);
+    product_tile<B, S, RKM, IMAGE>(l, r, g, out, at.split, row0, col0, smem);
   } else if constexpr (B == 256) {
     row0 += 128 * (at.quarter >> 1);
     col0 += 128 * (at.quarter & 1);
-    if (row0 < l.rows && col0 < r.rows) product_tile<128, RKM, IMAGE>(l, r, g, out, at.split, row0, col0, smem);
+    if (row0 < l.rows && col0 < r.rows) product_tile<128, 4, RKM, IMAGE>(l, r, g, out, at.split, row0, col0, smem);
   }
 #endif
 }
@@ -603,50 +652,52 @@ hipError_t allow_lds(std::atomic<uint64_t>& done, const void* kernel, int bytes)
   return hipSuccess;
 }
 
-template <int B, bool PROB, bool F32>
+template <int B, int S, bool PROB, bool F32>
 hipError_t logits_of(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, float2* stats,
                      long long stats_pitch, void* prob, long long prob_pitch, hipStream_t s) {
-  constexpr int lds = Tile<B, B, false, false>::kLds;
+  constexpr int lds = Tile<B, B, false, false, S>::kLds;
   static std::atomic<uint64_t> done{0};
-  if (hipError_t e = allow_lds(done, reinterpret_cast<const void*>(&head_logits_kernel<B, PROB, F32>), lds)) return e;
-  head_logits_kernel<B, PROB, F32><<<(unsigned)g.blocks(), 256, lds, s>>>(weight, hidden, tiles_of(g, pairs), unit, stats, stats_pitch, prob,
+  if (hipError_t e = allow_lds(done, reinterpret_cast<const void*>(&head_logits_kernel<B, S, PROB, F32>), lds)) return e;
+  head_logits_kernel<B, S, PROB, F32><<<(unsigned)g.blocks(), 256, lds, s>>>(weight, hidden, tiles_of(g, pairs), unit, stats, stats_pitch, prob,
                                                                      prob_pitch);
   return hipGetLastError();
 }
 
 hipError_t launch_head_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit,
                               float2* stats, long long stats_pitch, void* prob, long long prob_pitch, int prob_f32, hipStream_t s) {
-  auto go = [&](auto b) {
-    constexpr int B = decltype(b)::value;
-    if (!prob) return logits_of<B, false, false>(weight, hidden, g, pairs, unit, stats, stats_pitch, prob, prob_pitch, s);
-    if (prob_f32) return logits_of<B, true, true>(weight, hidden, g, pairs, unit, stats, stats_pitch, prob, prob_pitch, s);
-    return logits_of<B, true, false>(weight, hidden, g, pairs, unit, stats, stats_pitch, prob, prob_pitch, s);
-  };
-  return g.tile == 256 ? go(std::integral_constant<int, 256>{}) : go(std::integral_constant<int, 128>{});
+#define MUON_HEAD_CASE(B, S)                                                                                                              \
+  if (g.tile == B && (g.alone ? 4 : 2) == S)                                                                                              \
+    return !prob      ? logits_of<B, S, false, false>(weight, hidden, g, pairs, unit, stats, stats_pitch, prob, prob_pitch, s)            \
+           : prob_f32 ? logits_of<B, S, true, true>(weight, hidden, g, pairs, unit, stats, stats_pitch, prob, prob_pitch, s)              \
+                      : logits_of<B, S, true, false>(weight, hidden, g, pairs, unit, stats, stats_pitch, prob, prob_pitch, s)
+  MUON_HEAD_CASE(256, 2);
+  MUON_HEAD_CASE(128, 2);
+  MUON_HEAD_CASE(128, 4);
+#undef MUON_HEAD_CASE
+  return hipErrorInvalidValue;
 }
 
-template <int B, bool RKM, bool IMAGE>
+template <int B, int S, bool RKM, bool IMAGE>
 hipError_t product_of(const HeadOperand& l, const HeadOperand& r, const HeadProduct& g, int pairs, const HeadOut& out, hipStream_t s) {
-  constexpr int lds = Tile<B, B, true, RKM>::kLds;
+  constexpr int lds = Tile<B, B, true, RKM, S>::kLds;
   static std::atomic<uint64_t> done{0};
-  if (hipError_t e = allow_lds(done, reinterpret_cast<const void*>(&head_product_kernel<B, RKM, IMAGE>), lds)) return e;
-  head_product_kernel<B, RKM, IMAGE><<<(unsigned)g.blocks(), 256, lds, s>>>(l, r, tiles_of(g, pairs), out);
+  if (hipError_t e = allow_lds(done, reinterpret_cast<const void*>(&head_product_kernel<B, S, RKM, IMAGE>), lds)) return e;
+  head_product_kernel<B, S, RKM, IMAGE><<<(unsigned)g.blocks(), 256, lds, s>>>(l, r, tiles_of(g, pairs), out);
   return hipGetLastError();
 }
 
 hipError_t launch_head_product(const HeadOperand& l, const HeadOperand& r, int r_kmajor, const HeadProduct& g, int pairs,
                                const HeadOut& out, hipStream_t s) {
   const bool image = g.splits == 1 && !out.f32 && !out.add && !out.keep;
-#define MUON_HEAD_CASE(B, KM, IMAGE) \
-  if (g.tile == B && (r_kmajor != 0) == KM && image == IMAGE) return product_of<B, KM, IMAGE>(l, r, g, pairs, out, s)
-  MUON_HEAD_CASE(256, false, true);
-  MUON_HEAD_CASE(256, false, false);
-  MUON_HEAD_CASE(256, true, true);
-  MUON_HEAD_CASE(256, true, false);
-  MUON_HEAD_CASE(128, false, true);
-  MUON_HEAD_CASE(128, false, false);
-  MUON_HEAD_CASE(128, true, true);
-  MUON_HEAD_CASE(128, true, false);
+#define MUON_HEAD_CASE(B, S, KM)                                                                     \
+  if (g.tile == B && (g.alone ? 4 : 2) == S && (r_kmajor != 0) == KM)                                \
+    return image ? product_of<B, S, KM, true>(l, r, g, pairs, out, s) : product_of<B, S, KM, false>(l, r, g, pairs, out, s)
+  MUON_HEAD_CASE(256, 2, false);
+  MUON_HEAD_CASE(256, 2, true);
+  MUON_HEAD_CASE(128, 2, false);
+  MUON_HEAD_CASE(128, 2, true);
+  MUON_HEAD_CASE(128, 4, false);
+  MUON_HEAD_CASE(128, 4, true);
 #undef MUON_HEAD_CASE
   return hipErrorInvalidValue;
 }
@@ -670,15 +721,16 @@ hipError_t launch_head_entries(const HeadTarget& t, const void* hidden, long lon
 }
 
 hipError_t launch_head_peak(const float* token_scale, long long tokens, float* peak, hipStream_t s) {
+  if (tokens <= kPeakInJoin) return hipSuccess;  // launch_head_join finds it
   head_peak_kernel<<<1, 1024, 0, s>>>(token_scale, tokens, peak);
   return hipGetLastError();
 }
 
-hipError_t launch_head_join(const HeadTarget& t, float unit, const float* peak, const float2* stats, long long stats_pitch, long long blocks,
-                            const float* entry, long long tokens, long long vocab, float* loss, float* lse, float* value, float* scale,
-                            float2* log2sum, hipStream_t s) {
-  head_join_kernel<<<(unsigned)((tokens + 15) / 16), 1024, 0, s>>>(t, unit, peak, stats, stats_pitch, blocks, entry, tokens, vocab, loss, lse,
-                                                                  value, scale, log2sum);
+hipError_t launch_head_join(const HeadTarget& t, float unit, const float* all_scales, long long all_tokens, float* peak, const float2* stats,
+                            long long stats_pitch, long long blocks, const float* entry, long long tokens, long long vocab, float* loss,
+                            float* lse, float* value, float* scale, float2* log2sum, hipStream_t s) {
+  head_join_kernel<<<(unsigned)((tokens + 15) / 16), 1024, 0, s>>>(t, unit, peak && all_tokens <= kPeakInJoin ? all_scales : nullptr, all_tokens, peak,
+                                                                  stats, stats_pitch, blocks, entry, tokens, vocab, loss, lse, value, scale, log2sum);
   return hipGetLastError();
 }
 
