@@ -10,6 +10,8 @@
 // order does not matter.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "experts_launch.h"
 
 namespace muon {
@@ -17,7 +19,6 @@ namespace {
 
 typedef unsigned short u16;
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -139,59 +140,62 @@ __global__ __launch_bounds__(256) void expert_place_kernel(const void* __restric
 }
 
 // ---- rows ----
-// A piece of a row in one thread: BYTES of bf16 or fp32 elements.
-template <int BYTES>
-struct RawOf;
-template <> struct RawOf<16> { typedef u32x4 type; };
-template <> struct RawOf<8> { typedef u32x2 type; };
-template <> struct RawOf<4> { typedef unsigned type; };
-template <> struct RawOf<2> { typedef u16 type; };
+// A thread moves 16 bytes of a row at a time, whatever the rows' alignment (global memory takes that at any address of an element; rows of
+// 1409 fp32: 34 us for combine and its gradients in pieces of 4 bytes, 23 in these); what a row has left behind its last whole piece goes
+// by element.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
-template <int BYTES, bool F32>
+template <bool F32>
 struct Piece {
-  static constexpr int N = BYTES / (F32 ? 4 : 2);
-  typedef typename RawOf<BYTES>::type Raw;
-  static __device__ __forceinline__ void unpack(Raw raw, float (&v)[N]) {
+  static constexpr int N = F32 ? 4 : 8;
+  typedef std::conditional_t<F32, float, u16> Elem;
+  static __device__ __forceinline__ u32x4 load(const Elem* p) { return *reinterpret_cast<const u32x4_any*>(p); }
+  static __device__ __forceinline__ void store(Elem* p, u32x4 v) { *reinterpret_cast<u32x4_any*>(p) = v; }
+  static __device__ __forceinline__ void unpack(u32x4 raw, float (&v)[N]) {
     if constexpr (F32) {
-      if constexpr (N == 1) v[0] = __uint_as_float(raw);
-      else
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = __uint_as_float(raw[e]);
-    } else if constexpr (N == 1) {
-      v[0] = __uint_as_float((unsigned)raw << 16);
+      for (int e = 0; e < N; ++e) v[e] = __uint_as_float(raw[e]);
     } else {
 #pragma unroll
       for (int e = 0; e < N / 2; ++e) {
-        unsigned w;
-        if constexpr (N == 2) w = raw;
-        else w = raw[e];
-        v[2 * e] = __uint_as_float(w << 16);
-        v[2 * e + 1] = __uint_as_float(w & 0xffff0000u);
+        v[2 * e] = __uint_as_float(raw[e] << 16);
+        v[2 * e + 1] = __uint_as_float(raw[e] & 0xffff0000u);
       }
     }
   }
-  static __device__ __forceinline__ Raw pack(const float (&v)[N]) {
-    Raw raw;
-    if constexpr (F32) {
-      if constexpr (N == 1) raw = __float_as_uint(v[0]);
-      else
+  static __device__ __forceinline__ u32x4 pack(const float (&v)[N]) {
+    u32x4 raw;
 #pragma unroll
-        for (int e = 0; e < N; ++e) raw[e] = __float_as_uint(v[e]);
-    } else if constexpr (N == 1) {
-      const f32x2 two = {v[0], 0.f};
-      raw = (u16)(__builtin_bit_cast(unsigned, __builtin_convertvector(two, bf16x2)) & 0xffffu);
-    } else {
-#pragma unroll
-      for (int e = 0; e < N / 2; ++e) {
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (F32) {
+        raw[e] = __float_as_uint(v[e]);
+      } else {
         const f32x2 two = {v[2 * e], v[2 * e + 1]};
-        const unsigned w = __builtin_bit_cast(unsigned, __builtin_convertvector(two, bf16x2));
-        if constexpr (N == 2) raw = w;
-        else raw[e] = w;
+        raw[e] = __builtin_bit_cast(unsigned, __builtin_convertvector(two, bf16x2));
       }
     }
     return raw;
   }
+  static __device__ __forceinline__ float value(Elem x) {
+    if constexpr (F32) return x;
+    else return __uint_as_float((unsigned)x << 16);
+  }
+  static __device__ __forceinline__ Elem elem(float x) {
+    if constexpr (F32) {
+      return x;
+    } else {
+      const f32x2 two = {x, 0.f};
+      return (u16)(__builtin_bit_cast(unsigned, __builtin_convertvector(two, bf16x2)) & 0xffffu);
+    }
+  }
 };
+
+// The token of a thread, its place among the token's `lanes` threads (whole waves), the token's first element in dense rows.
+struct Place {
+  long long token;
+  int at;
+};
+__device__ __forceinline__ Place place(int lanes) { return {blockIdx.x * (256ll / lanes) + threadIdx.x / lanes, (int)(threadIdx.x % lanes)}; }
 
 // The row of pair i, or -1: what is no row of this call counts as dropped.
 __device__ __forceinline__ long long row_of(const ExpertRows& r, long long i) {
@@ -199,127 +203,165 @@ __device__ __forceinline__ long long row_of(const ExpertRows& r, long long i) {
   return p >= 0 && p < r.tokens * r.top ? p : -1;
 }
 // Rows behind the last pair's are zero.  Each token clears those with its own pairs' numbers.
-template <typename Raw>
-__device__ __forceinline__ void clear_tail(const ExpertRows& r, long long token, Raw* rows, long long pieces, int at, int lanes) {
+template <bool F32>
+__device__ __forceinline__ void clear_tail(const ExpertRows& r, long long token, typename Piece<F32>::Elem* rows, int at, int lanes) {
+  using P = Piece<F32>;
   const long long count = *r.count;
   for (int j = 0; j < r.top; ++j) {
     const long long row = token * r.top + j;
     if (row < count) continue;
-    for (long long c = at; c < pieces; c += lanes) rows[row * pieces + c] = Raw{};
-  }
-}
-
-template <typename Raw>
-__global__ __launch_bounds__(256) void expert_dispatch_kernel(ExpertRows r, const unsigned char* __restrict__ x, long long x_stride,
-                                                              Raw* __restrict__ rows, long long pieces, int lanes) {
-  const long long token = blockIdx.x * (256ll / lanes) + threadIdx.x / lanes;
-  const int at = threadIdx.x % lanes;
-  if (token >= r.tokens) return;
-  const Raw* mine = reinterpret_cast<const Raw*>(x + token * x_stride);
-  for (long long c = at; c < pieces; c += lanes) {
-    const Raw v = mine[c];
-    for (int j = 0; j < r.top; ++j) {
-      const long long row = row_of(r, token * r.top + j);
-      if (row >= 0) rows[row * pieces + c] = v;
+    for (long long c = (long long)at * P::N; c < r.width; c += (long long)lanes * P::N) {
+      if (c + P::N <= r.width) P::store(rows + row * r.width + c, u32x4{0u, 0u, 0u, 0u});
+      else
+        for (long long e = c; e < r.width; ++e) rows[row * r.width + e] = 0;
     }
   }
-  clear_tail(r, token, rows, pieces, at, lanes);
 }
 
-template <int BYTES, bool F32>
+template <bool F32>
+__global__ __launch_bounds__(256) void expert_dispatch_kernel(ExpertRows r, const void* __restrict__ x, long long x_stride,
+                                                              void* __restrict__ rows_, int lanes) {
+  using P = Piece<F32>;
+  using Elem = typename P::Elem;
+  const Place here = place(lanes);
+  if (here.token >= r.tokens) return;
+  const Elem* mine = static_cast<const Elem*>(x) + here.token * x_stride;
+  Elem* rows = static_cast<Elem*>(rows_);
+  for (long long c = (long long)here.at * P::N; c < r.width; c += (long long)lanes * P::N) {
+    if (c + P::N <= r.width) {
+      const u32x4 v = P::load(mine + c);
+      for (int j = 0; j < r.top; ++j) {
+        const long long row = row_of(r, here.token * r.top + j);
+        if (row >= 0) P::store(rows + row * r.width + c, v);
+      }
+    } else {
+      for (int j = 0; j < r.top; ++j) {
+        const long long row = row_of(r, here.token * r.top + j);
+        if (row >= 0)
+          for (long long e = c; e < r.width; ++e) rows[row * r.width + e] = mine[e];
+      }
+    }
+  }
+  clear_tail<F32>(r, here.token, rows, here.at, lanes);
+}
+
+// ROWS rows of a token on their way at a time.
+template <bool F32, int ROWS>
 __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows r, const void* __restrict__ rows_, const float* __restrict__ weights,
-                                                             void* __restrict__ out_, long long pieces, int lanes) {
-  constexpr int ROWS = 8;
-  using P = Piece<BYTES, F32>;
-  using Raw = typename P::Raw;
-  const Raw* rows = static_cast<const Raw*>(rows_);
-  Raw* out = static_cast<Raw*>(out_);
-  const long long token = blockIdx.x * (256ll / lanes) + threadIdx.x / lanes;
-  if (token >= r.tokens) return;
-  for (long long c = threadIdx.x % lanes; c < pieces; c += lanes) {
+                                                             void* __restrict__ out_, int lanes) {
+  using P = Piece<F32>;
+  using Elem = typename P::Elem;
+  const Place here = place(lanes);
+  if (here.token >= r.tokens) return;
+  const Elem* rows = static_cast<const Elem*>(rows_);
+  Elem* out = static_cast<Elem*>(out_) + here.token * r.width;
+  for (long long c = (long long)here.at * P::N; c < r.width; c += (long long)lanes * P::N) {
+    const bool whole = c + P::N <= r.width;
     float sum[P::N];
 #pragma unroll
     for (int e = 0; e < P::N; ++e) sum[e] = 0.f;
-    for (int j0 = 0; j0 < r.top; j0 += ROWS) {   // ROWS rows on their way at a time
+    for (int j0 = 0; j0 < r.top; j0 += ROWS) {
       long long row[ROWS];
       float w[ROWS];
-      Raw v[ROWS];
+      u32x4 v[ROWS];
 #pragma unroll
       for (int u = 0; u < ROWS; ++u) {
-        const long long i = token * r.top + j0 + u;
+        const long long i = here.token * r.top + j0 + u;
         row[u] = j0 + u < r.top ? row_of(r, i) : -1;
         w[u] = row[u] < 0 ? 0.f : weights ? weights[i] : 1.f;
       }
+      if (whole) {
 #pragma unroll
-      for (int u = 0; u < ROWS; ++u) v[u] = row[u] < 0 ? Raw{} : rows[row[u] * pieces + c];
+        for (int u = 0; u < ROWS; ++u) v[u] = row[u] < 0 ? u32x4{0u, 0u, 0u, 0u} : P::load(rows + row[u] * r.width + c);
 #pragma unroll
-      for (int u = 0; u < ROWS; ++u) {
-        float f[P::N];
-        P::unpack(v[u], f);
+        for (int u = 0; u < ROWS; ++u) {
+          float f[P::N];
+          P::unpack(v[u], f);
 #pragma unroll
-        for (int e = 0; e < P::N; ++e) sum[e] = fmaf(w[u], f[e], sum[e]);
+          for (int e = 0; e < P::N; ++e)
+            if (row[u] >= 0) sum[e] = fmaf(w[u], f[e], sum[e]);
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u)
+#pragma unroll
+          for (int e = 0; e < P::N; ++e)
+            if (row[u] >= 0 && c + e < r.width) sum[e] = fmaf(w[u], P::value(rows[row[u] * r.width + c + e]), sum[e]);
       }
     }
-    out[token * pieces + c] = P::pack(sum);
+    if (whole) {
+      P::store(out + c, P::pack(sum));
+    } else {
+#pragma unroll
+      for (int e = 0; e < P::N; ++e)
+        if (c + e < r.width) out[c + e] = P::elem(sum[e]);
+    }
   }
 }
 
-template <int BYTES, bool F32>
-__global__ __launch_bounds__(256) void expert_combine_backward_kernel(ExpertRows r, const unsigned char* __restrict__ d_out,
-                                                                      long long d_out_stride, const void* __restrict__ rows_,
-                                                                      const float* __restrict__ weights, void* __restrict__ d_rows_,
-                                                                      float* __restrict__ d_weights, long long pieces, int lanes) {
-  using P = Piece<BYTES, F32>;
-  using Raw = typename P::Raw;
+template <bool F32>
+__global__ __launch_bounds__(256) void expert_combine_backward_kernel(ExpertRows r, const void* __restrict__ d_out, long long d_out_stride,
+                                                                      const void* __restrict__ rows_, const float* __restrict__ weights,
+                                                                      void* __restrict__ d_rows_, float* __restrict__ d_weights, int lanes) {
+  using P = Piece<F32>;
+  using Elem = typename P::Elem;
   __shared__ float dots[kMaxExpertTop][4];
-  const Raw* rows = static_cast<const Raw*>(rows_);
-  Raw* d_rows = static_cast<Raw*>(d_rows_);
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, at = threadIdx.x % lanes;
-  const long long token = blockIdx.x * (256ll / lanes) + threadIdx.x / lanes;
-  const bool there = token < r.tokens;           // (of a whole wave)
+  const Elem* rows = static_cast<const Elem*>(rows_);
+  Elem* d_rows = static_cast<Elem*>(d_rows_);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const Place here = place(lanes);
+  const bool there = here.token < r.tokens;      // (of a whole wave)
   if (there) {
-    const Raw* mine = reinterpret_cast<const Raw*>(d_out + token * d_out_stride);
+    const Elem* mine = static_cast<const Elem*>(d_out) + here.token * d_out_stride;
     for (int j = 0; j < r.top; ++j) {
-      const long long i = token * r.top + j, row = row_of(r, i);
+      const long long i = here.token * r.top + j, row = row_of(r, i);
       float dot = 0.f;
       if (row >= 0) {
         const float w = weights[i];
-        for (long long c = at; c < pieces; c += lanes) {
-          float g[P::N], y[P::N];
-          P::unpack(mine[c], g);
-          P::unpack(rows[row * pieces + c], y);
+        const Elem* y = rows + row * r.width;
+        Elem* dy = d_rows + row * r.width;
+        for (long long c = (long long)here.at * P::N; c < r.width; c += (long long)lanes * P::N) {
+          if (c + P::N <= r.width) {
+            float g[P::N], f[P::N];
+            P::unpack(P::load(mine + c), g);
+            P::unpack(P::load(y + c), f);
 #pragma unroll
-          for (int e = 0; e < P::N; ++e) {
-            dot = fmaf(g[e], y[e], dot);
-            g[e] *= w;
+            for (int e = 0; e < P::N; ++e) {
+              dot = fmaf(g[e], f[e], dot);
+              g[e] *= w;
+            }
+            P::store(dy + c, P::pack(g));
+          } else {
+            for (long long e = c; e < r.width; ++e) {
+              const float g = P::value(mine[e]);
+              dot = fmaf(g, P::value(y[e]), dot);
+              dy[e] = P::elem(w * g);
+            }
           }
-          d_rows[row * pieces + c] = P::pack(g);
         }
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) dot += __shfl_xor(dot, off, 64);
       }
       if (lane == 0) dots[j][wave] = dot;
     }
-    clear_tail(r, token, d_rows, pieces, at, lanes);
+    clear_tail<F32>(r, here.token, d_rows, here.at, lanes);
   }
   __syncthreads();
   if (!there) return;
   const int waves = lanes / 64, first = threadIdx.x / lanes * waves;
-  for (int j = at; j < r.top; j += lanes) {
+  for (int j = here.at; j < r.top; j += lanes) {
     float sum = 0.f;
     for (int u = 0; u < waves; ++u) sum += dots[j][first + u];
-    d_weights[token * r.top + j] = sum;
+    d_weights[here.token * r.top + j] = sum;
   }
 }
 
-// The widest piece that rows of that many bytes and these addresses come in.
-int piece_bytes(long long row_bytes, long long stride_bytes, const void* a, const void* b, const void* c) {
-  const unsigned long long all = (unsigned long long)row_bytes | (unsigned long long)stride_bytes | reinterpret_cast<uintptr_t>(a) |
-                                 reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c);
-  return all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : all % 4 == 0 ? 4 : 2;
-}
 // Threads per token: whole waves, as many as have a piece of the row each.
-int lanes_for(long long pieces) { return pieces <= 64 ? 64 : pieces <= 128 ? 128 : 256; }
+int lanes_for(const ExpertRows& r) {
+  const long long pieces = r.width * (r.f32 ? 4 : 2) / 16;
+  return pieces <= 64 ? 64 : pieces <= 128 ? 128 : 256;
+}
+unsigned blocks_for(const ExpertRows& r, int lanes) { return (unsigned)((r.tokens + 256 / lanes - 1) / (256 / lanes)); }
 
 }  // namespace
 
@@ -344,62 +386,30 @@ hipError_t launch_expert_sort(const void* expert, int index64, int64_t pairs, in
 }
 
 hipError_t launch_expert_dispatch(const ExpertRows& r, const void* x, long long x_stride, void* rows, hipStream_t s) {
-  const int size = r.f32 ? 4 : 2, bytes = piece_bytes(r.width * size, x_stride * size, x, rows, nullptr);
-  const long long pieces = r.width * size / bytes;
-  const int lanes = lanes_for(pieces), per = 256 / lanes;
-  const unsigned blocks = (unsigned)((r.tokens + per - 1) / per);
-  auto go = [&](auto raw) {
-    using Raw = decltype(raw);
-    expert_dispatch_kernel<Raw><<<blocks, 256, 0, s>>>(r, static_cast<const unsigned char*>(x), x_stride * size, static_cast<Raw*>(rows),
-                                                       pieces, lanes);
-    return hipGetLastError();
-  };
-  switch (bytes) {
-    case 16: return go(u32x4{});
-    case 8: return go(u32x2{});
-    case 4: return go(unsigned{});
-    default: return go(u16{});
-  }
+  const int lanes = lanes_for(r);
+  if (r.f32) expert_dispatch_kernel<true><<<blocks_for(r, lanes), 256, 0, s>>>(r, x, x_stride, rows, lanes);
+  else expert_dispatch_kernel<false><<<blocks_for(r, lanes), 256, 0, s>>>(r, x, x_stride, rows, lanes);
+  return hipGetLastError();
 }
 
 hipError_t launch_expert_combine(const ExpertRows& r, const void* rows, const float* weights, void* out, hipStream_t s) {
-  const int size = r.f32 ? 4 : 2, bytes = piece_bytes(r.width * size, 0, rows, out, nullptr);
-  const long long pieces = r.width * size / bytes;
-  const int lanes = lanes_for(pieces), per = 256 / lanes;
-  const unsigned blocks = (unsigned)((r.tokens + per - 1) / per);
+  const int lanes = lanes_for(r);
   auto go = [&](auto kernel) {
-    kernel<<<blocks, 256, 0, s>>>(r, rows, weights, out, pieces, lanes);
+    kernel<<<blocks_for(r, lanes), 256, 0, s>>>(r, rows, weights, out, lanes);
     return hipGetLastError();
   };
-  if (r.f32) return bytes == 16 ? go(expert_combine_kernel<16, true>) : bytes == 8 ? go(expert_combine_kernel<8, true>) : go(expert_combine_kernel<4, true>);
-  switch (bytes) {
-    case 16: return go(expert_combine_kernel<16, false>);
-    case 8: return go(expert_combine_kernel<8, false>);
-    case 4: return go(expert_combine_kernel<4, false>);
-    default: return go(expert_combine_kernel<2, false>);
-  }
+  if (r.top <= 2) return r.f32 ? go(expert_combine_kernel<true, 2>) : go(expert_combine_kernel<false, 2>);
+  return r.f32 ? go(expert_combine_kernel<true, 8>) : go(expert_combine_kernel<false, 8>);
 }
 
 hipError_t launch_expert_combine_backward(const ExpertRows& r, const void* d_out, long long d_out_stride, const void* rows,
                                           const float* weights, void* d_rows, float* d_weights, hipStream_t s) {
-  const int size = r.f32 ? 4 : 2, bytes = piece_bytes(r.width * size, d_out_stride * size, d_out, rows, d_rows);
-  const long long pieces = r.width * size / bytes;
-  const int lanes = lanes_for(pieces), per = 256 / lanes;
-  const unsigned blocks = (unsigned)((r.tokens + per - 1) / per);
+  const int lanes = lanes_for(r);
   auto go = [&](auto kernel) {
-    kernel<<<blocks, 256, 0, s>>>(r, static_cast<const unsigned char*>(d_out), d_out_stride * size, rows, weights, d_rows, d_weights, pieces,
-                                  lanes);
+    kernel<<<blocks_for(r, lanes), 256, 0, s>>>(r, d_out, d_out_stride, rows, weights, d_rows, d_weights, lanes);
     return hipGetLastError();
   };
-  if (r.f32)
-    return bytes == 16 ? go(expert_combine_backward_kernel<16, true>)
-           : bytes == 8 ? go(expert_combine_backward_kernel<8, true>) : go(expert_combine_backward_kernel<4, true>);
-  switch (bytes) {
-    case 16: return go(expert_combine_backward_kernel<16, false>);
-    case 8: return go(expert_combine_backward_kernel<8, false>);
-    case 4: return go(expert_combine_backward_kernel<4, false>);
-    default: return go(expert_combine_backward_kernel<2, false>);
-  }
+  return r.f32 ? go(expert_combine_backward_kernel<true>) : go(expert_combine_backward_kernel<false>);
 }
 
 }  // namespace muon
