@@ -285,7 +285,7 @@ int muon_adamw_step(const muon_adamw_param* params, int32_t n, const muon_adamw_
  * computed in fp32 and double.  Results do not depend on anything but the arguments: no atomics, fixed orders of summation.
  *
  * Tokens are processed in pieces, as many at a time as the workspace holds: per token of a piece vocab elements of 2 bytes (fp32: 10) where
- * gradients are asked for.  Asynchronous on hip_stream; nothing is allocated.
+ * gradients are asked for; with more than one piece and d_weight its sum so far as well, vocab x width fp32.  Asynchronous on hip_stream; nothing is allocated.
  */
 typedef struct {
   const void* hidden;       /* device; [tokens, width], rows hidden_stride apart                        */

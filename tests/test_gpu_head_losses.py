@@ -13,6 +13,7 @@ import pytest
 import torch
 
 from oracle import head_oracle as ho
+from tests.head_routes import ROUTES
 
 pytestmark = pytest.mark.gpu
 
@@ -122,6 +123,37 @@ def test_distill(losses, tokens, vocab, width, dtype, top, tau):
     head = losses.LossHead(tokens, vocab, width, DT[dtype])
     r = head.distill(h, w, index.cuda(), s.cuda(), temperature=tau, token_scale=scale)
     check(r, h, w, dtype, tau=tau, scale=scale, index=index.numpy(), teacher=s.double().numpy())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens,vocab,width", ROUTES)
+def test_every_form_of_launch(losses, tokens, vocab, width, dtype):
+    """Against the formulas in fp64 on the device (the oracle's rows one by one would take minutes), block by block of 64 x 64 of the
+    gradients: a wrong or missing tile shows in its own block."""
+    h, w, y, g = make(tokens, vocab, width, dtype)
+    y[torch.rand(tokens, generator=g) < 0.1] = -100
+    scale = (torch.rand(tokens, generator=g) + 0.5).cuda() / tokens
+    r = losses.LossHead(tokens, vocab, width, DT[dtype]).cross_entropy(h, w, y, token_scale=scale)
+    h64, w64, kept = h.double(), w.double(), y >= 0
+    z = torch.mm(h64, w64.T.contiguous())
+    lse = torch.logsumexp(z, 1)
+    at = y.clamp(min=0)[:, None]
+    loss = torch.where(kept, lse - z.gather(1, at)[:, 0], 0.0)
+    err = (4 + width ** 0.5) * 2.0 ** -23 * torch.mm(h64.abs(), w64.abs().T.contiguous()).amax(1) + 2.0 ** -21 + 2.0 ** -22 * lse.abs()
+    assert ((r.lse - lse).abs() <= err).all() and ((r.loss - loss).abs() <= 2 * err + 2.0 ** -23 * loss).all()
+    dz = (z - lse[:, None]).exp()
+    dz.scatter_add_(1, at, torch.full_like(loss, -1.0)[:, None])
+    dz *= (scale.double() * kept)[:, None]
+    for got, want in ((r.d_hidden, torch.mm(dz, w64)), (r.d_weight, torch.mm(dz.T.contiguous(), h64))):
+        rows, cols = -(-got.shape[0] // 64) * 64, -(-got.shape[1] // 64) * 64
+        blocks = []
+        for x in (got.double() - want, want):
+            full = torch.zeros(rows, cols, dtype=torch.float64, device="cuda")
+            full[:x.shape[0], :x.shape[1]] = x
+            blocks.append(full.view(rows // 64, 64, cols // 64, 64).square().sum((1, 3)).sqrt())
+        # twice the bar of the whole in a block (fewer roundings average), and never held to less than a thousandth of the typical block
+        bar = 2 * (5e-3 if dtype == "bf16" else 1e-5)
+        assert (blocks[0] <= bar * blocks[1].clamp(min=1e-3 * float(blocks[1].square().mean().sqrt()))).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
