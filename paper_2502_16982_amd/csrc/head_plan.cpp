@@ -109,7 +109,8 @@ bool head_plan(const HeadShape& s, size_t max_bytes, HeadPlan* p) {
   // Equal pieces of whole tiles, ever more of them until the workspace fits: what a query answers is one of these, so that a call
   // that is given as many bytes finds it (or an earlier one).
   const int64_t all = std::max<int64_t>(1, s.tokens);
-  for (int64_t pieces = max_bytes == 0 ? (all + kHeadPieceTokens - 1) / kHeadPieceTokens : 1;;) {
+  const int64_t most = max_bytes == 0 ? kHeadPieceTokens : std::min(kHeadMaxPiece, kHeadMaxProbs / p->vocab_pitch / 256 * 256);
+  for (int64_t pieces = (all + most - 1) / most;;) {
     const int64_t piece = std::min(all, up((all + pieces - 1) / pieces, 256));
     plan_piece(s, piece, p);
     if (max_bytes == 0 || p->total <= max_bytes) return true;

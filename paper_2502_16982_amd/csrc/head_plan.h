@@ -12,6 +12,8 @@ constexpr int kHeadMaxTop = 4096;
 constexpr int64_t kHeadMaxPitch = 1ll << 21;
 // Tokens of a piece where the caller sets no limit to the workspace.
 constexpr int64_t kHeadPieceTokens = 8192;
+// The most of a piece, and of a piece times the row pitch of its probabilities: a launch has fewer than 2^32 threads.
+constexpr int64_t kHeadMaxPiece = 1ll << 18, kHeadMaxProbs = 1ll << 35;
 
 struct HeadShape {
   int64_t tokens, vocab, width;

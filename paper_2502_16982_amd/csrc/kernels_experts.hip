@@ -190,12 +190,15 @@ struct Piece {
   }
 };
 
-// The token of a thread, its place among the token's `lanes` threads (whole waves), the token's first element in dense rows.
-struct Place {
-  long long token;
-  int at;
-};
-__device__ __forceinline__ Place place(int lanes) { return {blockIdx.x * (256ll / lanes) + threadIdx.x / lanes, (int)(threadIdx.x % lanes)}; }
+// A token's threads are `lanes` neighbours (whole waves); a block takes 256 / lanes tokens at a time, and the grid goes on until all are done
+// (a launch has fewer than 2^32 threads).  f(token, the thread's place among the token's).
+constexpr long long kMaxBlocks = 1ll << 22;
+template <typename F>
+__device__ __forceinline__ void each_token(const ExpertRows& r, int lanes, F&& f) {
+  const int per = 256 / lanes;
+  for (long long first = (long long)blockIdx.x * per; first < r.tokens; first += (long long)gridDim.x * per)
+    f(first + threadIdx.x / lanes, (int)(threadIdx.x % lanes));
+}
 
 // The row of pair i, or -1: what is no row of this call counts as dropped.
 __device__ __forceinline__ long long row_of(const ExpertRows& r, long long i) {
@@ -223,26 +226,27 @@ __global__ __launch_bounds__(256) void expert_dispatch_kernel(ExpertRows r, cons
                                                               void* __restrict__ rows_, int lanes) {
   using P = Piece<F32>;
   using Elem = typename P::Elem;
-  const Place here = place(lanes);
-  if (here.token >= r.tokens) return;
-  const Elem* mine = static_cast<const Elem*>(x) + here.token * x_stride;
   Elem* rows = static_cast<Elem*>(rows_);
-  for (long long c = (long long)here.at * P::N; c < r.width; c += (long long)lanes * P::N) {
-    if (c + P::N <= r.width) {
-      const u32x4 v = P::load(mine + c);
-      for (int j = 0; j < r.top; ++j) {
-        const long long row = row_of(r, here.token * r.top + j);
-        if (row >= 0) P::store(rows + row * r.width + c, v);
-      }
-    } else {
-      for (int j = 0; j < r.top; ++j) {
-        const long long row = row_of(r, here.token * r.top + j);
-        if (row >= 0)
-          for (long long e = c; e < r.width; ++e) rows[row * r.width + e] = mine[e];
+  each_token(r, lanes, [&](long long token, int at) {
+    if (token >= r.tokens) return;
+    const Elem* mine = static_cast<const Elem*>(x) + token * x_stride;
+    for (long long c = (long long)at * P::N; c < r.width; c += (long long)lanes * P::N) {
+      if (c + P::N <= r.width) {
+        const u32x4 v = P::load(mine + c);
+        for (int j = 0; j < r.top; ++j) {
+          const long long row = row_of(r, token * r.top + j);
+          if (row >= 0) P::store(rows + row * r.width + c, v);
+        }
+      } else {
+        for (int j = 0; j < r.top; ++j) {
+          const long long row = row_of(r, token * r.top + j);
+          if (row >= 0)
+            for (long long e = c; e < r.width; ++e) rows[row * r.width + e] = mine[e];
+        }
       }
     }
-  }
-  clear_tail<F32>(r, here.token, rows, here.at, lanes);
+    clear_tail<F32>(r, token, rows, at, lanes);
+  });
 }
 
 // ROWS rows of a token on their way at a time.
@@ -251,52 +255,53 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows r, const
                                                              void* __restrict__ out_, int lanes) {
   using P = Piece<F32>;
   using Elem = typename P::Elem;
-  const Place here = place(lanes);
-  if (here.token >= r.tokens) return;
   const Elem* rows = static_cast<const Elem*>(rows_);
-  Elem* out = static_cast<Elem*>(out_) + here.token * r.width;
-  for (long long c = (long long)here.at * P::N; c < r.width; c += (long long)lanes * P::N) {
-    const bool whole = c + P::N <= r.width;
-    float sum[P::N];
+  each_token(r, lanes, [&](long long token, int at) {
+    if (token >= r.tokens) return;
+    Elem* out = static_cast<Elem*>(out_) + token * r.width;
+    for (long long c = (long long)at * P::N; c < r.width; c += (long long)lanes * P::N) {
+      const bool whole = c + P::N <= r.width;
+      float sum[P::N];
 #pragma unroll
-    for (int e = 0; e < P::N; ++e) sum[e] = 0.f;
-    for (int j0 = 0; j0 < r.top; j0 += ROWS) {
-      long long row[ROWS];
-      float w[ROWS];
-      u32x4 v[ROWS];
-#pragma unroll
-      for (int u = 0; u < ROWS; ++u) {
-        const long long i = here.token * r.top + j0 + u;
-        row[u] = j0 + u < r.top ? row_of(r, i) : -1;
-        w[u] = row[u] < 0 ? 0.f : weights ? weights[i] : 1.f;
-      }
-      if (whole) {
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u) v[u] = row[u] < 0 ? u32x4{0u, 0u, 0u, 0u} : P::load(rows + row[u] * r.width + c);
+      for (int e = 0; e < P::N; ++e) sum[e] = 0.f;
+      for (int j0 = 0; j0 < r.top; j0 += ROWS) {
+        long long row[ROWS];
+        float w[ROWS];
+        u32x4 v[ROWS];
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
-          float f[P::N];
-          P::unpack(v[u], f);
-#pragma unroll
-          for (int e = 0; e < P::N; ++e)
-            if (row[u] >= 0) sum[e] = fmaf(w[u], f[e], sum[e]);
+          const long long i = token * r.top + j0 + u;
+          row[u] = j0 + u < r.top ? row_of(r, i) : -1;
+          w[u] = row[u] < 0 ? 0.f : weights ? weights[i] : 1.f;
         }
+        if (whole) {
+#pragma unroll
+          for (int u = 0; u < ROWS; ++u) v[u] = row[u] < 0 ? u32x4{0u, 0u, 0u, 0u} : P::load(rows + row[u] * r.width + c);
+#pragma unroll
+          for (int u = 0; u < ROWS; ++u) {
+            float f[P::N];
+            P::unpack(v[u], f);
+#pragma unroll
+            for (int e = 0; e < P::N; ++e)
+              if (row[u] >= 0) sum[e] = fmaf(w[u], f[e], sum[e]);
+          }
+        } else {
+#pragma unroll
+          for (int u = 0; u < ROWS; ++u)
+#pragma unroll
+            for (int e = 0; e < P::N; ++e)
+              if (row[u] >= 0 && c + e < r.width) sum[e] = fmaf(w[u], P::value(rows[row[u] * r.width + c + e]), sum[e]);
+        }
+      }
+      if (whole) {
+        P::store(out + c, P::pack(sum));
       } else {
 #pragma unroll
-        for (int u = 0; u < ROWS; ++u)
-#pragma unroll
-          for (int e = 0; e < P::N; ++e)
-            if (row[u] >= 0 && c + e < r.width) sum[e] = fmaf(w[u], P::value(rows[row[u] * r.width + c + e]), sum[e]);
+        for (int e = 0; e < P::N; ++e)
+          if (c + e < r.width) out[c + e] = P::elem(sum[e]);
       }
     }
-    if (whole) {
-      P::store(out + c, P::pack(sum));
-    } else {
-#pragma unroll
-      for (int e = 0; e < P::N; ++e)
-        if (c + e < r.width) out[c + e] = P::elem(sum[e]);
-    }
-  }
+  });
 }
 
 template <bool F32>
@@ -309,51 +314,54 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(ExpertRows
   const Elem* rows = static_cast<const Elem*>(rows_);
   Elem* d_rows = static_cast<Elem*>(d_rows_);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const Place here = place(lanes);
-  const bool there = here.token < r.tokens;      // (of a whole wave)
-  if (there) {
-    const Elem* mine = static_cast<const Elem*>(d_out) + here.token * d_out_stride;
-    for (int j = 0; j < r.top; ++j) {
-      const long long i = here.token * r.top + j, row = row_of(r, i);
-      float dot = 0.f;
-      if (row >= 0) {
-        const float w = weights[i];
-        const Elem* y = rows + row * r.width;
-        Elem* dy = d_rows + row * r.width;
-        for (long long c = (long long)here.at * P::N; c < r.width; c += (long long)lanes * P::N) {
-          if (c + P::N <= r.width) {
-            float g[P::N], f[P::N];
-            P::unpack(P::load(mine + c), g);
-            P::unpack(P::load(y + c), f);
+  each_token(r, lanes, [&](long long token, int at) {
+    const bool there = token < r.tokens;         // (of a whole wave)
+    if (there) {
+      const Elem* mine = static_cast<const Elem*>(d_out) + token * d_out_stride;
+      for (int j = 0; j < r.top; ++j) {
+        const long long i = token * r.top + j, row = row_of(r, i);
+        float dot = 0.f;
+        if (row >= 0) {
+          const float w = weights[i];
+          const Elem* y = rows + row * r.width;
+          Elem* dy = d_rows + row * r.width;
+          for (long long c = (long long)at * P::N; c < r.width; c += (long long)lanes * P::N) {
+            if (c + P::N <= r.width) {
+              float g[P::N], f[P::N];
+              P::unpack(P::load(mine + c), g);
+              P::unpack(P::load(y + c), f);
 #pragma unroll
-            for (int e = 0; e < P::N; ++e) {
-              dot = fmaf(g[e], f[e], dot);
-              g[e] *= w;
-            }
-            P::store(dy + c, P::pack(g));
-          } else {
-            for (long long e = c; e < r.width; ++e) {
-              const float g = P::value(mine[e]);
-              dot = fmaf(g, P::value(y[e]), dot);
-              dy[e] = P::elem(w * g);
+              for (int e = 0; e < P::N; ++e) {
+                dot = fmaf(g[e], f[e], dot);
+                g[e] *= w;
+              }
+              P::store(dy + c, P::pack(g));
+            } else {
+              for (long long e = c; e < r.width; ++e) {
+                const float g = P::value(mine[e]);
+                dot = fmaf(g, P::value(y[e]), dot);
+                dy[e] = P::elem(w * g);
+              }
             }
           }
-        }
 #pragma unroll
-        for (int off = 32; off > 0; off >>= 1) dot += __shfl_xor(dot, off, 64);
+          for (int off = 32; off > 0; off >>= 1) dot += __shfl_xor(dot, off, 64);
+        }
+        if (lane == 0) dots[j][wave] = dot;
       }
-      if (lane == 0) dots[j][wave] = dot;
+      clear_tail<F32>(r, token, d_rows, at, lanes);
     }
-    clear_tail<F32>(r, here.token, d_rows, here.at, lanes);
-  }
-  __syncthreads();
-  if (!there) return;
-  const int waves = lanes / 64, first = threadIdx.x / lanes * waves;
-  for (int j = here.at; j < r.top; j += lanes) {
-    float sum = 0.f;
-    for (int u = 0; u < waves; ++u) sum += dots[j][first + u];
-    d_weights[here.token * r.top + j] = sum;
-  }
+    __syncthreads();
+    if (there) {
+      const int waves = lanes / 64, first = threadIdx.x / lanes * waves;
+      for (int j = at; j < r.top; j += lanes) {
+        float sum = 0.f;
+        for (int u = 0; u < waves; ++u) sum += dots[j][first + u];
+        d_weights[token * r.top + j] = sum;
+      }
+    }
+    __syncthreads();                             // (the next token's dots go to the same place)
+  });
 }
 
 // Threads per token: whole waves, as many as have a piece of the row each.
@@ -361,7 +369,10 @@ int lanes_for(const ExpertRows& r) {
   const long long pieces = r.width * (r.f32 ? 4 : 2) / 16;
   return pieces <= 64 ? 64 : pieces <= 128 ? 128 : 256;
 }
-unsigned blocks_for(const ExpertRows& r, int lanes) { return (unsigned)((r.tokens + 256 / lanes - 1) / (256 / lanes)); }
+unsigned blocks_for(const ExpertRows& r, int lanes) {
+  const long long blocks = (r.tokens + 256 / lanes - 1) / (256 / lanes);
+  return (unsigned)(blocks < kMaxBlocks ? blocks : kMaxBlocks);
+}
 
 }  // namespace
 

@@ -5,6 +5,7 @@ the tensors' device.
 """
 from __future__ import annotations
 
+from functools import lru_cache
 from typing import NamedTuple, Optional, Tuple
 
 import torch
@@ -63,6 +64,9 @@ def _weights(t: torch.Tensor, position: torch.Tensor) -> int:
     return t.data_ptr()
 
 
+_sort_bytes = lru_cache(maxsize=256)(binding.muon_expert_sort_bytes)
+
+
 def sort_by_expert(expert: torch.Tensor, experts: int) -> Routing:
     """Stable sort of the pairs of ``expert`` [tokens, top] (int32 or int64) by expert; a pair whose expert is not in
     [0, experts) is dropped."""
@@ -72,7 +76,7 @@ def sort_by_expert(expert: torch.Tensor, experts: int) -> Routing:
         raise MuonError(-2, f"expert: int32 or int64, not {expert.dtype}")
     device = _device(expert)
     tokens, top = expert.shape
-    need = binding.muon_expert_sort_bytes(tokens, top, experts)
+    need = _sort_bytes(tokens, top, experts)
     with on(device):
         # one allocation for what is written; the workspace goes back to the stream it was used on
         pairs = tokens * top

@@ -41,6 +41,7 @@ static void check_plan(const HeadShape& s, const HeadPlan& p) {
   CHECK(s.tokens == 0 || (p.piece * p.pieces >= s.tokens && p.piece * (p.pieces - 1) < s.tokens), "pieces cover");
   CHECK(p.vocab_pitch % 256 == 0 && p.vocab_pitch >= s.vocab && p.width_k % 8 == 0 && p.width_k >= s.width, "pitches");
   CHECK(p.blocks * kHeadGrain >= s.vocab, "blocks");
+  CHECK(p.piece * 256 < (1ll << 32) && p.piece * (p.vocab_pitch / 4096 + 1) * 256 < (1ll << 32) + (1ll << 28), "threads");
   const int64_t last = s.tokens - (p.pieces - 1) * p.piece, row = (int64_t)p.planes * p.width_k * 2;
   for (int i = 0; i < 2; ++i) {
     check_product(p.logits[i], p.pairs);
@@ -114,6 +115,8 @@ int main(int argc, char** argv) {
             // a call finds a plan for what a query answered, also for a limit, and none below the smallest
             HeadPlan q;
             CHECK(head_plan(s, whole, &q) && q.total <= whole, "as much as the query said");
+            check_plan(s, q);
+            CHECK(head_plan(s, ~(size_t)0, &q), "all the memory there is");
             check_plan(s, q);
             if (t < 1000000) {
               HeadPlan least;
