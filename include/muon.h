@@ -1,5 +1,6 @@
 /*
- * muon.h - C ABI of the MI355X (gfx950) scaled-Muon optimizer step.
+ * muon.h - C ABI of the MI355X (gfx950) scaled-Muon optimizer step, and, below it, of the operators that make its largest gradients:
+ * the losses of a language model's head and a mixture's tokens to their experts and back.
  *
  * One call to muon_step() performs, for every 2-D matrix in a list, the update
  * rule of "Muon is Scalable for LLM Training" (arXiv 2502.16982):

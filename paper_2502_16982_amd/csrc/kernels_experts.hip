@@ -5,7 +5,8 @@
 //   out[t] = sum_j w[t, j] rows[position[t, j]]                         d_x[t] = sum_j d_rows[position[t, j]]   (w = 1)
 //   d_rows[position[t, j]] = w[t, j] d_out[t]                           d_w[t, j] = <d_out[t], rows[position[t, j]]>
 //
-// All of it is bound by memory.  Every kernel goes by token: a token's row is read once and kept in registers while its `top` rows are
+// All of it is bound by memory: 8192 tokens x 6 rows of 2048 in bf16, dispatch 39.5 us (5.9 TB/s), combine 52 (4.5; 68 where the rows were last
+// written long ago), combine_backward 82 (5.3), the sort 10 (two launches).  Every kernel goes by token: a token's row is read once and kept in registers while its `top` rows are
 // written or read, so that x, out and d_out cross once and not `top` times.  Nothing is atomic but the integer counts of the sort, whose
 // order does not matter.
 #include <hip/hip_runtime.h>
