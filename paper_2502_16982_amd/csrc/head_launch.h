@@ -66,10 +66,17 @@ hipError_t launch_head_entries(const HeadTarget& t, const void* hidden, long lon
 // *peak = the largest finite |token_scale| of all tokens, or 1: by a launch of its own, or, for few tokens, by the join.
 hipError_t launch_head_peak(const float* token_scale, long long tokens, float* peak, hipStream_t s);
 // Joins the pairs: loss and, if wanted, lse per token; with `value`, the gradients at the entries over tau and *peak, the scale of the others, and
-// log2 of the sum of 2^y in two floats.  peak null: all scales count as they are.
+// log2 of the sum of 2^y in two floats.  peak null: all scales count as they are.  entry null (up to kHeadJoinTop entries): the entries' logits
+// are computed here, from the rows themselves.
+constexpr int kHeadJoinTop = 4;
+struct HeadRows {
+  const void *hidden, *weight;
+  long long hidden_stride, weight_stride, width;
+  int f32;
+};
 hipError_t launch_head_join(const HeadTarget& t, float unit, const float* all_scales, long long all_tokens, float* peak, const float2* stats,
-                            long long stats_pitch, long long blocks, const float* entry, long long tokens, long long vocab, float* loss,
-                            float* lse, float* value, float* scale, float2* log2sum, hipStream_t s);
+                            long long stats_pitch, long long blocks, const float* entry, const HeadRows& rows, long long tokens, long long vocab,
+                            float* loss, float* lse, float* value, float* scale, float2* log2sum, hipStream_t s);
 // The logits' gradient in bf16 (in place of the probabilities) or three planes.
 hipError_t launch_head_grad(const HeadTarget& t, float unit, const float2* stats, long long stats_pitch, const float2* log2sum,
                             const float* value, const float* scale, long long tokens, long long vocab, const void* prob, long long pitch,

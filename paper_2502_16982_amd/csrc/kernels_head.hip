@@ -110,6 +110,20 @@ __device__ __forceinline__ float token_scale(const HeadTarget& t, long long toke
   return state.some && !state.beyond ? g : 0.f;
 }
 
+// <a, b> over `width` elements by a whole wave, in fp32.
+template <bool F32>
+__device__ __forceinline__ float row_dot(const void* a, long long a_at, const void* b, long long b_at, long long width) {
+  float sum = 0.f;
+  for (long long c = (threadIdx.x & 63) * 8; c < width; c += 512) {
+    const Row8 x = load_row8<F32>(a, a_at, c, width), y = load_row8<F32>(b, b_at, c, width);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf(x.v[e], y.v[e], sum);
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+  return sum;
+}
+
 // One block per token.  Each wave takes every fourth entry: a dot product of two rows in fp32.  Bound by W's rows, which come in no order:
 // 4096 tokens x 64 entries of width 2048 in bf16, 1.07 GB, 212 us (5.1 TB/s); one entry of 8192 tokens of width 4096, with the copy, 47 us.
 template <bool F32>
@@ -122,15 +136,7 @@ __global__ __launch_bounds__(256) void head_entries_kernel(HeadTarget t, const v
   for (int j = wave; j < t.top; j += 4) {
     const long long v = index_at(t, token * t.top + j);
     float sum = 0.f;
-    if (v >= 0 && v < vocab) {
-      for (long long c = lane * 8; c < width; c += 512) {
-        const Row8 a = load_row8<F32>(hidden, at, c, width), b = load_row8<F32>(weight, v * weight_stride, c, width);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum = fmaf(a.v[e], b.v[e], sum);
-      }
-#pragma unroll
-      for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    }
+    if (v >= 0 && v < vocab) sum = row_dot<F32>(hidden, at, weight, v * weight_stride, width);
     if (lane == 0) entry[token * t.top + j] = t.inv_tau * sum;
   }
   if (masked) {
@@ -294,8 +300,8 @@ constexpr long long kPeakInJoin = 16384;
 // per token for its entries, of which the first 64 are loaded at the start.
 __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float unit, const float* __restrict__ all_scales, long long all_tokens,
                                                          float* __restrict__ peak, const float2* __restrict__ stats, long long stats_pitch,
-                                                         long long blocks, const float* __restrict__ entry, long long tokens, long long vocab,
-                                                         float* __restrict__ loss, float* __restrict__ lse, float* __restrict__ value,
+                                                         long long blocks, const float* __restrict__ entry, HeadRows rows, long long tokens,
+                                                         long long vocab, float* __restrict__ loss, float* __restrict__ lse, float* __restrict__ value,
                                                          float* __restrict__ scale, float2* __restrict__ log2sum) {
   __shared__ float tops[64][17];
   __shared__ float sums[64][17];
@@ -314,12 +320,12 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
     if (v >= vocab) *beyond = true;
     if (v < 0 || v >= vocab) return e;
     e.s = t.logits ? teacher_at(t, i) : 0.f;
-    e.z = entry[i];
+    if (entry) e.z = entry[i];
     if (!(e.s == -INFINITY)) e.v = (int)v;
     return e;
   };
   bool beyond = false;
-  const Entry mine = load_entry(lane, &beyond);
+  Entry mine = load_entry(lane, &beyond);
   float g = tk < tokens && t.token_scale ? t.token_scale[tk] : 1.f;
   float most = 0.f;
   if (all_scales)
@@ -331,10 +337,23 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
   const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
   const long long token = blockIdx.x * 16ll + x, read = token < tokens ? token : tokens - 1;
   float top = -INFINITY, sum = 0.f;              // the sum is sum * 2^top
-  for (long long b0 = y; b0 < blocks; b0 += 64 * 8) {
-    float2 v[8];
+  float2 v[8];
+  auto load_stats = [&](long long b0) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) v[u] = b0 + 64 * u < blocks ? stats[(b0 + 64 * u) * stats_pitch + read] : make_float2(0.f, 0.f);
+  };
+  load_stats(y);
+  if (!entry && tk < tokens) {                   // few entries, and nobody has made their logits
+    for (int j = 0; j < t.top; ++j) {
+      const long long v = index_at(t, tk * t.top + j);
+      if (v < 0 || v >= vocab) continue;
+      const float z = t.inv_tau * (rows.f32 ? row_dot<true>(rows.hidden, tk * rows.hidden_stride, rows.weight, v * rows.weight_stride, rows.width)
+                                            : row_dot<false>(rows.hidden, tk * rows.hidden_stride, rows.weight, v * rows.weight_stride, rows.width));
+      if (lane == j) mine.z = z;
+    }
+  }
+  for (long long b0 = y; b0 < blocks; b0 += 64 * 8) {
+    if (b0 != y) load_stats(b0);
     float here = top;
 #pragma unroll
     for (int u = 0; u < 8; ++u)
@@ -735,10 +754,11 @@ hipError_t launch_head_peak(const float* token_scale, long long tokens, float* p
 }
 
 hipError_t launch_head_join(const HeadTarget& t, float unit, const float* all_scales, long long all_tokens, float* peak, const float2* stats,
-                            long long stats_pitch, long long blocks, const float* entry, long long tokens, long long vocab, float* loss,
-                            float* lse, float* value, float* scale, float2* log2sum, hipStream_t s) {
+                            long long stats_pitch, long long blocks, const float* entry, const HeadRows& rows, long long tokens, long long vocab,
+                            float* loss, float* lse, float* value, float* scale, float2* log2sum, hipStream_t s) {
   head_join_kernel<<<(unsigned)((tokens + 15) / 16), 1024, 0, s>>>(t, unit, peak && all_tokens <= kPeakInJoin ? all_scales : nullptr, all_tokens, peak,
-                                                                  stats, stats_pitch, blocks, entry, tokens, vocab, loss, lse, value, scale, log2sum);
+                                                                  stats, stats_pitch, blocks, entry, rows, tokens, vocab, loss, lse, value, scale,
+                                                                  log2sum);
   return hipGetLastError();
 }
 

@@ -46,12 +46,21 @@ class LossHead:
         self.dtype = dtype
         self.workspace = None
         self._stream = None
+        self._sizes = {}
         head = binding.muon_head(None, None, width, width, tokens, vocab, width, binding.dtype_code(dtype), 0)
         self._fit(head, 1, 3 if gradients else 0)
 
     def _fit(self, head: "binding.muon_head", top: int, gradients: int) -> None:
         """A workspace that holds the call; what there is stays where it suffices."""
-        need = binding.muon_head_workspace_bytes(head, top, gradients, self.max_workspace_bytes)
+        # what the size goes by: the pointers for their alignment only
+        key = (head.tokens, head.vocab, head.width, head.hidden_stride, head.weight_stride, head.dtype, (head.hidden or 0) % 16,
+               (head.weight or 0) % 16, top, gradients)
+        need = self._sizes.get(key)
+        if need is None:
+            need = binding.muon_head_workspace_bytes(head, top, gradients, self.max_workspace_bytes)
+            if len(self._sizes) > 1000:
+                self._sizes.clear()
+            self._sizes[key] = need
         stream = stream_handle(self.device)
         if self.workspace is None or self.workspace.numel() < need:
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
