@@ -32,7 +32,6 @@ __device__ __forceinline__ float bf16_hi(unsigned v) { return __uint_as_float(v 
 __device__ __forceinline__ float bf16_value(u16 v) { return __uint_as_float((unsigned)v << 16); }
 __device__ __forceinline__ u16 bf16_bits(float x) { return (u16)(pack_bf16(x, 0.f) & 0xffffu); }
 
-constexpr float kLog2e = 1.44269504088896340736f;
 // The largest power of a block is 2^15, high in f16's range: 2^-11 of relative precision holds down to 2^-29 of it.
 constexpr float kProbTop = 15.f;
 

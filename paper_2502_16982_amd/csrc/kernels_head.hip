@@ -3,9 +3,9 @@
 //   z = H W^T / tau     lse_t = log sum_v exp z_tv     dz_tv = g_t tau (p_tv - q_tv),  p = exp(z - lse)     dH = dz W     dW = dz^T H
 //
 // q is the target: one entry of 1 (cross entropy) or the softmax of a teacher's few best logits.  The logits' product runs over tiles of
-// vocabulary x tokens whose epilogue leaves, per block of the vocabulary and token, the maximum and the sum of exp(z - maximum), and, for
-// the gradient, exp(z - maximum) in f16.  Joining the blocks gives lse and loss; one pass scales the probabilities to dz in bf16, in
-// place, and writes the target's few entries from logits computed in fp32 (p - q there cancels); two more products give the gradients.
+// vocabulary x tokens whose epilogue leaves, per block of the vocabulary and token, a bias and the sum of 2^(z log2(e) + bias), and, for the
+// gradient, these powers in f16.  Joining the blocks gives lse and loss; one pass scales the powers to dz in bf16, in place, and writes
+// the target's few entries from logits computed in fp32 (p - q there cancels); two more products give the gradients.
 #include <hip/hip_runtime.h>
 
 #include <atomic>
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(1024) void head_peak_kernel(const float* __restrict
 // Where there are no more tokens than this, every block of the join looks through all scales itself: a launch less.
 constexpr long long kPeakInJoin = 16384;
 
-// Bound by the chain of its loads (4.5 us for 16 tokens of 256 blocks, 36 for 8192 of 1024).
+// Bound by the chain of its loads (6.4 us for 16 tokens of 256 blocks with their entries' logits, 36 for 8192 of 1024).
 // Sixteen tokens per block (a line of statistics), their blocks of the vocabulary over 64 threads each, eight loads at a time; then a wave
 // per token for its entries, of which the first 64 are loaded at the start.
 __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float unit, const float* __restrict__ all_scales, long long all_tokens,
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
 }
 
 // ---- dz ----
-// Bound by HBM: 8192 x 131072 in bf16, 2 bytes in and 2 out, 721 us (6.0 TB/s); fp32, 4 in and 6 out, 63 us for 1000 x 20011 (3.2).
+// Bound by HBM: 8192 x 131072 in bf16, 2 bytes in and 2 out, 721 us (6.0 TB/s); fp32, 4 in and 6 out, 34 us for 1000 x 20011 (5.9).
 constexpr int kGradSpan = 4096;                  // vocabulary entries per block
 template <bool F32>
 __global__ __launch_bounds__(256) void head_grad_kernel(HeadTarget t, float unit, const float2* __restrict__ stats, long long stats_pitch,
@@ -483,9 +483,13 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadTarget t, float unit
     Row8 r{};
     if (g != 0.f && v < vocab) {
       if constexpr (F32) {
-        const float* z = static_cast<const float*>(prob) + row + v;
+        const f32x4* z = reinterpret_cast<const f32x4*>(static_cast<const float*>(prob) + row + v);     // (rows end on whole tiles)
+        const f32x4 two[2] = {z[0], z[1]};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r.v[e] = v + e < vocab ? g * __builtin_amdgcn_exp2f(fmaf(unit, z[e], -l.x) - l.y) : 0.f;
+        for (int e = 0; e < 8; ++e) {
+          const float x = two[e / 4][e % 4];
+          r.v[e] = v + e < vocab ? g * __builtin_amdgcn_exp2f(fmaf(unit, x, -l.x) - l.y) : 0.f;
+        }
       } else {
         const u32x4 p = *reinterpret_cast<const u32x4*>(static_cast<const u16*>(prob) + row + v);
         const float f = g * __builtin_amdgcn_exp2f(-stats[v / kHeadGrain * stats_pitch + token].x - l.x - l.y);
@@ -519,14 +523,22 @@ __global__ __launch_bounds__(256) void head_grad_kernel(HeadTarget t, float unit
 // L (hidden states or weight) is read K-major, so that a lane's four accumulator rows are four neighbours of the result's row; so is dz for
 // the weight's gradient: nothing is transposed in memory.  Bound by the matrix cores under the power limit: 8192 x 131072 x 4096 bf16
 // 6.5 ms (hidden, 1.35 PFLOP/s, cores busy 80 % at 1.61 GHz) and 6.7 (weight), the library's product 6.5 and 7.6.
-__device__ __forceinline__ void store_out(const HeadOut& o, long long at, float x) {
-  if (o.f32) static_cast<float*>(o.out)[at] = x;
-  else static_cast<u16*>(o.out)[at] = bf16_bits(x);
-}
-__device__ __forceinline__ void finish_out(const HeadOut& o, long long at, float x) {
-  if (o.add) x += o.sum[at];
-  if (o.keep) o.sum[at] = x;
-  else store_out(o, at, x);
+// Four neighbours of the results, or as many of them as there are.
+__device__ __forceinline__ void finish_out4(const HeadOut& o, long long at, f32x4 x, int count) {
+  float* to = o.keep ? o.sum : o.f32 ? static_cast<float*>(o.out) : nullptr;
+  if (count >= 4) {
+    if (o.add) x += *reinterpret_cast<const f32x4_any*>(o.sum + at);
+    if (to) *reinterpret_cast<f32x4_any*>(to + at) = x;
+    else *reinterpret_cast<u32x2_any*>(static_cast<u16*>(o.out) + at) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (e >= count) continue;
+    const float y = o.add ? x[e] + o.sum[at + e] : x[e];
+    if (to) to[at + e] = y;
+    else static_cast<u16*>(o.out)[at + e] = bf16_bits(y);
+  }
 }
 
 // fp32 results, parts of a sum, or both: four elements per lane and store.
@@ -534,9 +546,6 @@ template <typename T>
 __device__ __forceinline__ void store_parts(const T& tile, const HeadOperand& l, const HeadOperand& r, const HeadTiles& g, const HeadOut& out, float scale,
                                             int split, long long row0, long long col0) {
   const int fr = tile.lane & 31, fh = tile.lane >> 5;
-  // fp32 destination, or none: then it is the bf16 result
-  float* to = g.splits > 1 ? out.partial + (long long)split * r.rows * l.rows : out.keep ? out.sum : out.f32 ? static_cast<float*>(out.out) : nullptr;
-  const float* add = g.splits > 1 || !out.add ? nullptr : out.sum;
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
     const long long n = col0 + tile.wn * T::WN + 32 * j + fr;
@@ -549,18 +558,14 @@ __device__ __forceinline__ void store_parts(const T& tile, const HeadOperand& l,
         f32x4 x;
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = scale * tile.acc[i][j][4 * q + e];
-        if (m + 4 <= l.rows) {
-          if (add) x += *reinterpret_cast<const f32x4_any*>(add + p);
-          if (to) *reinterpret_cast<f32x4_any*>(to + p) = x;
-          else *reinterpret_cast<u32x2_any*>(static_cast<u16*>(out.out) + p) = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+        const int count = (int)(l.rows - m < 4 ? l.rows - m : 4);
+        if (g.splits == 1) {
+          finish_out4(out, p, x, count);
         } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (m + e >= l.rows) continue;
-            const float y = add ? x[e] + add[p + e] : x[e];
-            if (to) to[p + e] = y;
-            else static_cast<u16*>(out.out)[p + e] = bf16_bits(y);
-          }
+          float* part = out.partial + (long long)split * r.rows * l.rows + p;
+          if (count == 4) *reinterpret_cast<f32x4_any*>(part) = x;
+          else
+            for (int e = 0; e < count; ++e) part[e] = x[e];
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -649,9 +654,7 @@ __global__ __launch_bounds__(256) void head_sum_splits_kernel(HeadOut out, int s
   if (wave > 0) return;
 #pragma unroll
   for (int w = 0; w < 3; ++w) x += parts[w][lane];
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (at + e < count) finish_out(out, at + e, x[e]);
+  if (at < count) finish_out4(out, at, x, (int)(count - at < 4 ? count - at : 4));
 }
 
 __global__ __launch_bounds__(256) void fill_zero_kernel(u16* p, size_t n) {
