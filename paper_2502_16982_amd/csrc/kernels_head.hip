@@ -167,6 +167,24 @@ __device__ __forceinline__ void logits_tile(const HeadOperand& weight, const Hea
   // rows of the wave's that there are; MASKED: not all of them
   const int there = (int)(weight.rows - v0 < T::WM ? weight.rows - v0 : T::WM);
   auto row = [&](int i, int v) { return 32 * i + 8 * (v / 4) + 4 * fh + v % 4; };
+  if constexpr (PROB && F32) {
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+      const long long token = col0 + tile.wn * T::WN + 32 * j + fr;
+      float* z = static_cast<float*>(prob) + token * prob_pitch + v0 + 4 * fh;
+      if (token >= hidden.rows) continue;
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          f32x4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = tile.acc[i][j][4 * q + e];
+          *reinterpret_cast<f32x4*>(z + 32 * i + 8 * q) = x;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+  }
   float top[T::FN];
   auto find_top = [&](auto masked) {
 #pragma unroll
@@ -221,24 +239,6 @@ __device__ __forceinline__ void logits_tile(const HeadOperand& weight, const Hea
   };
   if (there == T::WM) take_powers(std::false_type{});
   else take_powers(std::true_type{});
-  if constexpr (PROB && F32) {
-#pragma unroll
-    for (int j = 0; j < T::FN; ++j) {
-      const long long token = col0 + tile.wn * T::WN + 32 * j + fr;
-      float* z = static_cast<float*>(prob) + token * prob_pitch + v0 + 4 * fh;
-      if (token >= hidden.rows) continue;
-#pragma unroll
-      for (int i = 0; i < T::FM; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          f32x4 x;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = tile.acc[i][j][4 * q + e];
-          *reinterpret_cast<f32x4*>(z + 32 * i + 8 * q) = x;
-          __builtin_amdgcn_sched_barrier(0);
-        }
-    }
-  }
   if constexpr (B == 128 || (PROB && !F32)) __syncthreads();
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
