@@ -111,6 +111,26 @@ def test_strides_and_alignment(experts, dtype, extra, start):
         assert torch.allclose(a, b, rtol=2.0 ** -20, atol=1e-4)         # another width of access sums in another order
 
 
+def test_offsets_beyond_32_bits(experts):
+    """Rows of 6.9 GB: their last ones go where they belong, both ways."""
+    tokens, top, width = 70000, 6, 8192
+    e = random_experts(tokens, top, 64, 9, 0.0)
+    position, source, _ = fast_sort(e, 64)
+    r = experts.sort_by_expert(torch.tensor(e, dtype=torch.int32, device="cuda"), 64)
+    x = torch.randn(tokens, width, device="cuda").bfloat16()
+    rows = experts.dispatch(x, r)
+    some = torch.tensor(np.concatenate([np.arange(0, tokens * top, 9973), np.arange(tokens * top - 50, tokens * top)]), device="cuda")
+    assert torch.equal(rows[some], x[torch.tensor(source, device="cuda")[some] // top])
+    back = experts.dispatch_backward(rows, r)
+    assert torch.equal(back, (6 * x.float()).bfloat16())                    # six copies of the token's own row
+    w = torch.rand(tokens, top, device="cuda")
+    d_rows, d_w = experts.combine_backward(x, rows, w, r)
+    want = x.double().square().sum(1, keepdim=True)
+    assert ((d_w - want).abs() <= (4 + width ** 0.5) * 2.0 ** -23 * want).all()
+    at = torch.tensor(position[-1], device="cuda")
+    assert torch.equal(d_rows[at], (w[-1, :, None] * x[-1].float()).bfloat16())
+
+
 def test_gradients_against_differences(experts):
     """combine is linear in rows and in weights: one difference is exact but for rounding."""
     e = random_experts(60, 4, 9, 2)

@@ -218,6 +218,26 @@ def test_pieces_of_tokens(losses, dtype):
           index=index.numpy(), teacher=s.bfloat16().double().numpy())
 
 
+def test_offsets_beyond_32_bits(losses):
+    """One piece whose probabilities take 5 GB: every loss, and the gradients' last rows, against fp64 on the device."""
+    tokens, vocab, width = 20000, 131072, 64
+    h, w, y, _ = make(tokens, vocab, width, "bf16")
+    head = losses.LossHead(tokens, vocab, width, max_workspace_bytes=8 << 30)
+    assert head.workspace.numel() > tokens * vocab * 2
+    r = head.cross_entropy(h, w, y)
+    w64, last, d_last = w.double(), vocab - 100, torch.zeros(100, width, dtype=torch.float64, device="cuda")
+    for a in range(0, tokens, 2000):
+        h64, at = h[a:a + 2000].double(), y[a:a + 2000, None]
+        z = torch.mm(h64, w64.T.contiguous())
+        lse = torch.logsumexp(z, 1)
+        assert (r.loss[a:a + 2000] - (lse - z.gather(1, at)[:, 0])).abs().max() <= 1e-4
+        dz = (z - lse[:, None]).exp().scatter_add_(1, at, torch.full_like(lse, -1.0)[:, None])
+        d_last += torch.mm(dz[:, last:].T.contiguous(), h64)
+        d_hidden = torch.mm(dz, w64)
+        assert (r.d_hidden[a:a + 2000].double() - d_hidden).norm() <= 5e-3 * d_hidden.norm()
+    assert (r.d_weight[last:].double() - d_last).norm() <= 5e-3 * d_last.norm()
+
+
 def test_one_gradient_at_a_time(losses):
     h, w, y, _ = make(100, 600, 64, "bf16")
     head = losses.LossHead(100, 600, 64)
