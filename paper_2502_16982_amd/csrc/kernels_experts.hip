@@ -5,8 +5,8 @@
 //   out[t] = sum_j w[t, j] rows[position[t, j]]                         d_x[t] = sum_j d_rows[position[t, j]]   (w = 1)
 //   d_rows[position[t, j]] = w[t, j] d_out[t]                           d_w[t, j] = <d_out[t], rows[position[t, j]]>
 //
-// All of it is bound by memory: 8192 tokens x 6 rows of 2048 in bf16, dispatch 39.5 us (5.9 TB/s), combine 52 (4.5; 68 where the rows were last
-// written long ago), combine_backward 82 (5.3), the sort 10 (two launches).  Every kernel goes by token: a token's row is read once and kept in registers while its `top` rows are
+// All of it is bound by memory: 8192 tokens x 6 rows of 2048 in bf16, dispatch 36 to 40 us (5.9 to 6.5 TB/s), combine 46 (5.1),
+// combine_backward 79 (5.5), the sort 10 (two launches).  Every kernel goes by token: a token's row is read once and kept in registers while its `top` rows are
 // written or read, so that x, out and d_out cross once and not `top` times.  Nothing is atomic but the integer counts of the sort, whose
 // order does not matter.
 #include <hip/hip_runtime.h>
@@ -151,6 +151,12 @@ struct Piece {
   static constexpr int N = F32 ? 4 : 8;
   typedef std::conditional_t<F32, float, u16> Elem;
   static __device__ __forceinline__ u32x4 load(const Elem* p) { return *reinterpret_cast<const u32x4_any*>(p); }
+  // ONCE: with the streaming hint
+  template <bool ONCE>
+  static __device__ __forceinline__ u32x4 load_row(const Elem* p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
+    else return load(p);
+  }
   static __device__ __forceinline__ void store(Elem* p, u32x4 v) { *reinterpret_cast<u32x4_any*>(p) = v; }
   static __device__ __forceinline__ void unpack(u32x4 raw, float (&v)[N]) {
     if constexpr (F32) {
@@ -251,7 +257,7 @@ __global__ __launch_bounds__(256) void expert_dispatch_kernel(ExpertRows r, cons
 }
 
 // ROWS rows of a token on their way at a time.
-template <bool F32, int ROWS>
+template <bool F32, int ROWS, bool ONCE>
 __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows r, const void* __restrict__ rows_, const float* __restrict__ weights,
                                                              void* __restrict__ out_, int lanes) {
   using P = Piece<F32>;
@@ -277,7 +283,7 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows r, const
         }
         if (whole) {
 #pragma unroll
-          for (int u = 0; u < ROWS; ++u) v[u] = row[u] < 0 ? u32x4{0u, 0u, 0u, 0u} : P::load(rows + row[u] * r.width + c);
+          for (int u = 0; u < ROWS; ++u) v[u] = row[u] < 0 ? u32x4{0u, 0u, 0u, 0u} : P::template load_row<ONCE>(rows + row[u] * r.width + c);
 #pragma unroll
           for (int u = 0; u < ROWS; ++u) {
             float f[P::N];
@@ -305,7 +311,7 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows r, const
   });
 }
 
-template <bool F32>
+template <bool F32, bool ONCE>
 __global__ __launch_bounds__(256) void expert_combine_backward_kernel(ExpertRows r, const void* __restrict__ d_out, long long d_out_stride,
                                                                       const void* __restrict__ rows_, const float* __restrict__ weights,
                                                                       void* __restrict__ d_rows_, float* __restrict__ d_weights, int lanes) {
@@ -330,7 +336,7 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(ExpertRows
             if (c + P::N <= r.width) {
               float g[P::N], f[P::N];
               P::unpack(P::load(mine + c), g);
-              P::unpack(P::load(y + c), f);
+              P::unpack(P::template load_row<ONCE>(y + c), f);
 #pragma unroll
               for (int e = 0; e < P::N; ++e) {
                 dot = fmaf(g[e], f[e], dot);
@@ -365,6 +371,10 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(ExpertRows
   });
 }
 
+// Rows that fill the memory-side cache (256 MB) are read with the streaming hint: 8192 x 6 rows of 2048 bf16 (201 MB), dispatch with its gradient
+// 116 -> 94 to 102 us, combine with its gradients 140 -> 125 to 138 (by what else the cache holds); rows that stay in the cache without it lose
+// by it (34 MB: 23 -> 30).
+bool rows_once(const ExpertRows& r) { return r.tokens * r.top * r.width * (r.f32 ? 4 : 2) >= 128ll << 20; }
 // Threads per token: whole waves, as many as have a piece of the row each.
 int lanes_for(const ExpertRows& r) {
   const long long pieces = r.width * (r.f32 ? 4 : 2) / 16;
@@ -410,8 +420,19 @@ hipError_t launch_expert_combine(const ExpertRows& r, const void* rows, const fl
     kernel<<<blocks_for(r, lanes), 256, 0, s>>>(r, rows, weights, out, lanes);
     return hipGetLastError();
   };
-  if (r.top <= 2) return r.f32 ? go(expert_combine_kernel<true, 2>) : go(expert_combine_kernel<false, 2>);
-  return r.f32 ? go(expert_combine_kernel<true, 8>) : go(expert_combine_kernel<false, 8>);
+#define MUON_COMBINE_CASE(F32, ROWS, ONCE) \
+  if ((r.f32 != 0) == F32 && (r.top <= 2 ? 2 : 8) == ROWS && once == ONCE) return go(expert_combine_kernel<F32, ROWS, ONCE>)
+  const bool once = rows_once(r);
+  MUON_COMBINE_CASE(false, 2, false);
+  MUON_COMBINE_CASE(false, 2, true);
+  MUON_COMBINE_CASE(false, 8, false);
+  MUON_COMBINE_CASE(false, 8, true);
+  MUON_COMBINE_CASE(true, 2, false);
+  MUON_COMBINE_CASE(true, 2, true);
+  MUON_COMBINE_CASE(true, 8, false);
+  MUON_COMBINE_CASE(true, 8, true);
+#undef MUON_COMBINE_CASE
+  return hipErrorInvalidValue;
 }
 
 hipError_t launch_expert_combine_backward(const ExpertRows& r, const void* d_out, long long d_out_stride, const void* rows,
@@ -421,7 +442,8 @@ hipError_t launch_expert_combine_backward(const ExpertRows& r, const void* d_out
     kernel<<<blocks_for(r, lanes), 256, 0, s>>>(r, d_out, d_out_stride, rows, weights, d_rows, d_weights, lanes);
     return hipGetLastError();
   };
-  return r.f32 ? go(expert_combine_backward_kernel<true>) : go(expert_combine_backward_kernel<false>);
+  if (rows_once(r)) return r.f32 ? go(expert_combine_backward_kernel<true, true>) : go(expert_combine_backward_kernel<false, true>);
+  return r.f32 ? go(expert_combine_backward_kernel<true, false>) : go(expert_combine_backward_kernel<false, false>);
 }
 
 }  // namespace muon
