@@ -305,9 +305,11 @@ enum { MUON_HEAD_D_HIDDEN = 1, MUON_HEAD_D_WEIGHT = 2 };
 /*
  * Bytes of workspace (256-byte aligned device memory) for a call with this head.  top: entries per token (1 for muon_cross_entropy, up to
  * 4096); gradients: which of MUON_HEAD_D_HIDDEN | MUON_HEAD_D_WEIGHT will be asked for.  max_bytes: the most that may be answered, in
- * exchange for smaller pieces (the smallest workspace there is may be larger); 0: pieces of up to 8192 tokens.  The pointers in *head are
- * read for their alignment only and may be null.  A call takes any workspace of at least the smallest size, and larger pieces in a
- * larger one.
+ * exchange for smaller pieces and fewer products split over the chip (the smallest workspace there is may be larger than that; it is never larger
+ * than the answer without a limit); 0: what pieces of up to 8192 tokens take.  The pointers in *head are read for their alignment only and
+ * may be null.  The answer is never smaller for more tokens, vocabulary, entries or gradients, so that a workspace of the largest call serves
+ * the smaller ones; rows that are copied first (bf16 whose width, stride or address is no multiple of 16 bytes) take more than rows that
+ * are not.  A call takes any workspace of at least the smallest size and cuts its work by what it is given: equal bytes, equal results.
  */
 int muon_head_workspace_bytes(const muon_head* head, int32_t top, int32_t gradients, size_t max_bytes, size_t* out);
 

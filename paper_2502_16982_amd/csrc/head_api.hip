@@ -125,9 +125,7 @@ int muon_head_workspace_bytes(const muon_head* head, int32_t top, int32_t gradie
     if (!out || gradients < 0 || gradients > 3) return MUON_E_INVALID_ARG;
     HeadShape shape;
     if (int st = head_shape(head, top, (gradients & MUON_HEAD_D_HIDDEN) != 0, (gradients & MUON_HEAD_D_WEIGHT) != 0, &shape)) return st;
-    HeadPlan p;
-    head_plan(shape, max_bytes, &p);             // the smallest there is where max_bytes do not suffice
-    *out = p.total;
+    *out = head_workspace(shape, max_bytes);
     return MUON_OK;
   });
 }

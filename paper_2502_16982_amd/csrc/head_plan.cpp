@@ -7,19 +7,80 @@ namespace {
 
 constexpr int64_t up(int64_t v, int64_t grain) { return (v + grain - 1) / grain * grain; }
 
-void plan_piece(const HeadShape& s, int64_t piece, HeadPlan* p) {
+constexpr int64_t kUnits = 256;                  // compute units
+// What a launch takes, in us, from the time of a slab of 64 of K: a 256-wide tile per compute unit 1.75; two 128-wide ones 1.17; one
+// alone, on the longer ring, 0.58; and 10, 4 or 6 to start and to store.  Both sides of the choices that are near: gradient of H at 2048 x 32768 x 1024
+// bf16, 256-wide in 8 runs of K 123 us + 14 to join, 128-wide alone in 2 runs 145 + 7; at 1000 x 20011 x 777 fp32 226 + 10 against 293 + 6;
+// 4096 x 65537 x 2048 bf16 in 2 runs 899 + 21 against tiles of 128 in whole 1197; its gradient of W, 257 x 8 tiles, with the last round in
+// quarters 991 against 1032.
+double time_wide(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (1.75 * slabs + 10); }
+double time_narrow(int64_t blocks, double slabs) { return (double)((blocks + 2 * kUnits - 1) / (2 * kUnits)) * (1.17 * slabs + 4); }
+double time_alone(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (0.58 * slabs + 6); }
+// Runs of K, and slabs that a run has at least.
+constexpr int64_t kMaxSplits = 64, kMinRun = 8;
+
+}  // namespace
+
+// The fastest by the times above of: tiles of 256, with what the last round holds in tiles of 128 where that is quicker; tiles of 128;
+// either with K in up to 64 runs of at least eight slabs, whose fp32 results are written and read once more (at 5 bytes per ps, and a launch),
+// where these take no more than partial_bytes.
+HeadProduct head_product(int64_t m, int64_t n, int64_t k, int pairs, int64_t partial_bytes) {
+  HeadProduct p{};
+  p.m = m;
+  p.n = n;
+  p.k = k;
+  auto tiles = [&](int64_t tile) { return ((m + tile - 1) / tile) * ((n + tile - 1) / tile); };
+  const int64_t wide = tiles(256), narrow = tiles(128), slabs = std::max<int64_t>(1, (k + kHeadSlab - 1) / kHeadSlab * pairs);
+  double best = 0;
+  int64_t splits = 1;
+  auto offer = [&](double us, int tile, bool alone, int64_t whole, int64_t s) {
+    if (p.tile && us >= best) return;
+    best = us;
+    p.tile = tile;
+    p.alone = alone;
+    p.whole = (int)whole;
+    splits = s;
+  };
+  if (narrow <= kUnits) offer(time_alone(narrow, (double)slabs), 128, true, narrow, 1);
+  offer(time_narrow(narrow, (double)slabs), 128, false, narrow, 1);
+  offer(time_wide(wide, (double)slabs), 256, false, wide, 1);
+  const int64_t rest = wide % kUnits;
+  if (wide > kUnits && rest) offer(time_wide(wide - rest, (double)slabs) + time_alone(4 * rest, (double)slabs), 256, false, wide - rest, 1);
+  for (int64_t s = 2; s <= kMaxSplits && slabs / s >= kMinRun && s * m * n * 4 <= partial_bytes; ++s) {
+    const double each = (double)((slabs + s - 1) / s), join = 4 + (double)(s * m * n) * 8e-6 / 5;
+    if (narrow * s <= kUnits) offer(time_alone(narrow * s, each) + join, 128, true, narrow, s);
+    if (narrow * s <= 2 * kUnits) offer(time_narrow(narrow * s, each) + join, 128, false, narrow, s);
+    if (wide * s <= 2 * kUnits) offer(time_wide(wide * s, each) + join, 256, false, wide, s);
+  }
+  p.tiles_m = (int)((m + p.tile - 1) / p.tile);
+  p.tiles_n = (int)((n + p.tile - 1) / p.tile);
+  p.slabs_per_split = (int)((slabs + splits - 1) / splits);
+  p.splits = (int)((slabs + p.slabs_per_split - 1) / p.slabs_per_split);
+  return p;
+}
+
+namespace {
+
+// What of a plan goes by the shape alone.
+HeadPlan plan_shape(const HeadShape& s) {
+  HeadPlan p{};
+  p.planes = s.f32 ? 3 : 1;
+  p.pairs = s.f32 ? 6 : 1;
+  p.width_k = up(s.width, 8);
+  p.vocab_pitch = up(s.vocab, 256);
+  p.blocks = up(s.vocab, kHeadGrain) / kHeadGrain;
+  // fp32 operands are split into planes; bf16 rows that do not come in whole aligned chunks of 16 bytes are copied
+  const bool ragged = s.f32 || s.width % 8 != 0;
+  p.pack_hidden = ragged || s.hidden_stride % 8 != 0 || s.hidden_stride > kHeadMaxPitch || !s.hidden_aligned;
+  p.pack_weight = ragged || s.weight_stride % 8 != 0 || s.weight_stride > kHeadMaxPitch || !s.weight_aligned;
+  return p;
+}
+
+// Lays out the sections for pieces of so many tokens; the splits' sums come last.
+void lay_out(const HeadShape& s, int64_t piece, int64_t partial, HeadPlan* p) {
   p->piece = piece;
   p->pieces = std::max<int64_t>(1, (s.tokens + piece - 1) / piece);
   const bool gradients = s.d_hidden || s.d_weight;
-  const int64_t sizes[2] = {piece, s.tokens - (p->pieces - 1) * piece};
-  int64_t partial = 0;
-  for (int i = 0; i < 2; ++i) {
-    p->logits[i] = head_product(s.vocab, sizes[i], p->width_k, p->pairs, false);
-    p->hidden[i] = head_product(s.width, sizes[i], s.vocab, p->pairs, true);
-    p->weight[i] = head_product(s.width, s.vocab, sizes[i], p->pairs, true);
-    if (s.d_hidden && p->hidden[i].splits > 1) partial = std::max(partial, p->hidden[i].splits * sizes[i] * s.width * 4);
-    if (s.d_weight && p->weight[i].splits > 1) partial = std::max(partial, p->weight[i].splits * s.vocab * s.width * 4);
-  }
   size_t at = 0;
   auto take = [&](bool wanted, int64_t bytes) {
     const size_t here = at;
@@ -43,84 +104,83 @@ void plan_piece(const HeadShape& s, int64_t piece, HeadPlan* p) {
   p->total = std::max<size_t>(at, 256);
 }
 
-}  // namespace
+// Bytes for pieces of so many tokens without any splits.  More tokens in a piece take more, but for the sum of d_weight, which one piece
+// does without.
+size_t bytes_unsplit(const HeadShape& s, int64_t piece) {
+  HeadPlan p = plan_shape(s);
+  lay_out(s, piece, 0, &p);
+  return p.total;
+}
 
-namespace {
-
-constexpr int64_t kUnits = 256;                  // compute units
-// What a launch takes, in us, from the time of a slab of 64 of K: a 256-wide tile per compute unit 1.75; two 128-wide ones 1.17; one
-// alone, on the longer ring, 0.58; and 10, 4 or 6 to start and to store.  Both sides of the choices that are near: gradient of H at 2048 x 32768 x 1024
-// bf16, 256-wide in 8 runs of K 123 us + 14 to join, 128-wide alone in 2 runs 145 + 7; at 1000 x 20011 x 777 fp32 226 + 10 against 293 + 6;
-// 4096 x 65537 x 2048 bf16 in 2 runs 899 + 21 against tiles of 128 in whole 1197; its gradient of W, 257 x 8 tiles, with the last round in
-// quarters 991 against 1032.
-double time_wide(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (1.75 * slabs + 10); }
-double time_narrow(int64_t blocks, double slabs) { return (double)((blocks + 2 * kUnits - 1) / (2 * kUnits)) * (1.17 * slabs + 4); }
-double time_alone(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (0.58 * slabs + 6); }
-
-}  // namespace
-
-// The fastest by the times above of: tiles of 256, with what the last round holds in tiles of 128 where that is quicker; tiles of 128;
-// either with K in up to 64 runs of at least eight slabs, whose fp32 results are written and read once more (at 5 bytes per ps, and a launch).
-HeadProduct head_product(int64_t m, int64_t n, int64_t k, int pairs, bool may_split) {
-  HeadProduct p{};
-  p.m = m;
-  p.n = n;
-  p.k = k;
-  auto tiles = [&](int64_t tile) { return ((m + tile - 1) / tile) * ((n + tile - 1) / tile); };
-  const int64_t wide = tiles(256), narrow = tiles(128), slabs = std::max<int64_t>(1, (k + kHeadSlab - 1) / kHeadSlab * pairs);
-  double best = 0;
-  int64_t splits = 1;
-  auto offer = [&](double us, int tile, bool alone, int64_t whole, int64_t s) {
-    if (p.tile && us >= best) return;
-    best = us;
-    p.tile = tile;
-    p.alone = alone;
-    p.whole = (int)whole;
-    splits = s;
+// Bytes that the sums of splits may take: what no choice of head_product goes beyond, so that it is never held back.  Unlike the choice
+// itself this grows with every size, which makes a workspace for more tokens one for fewer.
+int64_t bytes_split(const HeadShape& s, int64_t piece) {
+  auto product = [&](int64_t n, int64_t k) -> int64_t {
+    const int64_t splits = std::min(kMaxSplits, (k + kHeadSlab - 1) / kHeadSlab * (s.f32 ? 6 : 1) / kMinRun);
+    return splits < 2 ? 0 : std::min(2 * kUnits * 256 * 256 * 4, splits * s.width * n * 4);
   };
-  if (narrow <= kUnits) offer(time_alone(narrow, (double)slabs), 128, true, narrow, 1);
-  offer(time_narrow(narrow, (double)slabs), 128, false, narrow, 1);
-  offer(time_wide(wide, (double)slabs), 256, false, wide, 1);
-  const int64_t rest = wide % kUnits;
-  if (wide > kUnits && rest) offer(time_wide(wide - rest, (double)slabs) + time_alone(4 * rest, (double)slabs), 256, false, wide - rest, 1);
-  if (may_split) {
-    for (int64_t s = 2; s <= 64 && slabs / s >= 8; ++s) {
-      const double each = (double)((slabs + s - 1) / s), join = 4 + (double)(s * m * n) * 8e-6 / 5;
-      if (narrow * s <= kUnits) offer(time_alone(narrow * s, each) + join, 128, true, narrow, s);
-      if (narrow * s <= 2 * kUnits) offer(time_narrow(narrow * s, each) + join, 128, false, narrow, s);
-      if (wide * s <= 2 * kUnits) offer(time_wide(wide * s, each) + join, 256, false, wide, s);
-    }
+  return up(std::max(s.d_hidden ? product(piece, s.vocab) : 0, s.d_weight ? product(s.vocab, piece) : 0), 256);
+}
+
+// The most tokens of a piece that a launch takes.
+int64_t most_tokens(const HeadShape& s) { return std::min(kHeadMaxPiece, kHeadMaxProbs / up(s.vocab, 256) / 256 * 256); }
+
+}  // namespace
+
+size_t head_workspace(const HeadShape& s, size_t max_bytes) {
+  const int64_t all = std::max<int64_t>(1, s.tokens);
+  size_t want = ~(size_t)0, least = ~(size_t)0;
+  if (all <= most_tokens(s)) {                     // one piece
+    least = bytes_unsplit(s, all);
+    want = least + bytes_split(s, all);
   }
-  p.tiles_m = (int)((m + p.tile - 1) / p.tile);
-  p.tiles_n = (int)((n + p.tile - 1) / p.tile);
-  p.slabs_per_split = (int)((slabs + splits - 1) / splits);
-  p.splits = (int)((slabs + p.slabs_per_split - 1) / p.slabs_per_split);
-  return p;
+  if (max_bytes == 0) return all <= kHeadPieceTokens ? want : std::min(want, bytes_unsplit(s, kHeadPieceTokens) + bytes_split(s, kHeadPieceTokens));
+  if (want <= max_bytes) return want;
+  if (all > 256) least = std::min(least, bytes_unsplit(s, 256));
+  return std::max(least, max_bytes / 256 * 256);
 }
 
 bool head_plan(const HeadShape& s, size_t max_bytes, HeadPlan* p) {
-  *p = HeadPlan{};
-  p->planes = s.f32 ? 3 : 1;
-  p->pairs = s.f32 ? 6 : 1;
-  p->width_k = up(s.width, 8);
-  p->vocab_pitch = up(s.vocab, 256);
-  p->blocks = up(s.vocab, kHeadGrain) / kHeadGrain;
-  // fp32 operands are split into planes; bf16 rows that do not come in whole aligned chunks of 16 bytes are copied
-  const bool ragged = s.f32 || s.width % 8 != 0;
-  p->pack_hidden = ragged || s.hidden_stride % 8 != 0 || s.hidden_stride > kHeadMaxPitch || !s.hidden_aligned;
-  p->pack_weight = ragged || s.weight_stride % 8 != 0 || s.weight_stride > kHeadMaxPitch || !s.weight_aligned;
-  // Equal pieces of whole tiles, ever more of them until the workspace fits: what a query answers is one of these, so that a call
-  // that is given as many bytes finds it (or an earlier one).
-  const int64_t all = std::max<int64_t>(1, s.tokens);
-  const int64_t most = max_bytes == 0 ? kHeadPieceTokens : std::min(kHeadMaxPiece, kHeadMaxProbs / p->vocab_pitch / 256 * 256);
-  for (int64_t pieces = (all + most - 1) / most;;) {
-    const int64_t piece = std::min(all, up((all + pieces - 1) / pieces, 256));
-    plan_piece(s, piece, p);
-    if (max_bytes == 0 || p->total <= max_bytes) return true;
-    const int64_t smaller = (piece - 1) / 256 * 256;
-    if (smaller == 0) return false;
-    pieces = (all + smaller - 1) / smaller;
+  *p = plan_shape(s);
+  const int64_t all = std::max<int64_t>(1, s.tokens), most = max_bytes == 0 ? kHeadPieceTokens : most_tokens(s);
+  const size_t limit = max_bytes == 0 ? (size_t)1 << 62 : std::min(max_bytes, (size_t)1 << 62);
+  // all tokens in one piece, or as many whole tiles of them as fit
+  int64_t piece = all <= most && bytes_unsplit(s, all) <= limit ? all : 0;
+  if (piece == 0) {
+    auto largest = [&](auto&& bytes) {
+      int64_t low = 0, high = std::min(most, (all - 1) / 256 * 256) / 256;
+      while (low < high) {
+        const int64_t middle = (low + high + 1) / 2;
+        if (bytes(middle * 256) <= limit) low = middle;
+        else high = middle - 1;
+      }
+      return low * 256;
+    };
+    const int64_t alone = largest([&](int64_t n) { return bytes_unsplit(s, n); });
+    // with room for splits, unless that halves the pieces: a piece more reads the weight three times and the sum twice
+    const int64_t split = largest([&](int64_t n) { return bytes_unsplit(s, n) + (size_t)bytes_split(s, n); });
+    piece = 2 * split >= alone ? split : alone;
+    if (piece > 0) {                               // equal pieces
+      const int64_t pieces = (all + piece - 1) / piece;
+      piece = up((all + pieces - 1) / pieces, 256);
+    }
   }
+  const bool fits = piece > 0;
+  if (!fits) piece = std::min<int64_t>(all, 256);
+  const size_t unsplit = bytes_unsplit(s, piece);
+  const int64_t room = fits ? (int64_t)((limit - unsplit) / 256 * 256) : 0;
+  lay_out(s, piece, 0, p);                         // (how many pieces there are)
+  const int64_t sizes[2] = {piece, s.tokens - (p->pieces - 1) * piece};
+  int64_t partial = 0;
+  for (int i = 0; i < 2; ++i) {
+    p->logits[i] = head_product(s.vocab, sizes[i], p->width_k, p->pairs, 0);
+    p->hidden[i] = head_product(s.width, sizes[i], s.vocab, p->pairs, room);
+    p->weight[i] = head_product(s.width, s.vocab, sizes[i], p->pairs, room);
+    if (s.d_hidden && p->hidden[i].splits > 1) partial = std::max(partial, p->hidden[i].splits * sizes[i] * s.width * 4);
+    if (s.d_weight && p->weight[i].splits > 1) partial = std::max(partial, p->weight[i].splits * s.vocab * s.width * 4);
+  }
+  lay_out(s, piece, partial, p);
+  return fits;
 }
 
 }  // namespace muon

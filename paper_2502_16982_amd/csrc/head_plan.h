@@ -56,10 +56,13 @@ struct HeadPlan {
   size_t total;
 };
 
-// The product of an m x k by a k x n operand for a device of 256 compute units.
-HeadProduct head_product(int64_t m, int64_t n, int64_t k, int pairs, bool may_split);
-// The plan with the largest pieces whose workspace is at most max_bytes (0: pieces of kHeadPieceTokens), or, where none is, the one with
-// the smallest; for a call, which gives the bytes that there are, false where they do not suffice.
+// The product of an m x k by a k x n operand for a device of 256 compute units; the sums of K's runs may take partial_bytes (0: one run).
+HeadProduct head_product(int64_t m, int64_t n, int64_t k, int pairs, int64_t partial_bytes);
+// Workspace to give a call: what the fastest plan takes with pieces of kHeadPieceTokens (max_bytes 0), or with one piece of all tokens; where that is
+// more than max_bytes, all of these; the smallest workspace at least.  Never less for more tokens, vocabulary or entries, or for a higher limit.
+size_t head_workspace(const HeadShape& shape, size_t max_bytes);
+// The plan of a call that has so many bytes (0: pieces of kHeadPieceTokens, whatever they take): the largest pieces that fit, K in runs where
+// there is room for their sums.  False, with the plan of the smallest pieces, where nothing fits.
 bool head_plan(const HeadShape& shape, size_t max_bytes, HeadPlan* out);
 
 }  // namespace muon

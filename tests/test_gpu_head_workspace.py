@@ -1,0 +1,48 @@
+"""Workspaces of the head's losses on the device: smaller calls in a larger call's, and what outlives what."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def make(tokens, vocab, width, dtype="bf16", seed=0):
+    g = torch.Generator().manual_seed(seed)
+    w = torch.randn(vocab, width, generator=g) * 0.05
+    h = torch.randn(tokens, width, generator=g)
+    y = torch.randint(vocab, (tokens,), generator=g)
+    return h.to(DT[dtype]).cuda(), w.to(DT[dtype]).cuda(), y.cuda()
+
+
+def want64(h, w, y, scale=None):
+    """loss, d_hidden, d_weight of the sum in fp64 on the device."""
+    h64, w64, at = h.double(), w.double(), y[:, None]
+    z = torch.mm(h64, w64.T.contiguous())
+    lse = torch.logsumexp(z, 1)
+    dz = (z - lse[:, None]).exp()
+    dz.scatter_add_(1, at, torch.full_like(lse, -1.0)[:, None])
+    if scale is not None:
+        dz *= scale.double()[:, None]
+    return lse - z.gather(1, at)[:, 0], torch.mm(dz, w64), torch.mm(dz.T.contiguous(), h64)
+
+
+@pytest.mark.parametrize("limit", [0, 27 << 20])
+def test_fewer_tokens_in_the_workspace_of_more(limit):
+    """1680 tokens take K in one run, 1260 would take it in several; what the larger call was given serves the smaller one, through the C
+    ABI as well.  bf16: gradients as a whole within 5e-3, dz and the result rounded once each."""
+    from paper_2502_16982_amd import binding
+    tokens, fewer, vocab, width = 1680, 1260, 3817, 4096
+    h, w, y = make(tokens, vocab, width)
+    head = binding.muon_head(h.data_ptr(), w.data_ptr(), width, width, tokens, vocab, width, 1, 0)
+    workspace = torch.empty(binding.muon_head_workspace_bytes(head, 1, 3, limit), dtype=torch.uint8, device="cuda")
+    for n in (tokens, fewer, 1):
+        loss = torch.empty(n, device="cuda")
+        dh, dw = torch.empty_like(h[:n]), torch.empty_like(w)
+        head = binding.muon_head(h.data_ptr(), w.data_ptr(), width, width, n, vocab, width, 1, 0)
+        binding.muon_cross_entropy(head, y.data_ptr(), 8, 0, loss.data_ptr(), 0, dh.data_ptr(), dw.data_ptr(), workspace.data_ptr(),
+                                   workspace.numel(), torch.cuda.current_stream().cuda_stream)
+        want, want_h, want_w = want64(h[:n], w, y[:n])
+        assert (loss - want).abs().max() <= 1e-4
+        for got, ref in ((dh, want_h), (dw, want_w)):
+            assert (got.double() - ref).norm() <= 5e-3 * ref.norm()
