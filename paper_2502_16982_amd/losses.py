@@ -50,8 +50,9 @@ class LossHead:
         head = binding.muon_head(None, None, width, width, tokens, vocab, width, binding.dtype_code(dtype), 0)
         self._fit(head, 1, 3 if gradients else 0)
 
-    def _fit(self, head: "binding.muon_head", top: int, gradients: int) -> None:
-        """A workspace that holds the call; what there is stays where it suffices."""
+    def _fit(self, head: "binding.muon_head", top: int, gradients: int) -> int:
+        """Bytes of workspace for the call, which are there then.  The library cuts the call by these and not by all that there is, so that
+        results do not depend on earlier calls."""
         # what the size goes by: the pointers for their alignment only
         key = (head.tokens, head.vocab, head.width, head.hidden_stride, head.weight_stride, head.dtype, (head.hidden or 0) % 16,
                (head.weight or 0) % 16, top, gradients)
@@ -67,6 +68,7 @@ class LossHead:
             self._stream = stream
         elif stream != self._stream:                       # the memory outlives what this stream does with it
             self.workspace.record_stream(torch.cuda.current_stream(self.device))
+        return need
 
     def _head(self, hidden: torch.Tensor, weight: torch.Tensor) -> "binding.muon_head":
         if hidden.dim() != 2 or weight.dim() != 2 or hidden.shape[1] != weight.shape[1]:
@@ -121,9 +123,9 @@ class LossHead:
         size, scale = _index_bytes(targets, "targets"), self._scale(token_scale, hidden.shape[0])
         with on(self.device):
             out, which = self._outputs(hidden, weight, gradients)
-            self._fit(head, 1, which)
-            binding.muon_cross_entropy(head, targets.data_ptr(), size, scale, *self._pointers(out), self.workspace.data_ptr(),
-                                       self.workspace.numel(), stream_handle(self.device))
+            need = self._fit(head, 1, which)
+            binding.muon_cross_entropy(head, targets.data_ptr(), size, scale, *self._pointers(out), self.workspace.data_ptr(), need,
+                                       stream_handle(self.device))
         return out
 
     def distill(self, hidden: torch.Tensor, weight: torch.Tensor, teacher_index: torch.Tensor, teacher_logits: torch.Tensor,
@@ -141,8 +143,8 @@ class LossHead:
         size, scale, top = _index_bytes(teacher_index, "teacher_index"), self._scale(token_scale, hidden.shape[0]), teacher_index.shape[1]
         with on(self.device):
             out, which = self._outputs(hidden, weight, gradients)
-            self._fit(head, top, which)
+            need = self._fit(head, top, which)
             binding.muon_distill(head, teacher_index.data_ptr(), size, teacher_logits.data_ptr(), binding.dtype_code(teacher_logits.dtype),
-                                 top, temperature, scale, *self._pointers(out), self.workspace.data_ptr(), self.workspace.numel(),
+                                 top, temperature, scale, *self._pointers(out), self.workspace.data_ptr(), need,
                                  stream_handle(self.device))
         return out

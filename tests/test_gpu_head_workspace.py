@@ -46,3 +46,15 @@ def test_fewer_tokens_in_the_workspace_of_more(limit):
         assert (loss - want).abs().max() <= 1e-4
         for got, ref in ((dh, want_h), (dw, want_w)):
             assert (got.double() - ref).norm() <= 5e-3 * ref.norm()
+
+
+def test_results_do_not_depend_on_earlier_calls():
+    """Two pieces of tokens, also where an earlier call of a larger vocabulary left room for one."""
+    from paper_2502_16982_amd import losses
+    h, w, y = make(9000, 600, 64, "f32")
+    fresh = losses.LossHead(9000, 600, 64, torch.float32).cross_entropy(h, w, y)
+    head = losses.LossHead(9000, 600, 64, torch.float32)
+    head.cross_entropy(*make(9000, 20000, 64, "f32"))
+    again = head.cross_entropy(h, w, y)
+    for a, b in zip(fresh, again):
+        assert torch.equal(a, b)

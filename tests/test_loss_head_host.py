@@ -1,0 +1,40 @@
+"""What LossHead gives the library, on the CPU: the entry points are recorded instead of run."""
+import contextlib
+
+import pytest
+import torch
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    """(losses, list of the calls' (workspace address, bytes))"""
+    from paper_2502_16982_amd import binding, losses
+    calls = []
+    monkeypatch.setattr(losses, "stream_handle", lambda device: 7)
+    monkeypatch.setattr(losses, "on", lambda device: contextlib.nullcontext())
+    monkeypatch.setattr(binding, "muon_cross_entropy", lambda *a: calls.append((a[-3], a[-2])))
+    monkeypatch.setattr(binding, "muon_distill", lambda *a: calls.append((a[-3], a[-2])))
+    return losses, calls
+
+
+def inputs(tokens, vocab, width, dtype=torch.bfloat16):
+    return torch.zeros(tokens, width, dtype=dtype), torch.zeros(vocab, width, dtype=dtype), torch.zeros(tokens, dtype=torch.int64)
+
+
+def teacher(tokens, top):
+    return torch.zeros(tokens, top, dtype=torch.int32), torch.zeros(tokens, top)
+
+
+def test_a_call_is_cut_alike_whatever_came_before(recorded):
+    """The bytes that the library cuts a call by follow from the call, not from what a larger one left."""
+    losses, calls = recorded
+    args = inputs(9000, 600, 64)
+    losses.LossHead(9000, 600, 64, device="cpu").cross_entropy(*args)
+    used = losses.LossHead(9000, 600, 64, device="cpu")
+    used.cross_entropy(*inputs(9000, 20000, 64))
+    used.cross_entropy(*args)
+    used.distill(*args[:2], *teacher(9000, 5))
+    used.distill(*inputs(9000, 20000, 64)[:2], *teacher(9000, 5))
+    used.distill(*args[:2], *teacher(9000, 5))
+    assert calls[0][1] == calls[2][1] < calls[1][1]
+    assert calls[3][1] == calls[5][1] < calls[4][1]
