@@ -15,6 +15,9 @@ def stream_handle(device: torch.device) -> int:
     return _raw_stream(device.index) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
+capturing = torch.cuda.is_current_stream_capturing
+
+
 def on(device: torch.device):
     """Context with the device as the current one; nothing to do where it is."""
     return _here if torch.cuda.current_device() == device.index else torch.cuda.device(device)

@@ -10,7 +10,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding
-from ._device import on, stream_handle
+from ._device import capturing, on, stream_handle
 from .binding import MuonError
 
 
@@ -34,7 +34,8 @@ class LossHead:
     tokens, vocab, width, dtype: the largest call to expect; smaller ones, and other strides, use the same workspace, a larger
     one replaces it.  max_workspace_bytes: limit of the workspace, in exchange for smaller pieces of tokens (0: pieces of up to
     8192 tokens).  gradients: whether calls will ask for any (they may all the same).  Calls run on the current stream of the
-    device; calls on several streams at a time need a LossHead each.
+    device; calls on several streams at a time need a LossHead each.  Captured calls keep the workspace that they were captured with as long as
+    the LossHead is there: keep it while their graphs are replayed, and replay none beside other calls of it.
     """
 
     def __init__(self, tokens: int, vocab: int, width: int, dtype: torch.dtype = torch.bfloat16, max_workspace_bytes: int = 0,
@@ -46,6 +47,8 @@ class LossHead:
         self.dtype = dtype
         self.workspace = None
         self._stream = None
+        self._captured = False                             # whether a graph holds the workspace's address
+        self._kept = []                                    # replaced workspaces of which that is so
         self._sizes = {}
         head = binding.muon_head(None, None, width, width, tokens, vocab, width, binding.dtype_code(dtype), 0)
         self._fit(head, 1, 3 if gradients else 0)
@@ -64,10 +67,14 @@ class LossHead:
             self._sizes[key] = need
         stream = stream_handle(self.device)
         if self.workspace is None or self.workspace.numel() < need:
+            if self._captured:
+                self._kept.append(self.workspace)
+                self._captured = False
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
             self._stream = stream
         elif stream != self._stream:                       # the memory outlives what this stream does with it
             self.workspace.record_stream(torch.cuda.current_stream(self.device))
+        self._captured = self._captured or capturing()
         return need
 
     def _head(self, hidden: torch.Tensor, weight: torch.Tensor) -> "binding.muon_head":

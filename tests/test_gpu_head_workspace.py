@@ -58,3 +58,29 @@ def test_results_do_not_depend_on_earlier_calls():
     again = head.cross_entropy(h, w, y)
     for a, b in zip(fresh, again):
         assert torch.equal(a, b)
+
+
+def test_replays_after_a_larger_call():
+    """Calls that need more memory than a captured one replace the workspace, not the memory that the graph writes to."""
+    from paper_2502_16982_amd import losses
+    h, w, y = make(100, 1000, 64)
+    head = losses.LossHead(100, 1000, 64)
+    head.cross_entropy(h, w, y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = head.cross_entropy(h, w, y)
+    captured = head.workspace.data_ptr()
+    index, s = torch.randint(1000, (100, 600), device="cuda"), torch.randn(100, 600, device="cuda")
+    head.distill(h, w, index, s)
+    assert head.workspace.data_ptr() != captured
+    head.cross_entropy(*make(100, 40000, 64))
+    others = [torch.full((n,), 3, dtype=torch.uint8, device="cuda") for n in (1 << 16, 1 << 18, 1 << 19, 1 << 20, 1 << 21)]
+    want = losses.LossHead(100, 1000, 64).cross_entropy(h, w, y)
+    for _ in range(3):
+        for t in r[:2]:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(r, want):
+            assert torch.equal(a, b)
+    assert all((t == 3).all() for t in others)

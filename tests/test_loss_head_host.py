@@ -1,5 +1,6 @@
 """What LossHead gives the library, on the CPU: the entry points are recorded instead of run."""
 import contextlib
+import weakref
 
 import pytest
 import torch
@@ -12,6 +13,7 @@ def recorded(monkeypatch):
     calls = []
     monkeypatch.setattr(losses, "stream_handle", lambda device: 7)
     monkeypatch.setattr(losses, "on", lambda device: contextlib.nullcontext())
+    monkeypatch.setattr(losses, "capturing", lambda: False, raising=False)
     monkeypatch.setattr(binding, "muon_cross_entropy", lambda *a: calls.append((a[-3], a[-2])))
     monkeypatch.setattr(binding, "muon_distill", lambda *a: calls.append((a[-3], a[-2])))
     return losses, calls
@@ -38,3 +40,21 @@ def test_a_call_is_cut_alike_whatever_came_before(recorded):
     used.distill(*args[:2], *teacher(9000, 5))
     assert calls[0][1] == calls[2][1] < calls[1][1]
     assert calls[3][1] == calls[5][1] < calls[4][1]
+
+
+def test_a_workspace_that_a_captured_call_uses_stays(recorded, monkeypatch):
+    """A graph holds the address: a larger call gets other memory, and what the graph writes to is not given back."""
+    losses, calls = recorded
+    capturing = [False]
+    monkeypatch.setattr(losses, "capturing", lambda: capturing[0], raising=False)
+    head = losses.LossHead(16, 100, 32, device="cpu")
+    head.cross_entropy(*inputs(16, 100, 32))
+    capturing[0] = True
+    head.cross_entropy(*inputs(16, 100, 32))
+    capturing[0] = False
+    first, address = weakref.ref(head.workspace), calls[-1][0]
+    head.distill(*inputs(16, 5000, 32)[:2], *teacher(16, 500))
+    assert calls[-1][0] != address and first() is not None
+    second = weakref.ref(head.workspace)
+    head.distill(*inputs(16, 50000, 32)[:2], *teacher(16, 500))          # no graph holds the second one
+    assert first() is not None and second() is None
