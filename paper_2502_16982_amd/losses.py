@@ -31,15 +31,17 @@ def _index_bytes(t: torch.Tensor, what: str) -> int:
 class LossHead:
     """Workspace of a head's losses and the calls that use it.
 
-    tokens, vocab, width, dtype: the largest call to expect; smaller ones, and other strides, use the same workspace, a larger
-    one replaces it.  max_workspace_bytes: limit of the workspace, in exchange for smaller pieces of tokens (0: pieces of up to
-    8192 tokens).  gradients: whether calls will ask for any (they may all the same).  Calls run on the current stream of the
-    device; calls on several streams at a time need a LossHead each.  Captured calls keep the workspace that they were captured with as long as
-    the LossHead is there: keep it while their graphs are replayed, and replay none beside other calls of it.
+    tokens, vocab, width, dtype, top (entries per token of ``distill``): the largest call to expect; smaller ones use the same
+    workspace, a larger one replaces it, and so does one whose rows are copied first (bf16 of a width, stride or address that is no
+    multiple of 16 bytes, where the declared width is one).  max_workspace_bytes: limit of the workspace, in exchange for smaller
+    pieces of tokens (0: pieces of up to 8192 tokens).  gradients: whether calls will ask for any (they may all the same).  Calls run
+    on the current stream of the device; calls on several streams at a time need a LossHead each.  Captured calls keep the workspace
+    that they were captured with as long as the LossHead is there: keep it while their graphs are replayed, and replay none beside
+    other calls of it.
     """
 
     def __init__(self, tokens: int, vocab: int, width: int, dtype: torch.dtype = torch.bfloat16, max_workspace_bytes: int = 0,
-                 gradients: bool = True, device="cuda"):
+                 gradients: bool = True, device="cuda", top: int = 64):
         self.device = torch.device(device)
         if self.device.type == "cuda" and self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
@@ -51,7 +53,7 @@ class LossHead:
         self._kept = []                                    # replaced workspaces of which that is so
         self._sizes = {}
         head = binding.muon_head(None, None, width, width, tokens, vocab, width, binding.dtype_code(dtype), 0)
-        self._fit(head, 1, 3 if gradients else 0)
+        self._fit(head, top, 3 if gradients else 0)
 
     def _fit(self, head: "binding.muon_head", top: int, gradients: int) -> int:
         """Bytes of workspace for the call, which are there then.  The library cuts the call by these and not by all that there is, so that
@@ -70,6 +72,7 @@ class LossHead:
             if self._captured:
                 self._kept.append(self.workspace)
                 self._captured = False
+            self.workspace = None                          # its memory may serve the next one
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
             self._stream = stream
         elif stream != self._stream:                       # the memory outlives what this stream does with it

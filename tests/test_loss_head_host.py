@@ -58,3 +58,28 @@ def test_a_workspace_that_a_captured_call_uses_stays(recorded, monkeypatch):
     second = weakref.ref(head.workspace)
     head.distill(*inputs(16, 50000, 32)[:2], *teacher(16, 500))          # no graph holds the second one
     assert first() is not None and second() is None
+
+
+def test_a_workspace_makes_room_before_the_next_one(recorded, monkeypatch):
+    """Growing never holds two workspaces, and calls of the declared size do not grow it: distillation up to the entries declared."""
+    losses, calls = recorded
+    head = losses.LossHead(16, 100, 32, device="cpu")
+    before = head.workspace.data_ptr()
+    head.cross_entropy(*inputs(16, 100, 32))
+    head.distill(*inputs(16, 100, 32)[:2], *teacher(16, 64))
+    assert [c[0] for c in calls] == [before, before]
+    more = losses.LossHead(16, 100, 32, device="cpu", top=300)
+    before = more.workspace.data_ptr()
+    more.distill(*inputs(16, 100, 32)[:2], *teacher(16, 300))
+    assert calls[-1][0] == before
+
+    old, empty, left = weakref.ref(head.workspace), torch.empty, []
+
+    def spy(*size, **kw):
+        if kw.get("dtype") == torch.uint8:
+            left.append(old())
+        return empty(*size, **kw)
+
+    monkeypatch.setattr(torch, "empty", spy)
+    head.cross_entropy(*inputs(16, 5000, 32))
+    assert left == [None]
