@@ -86,7 +86,7 @@ __device__ __forceinline__ long long index_at(const HeadTarget& t, long long i) 
   return t.index64 ? static_cast<const long long*>(t.index)[i] : (long long)static_cast<const int*>(t.index)[i];
 }
 __device__ __forceinline__ float teacher_at(const HeadTarget& t, long long i) {
-  return t.inv_tau * (t.logits_bf16 ? bf16_value(static_cast<const u16*>(t.logits)[i]) : static_cast<const float*>(t.logits)[i]);
+  return t.logits_bf16 ? bf16_value(static_cast<const u16*>(t.logits)[i]) : static_cast<const float*>(t.logits)[i];
 }
 // Entry i is one: an index of the vocabulary whose teacher's logit is not -inf.
 __device__ __forceinline__ bool entry_there(const HeadTarget& t, long long i, long long vocab) {
@@ -425,19 +425,21 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) best = fmaxf(best, __shfl_xor(best, off, 64));
-    double mass = mine.v >= 0 ? exp((double)mine.s - (double)best) : 0.0;
+    // the teacher's logits over tau, from the best one down, in double: a lowest finite logit stays an entry whatever tau
+    auto behind = [&](const Entry& e) { return ((double)e.s - (double)best) * (double)t.inv_tau; };
+    double mass = mine.v >= 0 ? exp(behind(mine)) : 0.0;
     for (int j = lane + 64; j < t.top; j += 64) {
       const Entry e = load_entry(j, &ignored);
-      if (e.v >= 0) mass += exp((double)e.s - (double)best);
+      if (e.v >= 0) mass += exp(behind(e));
     }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) mass += __shfl_xor(mass, off, 64);
-    const double norm = (double)best + log(mass);
+    const double log_mass = log(mass);
     for (int j0 = 0; j0 < t.top; j0 += 64) {
       const int j = j0 + lane;
       const Entry e = j0 == 0 ? mine : load_entry(j, &ignored);
       const bool there = e.v >= 0;
-      const double z = (double)e.z, logq = there ? (double)e.s - norm : 0.0, own = there ? exp(logq) : 0.0;
+      const double z = (double)e.z, logq = there ? behind(e) - log_mass : 0.0, own = there ? exp(logq) : 0.0;
       if (there) sum_loss += own * (logq - z + l);
       if (value) {
         double q = 0.0;                          // of every entry with this index
@@ -447,7 +449,7 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
           if (k0 != j0) {
             const Entry o = k0 == 0 ? mine : load_entry(k0 + lane, &ignored);
             vk = o.v;
-            qk = o.v >= 0 ? exp((double)o.s - norm) : 0.0;
+            qk = o.v >= 0 ? exp(behind(o) - log_mass) : 0.0;
           }
           const int n = t.top - k0 < 64 ? t.top - k0 : 64;
           for (int w = 0; w < n; ++w) {
