@@ -53,12 +53,10 @@ int run_head(const muon_head* h, const HeadTarget& target, const HeadOutputs& ou
   auto f32_at = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
   const bool gradients = shape.d_hidden || shape.d_weight;
   const float unit = (float)(1.44269504088896340736 * (double)target.inv_tau);
-  // dz goes through the products over the largest scale: where all are alike the target's entries stay near -1, which bf16 holds exactly
-  float* peak = nullptr;
-  if (gradients && target.token_scale) {
-    peak = f32_at(p.peak);
-    MUON_HIP(launch_head_peak(target.token_scale, shape.tokens, peak, s));
-  }
+  // dz goes through the products over the largest scale of the piece's tokens that have a gradient: where all are alike the target's entries
+  // stay near -1, which bf16 holds exactly
+  float *peak = nullptr, *kept = nullptr;
+  if (gradients && target.token_scale) peak = f32_at(p.peak), kept = f32_at(p.kept);
 
   HeadOperand weight{static_cast<const uint16_t*>(h->weight), h->weight_stride, 0, shape.vocab};
   if (p.pack_weight) {
@@ -85,13 +83,14 @@ int run_head(const muon_head* h, const HeadTarget& target, const HeadOutputs& ou
     const bool entries = gradients || t.top > kHeadJoinTop;
     if (entries)
       MUON_HIP(launch_head_entries(t, rows, h->hidden_stride, h->weight, h->weight_stride, shape.f32, n, shape.vocab, shape.width,
-                                   f32_at(p.entry), masked, p.width_k, masked_plane, s));
+                                   f32_at(p.entry), masked, p.width_k, masked_plane, kept, s));
+    if (peak) MUON_HIP(launch_head_peak(kept, n, peak, s));
     float2* stats = reinterpret_cast<float2*>(ws + p.stats);
     MUON_HIP(launch_head_logits(weight, hidden, p.logits[last], p.pairs, unit, stats, p.piece, gradients ? ws + p.prob : nullptr,
                                 p.vocab_pitch, shape.f32, s));
     float2* log2sum = reinterpret_cast<float2*>(ws + p.lse);
     const HeadRows both{rows, h->weight, h->hidden_stride, h->weight_stride, shape.width, shape.f32};
-    MUON_HIP(launch_head_join(t, unit, target.token_scale, shape.tokens, peak, stats, p.piece, p.blocks, entries ? f32_at(p.entry) : nullptr,
+    MUON_HIP(launch_head_join(t, unit, kept, peak, stats, p.piece, p.blocks, entries ? f32_at(p.entry) : nullptr,
                               both, n, shape.vocab, out.loss + t0, out.lse ? out.lse + t0 : nullptr, gradients ? f32_at(p.value) : nullptr,
                               f32_at(p.scale), log2sum, s));
     if (!gradients) continue;

@@ -59,12 +59,13 @@ struct HeadTarget {
   float inv_tau, tau;
   const float* token_scale;
 };
-// The logits (over tau) of the tokens' entries, and, with `masked`, the tokens' hidden states as operand planes, zeros where the token has no gradient.
+// The logits (over tau) of the tokens' entries, and, with `masked`, the tokens' hidden states as operand planes, zeros where the token has no gradient;
+// with `kept`, the tokens' scales, 0 where there is no gradient.
 hipError_t launch_head_entries(const HeadTarget& t, const void* hidden, long long hidden_stride, const void* weight,
                                long long weight_stride, int f32, long long tokens, long long vocab, long long width, float* entry,
-                               uint16_t* masked, long long ld, long long plane, hipStream_t s);
-// *peak = the largest finite |token_scale| of all tokens, or 1: by a launch of its own, or, for few tokens, by the join.
-hipError_t launch_head_peak(const float* token_scale, long long tokens, float* peak, hipStream_t s);
+                               uint16_t* masked, long long ld, long long plane, float* kept, hipStream_t s);
+// *peak = the largest finite |kept|, or 1: by a launch of its own, or, for few tokens, by the join.
+hipError_t launch_head_peak(const float* kept, long long tokens, float* peak, hipStream_t s);
 // Joins the pairs: loss and, if wanted, lse per token; with `value`, the gradients at the entries over tau and *peak, the scale of the others, and
 // log2 of the sum of 2^y in two floats.  peak null: all scales count as they are.  entry null (up to kHeadJoinTop entries): the entries' logits
 // are computed here, from the rows themselves.
@@ -74,7 +75,7 @@ struct HeadRows {
   long long hidden_stride, weight_stride, width;
   int f32;
 };
-hipError_t launch_head_join(const HeadTarget& t, float unit, const float* all_scales, long long all_tokens, float* peak, const float2* stats,
+hipError_t launch_head_join(const HeadTarget& t, float unit, const float* kept, float* peak, const float2* stats,
                             long long stats_pitch, long long blocks, const float* entry, const HeadRows& rows, long long tokens, long long vocab,
                             float* loss, float* lse, float* value, float* scale, float2* log2sum, hipStream_t s);
 // The logits' gradient in bf16 (in place of the probabilities) or three planes.

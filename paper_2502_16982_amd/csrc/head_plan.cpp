@@ -98,6 +98,7 @@ void lay_out(const HeadShape& s, int64_t piece, int64_t partial, HeadPlan* p) {
   p->scale = take(true, piece * 4);
   p->lse = take(true, piece * 8);
   p->peak = take(gradients, 4);
+  p->kept = take(gradients, piece * 4);
   p->prob = take(gradients, piece * p->vocab_pitch * (s.f32 ? 4 : 2));
   p->grad = s.f32 ? take(gradients, 3 * piece * p->vocab_pitch * 2) : p->prob;      // bf16: in place of the probabilities
   p->partial = take(partial > 0, partial);

@@ -52,7 +52,7 @@ struct HeadPlan {
   int64_t blocks;           // pairs of statistics per token
   HeadProduct logits[2], hidden[2], weight[2];      // of a whole piece; of the last one
   // byte offsets of the workspace's sections
-  size_t packed_weight, packed_hidden, masked_hidden, stats, entry, value, scale, lse, peak, prob, grad, partial, sum;
+  size_t packed_weight, packed_hidden, masked_hidden, stats, entry, value, scale, lse, peak, kept, prob, grad, partial, sum;
   size_t total;
 };
 

@@ -130,7 +130,7 @@ template <bool F32>
 __global__ __launch_bounds__(256) void head_entries_kernel(HeadTarget t, const void* __restrict__ hidden, long long hidden_stride,
                                                            const void* __restrict__ weight, long long weight_stride, long long vocab,
                                                            long long width, float* __restrict__ entry, u16* __restrict__ masked, long long ld,
-                                                           long long plane) {
+                                                           long long plane, float* __restrict__ kept_scale) {
   const long long token = blockIdx.x, at = token * hidden_stride;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   for (int j = wave; j < t.top; j += 4) {
@@ -139,11 +139,13 @@ __global__ __launch_bounds__(256) void head_entries_kernel(HeadTarget t, const v
     if (v >= 0 && v < vocab) sum = row_dot<F32>(hidden, at, weight, v * weight_stride, width);
     if (lane == 0) entry[token * t.top + j] = t.inv_tau * sum;
   }
+  if (!masked && !kept_scale) return;
+  const float g = token_scale(t, token, token_state(t, token, vocab));
+  if (kept_scale && threadIdx.x == 0) kept_scale[token] = g;
   if (masked) {
-    const bool kept = token_scale(t, token, token_state(t, token, vocab)) != 0.f;
     for (long long c = threadIdx.x * 8; c < ld; c += 2048) {
       Row8 r{};
-      if (kept) r = load_row8<F32>(hidden, at, c, width);
+      if (g != 0.f) r = load_row8<F32>(hidden, at, c, width);
       store_planes8<F32>(r, masked + token * ld + c, plane);
     }
   }
@@ -275,11 +277,11 @@ __global__ __launch_bounds__(256, B == 128 && S == 2 ? 2 : 1) void head_logits_k
 }
 
 // ---- join ----
-__global__ __launch_bounds__(1024) void head_peak_kernel(const float* __restrict__ token_scale, long long tokens, float* __restrict__ peak) {
+__global__ __launch_bounds__(1024) void head_peak_kernel(const float* __restrict__ kept, long long tokens, float* __restrict__ peak) {
   __shared__ float waves[16];
   float top = 0.f;
   for (long long i = threadIdx.x; i < tokens; i += 1024) {
-    const float g = fabsf(token_scale[i]);
+    const float g = fabsf(kept[i]);
     if (g < INFINITY) top = fmaxf(top, g);
   }
 #pragma unroll
@@ -292,16 +294,16 @@ __global__ __launch_bounds__(1024) void head_peak_kernel(const float* __restrict
   }
 }
 
-// Where there are no more tokens than this, every block of the join looks through all scales itself: a launch less.
+// Where a piece has no more tokens than this, every block of the join looks through all its scales itself: a launch less.
 constexpr long long kPeakInJoin = 16384;
 
 // Bound by the chain of its loads (6.4 us for 16 tokens of 256 blocks with their entries' logits, 36 for 8192 of 1024).
 // Sixteen tokens per block (a line of statistics), their blocks of the vocabulary over 64 threads each, eight loads at a time; then a wave
 // per token for its entries, of which the first 64 are loaded at the start.
-__global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float unit, const float* __restrict__ all_scales, long long all_tokens,
-                                                         float* __restrict__ peak, const float2* __restrict__ stats, long long stats_pitch,
-                                                         long long blocks, const float* __restrict__ entry, HeadRows rows, long long tokens,
-                                                         long long vocab, float* __restrict__ loss, float* __restrict__ lse, float* __restrict__ value,
+__global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float unit, const float* __restrict__ kept, float* __restrict__ peak,
+                                                         const float2* __restrict__ stats, long long stats_pitch, long long blocks,
+                                                         const float* __restrict__ entry, HeadRows rows, long long tokens, long long vocab,
+                                                         float* __restrict__ loss, float* __restrict__ lse, float* __restrict__ value,
                                                          float* __restrict__ scale, float2* __restrict__ log2sum) {
   __shared__ float tops[64][17];
   __shared__ float sums[64][17];
@@ -328,9 +330,9 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
   Entry mine = load_entry(lane, &beyond);
   float g = tk < tokens && t.token_scale ? t.token_scale[tk] : 1.f;
   float most = 0.f;
-  if (all_scales)
-    for (long long i = threadIdx.x; i < all_tokens; i += 1024) {
-      const float x = fabsf(all_scales[i]);
+  if (kept)
+    for (long long i = threadIdx.x; i < tokens; i += 1024) {
+      const float x = fabsf(kept[i]);
       if (x < INFINITY) most = fmaxf(most, x);
     }
 
@@ -367,14 +369,14 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
   }
   tops[y][x] = top;
   sums[y][x] = sum;
-  if (all_scales) {
+  if (kept) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
     if (lane == 0) peaks[wave] = most;
   }
   __syncthreads();
   float largest = 1.f;
-  if (all_scales) {
+  if (kept) {
     most = 0.f;
 #pragma unroll
     for (int w = 0; w < 16; ++w) most = fmaxf(most, peaks[w]);
@@ -744,24 +746,24 @@ hipError_t launch_head_pack(const void* src, long long stride, int f32, long lon
 
 hipError_t launch_head_entries(const HeadTarget& t, const void* hidden, long long hidden_stride, const void* weight,
                                long long weight_stride, int f32, long long tokens, long long vocab, long long width, float* entry,
-                               u16* masked, long long ld, long long plane, hipStream_t s) {
+                               u16* masked, long long ld, long long plane, float* kept, hipStream_t s) {
   auto go = [&](auto kernel) {
-    kernel<<<(unsigned)tokens, 256, 0, s>>>(t, hidden, hidden_stride, weight, weight_stride, vocab, width, entry, masked, ld, plane);
+    kernel<<<(unsigned)tokens, 256, 0, s>>>(t, hidden, hidden_stride, weight, weight_stride, vocab, width, entry, masked, ld, plane, kept);
     return hipGetLastError();
   };
   return f32 ? go(head_entries_kernel<true>) : go(head_entries_kernel<false>);
 }
 
-hipError_t launch_head_peak(const float* token_scale, long long tokens, float* peak, hipStream_t s) {
+hipError_t launch_head_peak(const float* kept, long long tokens, float* peak, hipStream_t s) {
   if (tokens <= kPeakInJoin) return hipSuccess;  // launch_head_join finds it
-  head_peak_kernel<<<1, 1024, 0, s>>>(token_scale, tokens, peak);
+  head_peak_kernel<<<1, 1024, 0, s>>>(kept, tokens, peak);
   return hipGetLastError();
 }
 
-hipError_t launch_head_join(const HeadTarget& t, float unit, const float* all_scales, long long all_tokens, float* peak, const float2* stats,
+hipError_t launch_head_join(const HeadTarget& t, float unit, const float* kept, float* peak, const float2* stats,
                             long long stats_pitch, long long blocks, const float* entry, const HeadRows& rows, long long tokens, long long vocab,
                             float* loss, float* lse, float* value, float* scale, float2* log2sum, hipStream_t s) {
-  head_join_kernel<<<(unsigned)((tokens + 15) / 16), 1024, 0, s>>>(t, unit, peak && all_tokens <= kPeakInJoin ? all_scales : nullptr, all_tokens, peak,
+  head_join_kernel<<<(unsigned)((tokens + 15) / 16), 1024, 0, s>>>(t, unit, peak && tokens <= kPeakInJoin ? kept : nullptr, peak,
                                                                   stats, stats_pitch, blocks, entry, rows, tokens, vocab, loss, lse, value, scale,
                                                                   log2sum);
   return hipGetLastError();

@@ -45,3 +45,58 @@ def test_lowest_teacher_logits(losses, tau, teacher, top):
     off = 2 * tau * (12 * 2.0 ** -23 * float(h.abs().mm(w.abs().T).max()) / tau + 2.0 ** -21)
     assert (a.d_hidden - b.d_hidden).abs().max() <= off * w.abs().max()
     assert (a.d_weight - b.d_weight).abs().max() <= off * h.abs().sum(0).max()
+
+
+def want64(h, w, y, scale):
+    """loss, d_hidden and d_weight of cross entropy in fp64 on the device; tokens with y < 0 or y >= vocab have no gradient."""
+    h64, w64, there = h.double(), w.double(), (y >= 0) & (y < len(w))
+    z = torch.mm(h64, w64.T.contiguous())
+    lse = torch.logsumexp(z, 1)
+    at = torch.where(there, y, 0)[:, None]
+    dz = (z - lse[:, None]).exp()
+    dz.scatter_add_(1, at, torch.full_like(lse, -1.0)[:, None])
+    dz *= torch.where(there, scale.double(), 0.0)[:, None]
+    return torch.where(there, lse - z.gather(1, at)[:, 0], 0.0), torch.mm(dz, w64), torch.mm(dz.T.contiguous(), h64)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("limit", [0, 1, 8 << 30])
+@pytest.mark.parametrize("tokens", [70, 700, 20000])
+def test_scales_of_tokens_without_gradient_do_not_matter(losses, dtype, limit, tokens):
+    """Tokens with scales of their own, in one piece (with more than 16384 tokens the largest scale is found in a launch of its own) and in
+    many.  Ignored ones and those with a target beyond the vocabulary may have any scale: the others' gradients do not notice.  Against
+    fp64: bf16 rounds dz and the result once each, 5e-3 of a row or of the whole; fp32 1e-5."""
+    h, w, g = make(tokens, 50, 24, dtype)
+    y = torch.randint(50, (tokens,), generator=g).cuda()
+    scale = (torch.rand(tokens, generator=g) * 3 + 0.01).cuda() / tokens
+    y[3::7], y[5::11] = -100, 50
+    head = losses.LossHead(tokens, 50, 24, DT[dtype], max_workspace_bytes=limit)
+    gone = (y < 0) | (y >= 50)
+    a = head.cross_entropy(h, w, y, token_scale=torch.where(gone, 0.0, scale))
+    b = head.cross_entropy(h, w, y, token_scale=torch.where(gone, torch.finfo(torch.float32).max, scale))
+    assert torch.equal(torch.isnan(a.loss), y >= 50) and torch.equal(a.loss.nan_to_num(), b.loss.nan_to_num())
+    assert torch.equal(a.d_hidden, b.d_hidden) and torch.equal(a.d_weight, b.d_weight)
+    loss, d_hidden, d_weight = want64(h, w, y, scale)
+    bar = 5e-3 if dtype == "bf16" else 1e-5
+    assert (a.loss.nan_to_num() - loss).abs().max() <= 1e-5
+    assert not a.d_hidden[gone].any()
+    # a row of 24 elements has fewer roundings to average: twice the bar
+    assert ((a.d_hidden - d_hidden).norm(dim=1) <= 2 * bar * d_hidden.norm(dim=1)).all()
+    assert (a.d_weight - d_weight).norm() <= bar * d_weight.norm()
+
+
+@pytest.mark.parametrize("limit", [0, 1])
+def test_scales_of_a_distillation(losses, limit):
+    h, w, g = make(700, 50, 24, "f32")
+    index, s = torch.randint(50, (700, 3), generator=g).cuda(), torch.randn(700, 3, generator=g).cuda()
+    index[::5], s[1::5] = -1, -float("inf")
+    scale = torch.rand(700, generator=g).cuda() + 0.1
+    head = losses.LossHead(700, 50, 24, torch.float32, max_workspace_bytes=limit)
+    gone = torch.zeros(700, dtype=torch.bool, device="cuda")
+    gone[::5] = gone[1::5] = True
+    a, b = (head.distill(h, w, index, s, temperature=2.0, token_scale=torch.where(gone, x, scale)) for x in (0.0, 1e38))
+    for x, z in zip(a, b):
+        assert torch.equal(x, z)
+    each = [head.distill(h[t:t + 1], w, index[t:t + 1], s[t:t + 1], temperature=2.0) for t in (2, 3, 333, 699)]
+    for t, r in zip((2, 3, 333, 699), each):
+        assert (a.d_hidden[t] - scale[t] * r.d_hidden[0]).norm() <= 1e-5 * a.d_hidden[t].norm()
