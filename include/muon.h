@@ -283,7 +283,8 @@ int muon_adamw_step(const muon_adamw_param* params, int32_t n, const muon_adamw_
  * Types: H, W and their gradients all bf16 or all fp32.  Products of bf16 accumulate in fp32; dz is rounded to bf16 once, the gradients
  * once more (probabilities wait in f16, 2^-11 relative, those below 2^-29 of the largest in their block of the vocabulary 2^-40 of
  * it); products of fp32 run on three bf16 planes per operand (about 2^-23).  Statistics, losses and the target's entries of dz are
- * computed in fp32 and double.  Results do not depend on anything but the arguments: no atomics, fixed orders of summation.
+ * computed in fp32 and double.  Finite logits over tau are in range up to 2^22 in magnitude, where fp32 still tells halves apart; beyond, results
+ * may be infinite or NaN.  Results do not depend on anything but the arguments: no atomics, fixed orders of summation.
  *
  * Tokens are processed in pieces, as many at a time as the workspace holds: per token of a piece vocab elements of 2 bytes (fp32: 10) where
  * gradients are asked for; with more than one piece and d_weight its sum so far as well, vocab x width fp32.  Asynchronous on hip_stream; nothing is allocated.

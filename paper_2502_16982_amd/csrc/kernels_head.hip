@@ -412,11 +412,15 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
     }
   }
   double sum_loss = 0.0;
+  // log p of an entry.  Its logit was summed in another order than the ones in l: what rounding leaves above 0 is cut off (NaN stays)
+  auto log_p = [&](const Entry& e) {
+    const double d = (double)e.z - l;
+    return d > 0.0 ? 0.0 : d;
+  };
   if (!t.logits) {
-    const double z = (double)mine.z;
     if (lane == 0) {
-      sum_loss = some ? l - z : 0.0;
-      if (value) value[tk] = r == 0.f ? 0.f : (float)((double)r * expm1(z - l));
+      sum_loss = some ? -log_p(mine) : 0.0;
+      if (value) value[tk] = r == 0.f ? 0.f : (float)((double)r * expm1(log_p(mine)));
     }
   } else if (some) {
     bool ignored = false;
@@ -441,8 +445,8 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
       const int j = j0 + lane;
       const Entry e = j0 == 0 ? mine : load_entry(j, &ignored);
       const bool there = e.v >= 0;
-      const double z = (double)e.z, logq = there ? behind(e) - log_mass : 0.0, own = there ? exp(logq) : 0.0;
-      if (there) sum_loss += own * (logq - z + l);
+      const double logp = log_p(e), logq = there ? behind(e) - log_mass : 0.0, own = there ? exp(logq) : 0.0;
+      if (there) sum_loss += own * (logq - logp);
       if (value) {
         double q = 0.0;                          // of every entry with this index
         for (int k0 = 0; k0 < t.top; k0 += 64) {
@@ -460,7 +464,7 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
             if (vw == e.v) q += qw;
           }
         }
-        if (j < t.top) value[tk * t.top + j] = there && r != 0.f ? (float)((double)r * (exp(z - l) - q)) : 0.f;
+        if (j < t.top) value[tk * t.top + j] = there && r != 0.f ? (float)((double)r * (exp(logp) - q)) : 0.f;
       }
     }
 #pragma unroll

@@ -100,3 +100,23 @@ def test_scales_of_a_distillation(losses, limit):
     each = [head.distill(h[t:t + 1], w, index[t:t + 1], s[t:t + 1], temperature=2.0) for t in (2, 3, 333, 699)]
     for t, r in zip((2, 3, 333, 699), each):
         assert (a.d_hidden[t] - scale[t] * r.d_hidden[0]).norm() <= 1e-5 * a.d_hidden[t].norm()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [30.0, 1e3, 1e5])
+def test_certain_tokens(losses, dtype, size):
+    """Tokens that are predicted with certainty, at logits of any size in range: the probability of the target does not exceed 1, so that no
+    loss is below zero and no gradient points away from the target.  Every row of W but the target's is the target's turned round: then
+    d_hidden = g (p_y - 1) 2 w_y, opposite to w_y or zero."""
+    g = torch.Generator().manual_seed(3)
+    row = torch.randn(200, generator=g)
+    w = torch.stack([row, -row, -row, -row]).to(DT[dtype]).cuda()
+    h = (row[None] * (size / float(row @ row)) * (0.3 + 0.7 * torch.rand(500, 1, generator=g))).to(DT[dtype]).cuda()
+    h += torch.randn(500, 200, generator=g).to(DT[dtype]).cuda() * (size * 1e-3)
+    y = torch.zeros(500, dtype=torch.int64, device="cuda")
+    head = losses.LossHead(500, 4, 200, DT[dtype])
+    s = torch.zeros(500, 1, device="cuda")
+    for r in (head.cross_entropy(h, w, y), head.distill(h, w, y[:, None], s)):
+        assert torch.isfinite(r.d_hidden).all() and torch.isfinite(r.d_weight).all()
+        assert (r.loss >= 0).all() and (r.loss <= 1e-3 * max(size, 30.0)).all()
+        assert (r.d_hidden.float() @ w[0].float() <= 0).all()
