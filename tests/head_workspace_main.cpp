@@ -2,6 +2,7 @@
 // is answered without one never makes it larger, and no piece of tokens would do with less than the smallest.
 #include <cmath>
 #include <cstdio>
+#include <cstdlib>
 #include <random>
 
 #include "head_plan.h"
@@ -37,7 +38,20 @@ static void limited(const HeadShape& s, size_t limit) {
   if (least > 256 && head_plan(s, least - 256, &p)) fail("less than the smallest suffices", s, limit, p.total, least);
 }
 
-int main() {
+// "tokens vocab width f32 limit": how a call is cut that is given what a query with that limit answers.
+static int describe(char** argv) {
+  const HeadShape s = shape(std::atoll(argv[1]), std::atoll(argv[2]), std::atoll(argv[3]), std::atoi(argv[4]) != 0);
+  HeadPlan p;
+  head_plan(s, head_workspace(s, (size_t)std::atoll(argv[5])), &p);
+  std::printf("pieces %lld of %lld\n", (long long)p.pieces, (long long)p.piece);
+  for (int i = 0; i < 2; ++i)
+    std::printf("weight %d splits %d quarters %lld hidden %d splits %d\n", p.weight[i].tile, p.weight[i].splits,
+                (long long)(p.weight[i].tiles_m * (int64_t)p.weight[i].tiles_n - p.weight[i].whole), p.hidden[i].tile, p.hidden[i].splits);
+  return 0;
+}
+
+int main(int argc, char** argv) {
+  if (argc == 6) return describe(argv);
   // 1680 tokens in one run of K, 1260 in several
   serves(shape(1680, 3817, 4096), shape(1260, 3817, 4096), 0);
   serves(shape(1680, 3817, 4096), shape(1260, 3817, 4096), 27 << 20);

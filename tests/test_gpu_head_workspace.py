@@ -2,6 +2,8 @@
 import pytest
 import torch
 
+from tests.head_pieces import PIECES
+
 pytestmark = pytest.mark.gpu
 
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
@@ -84,3 +86,46 @@ def test_replays_after_a_larger_call():
         for a, b in zip(r, want):
             assert torch.equal(a, b)
     assert all((t == 3).all() for t in others)
+
+
+def blocks(x):
+    """Norms of the 64 x 64 blocks of a matrix."""
+    rows, cols = -(-x.shape[0] // 64) * 64, -(-x.shape[1] // 64) * 64
+    full = torch.zeros(rows, cols, dtype=torch.float64, device="cuda")
+    full[:x.shape[0], :x.shape[1]] = x
+    return full.view(rows // 64, 64, cols // 64, 64).square().sum((1, 3)).sqrt()
+
+
+@pytest.mark.parametrize("name", PIECES)
+@pytest.mark.parametrize("kind", ["cross entropy", "distillation"])
+def test_pieces_with_scales(name, kind):
+    """Several pieces of tokens whose scales differ, so that a piece that takes another's shows; block by block of 64 x 64 against fp64:
+    twice the bar of a whole gradient in a block (fewer roundings average), never held to less than a thousandth of the typical block."""
+    from paper_2502_16982_amd import losses
+    tokens, vocab, width, f32, limit = PIECES[name]
+    h, w, y = make(tokens, vocab, width, "f32" if f32 else "bf16")
+    scale = (1.0 + torch.arange(tokens, device="cuda") / 500.0) / tokens
+    y[::9] = -100
+    head = losses.LossHead(tokens, vocab, width, h.dtype, max_workspace_bytes=limit, top=1)
+    h64, w64, there = h.double(), w.double(), (y >= 0)[:, None]
+    z = torch.mm(h64, w64.T.contiguous())
+    if kind == "cross entropy":
+        r = head.cross_entropy(h, w, y, token_scale=scale)
+        tau, at, q = 1.0, y.clamp(min=0)[:, None], there.double()
+    else:
+        tau = 2.0
+        at = torch.stack([y, (y + 7) % vocab], 1)
+        s = torch.randn(tokens, 2, generator=torch.Generator().manual_seed(5)).cuda()
+        r = head.distill(h, w, torch.where(there, at, -1), s, temperature=tau, token_scale=scale)
+        at, q = at.clamp(min=0), torch.softmax(s.double() / tau, 1) * there
+        z /= tau
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    loss = tau * tau * (torch.special.xlogy(q, q) + q * (lse - z.gather(1, at))).sum(1)
+    assert (r.loss - loss).abs().max() <= 1e-4
+    dz = (z - lse).exp() * there
+    dz.scatter_add_(1, at, -q)
+    dz *= tau * scale.double()[:, None]
+    bar = 2 * (1e-5 if f32 else 5e-3)
+    for got, want in ((r.d_hidden, torch.mm(dz, w64)), (r.d_weight, torch.mm(dz.T.contiguous(), h64))):
+        off, size = blocks(got.double() - want), blocks(want)
+        assert (off <= bar * size.clamp(min=1e-3 * float(size.square().mean().sqrt()))).all()
