@@ -79,8 +79,9 @@ int run_head(const muon_head* h, const HeadTarget& target, const HeadOutputs& ou
     }
     uint16_t* masked = shape.d_weight ? u16_at(p.masked_hidden) : nullptr;
     const int64_t masked_plane = p.piece * p.width_k;
-    // forward only with few entries: the join makes their logits, a launch less (16 x 32768 x 1024: 21.3 -> 19.8 us)
-    const bool entries = gradients || t.top > kHeadJoinTop;
+    // forward only with one entry: the join makes its logit, a launch less (16 x 32768 x 1024: 23.5 -> 22.5 us on the device, 64 x 50257 x 768:
+    // 26.2 -> 25.2, 8192 x 16000 x 512: 163 -> 159); with two, one after the other, they take as long as the launch or longer (23.7 against 24.7)
+    const bool entries = gradients || t.top > 1;
     if (entries)
       MUON_HIP(launch_head_entries(t, rows, h->hidden_stride, h->weight, h->weight_stride, shape.f32, n, shape.vocab, shape.width,
                                    f32_at(p.entry), masked, p.width_k, masked_plane, kept, s));

@@ -67,9 +67,8 @@ hipError_t launch_head_entries(const HeadTarget& t, const void* hidden, long lon
 // *peak = the largest finite |kept|, or 1: by a launch of its own, or, for few tokens, by the join.
 hipError_t launch_head_peak(const float* kept, long long tokens, float* peak, hipStream_t s);
 // Joins the pairs: loss and, if wanted, lse per token; with `value`, the gradients at the entries over tau and *peak, the scale of the others, and
-// log2 of the sum of 2^y in two floats.  peak null: all scales count as they are.  entry null (up to kHeadJoinTop entries): the entries' logits
+// log2 of the sum of 2^y in two floats.  peak null: all scales count as they are.  entry null (one entry per token): the entries' logits
 // are computed here, from the rows themselves.
-constexpr int kHeadJoinTop = 4;
 struct HeadRows {
   const void *hidden, *weight;
   long long hidden_stride, weight_stride, width;

@@ -345,14 +345,11 @@ __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float uni
     for (int u = 0; u < 8; ++u) v[u] = b0 + 64 * u < blocks ? stats[(b0 + 64 * u) * stats_pitch + read] : make_float2(0.f, 0.f);
   };
   load_stats(y);
-  if (!entry && tk < tokens) {                   // few entries, and nobody has made their logits
-    for (int j = 0; j < t.top; ++j) {
-      const long long v = index_at(t, tk * t.top + j);
-      if (v < 0 || v >= vocab) continue;
-      const float z = t.inv_tau * (rows.f32 ? row_dot<true>(rows.hidden, tk * rows.hidden_stride, rows.weight, v * rows.weight_stride, rows.width)
-                                            : row_dot<false>(rows.hidden, tk * rows.hidden_stride, rows.weight, v * rows.weight_stride, rows.width));
-      if (lane == j) mine.z = z;
-    }
+  if (!entry && tk < tokens) {                   // one entry, and nobody has made its logit
+    const long long v = index_at(t, tk);
+    if (v >= 0 && v < vocab)
+      mine.z = t.inv_tau * (rows.f32 ? row_dot<true>(rows.hidden, tk * rows.hidden_stride, rows.weight, v * rows.weight_stride, rows.width)
+                                     : row_dot<false>(rows.hidden, tk * rows.hidden_stride, rows.weight, v * rows.weight_stride, rows.width));
   }
   for (long long b0 = y; b0 < blocks; b0 += 64 * 8) {
     if (b0 != y) load_stats(b0);
