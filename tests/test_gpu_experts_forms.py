@@ -58,3 +58,17 @@ def test_alignment_changes_no_bit(experts, dtype, width, extra, start):
     assert torch.equal(experts.combine(odd, w, r), experts.combine(rows, w, r))
     for a, b in zip(experts.combine_backward(x, odd, w, r), experts.combine_backward(x, rows, w, r)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("pairs", [1, 63, 64, 65, 255, 256, 257, 511, 513, 1023, 1024, 1025, 2047, 2049, 131071, 131073])
+@pytest.mark.parametrize("n", [1, 66, 4096])
+def test_sort_at_the_ends_of_its_blocks(experts, pairs, n):
+    g = torch.Generator(device="cuda").manual_seed(pairs)
+    e = torch.randint(-1, n + 1, (pairs, 1), generator=g, device="cuda", dtype=torch.int32)
+    r = experts.sort_by_expert(e, n)
+    key = torch.where((e[:, 0] >= 0) & (e[:, 0] < n), e[:, 0], n).long()
+    order = torch.sort(key, stable=True).indices
+    count = int((key < n).sum())
+    assert torch.equal(r.source[:count].long(), order[:count]) and (r.source[count:] == -1).all()
+    assert torch.equal(r.position[order[:count], 0].long(), torch.arange(count, device="cuda")) and (r.position[order[count:]] == -1).all()
+    assert torch.equal(r.offsets.long(), torch.cat([key.new_zeros(1), torch.bincount(key, minlength=n + 1)[:n].cumsum(0)]))
