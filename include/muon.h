@@ -288,6 +288,7 @@ int muon_adamw_step(const muon_adamw_param* params, int32_t n, const muon_adamw_
  *
  * Tokens are processed in pieces, as many at a time as the workspace holds: per token of a piece vocab elements of 2 bytes (fp32: 10) where
  * gradients are asked for; with more than one piece and d_weight its sum so far as well, vocab x width fp32.  Asynchronous on hip_stream; nothing is allocated.
+ * Calls may come from several host threads; calls that are given one workspace must follow each other, on one stream or by events.
  */
 typedef struct {
   const void* hidden;       /* device; [tokens, width], rows hidden_stride apart                        */

@@ -15,6 +15,7 @@ def stream_handle(device: torch.device) -> int:
     return _raw_stream(device.index) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
+current_stream = torch.cuda.current_stream
 capturing = torch.cuda.is_current_stream_capturing
 
 

@@ -10,7 +10,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding
-from ._device import capturing, on, stream_handle
+from ._device import capturing, current_stream, on, stream_handle
 from .binding import MuonError
 
 
@@ -35,9 +35,10 @@ class LossHead:
     workspace, a larger one replaces it, and so does one whose rows are copied first (bf16 of a width, stride or address that is no
     multiple of 16 bytes, where the declared width is one).  max_workspace_bytes: limit of the workspace, in exchange for smaller
     pieces of tokens (0: pieces of up to 8192 tokens).  gradients: whether calls will ask for any (they may all the same).  Calls run
-    on the current stream of the device; calls on several streams at a time need a LossHead each.  Captured calls keep the workspace
-    that they were captured with as long as the LossHead is there: keep it while their graphs are replayed, and replay none beside
-    other calls of it.
+    on the current stream of the device, on another one than the call before behind that call: streams that are to run at a time
+    need a LossHead each, and so do host threads.  Captured calls are ordered by their capture alone and keep the workspace that they
+    were captured with as long as the LossHead is there: keep it while their graphs are replayed, and replay none beside other calls
+    of it.
     """
 
     def __init__(self, tokens: int, vocab: int, width: int, dtype: torch.dtype = torch.bfloat16, max_workspace_bytes: int = 0,
@@ -48,7 +49,8 @@ class LossHead:
         self.max_workspace_bytes = int(max_workspace_bytes)
         self.dtype = dtype
         self.workspace = None
-        self._stream = None
+        self._stream = None                                # handle and object of the stream that used the workspace last
+        self._last = None
         self._captured = False                             # whether a graph holds the workspace's address
         self._kept = []                                    # replaced workspaces of which that is so
         self._sizes = {}
@@ -74,9 +76,13 @@ class LossHead:
                 self._captured = False
             self.workspace = None                          # its memory may serve the next one
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-            self._stream = stream
-        elif stream != self._stream:                       # the memory outlives what this stream does with it
-            self.workspace.record_stream(torch.cuda.current_stream(self.device))
+            self._stream, self._last = stream, current_stream(self.device)
+        elif stream != self._stream:                       # after the last call; and the memory outlives what this stream does with it
+            now = current_stream(self.device)
+            if not capturing():
+                now.wait_stream(self._last)
+            self.workspace.record_stream(now)
+            self._stream, self._last = stream, now
         self._captured = self._captured or capturing()
         return need
 

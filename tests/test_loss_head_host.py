@@ -14,6 +14,7 @@ def recorded(monkeypatch):
     monkeypatch.setattr(losses, "stream_handle", lambda device: 7)
     monkeypatch.setattr(losses, "on", lambda device: contextlib.nullcontext())
     monkeypatch.setattr(losses, "capturing", lambda: False, raising=False)
+    monkeypatch.setattr(losses, "current_stream", lambda device: None, raising=False)
     monkeypatch.setattr(binding, "muon_cross_entropy", lambda *a: calls.append((a[-3], a[-2])))
     monkeypatch.setattr(binding, "muon_distill", lambda *a: calls.append((a[-3], a[-2])))
     return losses, calls
@@ -83,3 +84,42 @@ def test_a_workspace_makes_room_before_the_next_one(recorded, monkeypatch):
     monkeypatch.setattr(torch, "empty", spy)
     head.cross_entropy(*inputs(16, 5000, 32))
     assert left == [None]
+
+
+class Stream:
+    """Stands for a stream: which others it was made to wait for."""
+
+    def __init__(self, handle):
+        self.handle, self.waited = handle, []
+
+    def wait_stream(self, other):
+        self.waited.append(other.handle)
+
+
+def test_calls_on_different_streams_wait_for_each_other(recorded, monkeypatch):
+    """There is one workspace: a call on another stream than the one before comes after it, and the first one after whatever held the memory on
+    the stream where it was allocated."""
+    losses, _ = recorded
+    now, captures, kept = [Stream(1)], [False], []
+    monkeypatch.setattr(losses, "stream_handle", lambda device: now[0].handle)
+    monkeypatch.setattr(losses, "current_stream", lambda device: now[0], raising=False)
+    monkeypatch.setattr(losses, "capturing", lambda: captures[0])
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: now[0])
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, stream: kept.append(stream.handle))
+    first, second, third = now[0], Stream(2), Stream(3)
+    head = losses.LossHead(16, 100, 32, device="cpu")
+    head.cross_entropy(*inputs(16, 100, 32))
+    assert first.waited == [] and kept == []
+    now[0] = second
+    head.cross_entropy(*inputs(16, 100, 32))
+    head.cross_entropy(*inputs(16, 100, 32))
+    assert second.waited == [1] and 2 in kept
+    now[0], captures[0] = third, True                       # a capture begins behind everything, and cannot wait for what is outside
+    head.cross_entropy(*inputs(16, 100, 32))
+    assert third.waited == [] and 3 in kept
+    now[0], captures[0] = first, False
+    head.cross_entropy(*inputs(16, 5000, 32))               # a new workspace comes from this stream
+    assert first.waited == [] or first.waited == [3]
+    now[0] = second
+    head.cross_entropy(*inputs(16, 5000, 32))
+    assert second.waited == [1, 1]
