@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import contextlib
+import warnings
 
 import torch
 
@@ -17,6 +18,13 @@ def stream_handle(device: torch.device) -> int:
 
 current_stream = torch.cuda.current_stream
 capturing = torch.cuda.is_current_stream_capturing
+
+
+def outside_autograd(where: str, *tensors) -> None:
+    """Warns of floating-point arguments that autograd follows: it does not see these calls, whose gradients are results or calls of their own."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        warnings.warn(f"{where} is not recorded by autograd and an argument requires grad: take the gradients from the results (or from the "
+                      f"*_backward calls), and call it under torch.no_grad()", stacklevel=3)
 
 
 def on(device: torch.device):

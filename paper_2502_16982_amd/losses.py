@@ -1,7 +1,8 @@
 """Losses of a language model's head with their gradients: softmax cross entropy over a large vocabulary and distillation
 from a teacher's top logits, from hidden states and the head's weight, without keeping the logits.
 
-Argument checks and memory only; the arithmetic is in the HIP library (``muon_cross_entropy``, ``muon_distill``).
+Argument checks and memory only; the arithmetic is in the HIP library (``muon_cross_entropy``, ``muon_distill``).  autograd does not see
+these calls: the gradients are in their results, for the token_scale given.
 """
 from __future__ import annotations
 
@@ -10,7 +11,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import binding
-from ._device import capturing, current_stream, on, stream_handle
+from ._device import capturing, current_stream, on, outside_autograd, stream_handle
 from .binding import MuonError
 
 
@@ -134,6 +135,7 @@ class LossHead:
         ``(token_scale * loss).sum()``."""
         head = self._head(hidden, weight)
         self._here(hidden=hidden, weight=weight, targets=targets, token_scale=token_scale)
+        outside_autograd("LossHead.cross_entropy", hidden, weight, token_scale)
         if targets.shape != (hidden.shape[0],) or not targets.is_contiguous():
             raise MuonError(-1, f"targets: contiguous [{hidden.shape[0]}], not {tuple(targets.shape)}")
         size, scale = _index_bytes(targets, "targets"), self._scale(token_scale, hidden.shape[0])
@@ -151,6 +153,7 @@ class LossHead:
         ``(token_scale * loss).sum()``."""
         head = self._head(hidden, weight)
         self._here(hidden=hidden, weight=weight, teacher_index=teacher_index, teacher_logits=teacher_logits, token_scale=token_scale)
+        outside_autograd("LossHead.distill", hidden, weight, teacher_logits, token_scale)
         if teacher_index.dim() != 2 or teacher_index.shape[0] != hidden.shape[0] or teacher_logits.shape != teacher_index.shape:
             raise MuonError(-1, f"teacher_index and teacher_logits: [{hidden.shape[0]}, top], not {tuple(teacher_index.shape)} and "
                                 f"{tuple(teacher_logits.shape)}")

@@ -1,4 +1,6 @@
 """The experts' kernels where a launch goes on to further tokens, and rows of any alignment bit for bit."""
+import warnings
+
 import pytest
 import torch
 
@@ -72,3 +74,14 @@ def test_sort_at_the_ends_of_its_blocks(experts, pairs, n):
     assert torch.equal(r.source[:count].long(), order[:count]) and (r.source[count:] == -1).all()
     assert torch.equal(r.position[order[:count], 0].long(), torch.arange(count, device="cuda")) and (r.position[order[count:]] == -1).all()
     assert torch.equal(r.offsets.long(), torch.cat([key.new_zeros(1), torch.bincount(key, minlength=n + 1)[:n].cumsum(0)]))
+
+
+def test_arguments_that_autograd_follows_are_warned_of(experts):
+    r = experts.sort_by_expert(torch.zeros(4, 2, dtype=torch.int32, device="cuda"), 1)
+    x, w, rows = torch.ones(4, 16, device="cuda", requires_grad=True), torch.ones(4, 2, device="cuda", requires_grad=True), torch.ones(8, 16, device="cuda")
+    for call in (lambda: experts.dispatch(x, r), lambda: experts.combine(rows, w, r), lambda: experts.combine_backward(x, rows, w, r)):
+        with pytest.warns(UserWarning, match="not recorded by autograd"):
+            call()
+        with torch.no_grad(), warnings.catch_warnings():
+            warnings.simplefilter("error")
+            call()

@@ -1,5 +1,6 @@
 """What LossHead gives the library, on the CPU: the entry points are recorded instead of run."""
 import contextlib
+import warnings
 import weakref
 
 import pytest
@@ -123,3 +124,19 @@ def test_calls_on_different_streams_wait_for_each_other(recorded, monkeypatch):
     now[0] = second
     head.cross_entropy(*inputs(16, 5000, 32))
     assert second.waited == [1, 1]
+
+
+def test_arguments_that_autograd_follows_are_warned_of(recorded):
+    losses, _ = recorded
+    head = losses.LossHead(16, 100, 32, device="cpu")
+    hidden, weight, targets = inputs(16, 100, 32)
+    weight.requires_grad_()
+    with pytest.warns(UserWarning, match="cross_entropy is not recorded by autograd"):
+        head.cross_entropy(hidden, weight, targets)
+    with pytest.warns(UserWarning, match="distill is not recorded by autograd"):
+        head.distill(hidden, weight, *teacher(16, 3))
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        head.cross_entropy(hidden, weight.detach(), targets)
+        with torch.no_grad():
+            assert not head.cross_entropy(hidden, weight, targets).loss.requires_grad
