@@ -20,9 +20,9 @@ current_stream = torch.cuda.current_stream
 capturing = torch.cuda.is_current_stream_capturing
 
 
-def outside_autograd(where: str, *tensors) -> None:
-    """Warns of floating-point arguments that autograd follows: it does not see these calls, whose gradients are results or calls of their own."""
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+def outside_autograd(where: str, required: bool) -> None:
+    """Warns where an argument requires grad and autograd is on: it does not see these calls, whose gradients are results or calls of their own."""
+    if required and torch.is_grad_enabled():
         warnings.warn(f"{where} is not recorded by autograd and an argument requires grad: take the gradients from the results (or from the "
                       f"*_backward calls), and call it under torch.no_grad()", stacklevel=3)
 

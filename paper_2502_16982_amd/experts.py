@@ -92,7 +92,7 @@ def dispatch(x: torch.Tensor, routing: Routing) -> torch.Tensor:
     """Rows [tokens * top, width] of ``x`` [tokens, width] in the experts' order; zero behind the last pair's."""
     r, device = _routing(routing), _device(x, routing.position, routing.offsets)
     stride, width = _tokens("x", x, r.tokens)
-    outside_autograd("experts.dispatch", x)
+    outside_autograd("experts.dispatch", x.requires_grad)
     with on(device):
         rows = torch.empty(r.tokens * r.top, width, dtype=x.dtype, device=device)
         binding.muon_expert_dispatch(r, x.data_ptr(), stride, width, binding.dtype_code(x.dtype), rows.data_ptr(), stream_handle(device))
@@ -109,7 +109,7 @@ def combine(rows: torch.Tensor, weights: Optional[torch.Tensor], routing: Routin
     r = _routing(routing)
     device = _device(rows, weights, routing.position, routing.offsets)
     width, at = _rows("rows", rows, routing.position), 0 if weights is None else _weights(weights, routing.position)
-    outside_autograd("experts.combine", rows, weights)
+    outside_autograd("experts.combine", rows.requires_grad or (weights is not None and weights.requires_grad))
     with on(device):
         out = torch.empty(r.tokens, width, dtype=rows.dtype, device=device)
         binding.muon_expert_combine(r, rows.data_ptr(), at, width, binding.dtype_code(rows.dtype), out.data_ptr(), stream_handle(device))
@@ -126,7 +126,7 @@ def combine_backward(d_out: torch.Tensor, rows: torch.Tensor, weights: torch.Ten
         raise MuonError(-1, f"d_out: [{r.tokens}, {width}], not {tuple(d_out.shape)}")
     if d_out.dtype != rows.dtype:
         raise MuonError(-2, f"d_out and rows of one dtype, not {d_out.dtype} and {rows.dtype}")
-    outside_autograd("experts.combine_backward", d_out, rows, weights)
+    outside_autograd("experts.combine_backward", d_out.requires_grad or rows.requires_grad or weights.requires_grad)
     with on(device):
         d_rows, d_weights = torch.empty_like(rows), torch.empty_like(weights)
         binding.muon_expert_combine_backward(r, d_out.data_ptr(), stride, rows.data_ptr(), at, width, binding.dtype_code(rows.dtype),

@@ -135,7 +135,7 @@ class LossHead:
         ``(token_scale * loss).sum()``."""
         head = self._head(hidden, weight)
         self._here(hidden=hidden, weight=weight, targets=targets, token_scale=token_scale)
-        outside_autograd("LossHead.cross_entropy", hidden, weight, token_scale)
+        outside_autograd("LossHead.cross_entropy", hidden.requires_grad or weight.requires_grad)
         if targets.shape != (hidden.shape[0],) or not targets.is_contiguous():
             raise MuonError(-1, f"targets: contiguous [{hidden.shape[0]}], not {tuple(targets.shape)}")
         size, scale = _index_bytes(targets, "targets"), self._scale(token_scale, hidden.shape[0])
@@ -153,7 +153,7 @@ class LossHead:
         ``(token_scale * loss).sum()``."""
         head = self._head(hidden, weight)
         self._here(hidden=hidden, weight=weight, teacher_index=teacher_index, teacher_logits=teacher_logits, token_scale=token_scale)
-        outside_autograd("LossHead.distill", hidden, weight, teacher_logits, token_scale)
+        outside_autograd("LossHead.distill", hidden.requires_grad or weight.requires_grad or teacher_logits.requires_grad)
         if teacher_index.dim() != 2 or teacher_index.shape[0] != hidden.shape[0] or teacher_logits.shape != teacher_index.shape:
             raise MuonError(-1, f"teacher_index and teacher_logits: [{hidden.shape[0]}, top], not {tuple(teacher_index.shape)} and "
                                 f"{tuple(teacher_logits.shape)}")
