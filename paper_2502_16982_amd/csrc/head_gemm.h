@@ -40,7 +40,6 @@ constexpr float kProbTop = 15.f;
 __device__ __forceinline__ int pair_left(int pairs, int pair) { return pairs == 1 ? 0 : (0x021010 >> 4 * (5 - pair)) & 15; }
 __device__ __forceinline__ int pair_right(int pairs, int pair) { return pairs == 1 ? 0 : (0x201100 >> 4 * (5 - pair)) & 15; }
 
-typedef const __attribute__((address_space(1))) void* gptr;
 typedef __attribute__((address_space(3))) void* lptr;
 
 // f(integral_constant<int, I>) for I = FIRST .. LAST-1, unrolled at compile time

@@ -12,7 +12,11 @@ constexpr int64_t kUnits = 256;                  // compute units
 // alone, on the longer ring, 0.58; and 10, 4 or 6 to start and to store.  Both sides of the choices that are near: gradient of H at 2048 x 32768 x 1024
 // bf16, 256-wide in 8 runs of K 123 us + 14 to join, 128-wide alone in 2 runs 145 + 7; at 1000 x 20011 x 777 fp32 226 + 10 against 293 + 6;
 // 4096 x 65537 x 2048 bf16 in 2 runs 899 + 21 against tiles of 128 in whole 1197; its gradient of W, 257 x 8 tiles, with the last round in
-// quarters 991 against 1032.
+// quarters 991 against 1032.  Held against the other forms (K in 1 to 64 runs) for each product of 15 calls that these times were not taken from (96 to
+// 8192 tokens, vocabularies of 8000 to 100277, widths of 512 to 4096, three of them fp32), the choice is the fastest or within 2.5 % of the
+// whole call in 41 of 45; the others: gradient of W at 200 x 32000 x 2048 in tiles of 256 (call 157 us) instead of 128 (144), of H at 2500 x 8192 x 4096 in 3
+// runs (526) instead of one (488), at 6000 x 24000 x 640 128 alone (777) instead of 128 in 2 runs (748), at 700 x 12000 x 768 fp32 256 in 28
+// runs (342) instead of 128 alone in 6 (316).
 double time_wide(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (1.75 * slabs + 10); }
 double time_narrow(int64_t blocks, double slabs) { return (double)((blocks + 2 * kUnits - 1) / (2 * kUnits)) * (1.17 * slabs + 4); }
 double time_alone(int64_t blocks, double slabs) { return (double)((blocks + kUnits - 1) / kUnits) * (0.58 * slabs + 6); }

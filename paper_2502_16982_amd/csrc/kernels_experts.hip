@@ -371,9 +371,11 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(ExpertRows
   });
 }
 
-// Rows that fill the memory-side cache (256 MB) are read with the streaming hint: 8192 x 6 rows of 2048 bf16 (201 MB), dispatch with its gradient
-// 116 -> 94 to 102 us, combine with its gradients 140 -> 125 to 138 (by what else the cache holds); rows that stay in the cache without it lose
-// by it (34 MB: 23 -> 30).
+// Rows from 128 MB on, which with what is written beside them fill the memory-side cache (256 MB), are read with the streaming hint.  Without -> with it, in us,
+// rows of 2048 bf16: combine and its gradients on new rows each time, 64 MB 44 -> 49, 96 MB 71 -> 69, 128 MB 96 -> 86, 192 MB 140 -> 124, 256 MB
+// 185 -> 182, 384 MB 271 -> 273; the gradients alone on rows read before, 96 MB 37 -> 44, 128 MB 59 -> 55, 192 MB 92 -> 78.  combine alone
+// loses by it where its rows are in the cache (128 MB 28 -> 31, 192 MB 38 -> 48), is even where they are not (33 -> 31, 46 -> 47) and wins
+// behind a dispatch of as many rows (201 MB: the two 116 -> 94).  fp32 rows of 1408 alike.
 bool rows_once(const ExpertRows& r) { return r.tokens * r.top * r.width * (r.f32 ? 4 : 2) >= 128ll << 20; }
 // Threads per token: whole waves, as many as have a piece of the row each.
 int lanes_for(const ExpertRows& r) {

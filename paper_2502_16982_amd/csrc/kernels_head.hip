@@ -297,7 +297,7 @@ __global__ __launch_bounds__(1024) void head_peak_kernel(const float* __restrict
 // Where a piece has no more tokens than this, every block of the join looks through all its scales itself: a launch less.
 constexpr long long kPeakInJoin = 16384;
 
-// Bound by the chain of its loads (6.4 us for 16 tokens of 256 blocks with their entries' logits, 36 for 8192 of 1024).
+// Bound by the chain of its loads (6.5 us for 16 tokens of 256 blocks with their entries' logits, 36 for 8192 of 1024).
 // Sixteen tokens per block (a line of statistics), their blocks of the vocabulary over 64 threads each, eight loads at a time; then a wave
 // per token for its entries, of which the first 64 are loaded at the start.
 __global__ __launch_bounds__(1024) void head_join_kernel(HeadTarget t, float unit, const float* __restrict__ kept, float* __restrict__ peak,
