@@ -149,41 +149,45 @@ bool head_plan(const HeadShape& s, size_t max_bytes, HeadPlan* p) {
   *p = plan_shape(s);
   const int64_t all = std::max<int64_t>(1, s.tokens), most = max_bytes == 0 ? kHeadPieceTokens : most_tokens(s);
   const size_t limit = max_bytes == 0 ? (size_t)1 << 62 : std::min(max_bytes, (size_t)1 << 62);
-  // all tokens in one piece, or as many whole tiles of them as fit
-  int64_t piece = all <= most && bytes_unsplit(s, all) <= limit ? all : 0;
-  if (piece == 0) {
-    auto largest = [&](auto&& bytes) {
-      int64_t low = 0, high = std::min(most, (all - 1) / 256 * 256) / 256;
-      while (low < high) {
-        const int64_t middle = (low + high + 1) / 2;
-        if (bytes(middle * 256) <= limit) low = middle;
-        else high = middle - 1;
+  // The products for pieces of so many tokens with so many bytes for the splits' sums, of which it answers what they take.
+  auto products = [&](int64_t piece, int64_t room) {
+    const int64_t before_last = (std::max<int64_t>(1, (s.tokens + piece - 1) / piece) - 1) * piece, sizes[2] = {piece, s.tokens - before_last};
+    int64_t partial = 0;
+    for (int i = 0; i < 2; ++i) {
+      p->logits[i] = head_product(s.vocab, sizes[i], p->width_k, p->pairs, 0);
+      p->hidden[i] = head_product(s.width, sizes[i], s.vocab, p->pairs, room);
+      p->weight[i] = head_product(s.width, s.vocab, sizes[i], p->pairs, room);
+      if (s.d_hidden && p->hidden[i].splits > 1) partial = std::max(partial, p->hidden[i].splits * sizes[i] * s.width * 4);
+      if (s.d_weight && p->weight[i].splits > 1) partial = std::max(partial, p->weight[i].splits * s.vocab * s.width * 4);
+    }
+    return up(partial, 256);
+  };
+  // All tokens in one piece, or equal pieces of as many whole tiles of them as fit.
+  auto equal = [&](int64_t most_each) {
+    const int64_t n = (all + most_each - 1) / most_each;
+    return up((all + n - 1) / n, 256);
+  };
+  int64_t piece = all;
+  bool fits = all <= most && bytes_unsplit(s, all) <= limit;
+  if (!fits) {
+    int64_t low = 0, high = std::min(most, (all - 1) / 256 * 256) / 256;
+    while (low < high) {
+      const int64_t middle = (low + high + 1) / 2;
+      if (bytes_unsplit(s, middle * 256) <= limit) low = middle;
+      else high = middle - 1;
+    }
+    fits = low > 0;
+    piece = fits ? equal(low * 256) : std::min<int64_t>(all, 256);
+    // smaller ones where these leave no room for the splits, but not by half: a piece more reads the weight three times and the sum twice
+    for (int64_t less = piece; fits && 2 * less > low * 256; less = equal(less - 256)) {
+      if (bytes_unsplit(s, less) + (size_t)products(less, bytes_split(s, less)) <= limit) {
+        piece = less;
+        break;
       }
-      return low * 256;
-    };
-    const int64_t alone = largest([&](int64_t n) { return bytes_unsplit(s, n); });
-    // with room for splits, unless that halves the pieces: a piece more reads the weight three times and the sum twice
-    const int64_t split = largest([&](int64_t n) { return bytes_unsplit(s, n) + (size_t)bytes_split(s, n); });
-    piece = 2 * split >= alone ? split : alone;
-    if (piece > 0) {                               // equal pieces
-      const int64_t pieces = (all + piece - 1) / piece;
-      piece = up((all + pieces - 1) / pieces, 256);
+      if (less <= 256) break;
     }
   }
-  const bool fits = piece > 0;
-  if (!fits) piece = std::min<int64_t>(all, 256);
-  const size_t unsplit = bytes_unsplit(s, piece);
-  const int64_t room = fits ? (int64_t)((limit - unsplit) / 256 * 256) : 0;
-  lay_out(s, piece, 0, p);                         // (how many pieces there are)
-  const int64_t sizes[2] = {piece, s.tokens - (p->pieces - 1) * piece};
-  int64_t partial = 0;
-  for (int i = 0; i < 2; ++i) {
-    p->logits[i] = head_product(s.vocab, sizes[i], p->width_k, p->pairs, 0);
-    p->hidden[i] = head_product(s.width, sizes[i], s.vocab, p->pairs, room);
-    p->weight[i] = head_product(s.width, s.vocab, sizes[i], p->pairs, room);
-    if (s.d_hidden && p->hidden[i].splits > 1) partial = std::max(partial, p->hidden[i].splits * sizes[i] * s.width * 4);
-    if (s.d_weight && p->weight[i].splits > 1) partial = std::max(partial, p->weight[i].splits * s.vocab * s.width * 4);
-  }
+  const int64_t partial = products(piece, fits ? (int64_t)((limit - bytes_unsplit(s, piece)) / 256 * 256) : 0);
   lay_out(s, piece, partial, p);
   return fits;
 }

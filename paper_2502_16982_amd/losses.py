@@ -35,7 +35,7 @@ class LossHead:
     tokens, vocab, width, dtype, top (entries per token of ``distill``): the largest call to expect; smaller ones use the same
     workspace, a larger one replaces it, and so does one whose rows are copied first (bf16 of a width, stride or address that is no
     multiple of 16 bytes, where the declared width is one).  max_workspace_bytes: limit of the workspace, in exchange for smaller
-    pieces of tokens (0: pieces of up to 8192 tokens).  gradients: whether calls will ask for any (they may all the same).  Calls run
+    pieces of tokens (0: what pieces of 8192 tokens take).  gradients: whether calls will ask for any (they may all the same).  Calls run
     on the current stream of the device, on another one than the call before behind that call: streams that are to run at a time
     need a LossHead each, and so do host threads.  Captured calls are ordered by their capture alone and keep the workspace that they
     were captured with as long as the LossHead is there: keep it while their graphs are replayed, and replay none beside other calls

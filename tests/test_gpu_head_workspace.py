@@ -51,12 +51,14 @@ def test_fewer_tokens_in_the_workspace_of_more(limit):
 
 
 def test_results_do_not_depend_on_earlier_calls():
-    """Two pieces of tokens, also where an earlier call of a larger vocabulary left room for one."""
+    """Pieces of tokens of one size, also where an earlier call of a larger vocabulary, whose smallest workspace is beyond the limit, left room
+    for larger ones."""
     from paper_2502_16982_amd import losses
     h, w, y = make(9000, 600, 64, "f32")
-    fresh = losses.LossHead(9000, 600, 64, torch.float32).cross_entropy(h, w, y)
-    head = losses.LossHead(9000, 600, 64, torch.float32)
+    fresh = losses.LossHead(9000, 600, 64, torch.float32, max_workspace_bytes=30 << 20).cross_entropy(h, w, y)
+    head = losses.LossHead(9000, 600, 64, torch.float32, max_workspace_bytes=30 << 20)
     head.cross_entropy(*make(9000, 20000, 64, "f32"))
+    assert head.workspace.numel() > 60 << 20
     again = head.cross_entropy(h, w, y)
     for a, b in zip(fresh, again):
         assert torch.equal(a, b)
