@@ -48,3 +48,11 @@ def test_the_gpu_tests_take_every_form_of_pieces(program):
         f = whole.split()
         tile, splits, quarters = int(f[1]), int(f[3]), int(f[5])
         assert (splits > 1) == ("runs of K" in name) and (tile == 256) == ("256" in name) and (quarters > 0) == ("quarters" in name), (name, text)
+
+
+@pytest.mark.parametrize("call,pieces,of", [((20000, 32768, 1024, 0, 300_000_000), 16, 1280), ((20000, 32768, 1024, 0, 0), 3, 6912),
+                                            ((1_000_000, 50257, 768, 0, 400_000_000), 652, 1536)])
+def test_pieces_are_as_large_as_their_splits_allow(program, call, pieces, of):
+    """Room is made for the sums of the runs of K that a plan has, a few megabytes of what any plan might have."""
+    text = subprocess.run([program, *map(str, call)], capture_output=True, text=True, check=True).stdout
+    assert text.splitlines()[0] == f"pieces {pieces} of {of}", text
