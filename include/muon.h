@@ -276,7 +276,7 @@ int muon_adamw_step(const muon_adamw_param* params, int32_t n, const muon_adamw_
  *
  * scale_t is the gradient of the training loss with respect to loss_t (1/count for a mean), given before the call; loss is unscaled.
  * A token without target (a negative target; every index negative, or every teacher's logit of the others -inf) has loss 0; so has a token
- * with scale 0 no gradient: its hidden state, whatever it holds, does not reach d_weight, and its row of d_hidden is zero.  An entry with a
+ * with scale 0 no gradient: its hidden state, whatever it holds, does not reach d_weight, and its row of d_hidden is zero (W finite).  An entry with a
  * negative index is no entry, whatever its logit.  An index that occurs twice counts twice.  An index of vocab or more makes the token's
  * loss NaN and gives no gradient.
  *
