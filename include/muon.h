@@ -1,6 +1,7 @@
 /*
- * muon.h - C ABI of the MI355X (gfx950) scaled-Muon optimizer step, and, below it, of the operators that make its largest gradients:
- * the losses of a language model's head and a mixture's tokens to their experts and back.
+ * muon.h - C ABI of the MI355X (gfx950) scaled-Muon optimizer step, and, below it, of the gradients' norm and clipping, of the operators
+ * that make its largest gradients (the losses and log probabilities of a language model's head, a mixture's tokens to their experts and
+ * back), and of a mixture's layer for few tokens.
  *
  * One call to muon_step() performs, for every 2-D matrix in a list, the update
  * rule of "Muon is Scalable for LLM Training" (arXiv 2502.16982):
@@ -150,6 +151,13 @@ int muon_step(muon_ctx* ctx, const muon_param* params, int32_t n, const muon_hpa
               void* hip_stream, float* update_rms_out);
 
 /*
+ * muon_step with G times *grad_scale in the place of G, for a device float that muon_grad_norm leaves (null: 1): the gradients of a step
+ * that is clipped are not written once more.  G * grad_scale is rounded to fp32.
+ */
+int muon_step_scaled(muon_ctx* ctx, const muon_param* params, int32_t n, const muon_hparams* hp, const float* grad_scale,
+                     void* hip_stream, float* update_rms_out);
+
+/*
  * muon_step for callers that cannot allocate device memory - code under HIP graph capture, tight serving loops,
  * harnesses that forbid hipMalloc: one call does what muon_init + muon_step do, with the tables and Newton-Schulz
  * temporaries in a fixed device array inside the library instead of a caller-provided workspace.  It calls no
@@ -262,6 +270,34 @@ typedef struct {
 } muon_adamw_hparams;
 
 int muon_adamw_step(const muon_adamw_param* params, int32_t n, const muon_adamw_hparams* hp, void* hip_stream);
+/* The same with g times *grad_scale (device; null: 1) in the place of g, rounded to fp32. */
+int muon_adamw_step_scaled(const muon_adamw_param* params, int32_t n, const muon_adamw_hparams* hp, const float* grad_scale, void* hip_stream);
+
+/*
+ * The norm of a list of gradients as one vector, and clipping:
+ *   norm = sqrt(sum of g^2 over all elements of all tensors);   scale = max_norm / norm where max_norm < norm < infinity, else 1.
+ * Squares are summed in double, in an order that depends on the sizes alone.  norm is a double, so that it holds whatever finite gradients
+ * give; scale is rounded to fp32 once.  A norm that is not finite leaves scale at 1: the caller sees it in norm.
+ * muon_grad_norm writes norm and, where it is not null, scale, for muon_grad_scale, muon_step_scaled and muon_adamw_step_scaled;
+ * muon_grad_scale multiplies the gradients in place, g * scale rounded to g's type, and touches nothing where scale is 1; muon_grad_clip does
+ * both.  With gradients on several devices or processes, add up the squares of their norms and hand a scale of your own to the others.
+ * max_norm: 0 and more, infinity for none.  Tensors are flat arrays of any alignment of an element; tensors that are scaled must not share
+ * memory.  n may be 0 and so may numel (g null then): the norm of nothing is 0.
+ * workspace: muon_grad_norm_bytes of the same sizes, 8-byte aligned device memory.  Asynchronous on hip_stream; nothing is allocated.
+ */
+typedef struct {
+  void* g;            /* device; gradient                                     */
+  int64_t numel;      /* 0 .. 2^42                                            */
+  int32_t dtype;      /* MUON_F32 or MUON_BF16                                */
+  int32_t reserved;   /* must be 0                                            */
+} muon_grad;
+
+int muon_grad_norm_bytes(const muon_grad* grads, int32_t n, size_t* out);
+int muon_grad_norm(const muon_grad* grads, int32_t n, double max_norm, double* norm, float* scale, void* workspace, size_t workspace_bytes,
+                   void* hip_stream);
+int muon_grad_scale(const muon_grad* grads, int32_t n, const float* scale, void* hip_stream);
+int muon_grad_clip(const muon_grad* grads, int32_t n, double max_norm, double* norm, float* scale, void* workspace, size_t workspace_bytes,
+                   void* hip_stream);
 
 /*
  * The losses of a language model's head, from its last hidden states H [tokens, width] and the head's weight W [vocab, width], with the
@@ -361,6 +397,42 @@ int muon_expert_combine(const muon_routing* routing, const void* rows, const flo
                         void* hip_stream);
 int muon_expert_combine_backward(const muon_routing* routing, const void* d_out, int64_t d_out_stride, const void* rows, const float* weights,
                                  int64_t width, int32_t dtype, void* d_rows, float* d_weights, void* hip_stream);
+
+/*
+ * A mixture's layer for few tokens, where reading the chosen experts' matrices is all the time there is: no sort, no rows in the experts'
+ * order, every chosen expert's matrices read once for all of its tokens.
+ *   out[t] = sum_j weights[t, j] h(t, j) Down_e,  h(t, j) = act(x[t] Gate_e) * (x[t] Up_e),  e = expert[t, j];  without a gate act(x[t] Up_e)
+ * over the pairs whose expert is in [0, experts); the others are dropped, whatever their weight; a token without any gets zero; an expert that a
+ * token names twice counts twice.  weights null: all 1.
+ * Gate and Up are width x inner and Down is inner x width per expert, rows contiguous and row_stride elements apart, experts expert_stride
+ * apart.  x, the matrices and out are all bf16 or all fp32, out dense, weights dense fp32.  Sums are fp32 in an order that depends on the
+ * sizes alone; in bf16 h is rounded to bf16 once, as out is.  tokens * top <= 2^14; width, inner <= 2^17.  More tokens than
+ * a few hundred are better sorted (muon_expert_sort) and multiplied expert by expert.
+ * workspace: muon_expert_layer_bytes, 256-byte aligned device memory.  Asynchronous on hip_stream; nothing is allocated.
+ */
+typedef enum { MUON_ACT_SILU = 0, MUON_ACT_RELU = 1 } muon_activation;
+
+typedef struct {
+  const void* w;            /* device; [experts][rows][columns]; gate: null for none                    */
+  int64_t expert_stride;    /* elements, 0 and more                                                     */
+  int64_t row_stride;       /* elements, >= columns                                                     */
+} muon_matrices;
+
+typedef struct {
+  muon_matrices gate, up, down;
+  int64_t tokens, width, inner;
+  int32_t top;              /* choices per token, 1 .. 64                                               */
+  int32_t experts;          /* 1 .. 4096                                                                */
+  int32_t dtype;            /* MUON_F32 or MUON_BF16                                                    */
+  int32_t activation;       /* muon_activation                                                          */
+  int64_t reserved;         /* must be 0                                                                */
+} muon_layer;
+
+/* Bytes of workspace; of the pointers only whether there is a gate is read. */
+int muon_expert_layer_bytes(const muon_layer* layer, size_t* out);
+/* x: [tokens, width], rows x_stride elements apart; expert: dense [tokens, top] of expert_bytes (4 or 8) each; out: dense [tokens, width]. */
+int muon_expert_layer(const muon_layer* layer, const void* x, int64_t x_stride, const void* expert, int32_t expert_bytes, const float* weights,
+                      void* out, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
  * Measurement aid (not part of the optimizer path; Section 2.1's Newton-Schulz products are what it prices):

@@ -31,6 +31,8 @@ EXPORTS = (
     "muon_plan_only", "muon_plan_tiles", "muon_step_static",
     "muon_head_workspace_bytes", "muon_cross_entropy", "muon_distill",
     "muon_expert_sort_bytes", "muon_expert_sort", "muon_expert_dispatch", "muon_expert_combine", "muon_expert_combine_backward",
+    "muon_step_scaled", "muon_adamw_step_scaled", "muon_grad_norm_bytes", "muon_grad_norm", "muon_grad_scale", "muon_grad_clip",
+    "muon_expert_layer_bytes", "muon_expert_layer",
 )
 PROF_NAMES = ("momentum_norm_cast", "norm_finalize", "gram", "poly", "apply_poly", "weight_update", "update_rms")
 
@@ -69,6 +71,23 @@ MUON_HEAD_D_HIDDEN, MUON_HEAD_D_WEIGHT = 1, 2
 
 class muon_routing(C.Structure):
     _fields_ = [("position", C.c_void_p), ("offsets", C.c_void_p), ("tokens", C.c_int64), ("top", C.c_int32), ("experts", C.c_int32)]
+
+
+class muon_matrices(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("expert_stride", C.c_int64), ("row_stride", C.c_int64)]
+
+
+class muon_layer(C.Structure):
+    _fields_ = [("gate", muon_matrices), ("up", muon_matrices), ("down", muon_matrices), ("tokens", C.c_int64), ("width", C.c_int64),
+                ("inner", C.c_int64), ("top", C.c_int32), ("experts", C.c_int32), ("dtype", C.c_int32), ("activation", C.c_int32),
+                ("reserved", C.c_int64)]
+
+
+ACTIVATIONS = {"silu": 0, "relu": 1}
+
+
+class muon_grad(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("numel", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
 
 
 class MuonError(RuntimeError):
@@ -156,6 +175,22 @@ def lib() -> C.CDLL:
     L.muon_expert_combine_backward.argtypes = [P(muon_routing), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
                                                C.c_void_p, C.c_void_p]
     L.muon_expert_combine_backward.restype = C.c_int
+    L.muon_step_scaled.argtypes = [C.c_void_p, P(muon_param), C.c_int32, P(muon_hparams), C.c_void_p, C.c_void_p, C.c_void_p]
+    L.muon_step_scaled.restype = C.c_int
+    L.muon_adamw_step_scaled.argtypes = [P(muon_adamw_param), C.c_int32, P(muon_adamw_hparams), C.c_void_p, C.c_void_p]
+    L.muon_adamw_step_scaled.restype = C.c_int
+    L.muon_grad_norm_bytes.argtypes = [P(muon_grad), C.c_int32, P(C.c_size_t)]
+    L.muon_grad_norm_bytes.restype = C.c_int
+    for entry in (L.muon_grad_norm, L.muon_grad_clip):
+        entry.argtypes = [P(muon_grad), C.c_int32, C.c_double, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        entry.restype = C.c_int
+    L.muon_grad_scale.argtypes = [P(muon_grad), C.c_int32, C.c_void_p, C.c_void_p]
+    L.muon_grad_scale.restype = C.c_int
+    L.muon_expert_layer_bytes.argtypes = [P(muon_layer), P(C.c_size_t)]
+    L.muon_expert_layer_bytes.restype = C.c_int
+    L.muon_expert_layer.argtypes = [P(muon_layer), C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                    C.c_void_p]
+    L.muon_expert_layer.restype = C.c_int
     _LIB = L
     return L
 
@@ -239,6 +274,11 @@ def muon_init(params, n: int, ns_dtype: int, workspace_ptr: int, workspace_bytes
 
 def muon_step(ctx, params, n: int, hp: muon_hparams, stream_ptr: int = 0, update_rms_ptr: int = 0) -> None:
     _check(lib().muon_step(ctx, params, n, C.byref(hp), C.c_void_p(stream_ptr), C.c_void_p(update_rms_ptr)), "muon_step")
+
+
+def muon_step_scaled(ctx, params, n: int, hp: muon_hparams, grad_scale_ptr: int, stream_ptr: int = 0, update_rms_ptr: int = 0) -> None:
+    _check(lib().muon_step_scaled(ctx, params, n, C.byref(hp), C.c_void_p(grad_scale_ptr), C.c_void_p(stream_ptr), C.c_void_p(update_rms_ptr)),
+           "muon_step_scaled")
 
 
 def muon_step_static(params, n: int, ns_dtype: int, hp: muon_hparams, stream_ptr: int = 0, update_rms_ptr: int = 0) -> None:
@@ -328,13 +368,15 @@ def _marshal():
 
 
 def muon_adamw_step(tensors, *, lr: float, weight_decay: float, beta1: float = 0.9, beta2: float = 0.95,
-                    eps: float = 1e-8, step: int = 1, stream_ptr: int = 0) -> None:
-    """tensors: iterable of (p, g, m, v) torch tensors of one size each (any shape, contiguous)."""
+                    eps: float = 1e-8, step: int = 1, stream_ptr: int = 0, grad_scale=None) -> None:
+    """tensors: iterable of (p, g, m, v) torch tensors of one size each (any shape, contiguous).  grad_scale: None or one fp32 element on
+    their device that the gradients count times."""
     tensors = [tuple(t) for t in tensors]
     hp = muon_adamw_hparams(lr, weight_decay, beta1, beta2, eps, step)
+    scale = () if grad_scale is None else (grad_scale_ptr(grad_scale, tensors[0][1].device if tensors else grad_scale.device),)
     native = _marshal()
     if native:
-        status = native.step(tensors, C.addressof(hp), C.c_void_p(stream_ptr).value or 0)
+        status = native.step(tensors, C.addressof(hp), C.c_void_p(stream_ptr).value or 0, *scale)
         if status is not None:
             return _check(status, "muon_adamw_step")
     # what the extension leaves to Python: tensor subclasses and the like, and whatever has to be refused
@@ -350,7 +392,38 @@ def muon_adamw_step(tensors, *, lr: float, weight_decay: float, beta1: float = 0
             raise MuonError(-2, f"tensor {i}: moments must be fp32")
         pack(arr, offset, p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), n, dtype_code(p.dtype), dtype_code(g.dtype))
         offset += size
+    if scale:
+        return _check(lib().muon_adamw_step_scaled(arr, len(tensors), C.byref(hp), *scale, C.c_void_p(stream_ptr)), "muon_adamw_step")
     _check(lib().muon_adamw_step(arr, len(tensors), C.byref(hp), C.c_void_p(stream_ptr)), "muon_adamw_step")
+
+
+def grad_scale_ptr(scale, device) -> int:
+    """Address of a gradients' scale: one fp32 element on the device."""
+    if dtype_code(scale.dtype) != MUON_F32:
+        raise MuonError(-2, f"grad_scale: fp32, not {scale.dtype}")
+    if scale.numel() != 1 or scale.device != device:
+        raise MuonError(-1, f"grad_scale: one element on {device}, not {tuple(scale.shape)} on {scale.device}")
+    return scale.data_ptr()
+
+
+def muon_grad_norm_bytes(grads, n: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().muon_grad_norm_bytes(grads, n, C.byref(out)), "muon_grad_norm_bytes")
+    return int(out.value)
+
+
+def muon_grad_norm(grads, n: int, max_norm: float, norm_ptr: int, scale_ptr: int, workspace_ptr: int, workspace_bytes: int,
+                   stream_ptr: int = 0) -> None:
+    _check(lib().muon_grad_norm(grads, n, max_norm, norm_ptr, scale_ptr, workspace_ptr, workspace_bytes, stream_ptr), "muon_grad_norm")
+
+
+def muon_grad_scale(grads, n: int, scale_ptr: int, stream_ptr: int = 0) -> None:
+    _check(lib().muon_grad_scale(grads, n, scale_ptr, stream_ptr), "muon_grad_scale")
+
+
+def muon_grad_clip(grads, n: int, max_norm: float, norm_ptr: int, scale_ptr: int, workspace_ptr: int, workspace_bytes: int,
+                   stream_ptr: int = 0) -> None:
+    _check(lib().muon_grad_clip(grads, n, max_norm, norm_ptr, scale_ptr, workspace_ptr, workspace_bytes, stream_ptr), "muon_grad_clip")
 
 
 def muon_head_workspace_bytes(head: muon_head, top: int, gradients: int, max_bytes: int = 0) -> int:
@@ -398,6 +471,18 @@ def muon_expert_combine_backward(routing: muon_routing, d_out_ptr: int, d_out_st
                                               d_weights_ptr, stream_ptr), "muon_expert_combine_backward")
 
 
+def muon_expert_layer_bytes(layer: muon_layer) -> int:
+    out = C.c_size_t(0)
+    _check(lib().muon_expert_layer_bytes(C.byref(layer), C.byref(out)), "muon_expert_layer_bytes")
+    return int(out.value)
+
+
+def muon_expert_layer(layer: muon_layer, x_ptr: int, x_stride: int, expert_ptr: int, expert_bytes: int, weights_ptr: int, out_ptr: int,
+                      workspace_ptr: int, workspace_bytes: int, stream_ptr: int = 0) -> None:
+    _check(lib().muon_expert_layer(C.byref(layer), x_ptr, x_stride, expert_ptr, expert_bytes, weights_ptr, out_ptr, workspace_ptr, workspace_bytes,
+                                   stream_ptr), "muon_expert_layer")
+
+
 def muon_destroy(ctx) -> None:
     lib().muon_destroy(ctx)
 
@@ -439,9 +524,13 @@ class MuonStepper:
             if dtype_code(m.dtype) != MUON_F32:
                 raise MuonError(-2, f"matrix {i}: momentum must be fp32")
 
-    def step(self, hp: muon_hparams, stream=None, update_rms=None) -> None:
+    def step(self, hp: muon_hparams, stream=None, update_rms=None, grad_scale=None) -> None:
+        """grad_scale: None or one fp32 element on the device that the gradients count times."""
         import torch
         s = stream if stream is not None else torch.cuda.current_stream(self.device)
+        if grad_scale is not None:
+            return muon_step_scaled(self.ctx, self.params, self.n, hp, grad_scale_ptr(grad_scale, self.device), s.cuda_stream,
+                                    0 if update_rms is None else update_rms.data_ptr())
         muon_step(self.ctx, self.params, self.n, hp, s.cuda_stream,
                   0 if update_rms is None else update_rms.data_ptr())
 

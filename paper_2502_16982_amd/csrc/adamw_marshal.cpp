@@ -47,11 +47,11 @@ bool modes_see_calls() {
   return false;
 }
 
-// step(list of tuples, address of a muon_adamw_hparams, stream) -> status of muon_adamw_step, or None
+// step(list of tuples, address of a muon_adamw_hparams, stream[, address of the gradients' scale]) -> status of the step, or None
 PyObject* step(PyObject*, PyObject* args) {
   PyObject* list = nullptr;
-  unsigned long long hp = 0, stream = 0;
-  if (!PyArg_ParseTuple(args, "O!KK", &PyList_Type, &list, &hp, &stream)) return nullptr;
+  unsigned long long hp = 0, stream = 0, scale = 0;
+  if (!PyArg_ParseTuple(args, "O!KK|K", &PyList_Type, &list, &hp, &stream, &scale)) return nullptr;
   try {
     if (modes_see_calls()) Py_RETURN_NONE;
     const Py_ssize_t n = PyList_GET_SIZE(list);
@@ -61,8 +61,8 @@ PyObject* step(PyObject*, PyObject* args) {
     if (n > INT32_MAX) Py_RETURN_NONE;
     int status = 0;
     Py_BEGIN_ALLOW_THREADS                       // the caller's list keeps the tensors alive
-    status = muon_adamw_step(records.data(), (int32_t)n, reinterpret_cast<const muon_adamw_hparams*>((uintptr_t)hp),
-                             reinterpret_cast<void*>((uintptr_t)stream));
+    status = muon_adamw_step_scaled(records.data(), (int32_t)n, reinterpret_cast<const muon_adamw_hparams*>((uintptr_t)hp),
+                                    reinterpret_cast<const float*>((uintptr_t)scale), reinterpret_cast<void*>((uintptr_t)stream));
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(status);
   } catch (...) {                                // a tensor without storage, say: the Python path raises it

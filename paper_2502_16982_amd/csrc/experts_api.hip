@@ -1,8 +1,9 @@
-// C ABI of the experts' sort, dispatch and combine (include/muon.h).
+// C ABI of the experts' sort, dispatch and combine and of a mixture's layer for few tokens (include/muon.h).
 #include <hip/hip_runtime.h>
 
 #include "api_guard.h"
 #include "experts_launch.h"
+#include "layer_launch.h"
 
 using namespace muon;
 
@@ -26,9 +27,65 @@ int expert_rows(const muon_routing* g, int64_t width, int32_t dtype, ExpertRows*
   return MUON_OK;
 }
 
+int layer_shape(const muon_layer* l, LayerShape* s) {
+  if (!l || l->reserved != 0) return MUON_E_INVALID_ARG;
+  if (l->dtype != MUON_F32 && l->dtype != MUON_BF16) return MUON_E_UNSUPPORTED_DTYPE;
+  if (l->activation != MUON_ACT_SILU && l->activation != MUON_ACT_RELU) return MUON_E_INVALID_ARG;
+  if (l->tokens < 0 || l->top < 1 || l->top > kLayerMaxTop || l->experts < 1 || l->experts > kLayerMaxExperts || l->tokens > kLayerMaxPairs / l->top ||
+      l->width < 1 || l->width > kLayerMaxWidth || l->inner < 1 || l->inner > kLayerMaxWidth)
+    return MUON_E_INVALID_ARG;
+  *s = {l->tokens, l->width, l->inner, l->top, l->experts, l->gate.w != nullptr, l->dtype == MUON_F32};
+  return MUON_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+int muon_expert_layer_bytes(const muon_layer* layer, size_t* out) {
+  return guarded([&]() -> int {
+    if (!out) return MUON_E_INVALID_ARG;
+    LayerShape s;
+    if (int st = layer_shape(layer, &s)) return st;
+    *out = layer_plan(s).total;
+    return MUON_OK;
+  });
+}
+
+int muon_expert_layer(const muon_layer* layer, const void* x, int64_t x_stride, const void* expert, int32_t expert_bytes, const float* weights,
+                      void* out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return guarded([&]() -> int {
+    LayerShape s;
+    if (int st = layer_shape(layer, &s)) return st;
+    if (expert_bytes != 4 && expert_bytes != 8) return MUON_E_INVALID_ARG;
+    if (s.tokens == 0) return MUON_OK;
+    const uintptr_t size = s.f32 ? 4 : 2;
+    const muon_matrices *up = &layer->up, *gate = &layer->gate, *down = &layer->down;
+    if (!x || !expert || !out || !up->w || !down->w || x_stride < s.width || up->row_stride < s.inner || down->row_stride < s.width ||
+        up->expert_stride < 0 || down->expert_stride < 0 || (s.gated && (gate->row_stride < s.inner || gate->expert_stride < 0)))
+      return MUON_E_INVALID_ARG;
+    if (!aligned(x, size) || !aligned(expert, expert_bytes) || !aligned(weights, 4) || !aligned(out, size) || !aligned(up->w, size) ||
+        !aligned(gate->w, size) || !aligned(down->w, size) || !aligned(workspace, 256))
+      return MUON_E_MISALIGNED;
+    const LayerPlan plan = layer_plan(s);
+    if (!workspace || workspace_bytes < plan.total) return MUON_E_WORKSPACE_TOO_SMALL;
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const LayerPairs pairs{expert, expert_bytes == 8, (int)(s.tokens * s.top), s.top, s.experts, plan.slots, plan.slot_is_pair};
+    const LayerMatrix wu{up->w, up->expert_stride, up->row_stride}, wg{gate->w, gate->expert_stride, gate->row_stride},
+        wd{down->w, down->expert_stride, down->row_stride};
+    const LayerRows tokens{x, x_stride, s.top}, inner{ws + plan.inner, s.inner, 1};
+    const int act = layer->activation;
+    const bool runs = plan.up.runs > 1;
+    MUON_HIP(launch_layer_product(pairs, plan.up, tokens, wu, s.gated ? &wg : nullptr, s.f32, runs ? -1 : act,
+                                  runs ? ws + plan.part : ws + plan.inner, stream));
+    if (runs)
+      MUON_HIP(launch_layer_act(pairs, plan.up.runs, s.inner, s.gated, s.f32, act, reinterpret_cast<const float*>(ws + plan.part), ws + plan.inner, stream));
+    MUON_HIP(launch_layer_product(pairs, plan.down, inner, wd, nullptr, s.f32, -1, ws + plan.rows, stream));
+    MUON_HIP(launch_layer_join(pairs, plan.down.runs, s.width, s.f32, reinterpret_cast<const float*>(ws + plan.rows), weights, out, stream));
+    return MUON_OK;
+  });
+}
 
 int muon_expert_sort_bytes(int64_t tokens, int32_t top, int32_t experts, size_t* out) {
   return guarded([&]() -> int {

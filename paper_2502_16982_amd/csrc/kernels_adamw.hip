@@ -80,9 +80,10 @@ __device__ __forceinline__ void st4(float* p, const float* in) { st_any<NT>(p, f
 template <bool NT>
 __device__ __forceinline__ void st4(u16* p, const float* in) { st_any<NT>(p, u32x2_any{pack2(in[0], in[1]), pack2(in[2], in[3])}); }
 
-template <bool NT, typename PT, typename GT>
+// SCALED: gradients count times gs.
+template <bool NT, bool SCALED, typename PT, typename GT>
 __device__ __forceinline__ void adamw_span(PT* p, const GT* g, float* m, float* v, long long begin, long long numel,
-                                           const AdamwScalars& h) {
+                                           const AdamwScalars& h, float gs) {
   const long long i0 = begin + threadIdx.x * 4;
   if (i0 + 4 <= numel) {
     float pv[4], gv[4], mv[4], vv[4];
@@ -91,21 +92,22 @@ __device__ __forceinline__ void adamw_span(PT* p, const GT* g, float* m, float* 
     ld4<NT>(p + i0, pv);
     ld4<NT>(g + i0, gv);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) adamw_elem(pv[e], gv[e], mv[e], vv[e], h);
+    for (int e = 0; e < 4; ++e) adamw_elem(pv[e], SCALED ? gs * gv[e] : gv[e], mv[e], vv[e], h);
     st4<NT>(m + i0, mv);
     st4<NT>(v + i0, vv);
     st4<NT>(p + i0, pv);
   } else {
     for (long long i = i0; i < numel; ++i) {     // the last, partial piece of a tensor
       float pv = ld1(p + i), mv = m[i], vv = v[i];
-      adamw_elem(pv, ld1(g + i), mv, vv, h);
+      adamw_elem(pv, SCALED ? gs * ld1(g + i) : ld1(g + i), mv, vv, h);
       m[i] = mv; v[i] = vv; st1(p + i, pv);
     }
   }
 }
 
-template <bool NT>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch batch, AdamwScalars h) {
+template <bool NT, bool SCALED>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch batch, AdamwScalars h, const float* __restrict__ grad_scale) {
+  const float gs = SCALED ? *grad_scale : 1.f;
   // the tensor that owns this block: block_start is a prefix sum over the tensors' block counts
   int t = 0;
 #pragma unroll
@@ -117,25 +119,31 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch batch, AdamwScala
   float* v = batch.v[t];
   const int pd = batch.p_dtype[t], gd = batch.g_dtype[t];
   if (pd == kDtypeBF16) {
-    if (gd == kDtypeBF16) adamw_span<NT>(static_cast<u16*>(batch.p[t]), static_cast<const u16*>(batch.g[t]), m, v, begin, numel, h);
-    else adamw_span<NT>(static_cast<u16*>(batch.p[t]), static_cast<const float*>(batch.g[t]), m, v, begin, numel, h);
+    if (gd == kDtypeBF16) adamw_span<NT, SCALED>(static_cast<u16*>(batch.p[t]), static_cast<const u16*>(batch.g[t]), m, v, begin, numel, h, gs);
+    else adamw_span<NT, SCALED>(static_cast<u16*>(batch.p[t]), static_cast<const float*>(batch.g[t]), m, v, begin, numel, h, gs);
   } else {
-    if (gd == kDtypeBF16) adamw_span<NT>(static_cast<float*>(batch.p[t]), static_cast<const u16*>(batch.g[t]), m, v, begin, numel, h);
-    else adamw_span<NT>(static_cast<float*>(batch.p[t]), static_cast<const float*>(batch.g[t]), m, v, begin, numel, h);
+    if (gd == kDtypeBF16) adamw_span<NT, SCALED>(static_cast<float*>(batch.p[t]), static_cast<const u16*>(batch.g[t]), m, v, begin, numel, h, gs);
+    else adamw_span<NT, SCALED>(static_cast<float*>(batch.p[t]), static_cast<const float*>(batch.g[t]), m, v, begin, numel, h, gs);
   }
 }
 
 }  // namespace
 
 hipError_t launch_adamw(const AdamwBatch& batch, int n_blocks, float lr, float wd, float beta1, float beta2, float eps,
-                        float inv_bc1, float inv_bc2, hipStream_t s) {
+                        float inv_bc1, float inv_bc2, const float* grad_scale, hipStream_t s) {
   if (n_blocks <= 0) return hipSuccess;
   AdamwScalars h{lr, wd, beta1, beta2, eps, inv_bc1, inv_bc2};
   long long bytes = 0;
   for (int t = 0; t < batch.n; ++t)
     bytes += batch.numel[t] * (16 + (batch.p_dtype[t] == kDtypeBF16 ? 4 : 8) + (batch.g_dtype[t] == kDtypeBF16 ? 2 : 4));
-  if (bytes >= kStreamBytes) adamw_kernel<true><<<n_blocks, 256, 0, s>>>(batch, h);
-  else adamw_kernel<false><<<n_blocks, 256, 0, s>>>(batch, h);
+  const bool nt = bytes >= kStreamBytes;
+  if (grad_scale) {
+    if (nt) adamw_kernel<true, true><<<n_blocks, 256, 0, s>>>(batch, h, grad_scale);
+    else adamw_kernel<false, true><<<n_blocks, 256, 0, s>>>(batch, h, grad_scale);
+  } else {
+    if (nt) adamw_kernel<true, false><<<n_blocks, 256, 0, s>>>(batch, h, nullptr);
+    else adamw_kernel<false, false><<<n_blocks, 256, 0, s>>>(batch, h, nullptr);
+  }
   return hipGetLastError();
 }
 

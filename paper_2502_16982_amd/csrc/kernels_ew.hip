@@ -172,9 +172,9 @@ __device__ __forceinline__ float ns_load1(const XT* p, size_t plane) {
 // 50 of 2047 x 1401 3074 -> 404 us, six matrices of odd widths 106 -> 32 us, against scalar accesses whose loads waited
 // for the stores before them.  Non-temporal hints: -4 % on aligned rows, +40 % on odd ones, not used.
 // ------------------------------------------------------------------------------------------------------
-template <typename GT, typename XT, int PL>
+template <typename GT, typename XT, int PL, bool SCALED>
 __device__ __forceinline__ void momentum_tile(const MatDesc& d, const MatPtrs& pt, int tr, int tc, float mu, int nesterov,
-                                              bool both, float (*lds)[kEwTile + 1], float* red) {
+                                              bool both, float gs, float (*lds)[kEwTile + 1], float* red) {
   const int tid = threadIdx.x;
   const int lr = tid >> 4, lc = (tid & 15) * 4;
   const int r0 = tr * kEwTile + lr, c0 = tc * kEwTile + lc;
@@ -207,6 +207,7 @@ __device__ __forceinline__ void momentum_tile(const MatDesc& d, const MatPtrs& p
     const size_t base = (size_t)r * (size_t)B + (size_t)c0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      if constexpr (SCALED) gv[j][i] *= gs;
       const float mn = fmaf(mu, mv[j][i], gv[j][i]);
       mv[j][i] = mn;
       u[j][i] = nesterov ? fmaf(mu, mn, gv[j][i]) : mn;
@@ -269,28 +270,29 @@ __device__ __forceinline__ EwTile load_item(const EwTile* __restrict__ tiles) {
   return t;
 }
 
-template <typename XT, int PL>
-__device__ __forceinline__ void momentum_item(const MatDesc& d, const MatPtrs& pt, const EwTile& t, float mu, int nesterov, int both) {
+template <typename XT, int PL, bool SCALED>
+__device__ __forceinline__ void momentum_item(const MatDesc& d, const MatPtrs& pt, const EwTile& t, float mu, int nesterov, int both, float gs) {
   __shared__ float lds[kEwTile][kEwTile + 1];
   __shared__ float red[256];
   for (int k = 0; k < t.count; ++k) {
     if (k) __syncthreads();     // the LDS tile and the reduction scratch are reused
     if (d.g_dtype == kDtypeBF16)
-      momentum_tile<u16, XT, PL>(d, pt, t.tr, t.tc + k, mu, nesterov, both != 0, lds, red);
+      momentum_tile<u16, XT, PL, SCALED>(d, pt, t.tr, t.tc + k, mu, nesterov, both != 0, gs, lds, red);
     else
-      momentum_tile<float, XT, PL>(d, pt, t.tr, t.tc + k, mu, nesterov, both != 0, lds, red);
+      momentum_tile<float, XT, PL, SCALED>(d, pt, t.tr, t.tc + k, mu, nesterov, both != 0, gs, lds, red);
   }
 }
 
-template <typename XT, int PL>
+// SCALED: G counts times *g_scale.
+template <typename XT, int PL, bool SCALED>
 __global__ __launch_bounds__(256) void momentum_norm_cast_kernel(const MatDesc* __restrict__ mats,
                                                                   const MatPtrs* __restrict__ ptrs,
                                                                   const EwTile* __restrict__ tiles, float mu,
-                                                                  int nesterov, int both) {
+                                                                  int nesterov, int both, const float* __restrict__ g_scale) {
   const EwTile t = load_item(tiles);
   const MatDesc& d = mats[t.mat];     // read in place (uniform address: scalar loads); see o_source
   const MatPtrs pt = ptrs[t.mat];
-  momentum_item<XT, PL>(d, pt, t, mu, nesterov, both);
+  momentum_item<XT, PL, SCALED>(d, pt, t, mu, nesterov, both, SCALED ? *g_scale : 1.f);
 }
 
 // The same with the step's pointers as a kernel argument; a matrix's first block leaves them in the table for the passes
@@ -304,7 +306,7 @@ __global__ __launch_bounds__(256) void momentum_norm_cast_pack_kernel(const MatD
   const MatDesc& d = mats[t.mat];
   const MatPtrs pt = pack.p[t.mat];
   if (t.tr == 0 && t.tc == 0 && threadIdx.x == 0) ptrs[t.mat] = pt;
-  momentum_item<XT, PL>(d, pt, t, mu, nesterov, both);
+  momentum_item<XT, PL, false>(d, pt, t, mu, nesterov, both, 1.f);
 }
 
 // ------------------------------------------------------------------------------------------------------
@@ -553,15 +555,20 @@ __global__ __launch_bounds__(256) void read_update_kernel(const MatDesc* __restr
   }
 
 hipError_t launch_momentum_norm_cast(const MatDesc* mats, MatPtrs* ptrs, const PtrPack* pack, const EwTile* tiles, int n_tiles,
-                                     float mu, int nesterov, int both_layouts, int ns_dtype, hipStream_t s) {
+                                     float mu, int nesterov, int both_layouts, int ns_dtype, const float* g_scale, hipStream_t s) {
   if (n_tiles <= 0) return hipSuccess;
-  if (pack) {
+  if (g_scale) {
+#define MUON_CALL(XT, PL) \
+  momentum_norm_cast_kernel<XT, PL, true><<<n_tiles, 256, 0, s>>>(mats, ptrs, tiles, mu, nesterov, both_layouts, g_scale)
+    MUON_NS_DISPATCH(ns_dtype, MUON_CALL)
+#undef MUON_CALL
+  } else if (pack) {
 #define MUON_CALL(XT, PL) \
   momentum_norm_cast_pack_kernel<XT, PL><<<n_tiles, 256, 0, s>>>(mats, *pack, ptrs, tiles, mu, nesterov, both_layouts)
     MUON_NS_DISPATCH(ns_dtype, MUON_CALL)
 #undef MUON_CALL
   } else {
-#define MUON_CALL(XT, PL) momentum_norm_cast_kernel<XT, PL><<<n_tiles, 256, 0, s>>>(mats, ptrs, tiles, mu, nesterov, both_layouts)
+#define MUON_CALL(XT, PL) momentum_norm_cast_kernel<XT, PL, false><<<n_tiles, 256, 0, s>>>(mats, ptrs, tiles, mu, nesterov, both_layouts, nullptr)
     MUON_NS_DISPATCH(ns_dtype, MUON_CALL)
 #undef MUON_CALL
   }

@@ -314,7 +314,8 @@ int enqueue_paired(muon_ctx* ctx, const Chunk& ch, const muon_hparams* hp, const
 
 // Enqueues every kernel of one step on stream s.  The pointer table is already on its way on the same stream, or (pack, plans
 // of one chunk) the first pass takes the pointers as an argument and fills it.
-int enqueue_step(muon_ctx* ctx, const muon_hparams* hp, hipStream_t s, float* update_rms_out, const PtrPack* pack = nullptr) {
+int enqueue_step(muon_ctx* ctx, const muon_hparams* hp, hipStream_t s, float* update_rms_out, const PtrPack* pack = nullptr,
+                 const float* grad_scale = nullptr) {
   const int N = hp->ns_steps;
   const int use_s = N == 0;
   const bool mc = on_matrix_cores(ctx->ns_dtype);   // bf16 or split-bf16: the MFMA kernels and their one-layout plan
@@ -338,7 +339,7 @@ int enqueue_step(muon_ctx* ctx, const muon_hparams* hp, hipStream_t s, float* up
     const Chunk& ch = ctx->plan.chunks[ci];
     const EwTile* ew = reinterpret_cast<const EwTile*>(ctx->ws + ch.ew_tiles_off);
     MUON_TIMED(MUON_PROF_MOMENTUM, launch_momentum_norm_cast(ctx->d_mats, ctx->d_ptrs, pack, ew, ch.n_ew_tiles, (float)hp->momentum,
-                                                             hp->nesterov != 0, (!mc || N == 0) ? 1 : 0, ctx->ns_dtype, s));
+                                                             hp->nesterov != 0, (!mc || N == 0) ? 1 : 0, ctx->ns_dtype, grad_scale, s));
     const bool fold = ch.fold_norm && N > 0;
     if (!fold) MUON_TIMED(MUON_PROF_NORM, launch_norm_finalize(ctx->d_mats, ch.first, ch.count, hp->eps, gram_gain, s));
     if (ch.paired) {
@@ -401,7 +402,7 @@ int enqueue_step(muon_ctx* ctx, const muon_hparams* hp, hipStream_t s, float* up
 }
 
 int step_impl(muon_ctx* ctx, const muon_param* params, int32_t n, const muon_hparams* hp, void* hip_stream,
-              float* update_rms_out) {
+              float* update_rms_out, const float* grad_scale = nullptr) {
   bool changed = false;
   const int st = check_step_args(ctx, params, n, hp, &changed);
   if (st != MUON_OK) return st;
@@ -418,7 +419,7 @@ int step_impl(muon_ctx* ctx, const muon_param* params, int32_t n, const muon_hpa
     for (int i = 0; i < n; ++i) ctx->last_ptrs[i] = ctx->h_ptrs_pinned[i];
     ctx->ptrs_valid = true;
   }
-  return enqueue_step(ctx, hp, s, update_rms_out);
+  return enqueue_step(ctx, hp, s, update_rms_out, nullptr, grad_scale);
 }
 
 }  // namespace
@@ -501,6 +502,12 @@ int muon_plan_tiles(const muon_ctx* ctx, int32_t chunk, int32_t product, int32_t
 int muon_step(muon_ctx* ctx, const muon_param* params, int32_t n, const muon_hparams* hp, void* hip_stream,
               float* update_rms_out) {
   return guarded([&]() { return step_impl(ctx, params, n, hp, hip_stream, update_rms_out); });
+}
+
+int muon_step_scaled(muon_ctx* ctx, const muon_param* params, int32_t n, const muon_hparams* hp, const float* grad_scale, void* hip_stream,
+                     float* update_rms_out) {
+  if (reinterpret_cast<uintptr_t>(grad_scale) & 3u) return MUON_E_MISALIGNED;
+  return guarded([&]() { return step_impl(ctx, params, n, hp, hip_stream, update_rms_out, grad_scale); });
 }
 
 }  // extern "C"
@@ -649,6 +656,11 @@ int muon_profile_read(muon_ctx* ctx, double* ms_out, int64_t* launches_out, int 
 }
 
 int muon_adamw_step(const muon_adamw_param* params, int32_t n, const muon_adamw_hparams* hp, void* hip_stream) {
+  return muon_adamw_step_scaled(params, n, hp, nullptr, hip_stream);
+}
+
+int muon_adamw_step_scaled(const muon_adamw_param* params, int32_t n, const muon_adamw_hparams* hp, const float* grad_scale, void* hip_stream) {
+  if (reinterpret_cast<uintptr_t>(grad_scale) & 3u) return MUON_E_MISALIGNED;
   if (!params || !hp || n <= 0) return MUON_E_INVALID_ARG;
   if (!(hp->beta1 >= 0.0 && hp->beta1 < 1.0) || !(hp->beta2 >= 0.0 && hp->beta2 < 1.0) || !(hp->eps >= 0.0) || hp->step < 1 ||
       !std::isfinite(hp->lr) || !std::isfinite(hp->weight_decay) || !std::isfinite(hp->eps))
@@ -672,7 +684,7 @@ int muon_adamw_step(const muon_adamw_param* params, int32_t n, const muon_adamw_
   AdamwCursor at;
   while (const int blocks = adamw_next_batch(params, n, at, b))
     MUON_HIP(launch_adamw(b, blocks, (float)hp->lr, (float)hp->weight_decay, (float)hp->beta1, (float)hp->beta2, (float)hp->eps,
-                          inv_bc1, inv_bc2, s));
+                          inv_bc1, inv_bc2, grad_scale, s));
   return MUON_OK;
 }
 

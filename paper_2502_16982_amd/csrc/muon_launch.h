@@ -81,12 +81,13 @@ int gemm_coarse_blocks();
 // a1-a3: momentum, sum of squares, cast + orient.  both_layouts != 0: U goes to X and Xt[0] (one holds U, the other
 // U^T); 0: only X (the orientation with rows <= cols) is written.  One block per EwTile.
 // pack != null: the pointers come as a kernel argument and the pass leaves them in `ptrs` for the kernels behind it.
+// g_scale != null (device; not with pack): G counts times *g_scale.
 constexpr int kPackSlots = 64;
 struct PtrPack {
   MatPtrs p[kPackSlots];
 };
 hipError_t launch_momentum_norm_cast(const MatDesc* mats, MatPtrs* ptrs, const PtrPack* pack, const EwTile* tiles, int n_tiles,
-                                     float mu, int nesterov, int both_layouts, int ns_dtype, hipStream_t s);
+                                     float mu, int nesterov, int both_layouts, int ns_dtype, const float* g_scale, hipStream_t s);
 
 // a2 second stage: fixed-order sum of the partials of each matrix, s = 1/(sqrt(sum)+eps).
 // gram_gain: store_norm's gain for matrices of the Gram route (0: they are iterated as Eq. 2 is written).
@@ -157,8 +158,9 @@ hipError_t launch_update_rms(const MatDesc* mats, int first_mat, int n_mats, int
 hipError_t launch_read_update(const MatDesc* mats, int mat, int o_sel, int use_s, int ns_dtype, void* dst,
                               int dst_dtype, hipStream_t s);
 
-// AdamW (non-matrix parameters): one launch over the pieces of a batch (adamw_batch.h).
+// AdamW (non-matrix parameters): one launch over the pieces of a batch (adamw_batch.h).  grad_scale != null (device): gradients
+// count times *grad_scale.
 hipError_t launch_adamw(const AdamwBatch& batch, int n_blocks, float lr, float wd, float beta1, float beta2, float eps,
-                        float inv_bc1, float inv_bc2, hipStream_t s);
+                        float inv_bc1, float inv_bc2, const float* grad_scale, hipStream_t s);
 
 }  // namespace muon

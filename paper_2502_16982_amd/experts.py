@@ -1,4 +1,4 @@
-"""A mixture's tokens to their experts and back, with gradients.
+"""A mixture's tokens to their experts and back, with gradients; the whole layer for a few tokens.
 
 Argument checks and memory only; the work is in the HIP library (``muon_expert_*``).  Everything runs on the current stream of
 the tensors' device.  autograd does not see these calls: ``dispatch_backward`` and ``combine_backward`` are the gradients.
@@ -132,3 +132,48 @@ def combine_backward(d_out: torch.Tensor, rows: torch.Tensor, weights: torch.Ten
         binding.muon_expert_combine_backward(r, d_out.data_ptr(), stride, rows.data_ptr(), at, width, binding.dtype_code(rows.dtype),
                                              d_rows.data_ptr(), d_weights.data_ptr(), stream_handle(device))
     return d_rows, d_weights
+
+
+def _matrices(name: str, t: torch.Tensor, experts: int, rows: int, columns: int, dtype: torch.dtype) -> "binding.muon_matrices":
+    if t.dim() != 3 or tuple(t.shape) != (experts, rows, columns):
+        raise MuonError(-1, f"{name}: [{experts}, {rows}, {columns}], not {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise MuonError(-2, f"{name}: {dtype} as x, not {t.dtype}")
+    if t.stride(2) != 1 and columns > 1:
+        raise MuonError(-1, f"{name}: rows must be contiguous")
+    return binding.muon_matrices(t.data_ptr(), t.stride(0) if experts > 1 else 0, t.stride(1) if rows > 1 else columns)
+
+
+def layer(x: torch.Tensor, up: torch.Tensor, down: torch.Tensor, expert: torch.Tensor, weights: Optional[torch.Tensor] = None,
+          gate: Optional[torch.Tensor] = None, activation: str = "silu") -> torch.Tensor:
+    """[tokens, width]: the experts of a mixture on a few tokens ``x`` [tokens, width] without sorting them.
+
+    Token t gets the sum over its ``expert`` [tokens, top] (int32 or int64; not in [0, experts): dropped) of ``weights`` (fp32, None: all 1)
+    times ``(act(x gate[e]) * (x up[e])) down[e]``, without ``gate`` ``act(x up[e]) down[e]``; act is "silu" or "relu".  ``gate`` and ``up``
+    are [experts, width, inner], ``down`` is [experts, inner, width], of x's type.  For more tokens than a few hundred sort and dispatch them.
+    """
+    if expert.dim() != 2 or not expert.is_contiguous():
+        raise MuonError(-1, f"expert: contiguous [tokens, top], not {tuple(expert.shape)}")
+    if expert.dtype not in (torch.int32, torch.int64):
+        raise MuonError(-2, f"expert: int32 or int64, not {expert.dtype}")
+    if activation not in binding.ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(binding.ACTIVATIONS)}")
+    device = _device(x, up, down, expert, weights, gate)
+    tokens, top = expert.shape
+    stride, width = _tokens("x", x, tokens)
+    if up.dim() != 3:
+        raise MuonError(-1, f"up: [experts, {width}, inner], not {tuple(up.shape)}")
+    experts, _, inner = up.shape
+    none = binding.muon_matrices(None, 0, 0)
+    args = binding.muon_layer(none if gate is None else _matrices("gate", gate, experts, width, inner, x.dtype),
+                              _matrices("up", up, experts, width, inner, x.dtype), _matrices("down", down, experts, inner, width, x.dtype),
+                              tokens, width, inner, top, experts, binding.dtype_code(x.dtype), binding.ACTIVATIONS[activation], 0)
+    at = 0 if weights is None else _weights(weights, expert)
+    outside_autograd("experts.layer", any(t is not None and t.requires_grad for t in (x, up, down, weights, gate)))
+    need = binding.muon_expert_layer_bytes(args)
+    with on(device):
+        out = torch.empty(tokens, width, dtype=x.dtype, device=device)
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        binding.muon_expert_layer(args, x.data_ptr(), stride, expert.data_ptr(), expert.element_size(), at, out.data_ptr(),
+                                  workspace.data_ptr(), need, stream_handle(device))
+    return out
