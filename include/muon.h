@@ -364,6 +364,35 @@ int muon_distill(const muon_head* head, const void* index, int32_t index_bytes, 
                  size_t workspace_bytes, void* hip_stream);
 
 /*
+ * Log probabilities of given tokens from the same hidden states and weight, with z = H W^T / temperature, p = softmax(z):
+ *
+ *   log_prob_t = z_t,y(t) - lse_t     entropy_t = -sum_v p_tv log p_tv     the top largest z_t with their log probabilities
+ *
+ * and the gradients of sum_t (d_log_prob_t log_prob_t + d_entropy_t entropy_t), by a second call that is given what the first one found:
+ *
+ *   dz_tv = d_log_prob_t ([v = y_t] - p_tv) - d_entropy_t p_tv (log p_tv + entropy_t),   d_hidden = dz W / temperature,  d_weight = dz^T H / temperature
+ *
+ * A token without target (negative) has log_prob 0 and none of its gradient; one of vocab or more makes log_prob NaN and gives none; both have
+ * their entropy and alternatives all the same.  A token both of whose gradients are 0 reaches nothing, whatever its hidden state holds (d_weight;
+ * its row of d_hidden is zero for finite W).  Alternatives are in falling order of their logits as summed in double, equal ones by index, chosen
+ * among the top + 8 that fp32 sums find largest (and whatever is as large as the last of these); logits that are NaN come last.
+ * Types, precision, pieces of tokens and what may run when are those of muon_cross_entropy; the log probabilities' own logits are summed in
+ * double, dz is rounded to bf16 once.  lse_rest is what fp32 leaves of lse.
+ */
+/* Bytes of workspace (256-byte aligned) of muon_log_probs; top: 0 (no alternatives) .. min(64, vocab); max_bytes as above.
+ * muon_log_probs_backward takes muon_head_workspace_bytes(head, 1, gradients, ..). */
+int muon_log_probs_bytes(const muon_head* head, int32_t top, size_t max_bytes, size_t* out);
+/* targets: [tokens] of targets_bytes (4 or 8) each, or null, and log_prob then too.  log_prob, entropy, lse, lse_rest: [tokens]; top_index,
+ * top_log_prob: [tokens, top], null where top is 0. */
+int muon_log_probs(const muon_head* head, const void* targets, int32_t targets_bytes, int32_t top, double temperature, float* log_prob, float* entropy,
+                   float* lse, float* lse_rest, int64_t* top_index, float* top_log_prob, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* lse, lse_rest, entropy: as muon_log_probs left them for the same head, targets and temperature.  d_log_prob: [tokens], null with null targets;
+ * d_entropy: [tokens] or null (0).  d_hidden, d_weight: dense, overwritten, or null where not wanted. */
+int muon_log_probs_backward(const muon_head* head, const void* targets, int32_t targets_bytes, double temperature, const float* lse, const float* lse_rest,
+                            const float* entropy, const float* d_log_prob, const float* d_entropy, void* d_hidden, void* d_weight, void* workspace,
+                            size_t workspace_bytes, void* hip_stream);
+
+/*
  * A mixture's tokens to their experts and back.  muon_expert_sort ranks the tokens' pairs (token t, choice j) by expert, pairs of one expert
  * in their own order:
  *   position[t, j]  the pair's row in that order, -1 where its expert is not in [0, experts): such a pair is dropped

@@ -32,7 +32,7 @@ EXPORTS = (
     "muon_head_workspace_bytes", "muon_cross_entropy", "muon_distill",
     "muon_expert_sort_bytes", "muon_expert_sort", "muon_expert_dispatch", "muon_expert_combine", "muon_expert_combine_backward",
     "muon_step_scaled", "muon_adamw_step_scaled", "muon_grad_norm_bytes", "muon_grad_norm", "muon_grad_scale", "muon_grad_clip",
-    "muon_expert_layer_bytes", "muon_expert_layer",
+    "muon_expert_layer_bytes", "muon_expert_layer", "muon_log_probs_bytes", "muon_log_probs", "muon_log_probs_backward",
 )
 PROF_NAMES = ("momentum_norm_cast", "norm_finalize", "gram", "poly", "apply_poly", "weight_update", "update_rms")
 
@@ -191,6 +191,14 @@ def lib() -> C.CDLL:
     L.muon_expert_layer.argtypes = [P(muon_layer), C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
                                     C.c_void_p]
     L.muon_expert_layer.restype = C.c_int
+    L.muon_log_probs_bytes.argtypes = [P(muon_head), C.c_int32, C.c_size_t, P(C.c_size_t)]
+    L.muon_log_probs_bytes.restype = C.c_int
+    L.muon_log_probs.argtypes = [P(muon_head), C.c_void_p, C.c_int32, C.c_int32, C.c_double, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                 C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    L.muon_log_probs.restype = C.c_int
+    L.muon_log_probs_backward.argtypes = [P(muon_head), C.c_void_p, C.c_int32, C.c_double, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    L.muon_log_probs_backward.restype = C.c_int
     _LIB = L
     return L
 
@@ -443,6 +451,27 @@ def muon_distill(head: muon_head, index_ptr: int, index_bytes: int, logits_ptr: 
                  workspace_bytes: int, stream_ptr: int = 0) -> None:
     _check(lib().muon_distill(C.byref(head), index_ptr, index_bytes, logits_ptr, logits_dtype, top, temperature, scale_ptr, loss_ptr,
                               lse_ptr, d_hidden_ptr, d_weight_ptr, workspace_ptr, workspace_bytes, stream_ptr), "muon_distill")
+
+
+def muon_log_probs_bytes(head: muon_head, top: int, max_bytes: int = 0) -> int:
+    out = C.c_size_t(0)
+    _check(lib().muon_log_probs_bytes(C.byref(head), top, max_bytes, C.byref(out)), "muon_log_probs_bytes")
+    return int(out.value)
+
+
+def muon_log_probs(head: muon_head, targets_ptr: int, targets_bytes: int, top: int, temperature: float, log_prob_ptr: int, entropy_ptr: int,
+                   lse_ptr: int, lse_rest_ptr: int, top_index_ptr: int, top_log_prob_ptr: int, workspace_ptr: int, workspace_bytes: int,
+                   stream_ptr: int = 0) -> None:
+    _check(lib().muon_log_probs(C.byref(head), targets_ptr, targets_bytes, top, temperature, log_prob_ptr, entropy_ptr, lse_ptr, lse_rest_ptr,
+                                top_index_ptr, top_log_prob_ptr, workspace_ptr, workspace_bytes, stream_ptr), "muon_log_probs")
+
+
+def muon_log_probs_backward(head: muon_head, targets_ptr: int, targets_bytes: int, temperature: float, lse_ptr: int, lse_rest_ptr: int,
+                            entropy_ptr: int, d_log_prob_ptr: int, d_entropy_ptr: int, d_hidden_ptr: int, d_weight_ptr: int,
+                            workspace_ptr: int, workspace_bytes: int, stream_ptr: int = 0) -> None:
+    _check(lib().muon_log_probs_backward(C.byref(head), targets_ptr, targets_bytes, temperature, lse_ptr, lse_rest_ptr, entropy_ptr,
+                                         d_log_prob_ptr, d_entropy_ptr, d_hidden_ptr, d_weight_ptr, workspace_ptr, workspace_bytes,
+                                         stream_ptr), "muon_log_probs_backward")
 
 
 def muon_expert_sort_bytes(tokens: int, top: int, experts: int) -> int:

@@ -16,7 +16,7 @@ MARSHAL_PATH = os.path.join(PKG_DIR, "_adamw_marshal.so")
 # the planners are plain C++ (they also build with g++ alone, see tests/test_plan_sanitized.py); the rest is HIP
 SOURCES = ("muon_api.hip", "muon_plan.cpp", "kernels_ew.hip", "kernels_gemm_bf16.hip", "kernels_gemm_pair.hip", "kernels_gemm_f32.hip",
            "kernels_adamw.hip", "head_api.hip", "head_plan.cpp", "kernels_head.hip", "experts_api.hip", "kernels_experts.hip",
-           "probe_mfma.hip", "clip_api.hip", "kernels_clip.hip", "kernels_layer.hip")
+           "probe_mfma.hip", "clip_api.hip", "kernels_clip.hip", "kernels_layer.hip", "score_api.hip", "score_plan.cpp", "kernels_score.hip")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -24,6 +24,8 @@ struct HeadTiles {
   int splits, slabs_per_split;
 };
 
+inline HeadTiles tiles_of(const HeadProduct& g, int pairs) { return {g.k, pairs, g.tiles_m, g.tiles_n, g.whole, g.splits, g.slabs_per_split}; }
+
 // Where a gradient's tiles go.  out: n rows of m elements, dense.  partial (splits > 1): [split][n][m] in fp32.  sum: fp32 [n][m],
 // the pieces of tokens before (add) and with this one (keep).  Results are times `scale` and *peak (null: 1).
 struct HeadOut {

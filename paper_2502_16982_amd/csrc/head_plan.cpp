@@ -63,10 +63,7 @@ HeadProduct head_product(int64_t m, int64_t n, int64_t k, int pairs, int64_t par
   return p;
 }
 
-namespace {
-
-// What of a plan goes by the shape alone.
-HeadPlan plan_shape(const HeadShape& s) {
+HeadPlan head_plan_shape(const HeadShape& s) {
   HeadPlan p{};
   p.planes = s.f32 ? 3 : 1;
   p.pairs = s.f32 ? 6 : 1;
@@ -79,6 +76,8 @@ HeadPlan plan_shape(const HeadShape& s) {
   p.pack_weight = ragged || s.weight_stride % 8 != 0 || s.weight_stride > kHeadMaxPitch || !s.weight_aligned;
   return p;
 }
+
+namespace {
 
 // Lays out the sections for pieces of so many tokens; the splits' sums come last.
 void lay_out(const HeadShape& s, int64_t piece, int64_t partial, HeadPlan* p) {
@@ -112,7 +111,7 @@ void lay_out(const HeadShape& s, int64_t piece, int64_t partial, HeadPlan* p) {
 // Bytes for pieces of so many tokens without any splits.  More tokens in a piece take more, but for the sum of d_weight, which one piece
 // does without.
 size_t bytes_unsplit(const HeadShape& s, int64_t piece) {
-  HeadPlan p = plan_shape(s);
+  HeadPlan p = head_plan_shape(s);
   lay_out(s, piece, 0, &p);
   return p.total;
 }
@@ -146,7 +145,7 @@ size_t head_workspace(const HeadShape& s, size_t max_bytes) {
 }
 
 bool head_plan(const HeadShape& s, size_t max_bytes, HeadPlan* p) {
-  *p = plan_shape(s);
+  *p = head_plan_shape(s);
   const int64_t all = std::max<int64_t>(1, s.tokens), most = max_bytes == 0 ? kHeadPieceTokens : most_tokens(s);
   const size_t limit = max_bytes == 0 ? (size_t)1 << 62 : std::min(max_bytes, (size_t)1 << 62);
   // The products for pieces of so many tokens with so many bytes for the splits' sums, of which it answers what they take.

@@ -56,6 +56,8 @@ struct HeadPlan {
   size_t total;
 };
 
+// What of a plan goes by the shape alone: planes, pairs, pitches, what is copied first, blocks of statistics.
+HeadPlan head_plan_shape(const HeadShape& s);
 // The product of an m x k by a k x n operand for a device of 256 compute units; the sums of K's runs may take partial_bytes (0: one run).
 HeadProduct head_product(int64_t m, int64_t n, int64_t k, int pairs, int64_t partial_bytes);
 // Workspace to give a call: what the fastest plan takes with pieces of kHeadPieceTokens (max_bytes 0), or with one piece of all tokens; where that is

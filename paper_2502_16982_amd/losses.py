@@ -1,12 +1,13 @@
 """Losses of a language model's head with their gradients: softmax cross entropy over a large vocabulary and distillation
-from a teacher's top logits, from hidden states and the head's weight, without keeping the logits.
+from a teacher's top logits, from hidden states and the head's weight, without keeping the logits; and log probabilities of given tokens
+with entropies and top alternatives, from the same, with a backward call of their own.
 
-Argument checks and memory only; the arithmetic is in the HIP library (``muon_cross_entropy``, ``muon_distill``).  autograd does not see
-these calls: the gradients are in their results, for the token_scale given.
+Argument checks and memory only; the arithmetic is in the HIP library (``muon_cross_entropy``, ``muon_distill``, ``muon_log_probs``).
+autograd does not see these calls: the losses' gradients are in their results, for the token_scale given.
 """
 from __future__ import annotations
 
-from typing import NamedTuple, Optional
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -21,6 +22,17 @@ class HeadResult(NamedTuple):
     lse: torch.Tensor
     d_hidden: Optional[torch.Tensor]
     d_weight: Optional[torch.Tensor]
+
+
+class TokenScores(NamedTuple):
+    """log_prob: [tokens] in fp32, or None without targets; entropy, lse: [tokens] in fp32; lse_rest: what fp32 leaves of lse; top_index:
+    [tokens, top] in int64, top_log_prob: in fp32, or None where not asked for."""
+    log_prob: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    lse_rest: torch.Tensor
+    top_index: Optional[torch.Tensor]
+    top_log_prob: Optional[torch.Tensor]
 
 
 def _index_bytes(t: torch.Tensor, what: str) -> int:
@@ -58,15 +70,16 @@ class LossHead:
         head = binding.muon_head(None, None, width, width, tokens, vocab, width, binding.dtype_code(dtype), 0)
         self._fit(head, top, 3 if gradients else 0)
 
-    def _fit(self, head: "binding.muon_head", top: int, gradients: int) -> int:
-        """Bytes of workspace for the call, which are there then.  The library cuts the call by these and not by all that there is, so that
-        results do not depend on earlier calls."""
+    def _fit(self, head: "binding.muon_head", top: int, gradients: int, scores: bool = False) -> int:
+        """Bytes of workspace for the call (scores: of ``log_probs``), which are there then.  The library cuts the call by these and not by all
+        that there is, so that results do not depend on earlier calls."""
         # what the size goes by: the pointers for their alignment only
         key = (head.tokens, head.vocab, head.width, head.hidden_stride, head.weight_stride, head.dtype, (head.hidden or 0) % 16,
-               (head.weight or 0) % 16, top, gradients)
+               (head.weight or 0) % 16, top, gradients, scores)
         need = self._sizes.get(key)
         if need is None:
-            need = binding.muon_head_workspace_bytes(head, top, gradients, self.max_workspace_bytes)
+            need = (binding.muon_log_probs_bytes(head, top, self.max_workspace_bytes) if scores else
+                    binding.muon_head_workspace_bytes(head, top, gradients, self.max_workspace_bytes))
             if len(self._sizes) > 1000:
                 self._sizes.clear()
             self._sizes[key] = need
@@ -114,15 +127,18 @@ class LossHead:
             raise MuonError(-1, f"token_scale: contiguous [{tokens}], not {tuple(token_scale.shape)}")
         return token_scale.data_ptr()
 
-    def _outputs(self, hidden, weight, gradients):
+    def _gradients(self, hidden, weight, gradients):
         """gradients: True, False, or the names of those wanted."""
         wanted = {True: ("hidden", "weight"), False: ()}.get(gradients, gradients) if isinstance(gradients, bool) else tuple(gradients)
         if not set(wanted) <= {"hidden", "weight"}:
             raise ValueError("gradients: True, False, or a sequence of 'hidden' and 'weight'")
-        tokens = hidden.shape[0]
-        loss, lse = torch.empty(2, tokens, dtype=torch.float32, device=self.device).unbind(0)
         dh = torch.empty(hidden.shape, dtype=hidden.dtype, device=self.device) if "hidden" in wanted else None
         dw = torch.empty(weight.shape, dtype=weight.dtype, device=self.device) if "weight" in wanted else None
+        return dh, dw
+
+    def _outputs(self, hidden, weight, gradients):
+        dh, dw = self._gradients(hidden, weight, gradients)
+        loss, lse = torch.empty(2, hidden.shape[0], dtype=torch.float32, device=self.device).unbind(0)
         return HeadResult(loss, lse, dh, dw), (1 if dh is not None else 0) | (2 if dw is not None else 0)
 
     @staticmethod
@@ -167,3 +183,60 @@ class LossHead:
                                  top, temperature, scale, *self._pointers(out), self.workspace.data_ptr(), need,
                                  stream_handle(self.device))
         return out
+
+    def _targets(self, targets: Optional[torch.Tensor], tokens: int):
+        """(address, bytes of an index); no targets: (0, 8)."""
+        if targets is None:
+            return 0, 8
+        if targets.shape != (tokens,) or not targets.is_contiguous():
+            raise MuonError(-1, f"targets: contiguous [{tokens}], not {tuple(targets.shape)}")
+        return targets.data_ptr(), _index_bytes(targets, "targets")
+
+    def log_probs(self, hidden: torch.Tensor, weight: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0,
+                  temperature: float = 1.0) -> TokenScores:
+        """Log probabilities of ``targets`` (negative: no token, 0) under the softmax of ``hidden @ weight.T / temperature``, the entropy of
+        each row's whole distribution, and its ``top`` (up to 64) most likely entries with their log probabilities, the likeliest first, equal
+        ones by index."""
+        head = self._head(hidden, weight)
+        self._here(hidden=hidden, weight=weight, targets=targets)
+        outside_autograd("LossHead.log_probs", hidden.requires_grad or weight.requires_grad)
+        tokens = hidden.shape[0]
+        at, size = self._targets(targets, tokens)
+        with on(self.device):
+            need = self._fit(head, top, 0, scores=True)
+            values = torch.empty(4, tokens, dtype=torch.float32, device=self.device).unbind(0)
+            out = TokenScores(None if targets is None else values[0], *values[1:],
+                              torch.empty(tokens, top, dtype=torch.int64, device=self.device) if top else None,
+                              torch.empty(tokens, top, dtype=torch.float32, device=self.device) if top else None)
+            binding.muon_log_probs(head, at, size, top, temperature, *(0 if t is None else t.data_ptr() for t in out),
+                                   self.workspace.data_ptr(), need, stream_handle(self.device))
+        return out
+
+    def log_probs_backward(self, hidden: torch.Tensor, weight: torch.Tensor, targets: Optional[torch.Tensor], scores: TokenScores,
+                           d_log_prob: Optional[torch.Tensor], d_entropy: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                           gradients=True) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+        """(d_hidden, d_weight) of ``(d_log_prob * log_prob + d_entropy * entropy).sum()`` with the ``scores`` that ``log_probs`` gave for the
+        same hidden states, weight, targets and temperature.  ``d_log_prob`` is None without targets, ``d_entropy`` None for 0."""
+        head = self._head(hidden, weight)
+        self._here(hidden=hidden, weight=weight, targets=targets, d_log_prob=d_log_prob, d_entropy=d_entropy, lse=scores.lse)
+        outside_autograd("LossHead.log_probs_backward", hidden.requires_grad or weight.requires_grad)
+        tokens = hidden.shape[0]
+        at, size = self._targets(targets, tokens)
+        if (targets is None) != (d_log_prob is None):
+            raise MuonError(-1, "targets and d_log_prob: both or neither")
+        if d_log_prob is None and d_entropy is None:
+            raise MuonError(-1, "d_log_prob or d_entropy")
+        given = []
+        for name, t in (("lse", scores.lse), ("lse_rest", scores.lse_rest), ("entropy", scores.entropy), ("d_log_prob", d_log_prob),
+                        ("d_entropy", d_entropy)):
+            if t is not None and (t.shape != (tokens,) or not t.is_contiguous()):
+                raise MuonError(-1, f"{name}: contiguous [{tokens}], not {tuple(t.shape)}")
+            if t is not None and t.dtype != torch.float32:
+                raise MuonError(-2, f"{name}: fp32, not {t.dtype}")
+            given.append(0 if t is None else t.data_ptr())
+        with on(self.device):
+            dh, dw = self._gradients(hidden, weight, gradients)
+            need = self._fit(head, 1, (1 if dh is not None else 0) | (2 if dw is not None else 0))
+            binding.muon_log_probs_backward(head, at, size, temperature, *given, *(0 if t is None else t.data_ptr() for t in (dh, dw)),
+                                            self.workspace.data_ptr(), need, stream_handle(self.device))
+        return dh, dw

@@ -1,0 +1,344 @@
+"""Log probabilities, entropies, alternatives and their gradients through the HIP library against the fp64 oracle on the same inputs.
+
+Tolerances.  A logit in the sums is an fp32 sum of D products: its error is below d = (4 + sqrt(D)) 2^-23 A with A = sum_d |h_d w_d| / tau, the
+largest of the row.  lse carries d and a few roundings of its own size; log probabilities that and their own rounding, for their logits are
+summed in double.  The entropy's derivative is -p (log p + entropy), whose magnitudes add up to 2 H at most: 2 H (d + 2^-20), 2^-20 for
+the exponentials, plus 2^-20 (1 + H + log V) for the sums.  dz = g ([v = y] - p) - h p (log p + H): p carries 2 d (its logit's error and lse's),
+log p + H that and the entropy's; bf16 rounds dz once, 2^-8 relative, and the result once more (2^-8); sums of K products add (8 + sqrt K) 2^-23 of their magnitudes.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import score_oracle as so
+from tests.head_routes import ROUTES
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def losses():
+    from paper_2502_16982_amd import losses as l
+    return l
+
+
+def as64(t):
+    return None if t is None else t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def make(tokens, vocab, width, dtype, seed=0, pull=6.0):
+    g = torch.Generator().manual_seed(seed)
+    w = torch.randn(vocab, width, generator=g) * 0.05
+    y = torch.randint(vocab, (tokens,), generator=g)
+    h = torch.randn(tokens, width, generator=g)
+    h += torch.rand(tokens, 1, generator=g) * pull * w[y] / (0.05 ** 2 * width)
+    return h.to(DT[dtype]).cuda(), w.to(DT[dtype]).cuda(), y.cuda(), g
+
+
+def errors(h64, w64, tau, lse, entropy):
+    """(logit's, lse's, entropy's) per token."""
+    live = np.isfinite(h64).all(axis=1)
+    mag = np.abs(np.where(live[:, None], h64, 0.0)) @ np.abs(np.where(np.isfinite(w64), w64, 0.0)).T
+    d = (4 + np.sqrt(h64.shape[1])) * 2.0 ** -23 * mag.max(axis=1) / tau + 2.0 ** -21
+    big = np.nan_to_num(entropy)
+    return d, d + 2.0 ** -22 * np.abs(np.nan_to_num(lse)), 2 * big * (d + 2.0 ** -20) + 2.0 ** -20 * (1 + big + np.log(w64.shape[0]))
+
+
+def check(s, h, w, y, top=0, tau=1.0, live=None):
+    h64, w64 = as64(h), as64(w)
+    want = so.scores(h64, w64, None if y is None else y.cpu().numpy(), top, tau)
+    live = np.isfinite(h64).all(axis=1) if live is None else live
+    d, lse_err, h_err = errors(h64, w64, tau, want["lse"], want["entropy"])
+    assert (np.abs(as64(s.lse) - want["lse"])[live] <= lse_err[live]).all()
+    assert (np.abs(as64(s.entropy) - want["entropy"])[live] <= (h_err + 2.0 ** -23 * want["entropy"])[live]).all()
+    assert (as64(s.entropy)[live] >= 0).all()
+    if y is not None:
+        lp = as64(s.log_prob)
+        assert np.array_equal(np.isnan(lp)[live], np.isnan(want["log_prob"])[live])
+        ok = live & ~np.isnan(want["log_prob"])
+        assert (np.abs(lp - want["log_prob"])[ok] <= (lse_err + 2.0 ** -22 * np.abs(want["log_prob"]))[ok]).all()
+        assert (lp[ok] <= 0).all()
+    if top:
+        assert np.array_equal(s.top_index.cpu().numpy()[live], want["top_index"][live])
+        got, ref = as64(s.top_log_prob)[live], want["top_log_prob"][live]
+        assert (got <= 0).all() and (np.abs(got - ref) <= lse_err[live][:, None] + 2.0 ** -22 * np.abs(ref)).all()
+    return want
+
+
+def check_backward(grads, s, h, w, y, dl, de, tau=1.0, dtype="bf16"):
+    h64, w64 = as64(h), as64(w)
+    dl64, de64 = as64(dl), as64(de)
+    want = so.scores(h64, w64, None if y is None else y.cpu().numpy(), 0, tau, dl64, de64)
+    d, _, h_err = errors(h64, w64, tau, want["lse"], want["entropy"])
+    tokens, vocab = len(h64), len(w64)
+    yy = np.full(tokens, -1) if y is None else y.cpu().numpy()
+    g = np.where((yy >= 0) & (yy < vocab), 0.0 if dl64 is None else dl64, 0.0)
+    e = np.zeros(tokens) if de64 is None else de64
+    kept = (g != 0) | (e != 0)
+    with np.errstate(all="ignore"):
+        logp = h64 @ w64.T / tau - want["lse"][:, None]
+        p = np.exp(logp)
+        bend = np.where(p == 0, 0.0, p * np.abs(logp + want["entropy"][:, None]))
+    p, bend = np.where(kept[:, None], p, 0.0), np.where(kept[:, None], bend, 0.0)
+    dz, g, e = np.abs(want["d_logits"]), np.abs(g)[:, None], np.abs(e)[:, None]
+    spread = dz + 2 * g * p + 2 * e * bend                                 # where its parts cancel, their errors stay
+    loose = spread * 2 * d[:, None] + e * p * (2 * d + np.nan_to_num(h_err))[:, None]
+    h0 = np.where(kept[:, None], h64, 0.0)
+    for got, ref, left, b, k in ((grads[0], want["d_hidden"], True, np.abs(w64), vocab), (grads[1], want["d_weight"], False, np.abs(h0), tokens)):
+        if got is None:
+            continue
+        got = as64(got)
+        assert np.isfinite(got).all()
+        err = loose + spread * (8 + np.sqrt(k)) * 2.0 ** -23 + (dz * 2.0 ** -8 if dtype == "bf16" else 0.0)
+        bound = (err @ b if left else err.T @ b) / tau + np.abs(ref) * (2.0 ** -7.99 if dtype == "bf16" else 2.0 ** -23) + 1e-37
+        assert (np.abs(got - ref) <= bound).all(), np.max(np.abs(got - ref) / bound)
+        noise = np.linalg.norm((loose @ b if left else loose.T @ b) / tau)
+        assert np.linalg.norm(got - ref) <= (5e-3 if dtype == "bf16" else 1e-5) * np.linalg.norm(ref) + noise
+
+
+SIZES = [(1, 1, 1, 1), (1, 7, 8, 7), (3, 129, 24, 2), (17, 1000, 64, 5), (64, 511, 136, 64), (65, 257, 33, 8), (130, 1027, 100, 0), (257, 130, 256, 3),
+         (300, 2050, 520, 16), (2, 64, 16, 64), (5, 72, 40, 64), (9, 4099, 16, 33)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sizes", SIZES, ids=str)
+def test_sizes(losses, sizes, dtype):
+    tokens, vocab, width, top = sizes
+    h, w, y, g = make(tokens, vocab, width, dtype)
+    y = torch.where(torch.rand(tokens, generator=g).cuda() < 0.2, -1, y)
+    dl, de = torch.randn(tokens, generator=g).cuda(), torch.randn(tokens, generator=g).cuda() * 0.3
+    for tau in (1.0, 0.7):
+        head = losses.LossHead(tokens, vocab, width, DT[dtype])
+        s = head.log_probs(h, w, y, top=top, temperature=tau)
+        check(s, h, w, y, top, tau)
+        check_backward(head.log_probs_backward(h, w, y, s, dl, de, temperature=tau), s, h, w, y, dl, de, tau, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_forms(losses, dtype):
+    """int32 targets, none, one gradient alone, indexes beyond the vocabulary, no entropy's gradient, neither's."""
+    h, w, y, g = make(70, 700, 96, dtype)
+    head = losses.LossHead(70, 700, 96, DT[dtype])
+    dl, de = torch.randn(70, generator=g).cuda(), torch.randn(70, generator=g).cuda()
+    y[3], y[4], y[5] = -100, 700, 1 << 40
+    s = head.log_probs(h, w, y, top=3)
+    want = check(s, h, w, y, 3)
+    assert np.isnan(want["log_prob"][4:6]).all() and float(s.log_prob[3]) == 0.0
+    small = torch.where(y > 2 ** 31 - 1, 2 ** 31 - 1, y).to(torch.int32)
+    again = head.log_probs(h, w, small, top=3)
+    assert all(torch.equal(a.nan_to_num(9.0), b.nan_to_num(9.0)) for a, b in zip(s, again))
+    none = head.log_probs(h, w)
+    assert none.log_prob is None and none.top_index is None and torch.equal(none.entropy, s.entropy) and torch.equal(none.lse, s.lse)
+    both = head.log_probs_backward(h, w, y, s, dl, de)
+    check_backward(both, s, h, w, y, dl, de, 1.0, dtype)
+    dh, nothing = head.log_probs_backward(h, w, y, s, dl, de, gradients=("hidden",))
+    assert nothing is None and torch.equal(dh, both[0])
+    nothing, dw = head.log_probs_backward(h, w, small, s, dl, de, gradients=("weight",))
+    assert nothing is None and torch.equal(dw, both[1])
+    check_backward(head.log_probs_backward(h, w, y, s, dl), s, h, w, y, dl, None, 1.0, dtype)
+    check_backward(head.log_probs_backward(h, w, None, s, None, de), s, h, w, None, None, de, 1.0, dtype)
+    zero = head.log_probs_backward(h, w, y, s, torch.zeros_like(dl))
+    assert (zero[0] == 0).all() and (zero[1] == 0).all()
+    assert head.log_probs_backward(h, w, y, s, dl, de, gradients=False) == (None, None)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_ties(losses, dtype):
+    """Equal logits go by index: rows of zeros, weight rows that come twice, all of them alike."""
+    h, w, y, _ = make(40, 5000, 64, dtype)
+    h[7] = 0
+    w[1000:2000] = w[:1000]
+    w[4000] = w[999]
+    head = losses.LossHead(40, 5000, 64, DT[dtype])
+    for top in (1, 8, 50):
+        s = head.log_probs(h, w, y, top=top)
+        assert s.top_index[7].tolist() == list(range(top))
+        if dtype == "bf16":                                                # sums of products of bf16 in double are exact here
+            check(s, h, w, y, top)
+    w[:] = w[5]
+    s = head.log_probs(h, w, y, top=20)
+    assert (s.top_index == torch.arange(20, device="cuda")).all()
+    assert ((s.entropy - np.log(5000)).abs() <= 2.0 ** -19 * 10).all() and ((s.log_prob + np.log(5000)).abs() <= 2.0 ** -19 * 10).all()
+
+
+def test_alternatives_that_lie_together(losses):
+    """The largest logits in neighbouring entries, whose groups have to be looked through."""
+    h, w, y, g = make(33, 3000, 64, "bf16")
+    for t in range(33):
+        at = (t * 89) % 2900
+        w[at:at + 40] = (h[t].float() * (0.2 + 0.002 * torch.randperm(40, generator=g).cuda()[:, None])).to(torch.bfloat16)
+    head = losses.LossHead(33, 3000, 64)
+    for top in (1, 5, 32, 64):
+        check(head.log_probs(h, w, y, top=top), h, w, y, top)
+
+
+def test_alternatives_that_few_threads_hold(losses):
+    """More groups above what the threads' own largest bound than the list holds: 71 of each 256 groups, 64 times."""
+    vocab, width = 1 << 19, 8
+    row = torch.arange(vocab)
+    group = row // 64 * 2 + row // 4 % 2
+    g = torch.Generator().manual_seed(5)
+    value = torch.rand(vocab, generator=g) + 3.0 * (group % 256 < 71)
+    w = torch.zeros(vocab, width)
+    w[:, 0] = value
+    h = torch.zeros(3, width)
+    h[:, 0] = torch.tensor([1.0, 2.0, -1.0])
+    head = losses.LossHead(3, vocab, width, torch.float32)
+    s = head.log_probs(h.cuda(), w.cuda(), None, top=64)
+    order = value.double().sort(descending=True, stable=True).indices
+    assert torch.equal(s.top_index[0].cpu(), order[:64]) and torch.equal(s.top_index[1].cpu(), order[:64])
+    assert torch.equal(s.top_index[2].cpu(), value.double().sort(stable=True).indices[:64])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_that_are_not_finite(losses, dtype):
+    """A token's hidden state that is NaN: its own results only, and no gradient of the weight unless it has one itself."""
+    h, w, y, g = make(50, 900, 72, dtype)
+    bad = h.clone()
+    bad[11], bad[30, 5], bad[49, 71] = float("nan"), float("inf"), float("nan")
+    rows = [11, 30, 49]
+    keep = np.ones(50, dtype=bool)
+    keep[rows] = False
+    head = losses.LossHead(50, 900, 72, DT[dtype])
+    s, clean = head.log_probs(bad, w, y, top=5), head.log_probs(h, w, y, top=5)
+    check(s, bad, w, y, 5, live=keep)
+    for a, b in zip(s, clean):
+        assert torch.equal(a[torch.from_numpy(keep).cuda()], b[torch.from_numpy(keep).cuda()])
+    assert s.lse[11].isnan() and s.log_prob[11].isnan() and s.entropy[11].isnan()
+    assert ((s.top_index >= 0) & (s.top_index < 900)).all()
+    dl, de = torch.randn(50, generator=g).cuda(), torch.randn(50, generator=g).cuda()
+    dl[rows], de[rows] = 0.0, 0.0
+    dh, dw = head.log_probs_backward(bad, w, y, s, dl, de)
+    want = head.log_probs_backward(h, w, y, clean, dl, de)
+    assert torch.equal(dw, want[1]) and torch.equal(dh, want[0]) and (dh[rows] == 0).all()
+
+
+def test_logits_of_minus_infinity(losses):
+    """Masked vocabulary entries: weights so low that their logits are -inf, whole blocks of them and single ones."""
+    h, w, y, g = make(20, 1500, 16, "f32")
+    h[:, 0], w[:, 0] = 2.0, 0.0
+    w[128:512, 0], w[700, 0], w[1499, 0] = -3e38, -3e38, -3e38
+    y = torch.where((y >= 128) & (y < 512), 5, y)
+    y[0] = 700
+    head = losses.LossHead(20, 1500, 16, torch.float32)
+    s = head.log_probs(h, w, y, top=64)
+    z = h.double().cpu() @ w.double().cpu().T
+    z[:, 128:512], z[:, 700], z[:, 1499] = -torch.inf, -torch.inf, -torch.inf
+    logp = torch.log_softmax(z, 1)
+    assert float(s.log_prob[0]) < -1e38 and not s.entropy.isnan().any()
+    assert (s.log_prob[1:].double().cpu() - logp.gather(1, y.cpu()[:, None])[1:, 0]).abs().nan_to_num(0.0, 0.0, 0.0).max() <= 1e-5
+    assert (s.entropy.double().cpu() - torch.special.entr(logp.exp()).sum(1)).abs().max() <= 1e-4
+    assert torch.equal(s.top_index.cpu(), logp.topk(64).indices)
+    y[0] = 3
+    s = head.log_probs(h, w, y)
+    de = torch.ones(20, device="cuda")
+    dh, dw = head.log_probs_backward(h[:, :], w, y, s, de, de)
+    assert not dw.isnan().any() and (dw[128:512] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens,vocab,width", ROUTES)
+def test_every_form_of_launch(losses, tokens, vocab, width, dtype):
+    """Sizes that take each form of tile, against 64 bits on the GPU."""
+    h, w, y, g = make(tokens, vocab, width, dtype, pull=9.0)
+    dl, de = torch.randn(tokens, generator=g).cuda() / tokens, torch.full((tokens,), 0.1 / tokens, device="cuda")
+    head = losses.LossHead(tokens, vocab, width, DT[dtype])
+    s = head.log_probs(h, w, y, top=4, temperature=1.3)
+    dh, dw = head.log_probs_backward(h, w, y, s, dl, de, temperature=1.3)
+    logp = torch.log_softmax(h.double() @ w.double().T.contiguous() / 1.3, 1)
+    entropy = torch.special.entr(logp.exp()).sum(1)
+    best = logp.topk(4)
+    assert torch.equal(s.top_index, best.indices)
+    for got, want in ((s.log_prob, logp.gather(1, y[:, None])[:, 0]), (s.entropy, entropy), (s.top_log_prob, best.values)):
+        assert (got.double() - want).norm() <= 2e-6 * want.norm()
+    p = logp.exp()
+    dz = -p * (dl.double()[:, None] + de.double()[:, None] * (logp + entropy[:, None]))
+    dz[torch.arange(tokens), y] += dl.double()
+    for got, want in ((dh, dz @ w.double() / 1.3), (dw, dz.T.contiguous() @ h.double() / 1.3)):
+        assert (got.double() - want).norm() <= (5e-3 if dtype == "bf16" else 1e-5) * want.norm()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pieces(losses, dtype):
+    """A limited workspace gives the same scores, in pieces of tokens; the weight's gradient is summed over them in fp32."""
+    h, w, y, g = make(1000, 1300, 80, dtype)
+    whole = losses.LossHead(1000, 1300, 80, DT[dtype])
+    few = losses.LossHead(1000, 1300, 80, DT[dtype], max_workspace_bytes=1)
+    a, b = whole.log_probs(h, w, y, top=6), few.log_probs(h, w, y, top=6)
+    check(b, h, w, y, 6)
+    assert torch.equal(a.top_index, b.top_index)
+    dl, de = torch.randn(1000, generator=g).cuda(), torch.randn(1000, generator=g).cuda()
+    check_backward(few.log_probs_backward(h, w, y, b, dl, de), b, h, w, y, dl, de, 1.0, dtype)
+    assert few.workspace.numel() < whole.workspace.numel()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides_and_alignment(losses, dtype):
+    h, w, y, g = make(60, 500, 64, dtype)
+    wide, tall = torch.zeros(60, 101, dtype=DT[dtype], device="cuda"), torch.zeros(500, 99, dtype=DT[dtype], device="cuda")
+    wide[:, 3:67], tall[:, 1:65] = h, w
+    head = losses.LossHead(60, 500, 64, DT[dtype])
+    dl = torch.randn(60, generator=g).cuda()
+    a, b = head.log_probs(h, w, y, top=4), head.log_probs(wide[:, 3:67], tall[:, 1:65], y, top=4)
+    assert all(torch.equal(x, z) for x, z in zip(a, b))
+    for x, z in zip(head.log_probs_backward(h, w, y, a, dl, dl), head.log_probs_backward(wide[:, 3:67], tall[:, 1:65], y, b, dl, dl)):
+        assert torch.equal(x, z)
+
+
+def test_beside_the_losses(losses):
+    """One LossHead for cross entropy, scores and their gradients in turn; the log probabilities are minus its loss, its gradients those of it."""
+    h, w, y, g = make(200, 3000, 128, "bf16")
+    y[::7] = -1
+    head = losses.LossHead(200, 3000, 128)
+    scale = torch.rand(200, generator=g).cuda()
+    ce = head.cross_entropy(h, w, y, token_scale=scale)
+    s = head.log_probs(h, w, y, top=2)
+    again = head.cross_entropy(h, w, y, token_scale=scale)
+    dh, dw = head.log_probs_backward(h, w, y, s, -scale)
+    assert torch.equal(ce.d_weight, again.d_weight) and torch.equal(ce.loss, again.loss)
+    assert (ce.loss + s.log_prob).abs().max() <= 1e-5 and (ce.lse - s.lse).abs().max() <= 1e-5
+    for a, b in ((dh, ce.d_hidden), (dw, ce.d_weight)):
+        assert (a.float() - b.float()).norm() <= 5e-3 * b.float().norm()
+
+
+def test_streams_and_capture(losses):
+    h, w, y, g = make(90, 2100, 96, "bf16")
+    dl, de = torch.randn(90, generator=g).cuda(), torch.randn(90, generator=g).cuda()
+    head = losses.LossHead(90, 2100, 96)
+
+    def both(h, y):
+        s = head.log_probs(h, w, y, top=5)
+        return [*s, *head.log_probs_backward(h, w, y, s, dl, de)]
+
+    want = both(h, y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        there = both(h, y)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(want, there))
+    hold_h, hold_y = h.clone(), y.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both(hold_h, hold_y)
+    for seed in range(3):
+        h2, _, y2, _ = make(90, 2100, 96, "bf16", seed=20 + seed)
+        hold_h.copy_(h2)
+        hold_y.copy_(y2)
+        eager = both(h2, y2)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, eager))
+
+
+def test_no_tokens(losses):
+    h, w, y, _ = make(4, 300, 32, "bf16")
+    head = losses.LossHead(4, 300, 32)
+    s = head.log_probs(h[:0], w, y[:0], top=3)
+    assert s.log_prob.shape == (0,) and s.top_index.shape == (0, 3)
+    dh, dw = head.log_probs_backward(h[:0], w, y[:0], s, s.log_prob)
+    assert dh.shape == (0, 32) and (dw == 0).all()
