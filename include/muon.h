@@ -375,7 +375,7 @@ int muon_distill(const muon_head* head, const void* index, int32_t index_bytes, 
  * A token without target (negative) has log_prob 0 and none of its gradient; one of vocab or more makes log_prob NaN and gives none; both have
  * their entropy and alternatives all the same.  A token both of whose gradients are 0 reaches nothing, whatever its hidden state holds (d_weight;
  * its row of d_hidden is zero for finite W).  Alternatives are in falling order of their logits as summed in double, equal ones by index, chosen
- * among the top + 8 that fp32 sums find largest (and whatever is as large as the last of these); logits that are NaN come last.
+ * among the top + 4 that fp32 sums find largest (and whatever is as large as the last of these); logits that are NaN come last.
  * Types, precision, pieces of tokens and what may run when are those of muon_cross_entropy; the log probabilities' own logits are summed in
  * double, dz is rounded to bf16 once.  lse_rest is what fp32 leaves of lse.
  */

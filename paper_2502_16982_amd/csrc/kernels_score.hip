@@ -32,6 +32,45 @@ __device__ __forceinline__ long long target_at(const ScoreTarget& t, long long i
   return t.index64 ? static_cast<const long long*>(t.index)[i] : (long long)static_cast<const int*>(t.index)[i];
 }
 
+// f over a wave's lanes, in all of them, with moves between registers only: rotations within 16 lanes, then exchanges of rows of 16 and 32.
+template <typename T>
+struct Words {
+  unsigned w[sizeof(T) / 4];
+};
+template <int CTRL, typename T>
+__device__ __forceinline__ T rotated(T x) {
+  Words<T> v = __builtin_bit_cast(Words<T>, x);
+#pragma unroll
+  for (auto& w : v.w) w = __builtin_amdgcn_update_dpp(0u, w, CTRL, 0xf, 0xf, true);
+  return __builtin_bit_cast(T, v);
+}
+template <bool BY32, typename T, typename F>
+__device__ __forceinline__ T across(T x, F&& f) {
+  const Words<T> v = __builtin_bit_cast(Words<T>, x);
+  Words<T> a, b;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 4; ++i) {
+    const auto both = BY32 ? __builtin_amdgcn_permlane32_swap(v.w[i], v.w[i], false, false) : __builtin_amdgcn_permlane16_swap(v.w[i], v.w[i], false, false);
+    a.w[i] = both[0];
+    b.w[i] = both[1];
+  }
+  return f(__builtin_bit_cast(T, a), __builtin_bit_cast(T, b));
+}
+template <typename T, typename F>
+__device__ __forceinline__ T wave_all(T x, F&& f) {
+  x = f(x, rotated<0x128>(x));
+  x = f(x, rotated<0x124>(x));
+  x = f(x, rotated<0x122>(x));
+  x = f(x, rotated<0x121>(x));
+  return across<true>(across<false>(x, f), f);
+}
+struct Add {
+  template <typename T>
+  __device__ __forceinline__ T operator()(T x, T y) const {
+    return x + y;
+  }
+};
+
 // <a, b> over `width` elements by a whole wave, in double.
 template <bool F32>
 __device__ __forceinline__ double row_dot64(const void* a, long long a_at, const void* b, long long b_at, long long width) {
@@ -41,9 +80,7 @@ __device__ __forceinline__ double row_dot64(const void* a, long long a_at, const
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum = fma((double)x.v[e], (double)y.v[e], sum);
   }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-  return sum;
+  return wave_all(sum, Add{});
 }
 
 // ---- forward: the product's epilogue ----
@@ -54,7 +91,7 @@ __device__ __forceinline__ int place_row(int place, int half) { return 32 * (pla
 
 template <int B, int S, bool BEST>
 __device__ __forceinline__ void score_tile(const HeadOperand& weight, const HeadOperand& hidden, const HeadTiles& g, float unit, ScoreStats* stats,
-                                           long long stats_pitch, ScoreBest* best, long long best_pitch, long long row0, long long col0,
+                                           ScoreBest* best, long long row0, long long col0,
                                            unsigned char* smem) {
   using T = Tile<B, B, false, false, S>;
   T tile;
@@ -62,12 +99,14 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
   const int fr = tile.lane & 31, fh = tile.lane >> 5;
   const long long v0 = row0 + tile.wm * T::WM;
   const int there = (int)(weight.rows - v0 < T::WM ? weight.rows - v0 : T::WM);      // rows of the wave's that there are
-  auto work = [&](auto masked) {
-    auto z = [&](int i, int j, int v) {
-      const float x = tile.acc[i][j][v];
-      return decltype(masked)::value && 32 * i + 8 * (v / 4) + 4 * fh + v % 4 >= there ? -INFINITY : x;
-    };
-    float top[T::FN];
+  auto row = [&](int i, int v) { return 32 * i + 8 * (v / 4) + 4 * fh + v % 4; };
+  // in LDS: what two waves tell each other, then what leaves, a token's neighbouring entries in whole lines
+  constexpr int kGroups = B / kScoreGroup, kBlocks = B / kHeadGrain;
+  float* notes = reinterpret_cast<float*>(smem);
+  ScoreStats* sheet = reinterpret_cast<ScoreStats*>(smem + 2048);                    // [column][block]
+  ScoreBest* image = reinterpret_cast<ScoreBest*>(smem + 2048 + B * kBlocks * 16);   // [column][group]
+  float top[T::FN];
+  auto find_top = [&](auto masked) {             // MASKED: not all rows of the wave's are there
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
       top[j] = -INFINITY;
@@ -79,7 +118,8 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
           for (int v = 0; v < 16; ++v) {
-            const float x = z(2 * s + u, j, v);
+            float x = tile.acc[2 * s + u][j][v];
+            if (decltype(masked)::value && row(2 * s + u, v) >= there) x = -INFINITY;
             if constexpr (BEST) {
               second = __builtin_amdgcn_fmed3f(first, second, x);
               place = x > first ? 16 * u + v : place;
@@ -89,23 +129,24 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
           __builtin_amdgcn_sched_barrier(0);
         }
         top[j] = fmaxf(top[j], first);
-        if constexpr (BEST) {
-          const long long token = col0 + tile.wn * T::WN + 32 * j + fr, group = (v0 / 64 + s) * 2 + fh;
-          if (token < hidden.rows && 64 * s < there)
-            best[token * best_pitch + group] = ScoreBest{first, (__float_as_uint(second) & ~31u) | (unsigned)place};
-        }
+        if constexpr (BEST)
+          image[(tile.wn * T::WN + 32 * j + fr) * kGroups + (tile.wm * T::WM / 64 + s) * 2 + fh] =
+              ScoreBest{first, (__float_as_uint(second) & ~31u) | (unsigned)place};
       }
       top[j] = fmaxf(top[j], __shfl_xor(top[j], 32, 64));
     }
-    float* notes = reinterpret_cast<float*>(smem);
-    if constexpr (B == 128) {                    // two waves share a block of statistics
+  };
+  if (there >= T::WM) find_top(std::false_type{});
+  else find_top(std::true_type{});
+  if constexpr (B == 128) {                      // two waves share a block of statistics
 #pragma unroll
-      for (int j = 0; j < T::FN; ++j) notes[tile.wm * 128 + tile.wn * 64 + 32 * j + fr] = top[j];
-      __syncthreads();
+    for (int j = 0; j < T::FN; ++j) notes[tile.wm * 128 + tile.wn * 64 + 32 * j + fr] = top[j];
+    __syncthreads();
 #pragma unroll
-      for (int j = 0; j < T::FN; ++j) top[j] = fmaxf(top[j], notes[(tile.wm ^ 1) * 128 + tile.wn * 64 + 32 * j + fr]);
-    }
-    float sums[T::FN], slopes[T::FN];
+    for (int j = 0; j < T::FN; ++j) top[j] = fmaxf(top[j], notes[(tile.wm ^ 1) * 128 + tile.wn * 64 + 32 * j + fr]);
+  }
+  float sums[T::FN], slopes[T::FN];
+  auto take_powers = [&](auto masked) {
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
       top[j] = top[j] == -INFINITY ? 0.f : unit * top[j];
@@ -116,7 +157,9 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
         for (int q = 0; q < 4; ++q) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float y = fmaf(unit, z(i, j, 4 * q + e), -top[j]), x = __builtin_amdgcn_exp2f(y);
+            const float y = fmaf(unit, tile.acc[i][j][4 * q + e], -top[j]);
+            float x = __builtin_amdgcn_exp2f(y);
+            if (decltype(masked)::value && row(i, 4 * q + e) >= there) x = 0.f;
             sum += x;
             slope = fmaf(x, fmaxf(y, kFarBelow), slope);
           }
@@ -131,37 +174,51 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
         }
       }
     }
-    if constexpr (B == 128) __syncthreads();
-#pragma unroll
-    for (int j = 0; j < T::FN; ++j) {
-      const int c = tile.wn * T::WN + 32 * j + fr;
-      if constexpr (B == 128) {
-        sums[j] += notes[256 + c];
-        slopes[j] += notes[384 + c];
-      }
-      if (fh == 0 && (B == 256 || tile.wm == 0) && v0 < weight.rows && col0 + c < hidden.rows)
-        stats[v0 / kHeadGrain * stats_pitch + col0 + c] = ScoreStats{top[j], sums[j], slopes[j], 0.f};
-    }
   };
-  if (weight.rows - row0 >= B) work(std::false_type{});              // (by tile, not by wave: both sides hold barriers)
-  else work(std::true_type{});
+  if (there >= T::WM) take_powers(std::false_type{});
+  else take_powers(std::true_type{});
+  if constexpr (B == 128) __syncthreads();
+#pragma unroll
+  for (int j = 0; j < T::FN; ++j) {
+    const int c = tile.wn * T::WN + 32 * j + fr;
+    if constexpr (B == 128) {
+      sums[j] += notes[256 + c];
+      slopes[j] += notes[384 + c];
+    }
+    if (fh == 0 && (B == 256 || tile.wm == 0)) sheet[c * kBlocks + (B == 256 ? tile.wm : 0)] = ScoreStats{top[j], sums[j], slopes[j], 0.f};
+  }
+  __syncthreads();
+  // 16 bytes per thread: a block's statistics, two groups
+  const long long blocks = (weight.rows + kHeadGrain - 1) / kHeadGrain;
+  for (int i = threadIdx.x; i < B * kBlocks; i += 256) {
+    const long long token = col0 + i / kBlocks, block = row0 / kHeadGrain + i % kBlocks;
+    if (token < hidden.rows && block < blocks) stats[token * blocks + block] = sheet[i];
+  }
+  if constexpr (BEST) {
+#pragma unroll
+    for (int i0 = 0; i0 < B * kGroups / 2; i0 += 256) {
+      const int i = i0 + threadIdx.x, pair = i % (kGroups / 2);
+      const long long token = col0 + i / (kGroups / 2), group = row0 / kScoreGroup + 2 * pair, groups = blocks * (kHeadGrain / kScoreGroup);
+      if (token < hidden.rows && group < groups)
+        *reinterpret_cast<u32x4*>(best + token * groups + group) = *reinterpret_cast<const u32x4*>(image + 2 * i);
+    }
+  }
 }
 
 template <int B, int S, bool BEST>
 __global__ __launch_bounds__(256, B == 128 && S == 2 ? 2 : 1) void score_logits_kernel(HeadOperand weight, HeadOperand hidden, HeadTiles g, float unit,
-                                                                             ScoreStats* __restrict__ stats, long long stats_pitch,
-                                                                             ScoreBest* __restrict__ best, long long best_pitch) {
+                                                                             ScoreStats* __restrict__ stats, ScoreBest* __restrict__ best) {
 #if defined(__HIP_DEVICE_COMPILE__)            // (the host's pass knows no buffer descriptors)
   extern __shared__ __align__(16) unsigned char smem[];
   const TileAt at = tile_at(g);
   long long row0 = (long long)at.m * B, col0 = (long long)at.n * B;
   if (B == 128 || at.quarter < 0) {
-    score_tile<B, S, BEST>(weight, hidden, g, unit, stats, stats_pitch, best, best_pitch, row0, col0, smem);
+    score_tile<B, S, BEST>(weight, hidden, g, unit, stats, best, row0, col0, smem);
   } else if constexpr (B == 256) {
     row0 += 128 * (at.quarter >> 1);
     col0 += 128 * (at.quarter & 1);
     if (row0 < weight.rows && col0 < hidden.rows)
-      score_tile<128, 4, BEST>(weight, hidden, g, unit, stats, stats_pitch, best, best_pitch, row0, col0, smem);
+      score_tile<128, 4, BEST>(weight, hidden, g, unit, stats, best, row0, col0, smem);
   }
 #endif
 }
@@ -175,52 +232,76 @@ __device__ __forceinline__ u64 key_of(float z, unsigned row) { return (u64)risin
 __device__ __forceinline__ unsigned key_row(u64 key) { return 0xffffffffu - (unsigned)key; }
 __device__ __forceinline__ float second_bound(unsigned w) { return __uint_as_float((int)w < 0 ? w & ~31u : w | 31u); }
 
-template <typename T, typename F>
-__device__ __forceinline__ T wave_all(T x, F&& f) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) x = f(x, __shfl_xor(x, off, 64));
-  return x;
-}
+constexpr int kPickGroups = 4096;                // groups whose keys stay in registers: all, up to 131072 vocabulary entries
+constexpr int kPickList = 256;
 
-template <bool F32>
-__global__ __launch_bounds__(256) void score_finish_kernel(ScoreTarget t, float inv_tau, float unit, const ScoreStats* __restrict__ stats, long long stats_pitch,
-                                                           long long blocks, const ScoreBest* __restrict__ best, long long groups, int top, HeadRows rows,
+// Bound by the chain of its memory accesses for a few tokens, by the rows whose logits are summed again for many.
+template <bool F32, bool PICK, int NT>
+__global__ __launch_bounds__(NT) void score_finish_kernel(ScoreTarget t, float inv_tau, float unit, const ScoreStats* __restrict__ stats, long long blocks,
+                                                           const ScoreBest* __restrict__ best, long long groups, int top, HeadRows rows,
                                                            long long vocab, ScoreOut out) {
-  constexpr int kPick = kScoreMaxTop + kScoreMargin, kList = 1024, kRows = kPick * 32;
-  __shared__ float tops[4];
-  __shared__ double sums[8];
-  __shared__ u64 list[kList], picked[kPick];
-  __shared__ double value[kRows];
-  __shared__ int row_of[kRows];
-  __shared__ int counts[3];
-  __shared__ u64 bound;
+  constexpr int NW = NT / 64, kPickKeys = kPickGroups / NT;
+  __shared__ float tops[NW];
+  __shared__ double sums[2 * NW];
+  __shared__ u64 bins[256], bound;               // PICK
+  __shared__ int counts[2];
+  extern __shared__ u64 dynamic[];               // PICK: a list of keys; logits and rows of the picks; the keys' seconds
   const long long token = blockIdx.x;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const auto larger = [](auto x, auto y) { return x > y ? x : y; };
-  const auto add = [](auto x, auto y) { return x + y; };
+
+  if constexpr (PICK) {
+    if (tid < 256) bins[tid] = 0;
+    if (tid < 2) counts[tid] = 0;
+    if (tid == 0) bound = 0;
+  }
+  // the groups' largest, on their way while the sums are joined
+  const ScoreBest* mine = best + token * groups;
+  ScoreBest held[kPickKeys];
+  if constexpr (PICK) {
+    static_for<0, kPickKeys>([&](auto n) {
+      constexpr int u = decltype(n)::value;
+      const long long g = tid + NT * u;
+      held[u] = g < groups ? mine[g] : ScoreBest{0.f, 0u};
+    });
+  }
 
   // lse and entropy: sums relative to the largest block's top, joined in double
   float m = -INFINITY, sum = 0.f, slope = 0.f;
-  for (long long b = tid; b < blocks; b += 256) {
-    const ScoreStats v = stats[b * stats_pitch + token];
-    if (v.sum == 0.f) continue;
-    const float now = fmaxf(m, v.top), down = m == -INFINITY ? 0.f : m - now, here = v.top - now, f = __builtin_amdgcn_exp2f(down), h = __builtin_amdgcn_exp2f(here);
-    slope = f * fmaf(sum, down, slope) + h * fmaf(v.sum, here, v.slope);
-    sum = f * sum + h * v.sum;
-    m = now;
+  for (long long b0 = tid; b0 < blocks; b0 += 4 * NT) {
+    ScoreStats v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = b0 + NT * u < blocks ? stats[token * blocks + b0 + NT * u] : ScoreStats{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (v[u].sum == 0.f) continue;
+      const float now = fmaxf(m, v[u].top), down = m == -INFINITY ? 0.f : m - now, here = v[u].top - now, f = __builtin_amdgcn_exp2f(down),
+                  h = __builtin_amdgcn_exp2f(here);
+      slope = f * fmaf(sum, down, slope) + h * fmaf(v[u].sum, here, v[u].slope);
+      sum = f * sum + h * v[u].sum;
+      m = now;
+    }
   }
+  // the given token's logit: here, or, with picks, beside theirs
+  const long long y = out.log_prob ? target_at(t, token) : -1;
+  const bool there = y >= 0 && y < vocab;
+  double given = 0.0;
+  if (!PICK && there && wave == NW - 1)
+    given = row_dot64<F32>(rows.hidden, token * rows.hidden_stride, rows.weight, y * rows.weight_stride, rows.width);
   const float wave_top = wave_all(m, larger);
   if (lane == 0) tops[wave] = wave_top;
-  if (tid < 3) counts[tid] = 0;
-  if (tid == 0) bound = 0;
   __syncthreads();
-  float all = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  float all = tops[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) all = fmaxf(all, tops[w]);
   if (all == -INFINITY) all = 0.f;
-  const double down = m == -INFINITY ? 0.0 : (double)m - (double)all, f = m == -INFINITY ? 0.0 : exp2(down);
-  const double s0 = wave_all(f * sum, add), e0 = wave_all(f * (slope + sum * down), add);
-  if (lane == 0) sums[wave] = s0, sums[4 + wave] = e0;
+  const double down = m == -INFINITY ? 0.0 : (double)m - (double)all, f = m == -INFINITY ? 0.0 : (double)__builtin_amdgcn_exp2f((float)down);
+  const double s0 = wave_all(f * sum, Add{}), e0 = wave_all(f * (slope + sum * down), Add{});
+  if (lane == 0) sums[wave] = s0, sums[NW + wave] = e0;
   __syncthreads();
-  const double mass = (sums[0] + sums[1]) + (sums[2] + sums[3]), tilt = (sums[4] + sums[5]) + (sums[6] + sums[7]);
+  double mass = 0.0, tilt = 0.0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) mass += sums[w], tilt += sums[NW + w];
   const double per = (double)inv_tau / (double)unit, l2 = log2(mass), lse = per * ((double)all + l2);
   if (tid == 0) {
     const double h = per * (l2 - tilt / mass);
@@ -233,117 +314,158 @@ __global__ __launch_bounds__(256) void score_finish_kernel(ScoreTarget t, float 
     const double d = (double)inv_tau * z - lse;
     return d > 0.0 ? 0.f : (float)d;
   };
-  const auto logit = [&](long long v) {
-    return row_dot64<F32>(rows.hidden, token * rows.hidden_stride, rows.weight, v * rows.weight_stride, rows.width);
-  };
-  if (out.log_prob && wave == 3) {
-    const long long y = target_at(t, token);
-    const float lp = y < 0 ? 0.f : y >= vocab ? __builtin_nanf("") : log_prob(logit(y));
-    if (lane == 0) out.log_prob[token] = lp;
-  }
-  if (!top) return;
+  if (out.log_prob && tid == NT - 64 && !(PICK && there)) out.log_prob[token] = y < 0 ? 0.f : y >= vocab ? __builtin_nanf("") : log_prob(given);
 
-  // the largest maxima: those of a thread's groups that reach what the threads' own largest ones bound from below
-  const ScoreBest* mine = best + token * groups;
-  const long long all_groups = groups;
-  const auto group_key = [&](long long g) -> u64 {
-    const ScoreBest b = mine[g];
-    const long long row = 64 * (g >> 1) + place_row((int)(b.second & 31u), (int)(g & 1));
-    return row < vocab ? key_of(b.z, (unsigned)row) : 0;
-  };
-  const auto there = [&](long long g) { return 64 * (g >> 1) + 4 * (g & 1) < vocab; };
-  u64 own = 0;
-  for (long long g = tid; g < all_groups; g += 256)
-    if (there(g)) own = larger(own, group_key(g));
-  list[tid] = own;
-  __syncthreads();
-  const int pick = top + kScoreMargin;
-  {
-    int rank = 0;
-    for (int i = 0; i < 256; ++i) rank += list[i] > own;
-    if (own && rank == pick - 1) bound = own;
-  }
-  __syncthreads();
-  const auto collect = [&](u64 from) {
-    for (long long g = tid; g < all_groups; g += 256) {
-      if (!there(g)) continue;
-      const u64 key = group_key(g);
-      if (key >= from && key) {
-        const int at = atomicAdd(&counts[0], 1);
-        if (at < kList) list[at] = key;
+  if constexpr (PICK) {
+    const int pick = top + kScoreMargin;
+    u64* list = dynamic;                                 // [kPickList]
+    u64* rank_of = list + kPickList;                     // [33 pick]
+    double* value = reinterpret_cast<double*>(rank_of + 33 * pick);    // [33 pick]
+    int* row_of = reinterpret_cast<int*>(value + 33 * pick);           // [33 pick]
+    int* open = row_of + 33 * pick;                      // [pick], rows whose groups are looked through
+    unsigned* seconds = reinterpret_cast<unsigned*>(open + pick);      // [kPickList], of the list
+    const auto key_at = [&](long long g, ScoreBest b) -> u64 {
+      const long long row = 64 * (g >> 1) + place_row((int)(b.second & 31u), (int)(g & 1));
+      return row < vocab && g < groups && 64 * (g >> 1) + 4 * (g & 1) < vocab ? key_of(b.z, (unsigned)row) : 0;
+    };
+    u64 keys[kPickKeys];
+    static_for<0, kPickKeys>([&](auto n) {
+      constexpr int u = decltype(n)::value;
+      keys[u] = key_at(tid + NT * u, held[u]);
+    });
+    // f(key, second) of each of the thread's groups
+    const auto each = [&](auto&& f) {
+      static_for<0, kPickKeys>([&](auto n) { f(keys[decltype(n)::value], held[decltype(n)::value].second); });
+      for (long long g = tid + NT * kPickKeys; g < groups; g += NT) {
+        const ScoreBest b = mine[g];
+        f(key_at(g, b), b.second);
       }
+    };
+    // A bound that at least `pick` keys reach: of the largest keys of 64 (for many picks 256) shares of the groups the pick-th largest.
+    u64 own = 0;
+    each([&](u64 key, unsigned) { own = larger(own, key); });
+    const bool coarse = pick <= 32;
+    const int shares = coarse ? 64 : 256;
+    if (own) atomicMax(&bins[tid % shares], own);
+    __syncthreads();
+    if (tid < shares) {
+      const u64 share = bins[tid];
+      int rank = 0;
+#pragma unroll 8
+      for (int i = 0; i < shares; ++i) rank += bins[i] > share;
+      if (share && rank == pick - 1) bound = share;
     }
-  };
-  collect(bound);
-  __syncthreads();
-  if (counts[0] > kList) {                               // a few threads hold most of the largest: the bound bit by bit instead
-    u64 from = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const u64 tried = from | 1ull << bit;
+    __syncthreads();
+    const auto collect = [&](u64 from) {
+      each([&](u64 key, unsigned second) {
+        if (key && key >= from) {
+          const int at = atomicAdd(&counts[0], 1);
+          if (at < kPickList) list[at] = key, seconds[at] = second;
+        }
+      });
+    };
+    collect(bound);
+    __syncthreads();
+    if (counts[0] > kPickList) {                         // a few shares hold most of the largest: the bound bit by bit instead
+      u64 from = 0;
+      for (int bit = 63; bit >= 0; --bit) {
+        const u64 tried = from | 1ull << bit;
+        __syncthreads();
+        if (tid == 0) counts[0] = 0;
+        __syncthreads();
+        int n = 0;
+        each([&](u64 key, unsigned) { n += key >= tried; });
+        n = wave_all(n, Add{});
+        if (lane == 0) atomicAdd(&counts[0], n);
+        __syncthreads();
+        if (counts[0] >= pick) from = tried;
+      }
       __syncthreads();
       if (tid == 0) counts[0] = 0;
       __syncthreads();
-      int n = 0;
-      for (long long g = tid; g < all_groups; g += 256) n += there(g) && group_key(g) >= tried;
-      n = wave_all(n, add);
-      if (lane == 0) atomicAdd(&counts[0], n);
+      collect(from);
       __syncthreads();
-      if (counts[0] >= pick) from = tried;
+    }
+    const int n = counts[0];
+    // the picks, by the threads that hold them: their rows, and all rows of a group whose second may be among the largest as well
+    u64 key = 0;
+    int rank = 0;
+    if (tid < n) {
+      key = list[tid];
+#pragma unroll 8
+      for (int k = 0; k < n; ++k) rank += list[k] > key;
+      if (rank == pick - 1) bound = key;
+    }
+    if (tid == 0 && n < pick) bound = 0;
+    const int have = n < pick ? n : pick;
+    __syncthreads();
+    if (tid < n && rank < pick) {
+      const unsigned row = key_row(key);
+      row_of[rank] = (int)row;
+      if (((u64)rising(__float_as_uint(second_bound(seconds[tid]))) << 32 | 0xffffffffu) >= bound) open[atomicAdd(&counts[1], 1)] = (int)row;
     }
     __syncthreads();
-    if (tid == 0) counts[0] = 0;
+    const int c = have + 32 * counts[1];
+    for (int i = have + tid; i < c; i += NT) {
+      const int row = open[(i - have) / 32], other = row / 64 * 64 + place_row((i - have) % 32, (row >> 2) & 1);
+      row_of[i] = other != row && other < vocab ? other : -1;
+    }
     __syncthreads();
-    collect(from);
-    __syncthreads();
-  }
-  const int n = counts[0];
-  for (int i = tid; i < n; i += 256) {
-    const u64 key = list[i];
-    int rank = 0;
-    for (int k = 0; k < n; ++k) rank += list[k] > key;
-    if (rank < pick) picked[rank] = key;
-  }
-  __syncthreads();
-  // their rows, and all rows of a group whose second may be among the largest as well
-  const int have = n < pick ? n : pick;
-  const u64 last = n >= pick ? picked[pick - 1] : 0;
-  if (tid < have) {
-    const unsigned row = key_row(picked[tid]);
-    const long long slab = row / 64, half = (row >> 2) & 1, g = 2 * slab + half;
-    row_of[tid] = (int)row;
-    if (((u64)rising(__float_as_uint(second_bound(mine[g].second))) << 32 | 0xffffffffu) >= last) {
-      const int at = have + 31 * atomicAdd(&counts[1], 1);
-      int k = 0;
-      for (int place = 0; place < 32; ++place) {
-        const long long other = 64 * slab + place_row(place, (int)half);
-        if (other != row) row_of[at + k++] = other < vocab ? (int)other : -1;
+    // the picks' logits and, behind them, the given token's; several rows of a wave at a time where there are more than waves
+    const int all_rows = c + there;
+    const auto sum_rows = [&](auto many) {
+      constexpr int U = decltype(many)::value;
+      for (int i0 = U * wave; i0 < all_rows; i0 += U * NW) {
+        double z[U];
+        long long at[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + u, row = i < c ? row_of[i] : i == c && there ? (int)y : -1;
+          z[u] = 0.0;
+          at[u] = (row < 0 ? 0 : row) * rows.weight_stride;
+        }
+        for (long long k = lane * 8; k < rows.width; k += 512) {
+          const Row8 x = load_row8<F32>(rows.hidden, token * rows.hidden_stride, k, rows.width);
+          Row8 w[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) w[u] = load_row8<F32>(rows.weight, at[u], k, rows.width);
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[u] = fma((double)x.v[e], (double)w[u].v[e], z[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          z[u] = wave_all(z[u], Add{});
+          const int i = i0 + u;
+          if (lane != 0 || i > c) continue;
+          if (i < c) {
+            value[i] = z[u];
+            const u64 bits = __double_as_longlong(z[u]);   // larger for larger logits, 0 for NaN and where there is no row
+            rank_of[i] = row_of[i] < 0 || z[u] != z[u] ? 0 : bits ^ ((u64)((long long)bits >> 63) | 0x8000000000000000ull);
+          } else if (there) {
+            out.log_prob[token] = log_prob(z[u]);
+          }
+        }
       }
-    }
-  }
-  __syncthreads();
-  const int c = have + 31 * counts[1];
-  for (int i = wave; i < c; i += 4) {
-    const int row = row_of[i];
-    const double z = row < 0 ? 0.0 : logit(row);
-    if (lane == 0) value[i] = z;
-  }
-  __syncthreads();
-  const auto order = [&](int i) -> u64 {                 // NaN below everything
-    const u64 bits = __double_as_longlong(value[i]);
-    return value[i] != value[i] ? 0 : bits ^ ((u64)((long long)bits >> 63) | 0x8000000000000000ull);
-  };
-  for (int i = tid; i < c; i += 256) {
-    if (row_of[i] < 0) continue;
-    const u64 own_order = order(i);
-    int rank = 0;
-    for (int k = 0; k < c; ++k) {
-      if (row_of[k] < 0) continue;
-      const u64 o = order(k);
-      rank += o > own_order || (o == own_order && row_of[k] < row_of[i]);
-    }
-    if (rank < top) {
-      out.top_index[token * top + rank] = row_of[i];
-      out.top_log_prob[token * top + rank] = log_prob(value[i]);
+    };
+    if (all_rows <= NW) sum_rows(std::integral_constant<int, 1>{});
+    else sum_rows(std::integral_constant<int, 4>{});
+    __syncthreads();
+    for (int i = tid; i < c; i += NT) {
+      const int row = row_of[i];
+      const u64 mine_is = rank_of[i];
+      int ahead = 0;
+#pragma unroll 8
+      for (int k = 0; k < c; ++k) {
+        const int other = row_of[k];
+        const u64 is = rank_of[k];
+        ahead += is > mine_is || (is == mine_is && other >= 0 && other < row);
+      }
+      if (row >= 0 && ahead < top) {
+        out.top_index[token * top + ahead] = row;
+        out.top_log_prob[token * top + ahead] = log_prob(value[i]);
+      }
     }
   }
 }
@@ -437,16 +559,16 @@ __device__ __forceinline__ void score_grad_tile(const HeadOperand& weight, const
     patch_row = target_at(t, col0 + column) - row0;
     patch = c.value[col0 + column];
   }
-  constexpr int kPlanes = F32 ? 3 : 1;
-#pragma unroll
-  for (int p = 0; p < kPlanes; ++p) {
-    if (p) __syncthreads();                              // the image has left
+  // fp32: a plane after the other, each from the accumulators themselves; kept remainders would not fit the registers
+#pragma unroll 1
+  for (int p = 0; p < (F32 ? 3 : 1); ++p) {
+    if (F32 && p) __syncthreads();                       // the image has left
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
       const long long token = col0 + tile.wn * T::WN + 32 * j + fr;
       float a = 0.f, b = 0.f;
       float2 l2 = make_float2(INFINITY, 0.f);
-      if (p == 0 && token < hidden.rows) {
+      if (token < hidden.rows) {
         a = c.a[token];
         b = c.b[token];
         l2 = c.log2sum[token];
@@ -458,22 +580,22 @@ __device__ __forceinline__ void score_grad_tile(const HeadOperand& weight, const
           float x[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            if (p == 0) {
-              const float y = fmaxf(fmaf(unit, tile.acc[i][j][4 * q + e], -l2.x) - l2.y, kFarBelow);
-              x[e] = -__builtin_amdgcn_exp2f(y) * fmaf(b, y, a);
+            const float y = fmaxf(fmaf(unit, tile.acc[i][j][4 * q + e], -l2.x) - l2.y, kFarBelow);
+            x[e] = -__builtin_amdgcn_exp2f(y) * fmaf(b, y, a);
+          }
+          if (there < T::WM) {                           // what ends the logits' rows is zero
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
               if (32 * i + 8 * q + 4 * fh + e >= there) x[e] = 0.f;
-            } else {
-              x[e] = tile.acc[i][j][4 * q + e];
+          }
+          u32x2 w = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+          if constexpr (F32) {
+            for (int k = 0; k < p; ++k) {                // what the planes before leave
+              x[0] -= bf16_lo(w.x), x[1] -= bf16_hi(w.x), x[2] -= bf16_lo(w.y), x[3] -= bf16_hi(w.y);
+              w = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
             }
           }
-          const u32x2 w = {pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
           tile.put(smem, i, j, q, w);
-          if constexpr (F32) {                           // what the plane leaves
-            tile.acc[i][j][4 * q] = x[0] - bf16_lo(w.x);
-            tile.acc[i][j][4 * q + 1] = x[1] - bf16_hi(w.x);
-            tile.acc[i][j][4 * q + 2] = x[2] - bf16_lo(w.y);
-            tile.acc[i][j][4 * q + 3] = x[3] - bf16_hi(w.y);
-          }
           __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -512,20 +634,20 @@ __global__ __launch_bounds__(256, B == 128 && S == 2 ? 2 : 1) void score_grad_ke
 
 template <int B, int S, bool BEST>
 hipError_t score_logits_of(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, ScoreStats* stats,
-                           long long stats_pitch, ScoreBest* best, long long best_pitch, hipStream_t s) {
+                           ScoreBest* best, hipStream_t s) {
   constexpr int lds = Tile<B, B, false, false, S>::kLds;
   static std::atomic<uint64_t> done{0};
   if (hipError_t e = allow_lds(done, reinterpret_cast<const void*>(&score_logits_kernel<B, S, BEST>), lds)) return e;
-  score_logits_kernel<B, S, BEST><<<(unsigned)g.blocks(), 256, lds, s>>>(weight, hidden, tiles_of(g, pairs), unit, stats, stats_pitch, best, best_pitch);
+  score_logits_kernel<B, S, BEST><<<(unsigned)g.blocks(), 256, lds, s>>>(weight, hidden, tiles_of(g, pairs), unit, stats, best);
   return hipGetLastError();
 }
 
 hipError_t launch_score_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, ScoreStats* stats,
-                               long long stats_pitch, ScoreBest* best, long long best_pitch, hipStream_t s) {
+                               ScoreBest* best, hipStream_t s) {
 #define MUON_SCORE_CASE(B, S)                                                                                             \
   if (g.tile == B && (g.alone ? 4 : 2) == S)                                                                              \
-    return best ? score_logits_of<B, S, true>(weight, hidden, g, pairs, unit, stats, stats_pitch, best, best_pitch, s)   \
-                : score_logits_of<B, S, false>(weight, hidden, g, pairs, unit, stats, stats_pitch, best, best_pitch, s)
+    return best ? score_logits_of<B, S, true>(weight, hidden, g, pairs, unit, stats, best, s)   \
+                : score_logits_of<B, S, false>(weight, hidden, g, pairs, unit, stats, best, s)
   MUON_SCORE_CASE(256, 2);
   MUON_SCORE_CASE(128, 2);
   MUON_SCORE_CASE(128, 4);
@@ -533,14 +655,19 @@ hipError_t launch_score_logits(const HeadOperand& weight, const HeadOperand& hid
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_score_finish(const ScoreTarget& t, float inv_tau, float unit, const ScoreStats* stats, long long stats_pitch, long long blocks,
+hipError_t launch_score_finish(const ScoreTarget& t, float inv_tau, float unit, const ScoreStats* stats, long long blocks,
                                const ScoreBest* best, long long groups, int top, const HeadRows& rows, long long tokens, long long vocab, const ScoreOut& out,
                                hipStream_t s) {
-  auto go = [&](auto kernel) {
-    kernel<<<(unsigned)tokens, 256, 0, s>>>(t, inv_tau, unit, stats, stats_pitch, blocks, best, groups, top, rows, vocab, out);
+  const unsigned lds = top ? (top + kScoreMargin) * (33 * 20 + 4) + kPickList * 12 : 0;
+  auto go = [&](auto kernel, int threads) {
+    kernel<<<(unsigned)tokens, threads, lds, s>>>(t, inv_tau, unit, stats, blocks, best, groups, top, rows, vocab, out);
     return hipGetLastError();
   };
-  return rows.f32 ? go(score_finish_kernel<true>) : go(score_finish_kernel<false>);
+  if (!top) return rows.f32 ? go(score_finish_kernel<true, false, 256>, 256) : go(score_finish_kernel<false, false, 256>, 256);
+  // few tokens: threads enough to fill the chip with one block or two per compute unit
+  if (tokens <= 256) return rows.f32 ? go(score_finish_kernel<true, true, 1024>, 1024) : go(score_finish_kernel<false, true, 1024>, 1024);
+  if (tokens <= 512) return rows.f32 ? go(score_finish_kernel<true, true, 512>, 512) : go(score_finish_kernel<false, true, 512>, 512);
+  return rows.f32 ? go(score_finish_kernel<true, true, 256>, 256) : go(score_finish_kernel<false, true, 256>, 256);
 }
 
 hipError_t launch_score_peak(const ScoreTarget& t, const ScoreGrads& d, long long tokens, long long vocab, float* peak, hipStream_t s) {

@@ -100,11 +100,11 @@ int muon_log_probs(const muon_head* h, const void* targets, int32_t targets_byte
       const HeadRows rows{behind(h->hidden, elem * t0 * h->hidden_stride), h->weight, h->hidden_stride, h->weight_stride, s.width, s.f32};
       HeadOperand hidden;
       if (int st = pack_rows(h, s, p.shape, rows.hidden, n, p.piece, ws + p.packed_hidden, &hidden, stream)) return st;
-      MUON_HIP(launch_score_logits(weight, hidden, p.logits[piece == p.pieces - 1], p.shape.pairs, scale.unit, stats, p.piece, best, p.groups, stream));
+      MUON_HIP(launch_score_logits(weight, hidden, p.logits[piece == p.pieces - 1], p.shape.pairs, scale.unit, stats, best, stream));
       const ScoreTarget t{behind(targets, targets_bytes * t0), targets_bytes == 8};
       const ScoreOut out{log_prob ? log_prob + t0 : nullptr, entropy + t0, lse + t0, lse_rest + t0,
                          top ? reinterpret_cast<long long*>(top_index) + t0 * top : nullptr, top ? top_log_prob + t0 * top : nullptr};
-      MUON_HIP(launch_score_finish(t, scale.inv_tau, scale.unit, stats, p.piece, p.shape.blocks, best, p.groups, top, rows, n, s.vocab, out, stream));
+      MUON_HIP(launch_score_finish(t, scale.inv_tau, scale.unit, stats, p.shape.blocks, best, p.groups, top, rows, n, s.vocab, out, stream));
     }
     return MUON_OK;
   });

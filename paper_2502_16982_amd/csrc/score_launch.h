@@ -12,7 +12,7 @@ struct ScoreTarget {
   int index64;
 };
 
-// What the logits' product leaves behind, y = unit z (units of log 2).  Per block of kHeadGrain vocabulary entries and token: its largest y as `top`,
+// What the logits' product leaves behind, y = unit z (units of log 2).  Per token and block of kHeadGrain vocabulary entries: its largest y as `top`,
 // sum of 2^(y - top), sum of 2^(y - top) (y - top).  With `best`, per token and group of kScoreGroup entries: its largest z, and its second largest
 // as a bound from above whose low five bits are the largest one's place in the group.
 struct ScoreStats {
@@ -23,7 +23,7 @@ struct ScoreBest {
   unsigned second;
 };
 hipError_t launch_score_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, ScoreStats* stats,
-                               long long stats_pitch, ScoreBest* best, long long best_pitch, hipStream_t s);
+                               ScoreBest* best, hipStream_t s);
 
 struct ScoreOut {
   float *log_prob, *entropy, *lse, *lse_rest;      // log_prob null where there are no targets
@@ -31,7 +31,7 @@ struct ScoreOut {
   float* top_log_prob;                             // [tokens, top]
 };
 // Joins the blocks; log probability of the given token and of the `top` largest logits, both from logits that are summed in double.
-hipError_t launch_score_finish(const ScoreTarget& t, float inv_tau, float unit, const ScoreStats* stats, long long stats_pitch, long long blocks,
+hipError_t launch_score_finish(const ScoreTarget& t, float inv_tau, float unit, const ScoreStats* stats, long long blocks,
                                const ScoreBest* best, long long groups, int top, const HeadRows& rows, long long tokens, long long vocab, const ScoreOut& out,
                                hipStream_t s);
 

@@ -6,7 +6,7 @@ namespace muon {
 
 constexpr int kScoreMaxTop = 64;
 // Alternatives are picked among so many more than are asked for: fp32 sums may order logits otherwise that are nearly alike.
-constexpr int kScoreMargin = 8;
+constexpr int kScoreMargin = 4;
 // Vocabulary entries of a group, of which the largest logit is kept.
 constexpr int kScoreGroup = 32;
 
