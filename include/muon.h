@@ -444,7 +444,7 @@ typedef enum { MUON_ACT_SILU = 0, MUON_ACT_RELU = 1 } muon_activation;
 typedef struct {
   const void* w;            /* device; [experts][rows][columns]; gate: null for none                    */
   int64_t expert_stride;    /* elements, 0 and more                                                     */
-  int64_t row_stride;       /* elements, >= columns                                                     */
+  int64_t row_stride;       /* elements, >= columns, up to 2^24                                         */
 } muon_matrices;
 
 typedef struct {

@@ -62,7 +62,8 @@ int muon_expert_layer(const muon_layer* layer, const void* x, int64_t x_stride, 
     const uintptr_t size = s.f32 ? 4 : 2;
     const muon_matrices *up = &layer->up, *gate = &layer->gate, *down = &layer->down;
     if (!x || !expert || !out || !up->w || !down->w || x_stride < s.width || up->row_stride < s.inner || down->row_stride < s.width ||
-        up->expert_stride < 0 || down->expert_stride < 0 || (s.gated && (gate->row_stride < s.inner || gate->expert_stride < 0)))
+        up->row_stride > kLayerMaxStride || down->row_stride > kLayerMaxStride || up->expert_stride < 0 || down->expert_stride < 0 ||
+        (s.gated && (gate->row_stride < s.inner || gate->row_stride > kLayerMaxStride || gate->expert_stride < 0)))
       return MUON_E_INVALID_ARG;
     if (!aligned(x, size) || !aligned(expert, expert_bytes) || !aligned(weights, 4) || !aligned(out, size) || !aligned(up->w, size) ||
         !aligned(gate->w, size) || !aligned(down->w, size) || !aligned(workspace, 256))
@@ -77,11 +78,11 @@ int muon_expert_layer(const muon_layer* layer, const void* x, int64_t x_stride, 
     const LayerRows tokens{x, x_stride, s.top}, inner{ws + plan.inner, s.inner, 1};
     const int act = layer->activation;
     const bool runs = plan.up.runs > 1;
-    MUON_HIP(launch_layer_product(pairs, plan.up, tokens, wu, s.gated ? &wg : nullptr, s.f32, runs ? -1 : act,
+    const LayerSums sums{reinterpret_cast<const float*>(ws + plan.part), s.inner, plan.up.runs, s.gated ? 2 : 1, act};
+    MUON_HIP(launch_layer_product(pairs, plan.up, tokens, wu, s.gated ? &wg : nullptr, nullptr, s.f32, runs ? -1 : act,
                                   runs ? ws + plan.part : ws + plan.inner, stream));
-    if (runs)
-      MUON_HIP(launch_layer_act(pairs, plan.up.runs, s.inner, s.gated, s.f32, act, reinterpret_cast<const float*>(ws + plan.part), ws + plan.inner, stream));
-    MUON_HIP(launch_layer_product(pairs, plan.down, inner, wd, nullptr, s.f32, -1, ws + plan.rows, stream));
+    if (runs && !plan.staged) MUON_HIP(launch_layer_act(pairs, plan.up.runs, s.inner, s.gated, s.f32, act, sums.part, ws + plan.inner, stream));
+    MUON_HIP(launch_layer_product(pairs, plan.down, inner, wd, nullptr, plan.staged ? &sums : nullptr, s.f32, -1, ws + plan.rows, stream));
     MUON_HIP(launch_layer_join(pairs, plan.down.runs, s.width, s.f32, reinterpret_cast<const float*>(ws + plan.rows), weights, out, stream));
     return MUON_OK;
   });

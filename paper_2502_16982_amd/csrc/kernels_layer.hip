@@ -36,12 +36,21 @@ __device__ __forceinline__ int expert_of(const LayerPairs& p, int i) {
 
 constexpr int kTile = 16;                        // pairs of a tile
 
-// Pairs of expert e numbered [base, base + room) into list, in their order; the number of all its pairs is returned.  By the whole block of
-// 256 threads; counts: 4 ints of LDS.
-__device__ __forceinline__ int find_pairs(const LayerPairs& p, int e, int base, int room, int* list, int* counts) {
+constexpr int kRoom = 2 * kTile;                 // pairs that a block takes at a time
+
+// Pairs of expert e numbered [base, base + kRoom) into the wave's list, in their order; the number of all its pairs is returned.  By the whole
+// block of THREADS threads; counts: an int of LDS per wave.
+template <int THREADS>
+__device__ __forceinline__ int find_pairs(const LayerPairs& p, int e, int base, int (*lists)[kRoom], int* counts) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (p.pairs <= 64) {                           // every wave for itself, without a barrier, which would wait for the loads on their way
+    const unsigned long long ballot = __ballot(lane < p.pairs && expert_of(p, lane) == e);
+    const int rank = __popcll(ballot & ((1ull << lane) - 1)) - base;
+    if ((ballot >> lane & 1) && rank >= 0 && rank < kRoom) lists[wave][rank] = lane;
+    return __popcll(ballot);
+  }
   int seen = 0;
-  for (int at = 0; at < p.pairs; at += 256) {
+  for (int at = 0; at < p.pairs; at += THREADS) {
     const int i = at + threadIdx.x;
     const bool mine = i < p.pairs && expert_of(p, i) == e;
     const unsigned long long ballot = __ballot(mine);
@@ -49,10 +58,15 @@ __device__ __forceinline__ int find_pairs(const LayerPairs& p, int e, int base, 
     if (lane == 0) counts[wave] = __popcll(ballot);
     __syncthreads();
     int before = seen;
-    for (int w = 0; w < wave; ++w) before += counts[w];
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      if (w < wave) before += counts[w];
+      seen += counts[w];
+    }
     const int rank = before + __popcll(ballot & ((1ull << lane) - 1)) - base;
-    if (mine && rank >= 0 && rank < room) list[rank] = i;
-    seen += counts[0] + counts[1] + counts[2] + counts[3];
+    if (mine && rank >= 0 && rank < kRoom)
+#pragma unroll
+      for (int w = 0; w < THREADS / 64; ++w) lists[w][rank] = i;
   }
   __syncthreads();
   return seen;
@@ -71,34 +85,35 @@ struct Elem<true> {
   static constexpr int COLS = 4, STEPS = 32;
 };
 
-// 32 rows of a matrix: 8 accesses of 16 bytes per lane.  Row of access j: bf16 8 g + j, fp32 16 (j / 4) + 4 g + j % 4, with g = lane / 16.
+// 32 rows of a matrix: 8 accesses of 16 bytes per lane.  Row of access j: bf16 8 g + j, fp32 16 (j / 4) + 4 g + j % 4, with g = lane / 16.  `at` is the
+// same for the whole wave, `lane` the lane's own offset in bytes (of its first row and column): scalar addresses, one register per lane.
 template <bool F32>
 struct Slab {
   u32x4 v[8];
-  static __device__ __forceinline__ int row(int j, int g) { return F32 ? 16 * (j / 4) + 4 * g + j % 4 : 8 * g + j; }
-  __device__ __forceinline__ void load(const typename Elem<F32>::T* w, long long stride, int g) {
+  static constexpr int kOwn = F32 ? 4 : 8;       // rows from a group of lanes to the next
+  static __device__ __forceinline__ constexpr int common(int j) { return F32 ? 16 * (j / 4) + j % 4 : j; }
+  __device__ __forceinline__ void load(const char* at, long long stride, unsigned lane) {
+    // (else the compiler adds the lane's offset to a base outside the loop, and every row has an address of two registers per lane)
+    asm volatile("" : "+v"(lane));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const u32x4_any*>(w + row(j, g) * stride);
+    for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const u32x4_any*>(at + common(j) * stride + lane);
   }
-  // rows [0, there) only; the others are zero
-  __device__ __forceinline__ void load_some(const typename Elem<F32>::T* w, long long stride, int g, int there) {
+  // the same of `cols` columns and of rows [0, there) only; the others are zero
+  __device__ __forceinline__ void load_some(const char* at, long long stride, unsigned lane, int g, int there, int cols) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       v[j] = u32x4{0u, 0u, 0u, 0u};
-      if (row(j, g) < there) v[j] = *reinterpret_cast<const u32x4_any*>(w + row(j, g) * stride);
-    }
-  }
-  // the same of `cols` columns
-  __device__ __forceinline__ void load_few(const typename Elem<F32>::T* w, long long stride, int g, int there, int cols) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[j] = u32x4{0u, 0u, 0u, 0u};
-      if (row(j, g) >= there) continue;
+      if (common(j) + kOwn * g >= there) continue;
+      const char* p = at + common(j) * stride + lane;
+      if (cols == Elem<F32>::COLS) {
+        v[j] = *reinterpret_cast<const u32x4_any*>(p);
+        continue;
+      }
 #pragma unroll
       for (int c = 0; c < Elem<F32>::COLS; ++c) {
         if (c >= cols) continue;
-        if constexpr (F32) v[j][c] = __float_as_uint(w[row(j, g) * stride + c]);
-        else v[j][c / 2] |= (unsigned)w[row(j, g) * stride + c] << 16 * (c & 1);
+        if constexpr (F32) v[j][c] = reinterpret_cast<const unsigned*>(p)[c];
+        else v[j][c / 2] |= (unsigned)reinterpret_cast<const u16*>(p)[c] << 16 * (c & 1);
       }
     }
   }
@@ -167,98 +182,127 @@ __device__ __forceinline__ void multiply(const Slab<F32>& w, const RowPart<F32> 
   }
 }
 
-// Block: (run of the summed axis, tile of columns, slot).  NT tiles of pairs at a time.
-template <bool F32, int MATS, int NT>
-__device__ __forceinline__ void product_tiles(const LayerPairs& p, const LayerProduct& g, const LayerRows& rows, const typename Elem<F32>::T* const (&w)[MATS],
-                                              const long long (&stride)[MATS], int run, long long col0, const int* list, int here, int act,
-                                              void* out, float* lds) {
-  using E = Elem<F32>;
-  using T = typename E::T;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, a = lane & 15, q = lane >> 4;
-  // a lane's columns end with the matrix at the latest: the last ones are then computed twice, alike
-  long long col = col0 + E::COLS * a;
-  const int cols = g.n < E::COLS ? (int)g.n : E::COLS;
-  if (col > g.n - cols) col = g.n - cols;
-  const long long k0 = (long long)run * g.run, k1 = k0 + g.run < g.k ? k0 + g.run : g.k;
+// A wave's part of a product: columns [col0, ..) and rows [k0, k1) of one expert's matrix, 32 rows at a time, every fourth of them.
+template <bool F32>
+struct Part {
+  static constexpr int COLS = Elem<F32>::COLS, kStep = kLayerRows * kLayerWaves;
+  const char* w;                                 // row 0 of the expert's matrix
+  long long stride;                              // bytes
+  unsigned own;                                  // bytes from a row of the wave's to the lane's columns in its own first row
+  long long k0, k1;
+  int cols, wave, lane;                          // wave: of those that share the matrix
+
+  __device__ __forceinline__ bool whole(long long k) const { return cols == COLS && k + kLayerRows <= k1; }
+  __device__ __forceinline__ long long first_row() const { return k0 + wave * kLayerRows; }
+  __device__ __forceinline__ void load(long long k, Slab<F32>& s) const { s.load(w + k * stride, stride, own); }
+  __device__ __forceinline__ void load_rest(long long k, Slab<F32>& s) const {
+    s.load_some(w + k * stride, stride, own, lane >> 4, k1 - k < kLayerRows ? (int)(k1 - k) : kLayerRows, cols);
+  }
+};
+
+// The part for NT tiles of pairs.  STAGED: the pairs' operand lies in LDS, [pair][row - k0] at a pitch of `staged` elements, zeros behind k1.
+// first: the wave's first rows, already loaded where `loaded`.
+template <bool F32, int NT, bool STAGED>
+__device__ __forceinline__ void multiply_part(const Part<F32>& part, const LayerRows& rows, const int* list, int here, const unsigned char* lds, int staged,
+                                              Slab<F32>& first, bool loaded, Acc<F32> (&acc)[NT]) {
+  using T = typename Elem<F32>::T;
+  const int a = part.lane & 15, q = part.lane >> 4;
   const T* x[NT];
   bool there[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     there[t] = t * kTile + a < here;
-    x[t] = static_cast<const T*>(rows.x) + (long long)(list[there[t] ? t * kTile + a : 0] / rows.per) * rows.stride;
+    const int at = there[t] ? t * kTile + a : 0;
+    if constexpr (STAGED) x[t] = reinterpret_cast<const T*>(lds) + at * staged - part.k0;
+    else x[t] = static_cast<const T*>(rows.x) + (long long)(list[at] / rows.per) * rows.stride;
+    acc[t].zero();
   }
-  Acc<F32> acc[MATS][NT];
+  const auto load_rows = [&](long long k, RowPart<F32> (&r)[NT]) {
 #pragma unroll
-  for (int m = 0; m < MATS; ++m)
+    for (int t = 0; t < NT; ++t) r[t].load(x[t] + k, q);
+  };
+  const auto take = [&](const Slab<F32>& s, RowPart<F32> (&r)[NT]) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[m][t].zero();
-  Slab<F32> s[MATS];
-  RowPart<F32> r[NT];
-  auto load = [&](long long k) {
-#pragma unroll
-    for (int m = 0; m < MATS; ++m) s[m].load(w[m] + k * stride[m] + col, stride[m], q);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      r[t].load(x[t] + k, q);
+    for (int t = 0; t < NT; ++t)
       if (!there[t]) r[t].zero();
-    }
+    multiply<F32, NT>(s, r, acc);
   };
-  auto take = [&]() {
-#pragma unroll
-    for (int m = 0; m < MATS; ++m) multiply<F32, NT>(s[m], r, acc[m]);
-  };
-  constexpr int kStep = kLayerRows * kLayerWaves;
-  long long k = k0 + wave * kLayerRows;
-  if (cols == E::COLS)
-    for (; k + kLayerRows <= k1; k += kStep) {
-      load(k);
-      take();
+  // 32 rows are multiplied while the next 32 are on their way
+  long long k = part.first_row();
+  RowPart<F32> r0[NT], r1[NT];
+  if (part.whole(k)) {
+    Slab<F32> second;
+    if (!loaded) part.load(k, first);
+    load_rows(k, r0);
+    for (;;) {
+      const long long next = k + part.kStep, after = next + part.kStep;
+      const bool more = part.whole(next);
+      if (more) {
+        part.load(next, second);
+        load_rows(next, r1);
+      }
+      take(first, r0);
+      k = next;
+      if (!more) break;
+      const bool again = part.whole(after);
+      if (again) {
+        part.load(after, first);
+        load_rows(after, r0);
+      }
+      take(second, r1);
+      k = after;
+      if (!again) break;
     }
-  for (; k < k1; k += kStep) {                   // the last rows, or a matrix of a few columns
-    const int left = k1 - k < kLayerRows ? (int)(k1 - k) : kLayerRows;
-#pragma unroll
-    for (int m = 0; m < MATS; ++m) {
-      if (cols == E::COLS) s[m].load_some(w[m] + k * stride[m] + col, stride[m], q, left);
-      else s[m].load_few(w[m] + k * stride[m] + col, stride[m], q, left, cols);
-    }
+  }
+  for (; k < part.k1; k += part.kStep) {         // the last rows, or a matrix of a few columns
+    part.load_rest(k, first);
+    const int left = part.k1 - k < kLayerRows ? (int)(part.k1 - k) : kLayerRows;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      r[t].zero();
-      if (there[t]) r[t].load_some(x[t] + k, q, left);
+      if constexpr (STAGED) r0[t].load(x[t] + k, q);
+      else r0[t].load_some(x[t] + k, q, left);
     }
-    take();
+    take(first, r0);
   }
-  // the waves' sums through LDS, [wave][pair][column]; then a thread has a pair's COLS neighbouring columns
-  constexpr int kColumns = 16 * E::COLS, kPitch = kColumns + 4;
-  const int pair = threadIdx.x >> 4, chunk = threadIdx.x & 15;
-  long long at = col0 + E::COLS * chunk;
-  if (at > g.n - cols) at = g.n - cols;
+}
+
+// The waves' sums through LDS, [wave][pair][column]; then a thread of the first 256 has a pair's COLS neighbouring columns, of both matrices.
+template <bool F32, int MATS, int NT>
+__device__ __forceinline__ void store_tiles(const LayerPairs& p, const Part<F32>& part, const Acc<F32> (&acc)[NT], long long col0, long long n, int run,
+                                            int apart, int matrix, const int* list, int here, int act, void* out, unsigned char* lds) {
+  using T = typename Elem<F32>::T;
+  constexpr int COLS = Elem<F32>::COLS, kPitch = 16 * COLS + 4, kWaves = kLayerWaves * MATS;
+  float* sums = reinterpret_cast<float*>(lds);
+  const int wave = threadIdx.x >> 6, a = part.lane & 15, q = part.lane >> 4, pair = threadIdx.x >> 4, chunk = threadIdx.x & 15;
+  long long at = col0 + COLS * chunk;
+  if (at > n - part.cols) at = n - part.cols;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    float sum[MATS][E::COLS];
+    __syncthreads();
 #pragma unroll
-    for (int m = 0; m < MATS; ++m) {
-      __syncthreads();
+    for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int i = 0; i < E::COLS; ++i) lds[(wave * 16 + a) * kPitch + E::COLS * (4 * q + u) + i] = acc[m][t].v[i][u];
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < E::COLS; ++i) {
-        float x0 = lds[pair * kPitch + E::COLS * chunk + i];
-#pragma unroll
-        for (int v = 1; v < kLayerWaves; ++v) x0 += lds[(v * 16 + pair) * kPitch + E::COLS * chunk + i];
-        sum[m][i] = x0;
-      }
-    }
+      for (int i = 0; i < COLS; ++i) sums[(wave * 16 + a) * kPitch + COLS * (4 * q + u) + i] = acc[t].v[i][u];
+    __syncthreads();
+    if (kWaves > 4 && threadIdx.x >= 256) continue;
     if (t * kTile + pair >= here) continue;
+    float sum[MATS][COLS];
+#pragma unroll
+    for (int m = 0; m < MATS; ++m)
+#pragma unroll
+      for (int i = 0; i < COLS; ++i) {
+        const float* of = sums + (m * kLayerWaves * 16 + pair) * kPitch + COLS * chunk + i;
+        float x = of[0];
+#pragma unroll
+        for (int v = 1; v < kLayerWaves; ++v) x += of[v * 16 * kPitch];
+        sum[m][i] = x;
+      }
     const long long id = list[t * kTile + pair];
     if (act >= 0) {
-      T* to = static_cast<T*>(out) + id * g.n + at;
+      T* to = static_cast<T*>(out) + id * n + at;
 #pragma unroll
-      for (int i = 0; i < E::COLS; ++i) {
-        if (i >= cols) continue;
+      for (int i = 0; i < COLS; ++i) {
+        if (i >= part.cols) continue;
         const float h = MATS == 2 ? activate(act, sum[MATS - 1][i]) * sum[0][i] : activate(act, sum[0][i]);
         if constexpr (F32) to[i] = h;
         else to[i] = (u16)(pack_bf16(h, 0.f) & 0xffffu);
@@ -266,47 +310,98 @@ __device__ __forceinline__ void product_tiles(const LayerPairs& p, const LayerPr
     } else {
 #pragma unroll
       for (int m = 0; m < MATS; ++m) {
-        float* to = static_cast<float*>(out) + (((long long)run * p.pairs + id) * MATS + m) * g.n + at;
+        float* to = static_cast<float*>(out) + (((long long)run * p.pairs + id) * (MATS * apart) + (MATS == 1 ? matrix : m)) * n + at;
 #pragma unroll
-        for (int i = 0; i < E::COLS; ++i)
-          if (i < cols) to[i] = sum[m][i];
+        for (int i = 0; i < COLS; ++i)
+          if (i < part.cols) to[i] = sum[m][i];
       }
     }
   }
 }
 
-template <bool F32, int MATS>
-__global__ __launch_bounds__(256) void layer_product_kernel(LayerPairs p, LayerProduct g, LayerRows rows, LayerMatrix w, LayerMatrix gate, int act,
-                                                            void* __restrict__ out) {
+// The operand of the second product from the sums of the first one's runs, activated, into LDS.
+template <bool F32>
+__device__ __forceinline__ void stage(const LayerPairs& p, const LayerSums& from, long long k0, long long k1, int staged, const int* list, int here,
+                                      unsigned char* lds) {
   using T = typename Elem<F32>::T;
-  __shared__ float lds[kLayerWaves * 16 * (16 * Elem<F32>::COLS + 4)];
-  __shared__ int list[2 * kTile];
-  __shared__ int counts[4];
+  for (int i = threadIdx.x; i < here * staged; i += 256) {
+    const int pair = i / staged;
+    const long long k = k0 + i % staged;
+    float h = 0.f;
+    if (k < k1) {
+      const float* at = from.part + (long long)list[pair] * from.mats * from.n + k;
+      const long long run = (long long)p.pairs * from.mats * from.n;
+      float up = 0.f, lead = 0.f;
+#pragma unroll 8
+      for (int r = 0; r < from.runs; ++r) {
+        up += at[r * run];
+        if (from.mats == 2) lead += at[r * run + from.n];
+      }
+      h = from.mats == 2 ? activate(from.act, lead) * up : activate(from.act, up);
+    }
+    if constexpr (F32) reinterpret_cast<T*>(lds)[i] = h;
+    else reinterpret_cast<T*>(lds)[i] = (u16)(pack_bf16(h, 0.f) & 0xffffu);
+  }
+  __syncthreads();
+}
+
+// Block: (matrix, run of the summed axis, tile of columns, slot); four waves to a matrix, MATS matrices to a block.  NT: tiles of pairs that there may
+// be at a time.
+template <bool F32, int MATS, int NT, bool STAGED>
+__global__ __launch_bounds__(256 * MATS, 2) void layer_product_kernel(LayerPairs p, LayerProduct g, LayerRows rows, LayerMatrix w, LayerMatrix gate, LayerSums from,
+                                                                      int act, void* __restrict__ out) {
+  using T = typename Elem<F32>::T;
+  using E = Elem<F32>;
+  constexpr int kThreads = 256 * MATS, kSums = kLayerWaves * MATS * 16 * (16 * E::COLS + 4) * 4;
+  __shared__ __align__(16) unsigned char lds[STAGED && kLayerStage > kSums ? kLayerStage : kSums];
+  __shared__ int lists[kThreads / 64][kRoom];
+  __shared__ int counts[kThreads / 64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int b = blockIdx.x;
+  const int apart = MATS == 1 ? g.mats : 1, matrix = MATS == 1 ? b % apart : wave / kLayerWaves;
+  b /= apart;
   const int run = b % g.runs;
   b /= g.runs;
   const int tile = b % g.tiles, slot = b / g.tiles;
-  const int e = p.slot_is_pair ? expert_of(p, slot) : slot;
+  const int e = __builtin_amdgcn_readfirstlane(p.slot_is_pair ? expert_of(p, slot) : slot);
   if (e < 0) return;
-  const int all = find_pairs(p, e, 0, 2 * kTile, list, counts);
+  const long long col0 = (long long)tile * (16 * E::COLS);
+  Part<F32> part;
+  part.wave = wave % kLayerWaves;
+  part.lane = threadIdx.x & 63;
+  part.k0 = (long long)run * g.run;
+  part.k1 = part.k0 + g.run < g.k ? part.k0 + g.run : g.k;
+  // a lane's columns end with the matrix at the latest: the last ones are then computed twice, alike
+  part.cols = g.n < E::COLS ? (int)g.n : E::COLS;
+  long long col = col0 + E::COLS * (part.lane & 15);
+  if (col > g.n - part.cols) col = g.n - part.cols;
+  const LayerMatrix& m = matrix ? gate : w;
+  part.w = reinterpret_cast<const char*>(static_cast<const T*>(m.w) + e * m.expert_stride);
+  part.stride = m.row_stride * (long long)sizeof(T);
+  part.own = (unsigned)((Slab<F32>::kOwn * (part.lane >> 4) * m.row_stride + col) * (long long)sizeof(T));
+  // where a slot stands for a pair it has tokens, so that the first rows can be on their way while they are looked up
+  Slab<F32> first;
+  const bool ahead = p.slot_is_pair && part.whole(part.first_row());
+  if (ahead) part.load(part.first_row(), first);
+  const int* list = lists[wave];
+  const int all = find_pairs<kThreads>(p, e, 0, lists, counts);
   if (all == 0 || (p.slot_is_pair && list[0] != slot)) return;       // nobody's, or another slot's
-  const T* base[MATS];
-  long long stride[MATS];
-  base[0] = static_cast<const T*>(w.w) + e * w.expert_stride;
-  stride[0] = w.row_stride;
-  if constexpr (MATS == 2) {
-    base[1] = static_cast<const T*>(gate.w) + e * gate.expert_stride;
-    stride[1] = gate.row_stride;
-  }
-  const long long col0 = (long long)tile * (16 * Elem<F32>::COLS);
-  for (int first = 0; first < all; first += 2 * kTile) {
-    if (first) {
+  const int staged = (int)((part.k1 - part.k0 + kLayerRows - 1) / kLayerRows * kLayerRows);
+  for (int at = 0; at < all; at += kRoom) {
+    if (at) {
       __syncthreads();
-      find_pairs(p, e, first, 2 * kTile, list, counts);
+      find_pairs<kThreads>(p, e, at, lists, counts);
     }
-    const int here = all - first < 2 * kTile ? all - first : 2 * kTile;
-    if (here <= kTile) product_tiles<F32, MATS, 1>(p, g, rows, base, stride, run, col0, list, here, act, out, lds);
-    else product_tiles<F32, MATS, 2>(p, g, rows, base, stride, run, col0, list, here, act, out, lds);
+    const int here = all - at < kRoom ? all - at : kRoom;
+    if constexpr (STAGED) stage<F32>(p, from, part.k0, part.k1, staged, list, here, lds);
+    const auto tiles = [&](auto count) {
+      constexpr int N = decltype(count)::value;
+      Acc<F32> acc[N];
+      multiply_part<F32, N, STAGED>(part, rows, list, here, lds, staged, first, ahead && at == 0, acc);
+      store_tiles<F32, MATS, N>(p, part, acc, col0, g.n, run, apart, matrix, list, here, act, out, lds);
+    };
+    if (NT == 1 || here <= kTile) tiles(std::integral_constant<int, 1>{});
+    else tiles(std::integral_constant<int, NT>{});
   }
 }
 
@@ -327,35 +422,70 @@ __global__ __launch_bounds__(256) void layer_act_kernel(LayerPairs p, int runs, 
   else static_cast<u16*>(inner)[pair * n + c] = (u16)(pack_bf16(h, 0.f) & 0xffffu);
 }
 
+// 128 columns of a token per block: four neighbouring ones per thread, the token's terms over eight groups of threads, joined in LDS.
+constexpr int kJoinColumns = 128;
 template <bool F32>
 __global__ __launch_bounds__(256) void layer_join_kernel(LayerPairs p, int runs, long long n, const float* __restrict__ rows, const float* __restrict__ weights,
                                                          void* __restrict__ out) {
-  const long long spans = (n + 255) / 256, token = blockIdx.x / spans, c = blockIdx.x % spans * 256 + threadIdx.x;
-  if (c >= n) return;
-  float sum = 0.f;
-  for (int j = 0; j < p.top; ++j) {
-    const int pair = (int)token * p.top + j;
-    if (expert_of(p, pair) < 0) continue;
-    float y = 0.f;
-    for (int r = 0; r < runs; ++r) y += rows[((long long)r * p.pairs + pair) * n + c];
-    sum = fmaf(weights ? weights[pair] : 1.f, y, sum);
+  __shared__ f32x4 parts[8][32];
+  const long long spans = (n + kJoinColumns - 1) / kJoinColumns, token = blockIdx.x / spans;
+  const int quad = threadIdx.x & 31, group = threadIdx.x >> 5, terms = p.top * runs;
+  const long long c = blockIdx.x % spans * kJoinColumns + 4 * quad;
+  const int count = c >= n ? 0 : n - c < 4 ? (int)(n - c) : 4;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = group; i < terms; i += 8) {
+    const int j = i / runs, pair = (int)token * p.top + j;
+    const bool there = expert_of(p, pair) >= 0;
+    const float w = !there ? 0.f : weights ? weights[pair] : 1.f;
+    const float* at = rows + ((long long)(i - j * runs) * p.pairs + pair) * n + c;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    if (there) {
+      if (count == 4) {
+        y = *reinterpret_cast<const f32x4_any*>(at);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (e < count) y[e] = at[e];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] = fmaf(w, y[e], sum[e]);
   }
-  if constexpr (F32) static_cast<float*>(out)[token * n + c] = sum;
-  else static_cast<u16*>(out)[token * n + c] = (u16)(pack_bf16(sum, 0.f) & 0xffffu);
+  parts[group][quad] = sum;
+  __syncthreads();
+  if (threadIdx.x >= kJoinColumns) return;
+  const long long at = blockIdx.x % spans * kJoinColumns + threadIdx.x;
+  if (at >= n) return;
+  const float* of = reinterpret_cast<const float*>(parts) + threadIdx.x;
+  float x = of[0];
+#pragma unroll
+  for (int g = 1; g < 8; ++g) x += of[g * kJoinColumns];
+  if constexpr (F32) static_cast<float*>(out)[token * n + at] = x;
+  else static_cast<u16*>(out)[token * n + at] = (u16)(pack_bf16(x, 0.f) & 0xffffu);
 }
 
 }  // namespace
 
-hipError_t launch_layer_product(const LayerPairs& p, const LayerProduct& g, const LayerRows& x, const LayerMatrix& w, const LayerMatrix* gate, bool f32,
-                                int act, void* out, hipStream_t s) {
-  const unsigned blocks = (unsigned)((long long)p.slots * g.tiles * g.runs);
+hipError_t launch_layer_product(const LayerPairs& p, const LayerProduct& g, const LayerRows& x, const LayerMatrix& w, const LayerMatrix* gate,
+                                const LayerSums* from, bool f32, int act, void* out, hipStream_t s) {
+  const bool together = gate && g.mats == 1;
+  const unsigned blocks = (unsigned)((long long)p.slots * g.tiles * g.runs * g.mats);
   const LayerMatrix none{};
+  const LayerSums rows{};
   auto go = [&](auto kernel) {
-    kernel<<<blocks, 256, 0, s>>>(p, g, x, w, gate ? *gate : none, act, out);
+    kernel<<<blocks, together ? 512 : 256, 0, s>>>(p, g, x, w, gate ? *gate : none, from ? *from : rows, act, out);
     return hipGetLastError();
   };
-  if (gate) return f32 ? go(layer_product_kernel<true, 2>) : go(layer_product_kernel<false, 2>);
-  return f32 ? go(layer_product_kernel<true, 1>) : go(layer_product_kernel<false, 1>);
+#define MUON_LAYER_CASE(NT)                                                                                            \
+  if (together) return f32 ? go(layer_product_kernel<true, 2, NT, false>) : go(layer_product_kernel<false, 2, NT, false>);     \
+  if (from) return f32 ? go(layer_product_kernel<true, 1, NT, true>) : go(layer_product_kernel<false, 1, NT, true>);           \
+  return f32 ? go(layer_product_kernel<true, 1, NT, false>) : go(layer_product_kernel<false, 1, NT, false>)
+  if (p.pairs <= 16) {
+    MUON_LAYER_CASE(1);
+  }
+  MUON_LAYER_CASE(2);
+#undef MUON_LAYER_CASE
 }
 
 hipError_t launch_layer_act(const LayerPairs& p, int runs, long long n, bool gated, bool f32, int act, const float* part, void* inner, hipStream_t s) {
@@ -366,7 +496,7 @@ hipError_t launch_layer_act(const LayerPairs& p, int runs, long long n, bool gat
 }
 
 hipError_t launch_layer_join(const LayerPairs& p, int runs, long long n, bool f32, const float* rows, const float* weights, void* out, hipStream_t s) {
-  const unsigned blocks = (unsigned)((n + 255) / 256 * (p.pairs / p.top));
+  const unsigned blocks = (unsigned)((n + kJoinColumns - 1) / kJoinColumns * (p.pairs / p.top));
   if (f32) layer_join_kernel<true><<<blocks, 256, 0, s>>>(p, runs, n, rows, weights, out);
   else layer_join_kernel<false><<<blocks, 256, 0, s>>>(p, runs, n, rows, weights, out);
   return hipGetLastError();

@@ -27,9 +27,17 @@ struct LayerRows {
   int per;
 };
 
-// out[run][pair][matrix][N] in fp32, or, one run and `act` >= 0, the activated rows [pair][N] in the inputs' type.
-hipError_t launch_layer_product(const LayerPairs& p, const LayerProduct& g, const LayerRows& x, const LayerMatrix& w, const LayerMatrix* gate, bool f32,
-                                int act, void* out, hipStream_t s);
+// Rows that the first product left as sums of its runs, [run][pair][matrix][n]; `act` is still to be applied.
+struct LayerSums {
+  const float* part;
+  long long n;
+  int runs, mats, act;
+};
+
+// out[run][pair][matrix][N] in fp32, or, one run and `act` >= 0, the activated rows [pair][N] in the inputs' type.  from: the rows instead of x; runs
+// of the summed axis of up to kLayerStage bytes for 2 x 16 pairs.
+hipError_t launch_layer_product(const LayerPairs& p, const LayerProduct& g, const LayerRows& x, const LayerMatrix& w, const LayerMatrix* gate,
+                                const LayerSums* from, bool f32, int act, void* out, hipStream_t s);
 // The activated rows from the sums of the runs.
 hipError_t launch_layer_act(const LayerPairs& p, int runs, long long n, bool gated, bool f32, int act, const float* part, void* inner, hipStream_t s);
 // out[t] = sum_j weights[t, j] sum_run rows[run][t, j].

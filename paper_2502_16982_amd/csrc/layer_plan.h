@@ -7,9 +7,12 @@
 namespace muon {
 
 constexpr int64_t kLayerMaxPairs = 1 << 14, kLayerMaxWidth = 1 << 17;
+// Rows further apart than this would leave the 32 bits of a lane's offset.
+constexpr int64_t kLayerMaxStride = 1 << 24;
 constexpr int kLayerMaxTop = 64, kLayerMaxExperts = 4096;
 constexpr int kLayerRows = 32;                   // rows of the summed axis that a wave takes at a time
 constexpr int kLayerWaves = 4;                   // of a block, which share its run of the summed axis
+constexpr int kLayerStage = 32768;               // bytes of LDS for the second product's operand, where it is made from sums of runs
 
 struct LayerShape {
   int64_t tokens, width, inner;
@@ -23,12 +26,14 @@ struct LayerProduct {
   int tiles;                                     // of columns
   int runs;
   int64_t run;                                   // rows of the summed axis in a run, a multiple of kLayerRows
+  int mats;                                      // matrices with blocks of their own: 2 where gate and up are summed in runs
 };
 
 struct LayerPlan {
   int slots;                                     // experts that may have pairs: one per pair, or all of them
   bool slot_is_pair;
   LayerProduct up, down;
+  bool staged;                                   // the second product makes its operand itself
   // byte offsets of the workspace's sections: sums of the first product in runs, the inner rows, sums of the second product
   size_t part, inner, rows;
   size_t total;
@@ -38,16 +43,21 @@ LayerPlan layer_plan(const LayerShape& s);
 
 inline int layer_columns(bool f32) { return f32 ? 64 : 128; }
 
-inline LayerProduct layer_product(int64_t k, int64_t n, int columns, int64_t slots) {
+// Blocks that the chip holds at a time.
+constexpr int64_t kLayerBlocks = 512;
+
+// One run where its blocks fill the chip; otherwise as many as it holds at a time, so that all of a product's loads are on their way at once, but none
+// below what its waves take at once.
+inline LayerProduct layer_product(int64_t k, int64_t n, int columns, int64_t slots, int mats) {
   LayerProduct p{};
   p.k = k;
   p.n = n;
   p.tiles = (int)((n + columns - 1) / columns);
-  // blocks enough to fill 256 compute units twice, but no run below what its waves take at once
-  const int64_t blocks = std::max<int64_t>(1, slots * p.tiles), want = std::max<int64_t>(1, (512 + blocks - 1) / blocks);
-  const int64_t least = kLayerRows * kLayerWaves, most = std::max<int64_t>(1, k / least), runs = std::min<int64_t>({want, most, 16});
+  const int64_t blocks = std::max<int64_t>(1, slots * p.tiles * mats), least = kLayerRows * kLayerWaves;
+  const int64_t runs = std::min<int64_t>({std::max<int64_t>(1, kLayerBlocks / blocks), std::max<int64_t>(1, k / least), 16});
   p.run = ((k + runs - 1) / runs + kLayerRows - 1) / kLayerRows * kLayerRows;
   p.runs = (int)((k + p.run - 1) / p.run);
+  p.mats = p.runs > 1 ? mats : 1;
   return p;
 }
 
@@ -56,8 +66,9 @@ inline LayerPlan layer_plan(const LayerShape& s) {
   const int64_t pairs = s.tokens * s.top;
   p.slot_is_pair = pairs <= s.experts;
   p.slots = (int)(p.slot_is_pair ? pairs : s.experts);
-  p.up = layer_product(s.width, s.inner, layer_columns(s.f32), p.slots);
-  p.down = layer_product(s.inner, s.width, layer_columns(s.f32), p.slots);
+  p.up = layer_product(s.width, s.inner, layer_columns(s.f32), p.slots, s.gated ? 2 : 1);
+  p.down = layer_product(s.inner, s.width, layer_columns(s.f32), p.slots, 1);
+  p.staged = p.up.runs > 1 && p.down.run * 32 * (s.f32 ? 4 : 2) <= kLayerStage;
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t here = at;
@@ -65,7 +76,7 @@ inline LayerPlan layer_plan(const LayerShape& s) {
     return here;
   };
   p.part = take(p.up.runs > 1 ? (int64_t)p.up.runs * pairs * (s.gated ? 2 : 1) * s.inner * 4 : 0);
-  p.inner = take(pairs * s.inner * (s.f32 ? 4 : 2));
+  p.inner = take(p.staged ? 0 : pairs * s.inner * (s.f32 ? 4 : 2));
   p.rows = take((int64_t)p.down.runs * pairs * s.width * 4);
   p.total = std::max<size_t>(at, 256);
   return p;

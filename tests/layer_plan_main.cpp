@@ -20,7 +20,9 @@ static void product(const LayerProduct& g, int64_t k, int64_t n, bool f32, int s
   CHECK(g.k == k && g.n == n && g.runs >= 1 && g.run % kLayerRows == 0);
   CHECK((g.runs - 1) * g.run < k && g.runs * g.run >= k);          // no run is empty
   CHECK((int64_t)g.tiles * layer_columns(f32) >= n && (int64_t)(g.tiles - 1) * layer_columns(f32) < n);
-  CHECK((int64_t)slots * g.tiles * g.runs < (int64_t{1} << 24));
+  CHECK((int64_t)slots * g.tiles * g.runs * g.mats < (int64_t{1} << 24));
+  CHECK(g.mats == 1 || (g.mats == 2 && g.runs > 1));
+  CHECK(g.runs == 1 || (int64_t)slots * g.tiles * g.runs * g.mats <= kLayerBlocks);
 }
 
 static void walk(const LayerShape& s) {
@@ -30,7 +32,8 @@ static void walk(const LayerShape& s) {
   product(p.up, s.width, s.inner, s.f32, p.slots);
   product(p.down, s.inner, s.width, s.f32, p.slots);
   const size_t part = p.up.runs > 1 ? (size_t)p.up.runs * pairs * (s.gated ? 2 : 1) * s.inner * 4 : 0;
-  CHECK(p.part == 0 && p.inner >= part && p.rows >= p.inner + (size_t)pairs * s.inner * (s.f32 ? 4 : 2));
+  CHECK(p.part == 0 && p.inner >= part && p.rows >= p.inner + (p.staged ? 0 : (size_t)pairs * s.inner * (s.f32 ? 4 : 2)));
+  CHECK(!p.staged || (p.up.runs > 1 && p.down.run * 32 * (s.f32 ? 4 : 2) <= kLayerStage));
   CHECK(p.total >= p.rows + (size_t)p.down.runs * pairs * s.width * 4 && p.total < (size_t{1} << 42));
   CHECK(p.inner % 256 == 0 && p.rows % 256 == 0);
   for (const int64_t n : {s.inner, s.width}) CHECK((n + 255) / 256 * pairs < (int64_t{1} << 24));

@@ -50,7 +50,11 @@ def test_call_refusals():
     m = binding.muon_matrices
     assert call(args(up=m(None, 2048, 32))) == call(args(down=m(None, 2048, 64))) == -1
     assert call(args(up=m(FAKE, 2048, 31))) == call(args(down=m(FAKE, 2048, 63))) == call(args(down=m(FAKE, -1, 64))) == -1
+    far = (1 << 24) + 1
+    assert call(args(up=m(FAKE, 2048, far))) == call(args(down=m(FAKE, 2048, far))) == -1
     g = args()
+    g.gate = m(FAKE, 2048, far)
+    assert call(g) == -1
     g.gate = m(FAKE, 2048, 31)
     assert call(g) == -1
     g.gate = m(FAKE + 1, 2048, 32)
