@@ -61,7 +61,8 @@ bool overlap(const muon_grad* grads, int32_t n) {
   return false;
 }
 
-int run_norm(const muon_grad* grads, int32_t n, double max_norm, double* norm, float* scale, void* workspace, size_t workspace_bytes,
+// in_place: and scales the gradients.
+int run_norm(const muon_grad* grads, int32_t n, double max_norm, double* norm, float* scale, bool in_place, void* workspace, size_t workspace_bytes,
              hipStream_t s) {
   if (!(max_norm >= 0.0) || !norm) return MUON_E_INVALID_ARG;
   if (!aligned(norm, 8) || !aligned(scale, 4) || !aligned(workspace, 8)) return MUON_E_MISALIGNED;
@@ -72,16 +73,16 @@ int run_norm(const muon_grad* grads, int32_t n, double max_norm, double* norm, f
   GradCursor at;
   int64_t done = 0;
   while (const int blocks = grad_next_batch(grads, n, at, b)) {
-    MUON_HIP(launch_grad_squares(b, blocks, partial + done, s));
+    MUON_HIP(launch_grad_squares(b, blocks, in_place, partial + done, s));
     done += blocks;
+    if (in_place && blocks == partials && blocks <= kGradFew) {
+      MUON_HIP(launch_grad_norm_scale(b, blocks, partial, blocks, max_norm, norm, scale, s));
+      return MUON_OK;
+    }
   }
   MUON_HIP(launch_grad_norm(partial, partials, max_norm, norm, scale, s));
-  return MUON_OK;
-}
-
-int run_scale(const muon_grad* grads, int32_t n, const float* scale, hipStream_t s) {
-  GradBatch b{};
-  GradCursor at;
+  if (!in_place) return MUON_OK;
+  at = GradCursor{};
   while (const int blocks = grad_next_batch(grads, n, at, b)) MUON_HIP(launch_grad_scale(b, blocks, scale, s));
   return MUON_OK;
 }
@@ -103,7 +104,7 @@ int muon_grad_norm(const muon_grad* grads, int32_t n, double max_norm, double* n
                    void* hip_stream) {
   return guarded([&]() -> int {
     if (int st = check_list(grads, n)) return st;
-    return run_norm(grads, n, max_norm, norm, scale, workspace, workspace_bytes, static_cast<hipStream_t>(hip_stream));
+    return run_norm(grads, n, max_norm, norm, scale, false, workspace, workspace_bytes, static_cast<hipStream_t>(hip_stream));
   });
 }
 
@@ -112,7 +113,10 @@ int muon_grad_scale(const muon_grad* grads, int32_t n, const float* scale, void*
     if (int st = check_list(grads, n)) return st;
     if (!scale || overlap(grads, n)) return MUON_E_INVALID_ARG;
     if (!aligned(scale, 4)) return MUON_E_MISALIGNED;
-    return run_scale(grads, n, scale, static_cast<hipStream_t>(hip_stream));
+    GradBatch b{};
+    GradCursor at;
+    while (const int blocks = grad_next_batch(grads, n, at, b)) MUON_HIP(launch_grad_scale(b, blocks, scale, static_cast<hipStream_t>(hip_stream)));
+    return MUON_OK;
   });
 }
 
@@ -121,9 +125,7 @@ int muon_grad_clip(const muon_grad* grads, int32_t n, double max_norm, double* n
   return guarded([&]() -> int {
     if (int st = check_list(grads, n)) return st;
     if (!scale || overlap(grads, n)) return MUON_E_INVALID_ARG;
-    const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    if (int st = run_norm(grads, n, max_norm, norm, scale, workspace, workspace_bytes, s)) return st;
-    return run_scale(grads, n, scale, s);
+    return run_norm(grads, n, max_norm, norm, scale, true, workspace, workspace_bytes, static_cast<hipStream_t>(hip_stream));
   });
 }
 
