@@ -134,14 +134,25 @@ def combine_backward(d_out: torch.Tensor, rows: torch.Tensor, weights: torch.Ten
     return d_rows, d_weights
 
 
-def _matrices(name: str, t: torch.Tensor, experts: int, rows: int, columns: int, dtype: torch.dtype) -> "binding.muon_matrices":
-    if t.dim() != 3 or tuple(t.shape) != (experts, rows, columns):
-        raise MuonError(-1, f"{name}: [{experts}, {rows}, {columns}], not {tuple(t.shape)}")
+def _matrices(name: str, t: torch.Tensor, shape: Tuple[int, int, int], dtype: torch.dtype) -> "binding.muon_matrices":
+    if t.shape != shape:
+        raise MuonError(-1, f"{name}: {list(shape)}, not {tuple(t.shape)}")
     if t.dtype != dtype:
         raise MuonError(-2, f"{name}: {dtype} as x, not {t.dtype}")
-    if t.stride(2) != 1 and columns > 1:
+    experts, rows, columns = shape
+    expert_stride, row_stride, stride = t.stride()
+    if stride != 1 and columns > 1:
         raise MuonError(-1, f"{name}: rows must be contiguous")
-    return binding.muon_matrices(t.data_ptr(), t.stride(0) if experts > 1 else 0, t.stride(1) if rows > 1 else columns)
+    return binding.muon_matrices(t.data_ptr(), expert_stride if experts > 1 else 0, row_stride if rows > 1 else columns)
+
+
+_none = binding.muon_matrices(None, 0, 0)
+_some = binding.muon_matrices(256, 0, 0)                    # (a size goes by whether there is a gate)
+
+
+@lru_cache(maxsize=256)
+def _layer_bytes(gated: bool, *sizes: int) -> int:
+    return binding.muon_expert_layer_bytes(binding.muon_layer(_some if gated else _none, _none, _none, *sizes, 0))
 
 
 def layer(x: torch.Tensor, up: torch.Tensor, down: torch.Tensor, expert: torch.Tensor, weights: Optional[torch.Tensor] = None,
@@ -156,7 +167,8 @@ def layer(x: torch.Tensor, up: torch.Tensor, down: torch.Tensor, expert: torch.T
         raise MuonError(-1, f"expert: contiguous [tokens, top], not {tuple(expert.shape)}")
     if expert.dtype not in (torch.int32, torch.int64):
         raise MuonError(-2, f"expert: int32 or int64, not {expert.dtype}")
-    if activation not in binding.ACTIVATIONS:
+    act = binding.ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError(f"activation must be one of {sorted(binding.ACTIVATIONS)}")
     device = _device(x, up, down, expert, weights, gate)
     tokens, top = expert.shape
@@ -164,15 +176,16 @@ def layer(x: torch.Tensor, up: torch.Tensor, down: torch.Tensor, expert: torch.T
     if up.dim() != 3:
         raise MuonError(-1, f"up: [experts, {width}, inner], not {tuple(up.shape)}")
     experts, _, inner = up.shape
-    none = binding.muon_matrices(None, 0, 0)
-    args = binding.muon_layer(none if gate is None else _matrices("gate", gate, experts, width, inner, x.dtype),
-                              _matrices("up", up, experts, width, inner, x.dtype), _matrices("down", down, experts, inner, width, x.dtype),
-                              tokens, width, inner, top, experts, binding.dtype_code(x.dtype), binding.ACTIVATIONS[activation], 0)
+    dtype, wide = x.dtype, (experts, width, inner)
+    sizes = (tokens, width, inner, top, experts, binding.dtype_code(dtype), act)
+    args = binding.muon_layer(_none if gate is None else _matrices("gate", gate, wide, dtype), _matrices("up", up, wide, dtype),
+                              _matrices("down", down, (experts, inner, width), dtype), *sizes, 0)
     at = 0 if weights is None else _weights(weights, expert)
-    outside_autograd("experts.layer", any(t is not None and t.requires_grad for t in (x, up, down, weights, gate)))
-    need = binding.muon_expert_layer_bytes(args)
+    outside_autograd("experts.layer", x.requires_grad or up.requires_grad or down.requires_grad or
+                     (weights is not None and weights.requires_grad) or (gate is not None and gate.requires_grad))
+    need = _layer_bytes(gate is not None, *sizes)
     with on(device):
-        out = torch.empty(tokens, width, dtype=x.dtype, device=device)
+        out = torch.empty(tokens, width, dtype=dtype, device=device)
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
         binding.muon_expert_layer(args, x.data_ptr(), stride, expert.data_ptr(), expert.element_size(), at, out.data_ptr(),
                                   workspace.data_ptr(), need, stream_handle(device))
