@@ -378,19 +378,23 @@ int muon_distill(const muon_head* head, const void* index, int32_t index_bytes, 
  * among the top + 4 that fp32 sums find largest (and whatever is as large as the last of these); logits that are NaN come last.
  * Types, precision, pieces of tokens and what may run when are those of muon_cross_entropy; the log probabilities' own logits are summed in
  * double, dz is rounded to bf16 once.  lse_rest is what fp32 leaves of lse.
+ * kept: device memory of the caller's (256-byte aligned, muon_log_probs_kept_bytes: 2 bytes per token and vocabulary entry, fp32 4) in which a forward
+ * call without alternatives leaves what the backward call reads instead of making the logits once more, as often as it is called; null for none.
  */
+int muon_log_probs_kept_bytes(const muon_head* head, size_t* out);
 /* Bytes of workspace (256-byte aligned) of muon_log_probs; top: 0 (no alternatives) .. min(64, vocab); max_bytes as above.
  * muon_log_probs_backward takes muon_head_workspace_bytes(head, 1, gradients, ..). */
 int muon_log_probs_bytes(const muon_head* head, int32_t top, size_t max_bytes, size_t* out);
 /* targets: [tokens] of targets_bytes (4 or 8) each, or null, and log_prob then too.  log_prob, entropy, lse, lse_rest: [tokens]; top_index,
  * top_log_prob: [tokens, top], null where top is 0. */
 int muon_log_probs(const muon_head* head, const void* targets, int32_t targets_bytes, int32_t top, double temperature, float* log_prob, float* entropy,
-                   float* lse, float* lse_rest, int64_t* top_index, float* top_log_prob, void* workspace, size_t workspace_bytes, void* hip_stream);
+                   float* lse, float* lse_rest, int64_t* top_index, float* top_log_prob, void* kept, size_t kept_bytes, void* workspace,
+                   size_t workspace_bytes, void* hip_stream);
 /* lse, lse_rest, entropy: as muon_log_probs left them for the same head, targets and temperature.  d_log_prob: [tokens], null with null targets;
  * d_entropy: [tokens] or null (0).  d_hidden, d_weight: dense, overwritten, or null where not wanted. */
 int muon_log_probs_backward(const muon_head* head, const void* targets, int32_t targets_bytes, double temperature, const float* lse, const float* lse_rest,
-                            const float* entropy, const float* d_log_prob, const float* d_entropy, void* d_hidden, void* d_weight, void* workspace,
-                            size_t workspace_bytes, void* hip_stream);
+                            const float* entropy, const float* d_log_prob, const float* d_entropy, const void* kept, size_t kept_bytes, void* d_hidden,
+                            void* d_weight, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
  * A mixture's tokens to their experts and back.  muon_expert_sort ranks the tokens' pairs (token t, choice j) by expert, pairs of one expert

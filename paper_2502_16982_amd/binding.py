@@ -33,6 +33,7 @@ EXPORTS = (
     "muon_expert_sort_bytes", "muon_expert_sort", "muon_expert_dispatch", "muon_expert_combine", "muon_expert_combine_backward",
     "muon_step_scaled", "muon_adamw_step_scaled", "muon_grad_norm_bytes", "muon_grad_norm", "muon_grad_scale", "muon_grad_clip",
     "muon_expert_layer_bytes", "muon_expert_layer", "muon_log_probs_bytes", "muon_log_probs", "muon_log_probs_backward",
+    "muon_log_probs_kept_bytes",
 )
 PROF_NAMES = ("momentum_norm_cast", "norm_finalize", "gram", "poly", "apply_poly", "weight_update", "update_rms")
 
@@ -193,11 +194,13 @@ def lib() -> C.CDLL:
     L.muon_expert_layer.restype = C.c_int
     L.muon_log_probs_bytes.argtypes = [P(muon_head), C.c_int32, C.c_size_t, P(C.c_size_t)]
     L.muon_log_probs_bytes.restype = C.c_int
+    L.muon_log_probs_kept_bytes.argtypes = [P(muon_head), P(C.c_size_t)]
+    L.muon_log_probs_kept_bytes.restype = C.c_int
     L.muon_log_probs.argtypes = [P(muon_head), C.c_void_p, C.c_int32, C.c_int32, C.c_double, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
-                                 C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+                                 C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t, C.c_void_p]
     L.muon_log_probs.restype = C.c_int
     L.muon_log_probs_backward.argtypes = [P(muon_head), C.c_void_p, C.c_int32, C.c_double, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
-                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+                                          C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     L.muon_log_probs_backward.restype = C.c_int
     _LIB = L
     return L
@@ -460,18 +463,25 @@ def muon_log_probs_bytes(head: muon_head, top: int, max_bytes: int = 0) -> int:
 
 
 def muon_log_probs(head: muon_head, targets_ptr: int, targets_bytes: int, top: int, temperature: float, log_prob_ptr: int, entropy_ptr: int,
-                   lse_ptr: int, lse_rest_ptr: int, top_index_ptr: int, top_log_prob_ptr: int, workspace_ptr: int, workspace_bytes: int,
-                   stream_ptr: int = 0) -> None:
+                   lse_ptr: int, lse_rest_ptr: int, top_index_ptr: int, top_log_prob_ptr: int, kept_ptr: int, kept_bytes: int, workspace_ptr: int,
+                   workspace_bytes: int, stream_ptr: int = 0) -> None:
     _check(lib().muon_log_probs(C.byref(head), targets_ptr, targets_bytes, top, temperature, log_prob_ptr, entropy_ptr, lse_ptr, lse_rest_ptr,
-                                top_index_ptr, top_log_prob_ptr, workspace_ptr, workspace_bytes, stream_ptr), "muon_log_probs")
+                                top_index_ptr, top_log_prob_ptr, kept_ptr, kept_bytes, workspace_ptr, workspace_bytes, stream_ptr),
+           "muon_log_probs")
+
+
+def muon_log_probs_kept_bytes(head: muon_head) -> int:
+    out = C.c_size_t(0)
+    _check(lib().muon_log_probs_kept_bytes(C.byref(head), C.byref(out)), "muon_log_probs_kept_bytes")
+    return int(out.value)
 
 
 def muon_log_probs_backward(head: muon_head, targets_ptr: int, targets_bytes: int, temperature: float, lse_ptr: int, lse_rest_ptr: int,
-                            entropy_ptr: int, d_log_prob_ptr: int, d_entropy_ptr: int, d_hidden_ptr: int, d_weight_ptr: int,
-                            workspace_ptr: int, workspace_bytes: int, stream_ptr: int = 0) -> None:
+                            entropy_ptr: int, d_log_prob_ptr: int, d_entropy_ptr: int, kept_ptr: int, kept_bytes: int, d_hidden_ptr: int,
+                            d_weight_ptr: int, workspace_ptr: int, workspace_bytes: int, stream_ptr: int = 0) -> None:
     _check(lib().muon_log_probs_backward(C.byref(head), targets_ptr, targets_bytes, temperature, lse_ptr, lse_rest_ptr, entropy_ptr,
-                                         d_log_prob_ptr, d_entropy_ptr, d_hidden_ptr, d_weight_ptr, workspace_ptr, workspace_bytes,
-                                         stream_ptr), "muon_log_probs_backward")
+                                         d_log_prob_ptr, d_entropy_ptr, kept_ptr, kept_bytes, d_hidden_ptr, d_weight_ptr, workspace_ptr,
+                                         workspace_bytes, stream_ptr), "muon_log_probs_backward")
 
 
 def muon_expert_sort_bytes(tokens: int, top: int, experts: int) -> int:

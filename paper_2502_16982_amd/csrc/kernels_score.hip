@@ -10,7 +10,8 @@
 // second may be among them is looked at again, so an eighth of the logits' own size is written and read.  One block per token then joins
 // all of it.  Which alternatives come first is decided by logits that are summed in double, as the given token's is: in fp32 sums the order of two
 // that are nearly alike would depend on the tiles.
-// Backward: with lse known the product is done again and its epilogue writes the logits' gradient itself; the other two products are the losses'.
+// Backward: where the forward call kept its powers (f16 under each block's own top; fp32: the logits), one pass makes the logits' gradient of them;
+// else, with lse known, the product is done again and its epilogue writes the gradient itself.  The other two products are the losses'.
 #include <hip/hip_runtime.h>
 
 #include <atomic>
@@ -89,10 +90,10 @@ constexpr float kFarBelow = -1e4f;               // 2^this is 0: an infinite exp
 // Groups of a token in order of (64 vocabulary entries, half): a lane's 32 accumulators of a column, in two MFMA tiles.
 __device__ __forceinline__ int place_row(int place, int half) { return 32 * (place >> 4) + 8 * ((place >> 2) & 3) + 4 * half + (place & 3); }
 
-template <int B, int S, bool BEST>
+// KEEP: 1 the powers in f16, up to 2^15 in a block, 2 the logits in fp32, 0 neither.
+template <int B, int S, bool BEST, int KEEP>
 __device__ __forceinline__ void score_tile(const HeadOperand& weight, const HeadOperand& hidden, const HeadTiles& g, float unit, ScoreStats* stats,
-                                           ScoreBest* best, long long row0, long long col0,
-                                           unsigned char* smem) {
+                                           ScoreBest* best, const ScoreKept& kept, long long row0, long long col0, unsigned char* smem) {
   using T = Tile<B, B, false, false, S>;
   T tile;
   tile.run(weight, hidden, row0, col0, g.k, g.pairs, 0, g.slabs_per_split, smem);
@@ -101,10 +102,31 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
   const int there = (int)(weight.rows - v0 < T::WM ? weight.rows - v0 : T::WM);      // rows of the wave's that there are
   auto row = [&](int i, int v) { return 32 * i + 8 * (v / 4) + 4 * fh + v % 4; };
   // in LDS: what two waves tell each other, then what leaves, a token's neighbouring entries in whole lines
+  // (in tiles of 128 behind the powers' image, in tiles of 256 after it)
   constexpr int kGroups = B / kScoreGroup, kBlocks = B / kHeadGrain;
-  float* notes = reinterpret_cast<float*>(smem);
-  ScoreStats* sheet = reinterpret_cast<ScoreStats*>(smem + 2048);                    // [column][block]
-  ScoreBest* image = reinterpret_cast<ScoreBest*>(smem + 2048 + B * kBlocks * 16);   // [column][group]
+  static_assert(KEEP == 0 || !BEST, "one of both");
+  unsigned char* room = smem + (B == 128 ? T::kStage : 0);
+  float* notes = reinterpret_cast<float*>(room);
+  ScoreStats* sheet = reinterpret_cast<ScoreStats*>(room + 2048);                    // [column][block]
+  ScoreBest* image = reinterpret_cast<ScoreBest*>(room + 2048 + B * kBlocks * 16);   // [column][group]
+  if constexpr (KEEP == 2) {
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+      const long long token = col0 + tile.wn * T::WN + 32 * j + fr;
+      if (token >= hidden.rows) continue;
+      float* z = static_cast<float*>(kept.values) + token * kept.pitch + v0 + 4 * fh;
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          f32x4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = tile.acc[i][j][4 * q + e];
+          *reinterpret_cast<f32x4*>(z + 32 * i + 8 * q) = x;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+  }
   float top[T::FN];
   auto find_top = [&](auto masked) {             // MASKED: not all rows of the wave's are there
 #pragma unroll
@@ -149,20 +171,22 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
   auto take_powers = [&](auto masked) {
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
-      top[j] = top[j] == -INFINITY ? 0.f : unit * top[j];
+      top[j] = (top[j] == -INFINITY ? 0.f : unit * top[j]) - (KEEP == 1 ? kProbTop : 0.f);
       float sum = 0.f, slope = 0.f;
 #pragma unroll
       for (int i = 0; i < T::FM; ++i)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
+          float x[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float y = fmaf(unit, tile.acc[i][j][4 * q + e], -top[j]);
-            float x = __builtin_amdgcn_exp2f(y);
-            if (decltype(masked)::value && row(i, 4 * q + e) >= there) x = 0.f;
-            sum += x;
-            slope = fmaf(x, fmaxf(y, kFarBelow), slope);
+            x[e] = __builtin_amdgcn_exp2f(y);
+            if (decltype(masked)::value && row(i, 4 * q + e) >= there) x[e] = 0.f;
+            sum += x[e];
+            slope = fmaf(x[e], fmaxf(y, kFarBelow), slope);
           }
+          if constexpr (KEEP == 1) tile.put(smem, i, j, q, u32x2{pack_f16(x[0], x[1]), pack_f16(x[2], x[3])});
           __builtin_amdgcn_sched_barrier(0);
         }
       sums[j] = sum + __shfl_xor(sum, 32, 64);
@@ -177,6 +201,13 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
   };
   if (there >= T::WM) take_powers(std::false_type{});
   else take_powers(std::true_type{});
+  if constexpr (KEEP == 1) {
+    __syncthreads();
+    tile.image_out(smem, [&](int c, int r, u32x4 v) {
+      if (col0 + c < hidden.rows) *reinterpret_cast<u32x4*>(static_cast<u16*>(kept.values) + (col0 + c) * kept.pitch + row0 + r) = v;
+    });
+    if constexpr (B == 256) __syncthreads();
+  }
   if constexpr (B == 128) __syncthreads();
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
@@ -192,7 +223,10 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
   const long long blocks = (weight.rows + kHeadGrain - 1) / kHeadGrain;
   for (int i = threadIdx.x; i < B * kBlocks; i += 256) {
     const long long token = col0 + i / kBlocks, block = row0 / kHeadGrain + i % kBlocks;
-    if (token < hidden.rows && block < blocks) stats[token * blocks + block] = sheet[i];
+    if (token < hidden.rows && block < blocks) {
+      stats[token * blocks + block] = sheet[i];
+      if constexpr (KEEP == 1) kept.tops[token * blocks + block] = sheet[i].top;
+    }
   }
   if constexpr (BEST) {
 #pragma unroll
@@ -205,20 +239,20 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
   }
 }
 
-template <int B, int S, bool BEST>
+template <int B, int S, bool BEST, int KEEP>
 __global__ __launch_bounds__(256, B == 128 && S == 2 ? 2 : 1) void score_logits_kernel(HeadOperand weight, HeadOperand hidden, HeadTiles g, float unit,
-                                                                             ScoreStats* __restrict__ stats, ScoreBest* __restrict__ best) {
+                                                                             ScoreStats* __restrict__ stats, ScoreBest* __restrict__ best, ScoreKept kept) {
 #if defined(__HIP_DEVICE_COMPILE__)            // (the host's pass knows no buffer descriptors)
   extern __shared__ __align__(16) unsigned char smem[];
   const TileAt at = tile_at(g);
   long long row0 = (long long)at.m * B, col0 = (long long)at.n * B;
   if (B == 128 || at.quarter < 0) {
-    score_tile<B, S, BEST>(weight, hidden, g, unit, stats, best, row0, col0, smem);
+    score_tile<B, S, BEST, KEEP>(weight, hidden, g, unit, stats, best, kept, row0, col0, smem);
   } else if constexpr (B == 256) {
     row0 += 128 * (at.quarter >> 1);
     col0 += 128 * (at.quarter & 1);
     if (row0 < weight.rows && col0 < hidden.rows)
-      score_tile<128, 4, BEST>(weight, hidden, g, unit, stats, best, row0, col0, smem);
+      score_tile<128, 4, BEST, KEEP>(weight, hidden, g, unit, stats, best, kept, row0, col0, smem);
   }
 #endif
 }
@@ -541,6 +575,58 @@ __global__ __launch_bounds__(256) void score_prepare_kernel(ScoreTarget t, float
   }
 }
 
+// The logits' gradient from what the forward call kept, by spans of a token's row.  Bound by memory: 2 bytes in and 2 out, fp32 4 and 6.
+constexpr int kDzSpan = 4096;
+template <bool F32>
+__global__ __launch_bounds__(256) void score_dz_kernel(ScoreTarget t, float unit, ScoreKept kept, long long blocks, ScoreCoef c, long long vocab, int spans,
+                                                       u16* __restrict__ grad, long long pitch, long long plane) {
+  const long long token = blockIdx.x / spans, v0 = (long long)(blockIdx.x % spans) * kDzSpan, row = token * pitch;
+  const float a = c.a[token], b = c.b[token];
+  const float2 l2 = c.log2sum[token];
+  const bool some = l2.x < INFINITY || l2.x != l2.x;     // (infinite: no gradient)
+  for (long long v = v0 + threadIdx.x * 8; v < v0 + kDzSpan && v < pitch; v += 2048) {
+    Row8 r{};
+    if (some && v < vocab) {
+      float y[8], p[8];
+      if constexpr (F32) {
+        const f32x4* z = reinterpret_cast<const f32x4*>(static_cast<const float*>(kept.values) + row + v);
+        const f32x4 two[2] = {z[0], z[1]};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          y[e] = fmaxf(fmaf(unit, two[e / 4][e % 4], -l2.x) - l2.y, kFarBelow);
+          p[e] = __builtin_amdgcn_exp2f(y[e]);
+        }
+      } else {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const u16*>(kept.values) + row + v);
+        const float shift = (kept.tops[token * blocks + v / kHeadGrain] - l2.x) - l2.y, f = __builtin_amdgcn_exp2f(shift);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const unsigned pair = w[e / 2];                // (a bit cast of the vector's element itself would take its first)
+          const f16x2 both = __builtin_bit_cast(f16x2, pair);
+          const float x = (float)both[e & 1];
+          p[e] = f * x;
+          y[e] = b == 0.f ? 0.f : fmaxf(__builtin_amdgcn_logf(x) + shift, kFarBelow);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r.v[e] = v + e < vocab ? -p[e] * fmaf(b, y[e], a) : 0.f;
+    }
+    store_planes8<F32>(r, grad + row + v, plane);
+  }
+  if (!some || !t.index) return;
+  __syncthreads();                                       // the target's entry goes over what this block wrote
+  const long long y = target_at(t, token);
+  if (threadIdx.x == 0 && y >= v0 && y < v0 + kDzSpan && y < vocab) {
+    float x = c.value[token];
+#pragma unroll
+    for (int q = 0; q < (F32 ? 3 : 1); ++q) {
+      const u16 bits = bf16_bits(x);
+      grad[q * plane + row + y] = bits;
+      x -= bf16_value(bits);
+    }
+  }
+}
+
 template <int B, int S, bool F32>
 __device__ __forceinline__ void score_grad_tile(const HeadOperand& weight, const HeadOperand& hidden, const HeadTiles& g, float unit, const ScoreTarget& t,
                                                 const ScoreCoef& c, u16* grad, long long pitch, long long plane, long long row0, long long col0,
@@ -632,22 +718,24 @@ __global__ __launch_bounds__(256, B == 128 && S == 2 ? 2 : 1) void score_grad_ke
 
 }  // namespace
 
-template <int B, int S, bool BEST>
+template <int B, int S, bool BEST, int KEEP>
 hipError_t score_logits_of(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, ScoreStats* stats,
-                           ScoreBest* best, hipStream_t s) {
+                           ScoreBest* best, const ScoreKept& kept, hipStream_t s) {
   constexpr int lds = Tile<B, B, false, false, S>::kLds;
   static std::atomic<uint64_t> done{0};
-  if (hipError_t e = allow_lds(done, reinterpret_cast<const void*>(&score_logits_kernel<B, S, BEST>), lds)) return e;
-  score_logits_kernel<B, S, BEST><<<(unsigned)g.blocks(), 256, lds, s>>>(weight, hidden, tiles_of(g, pairs), unit, stats, best);
+  if (hipError_t e = allow_lds(done, reinterpret_cast<const void*>(&score_logits_kernel<B, S, BEST, KEEP>), lds)) return e;
+  score_logits_kernel<B, S, BEST, KEEP><<<(unsigned)g.blocks(), 256, lds, s>>>(weight, hidden, tiles_of(g, pairs), unit, stats, best, kept);
   return hipGetLastError();
 }
 
 hipError_t launch_score_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, ScoreStats* stats,
-                               ScoreBest* best, hipStream_t s) {
-#define MUON_SCORE_CASE(B, S)                                                                                             \
-  if (g.tile == B && (g.alone ? 4 : 2) == S)                                                                              \
-    return best ? score_logits_of<B, S, true>(weight, hidden, g, pairs, unit, stats, best, s)   \
-                : score_logits_of<B, S, false>(weight, hidden, g, pairs, unit, stats, best, s)
+                               ScoreBest* best, const ScoreKept& kept, hipStream_t s) {
+#define MUON_SCORE_CASE(B, S)                                                                                                       \
+  if (g.tile == B && (g.alone ? 4 : 2) == S)                                                                                        \
+    return best          ? score_logits_of<B, S, true, 0>(weight, hidden, g, pairs, unit, stats, best, kept, s)                     \
+           : !kept.values ? score_logits_of<B, S, false, 0>(weight, hidden, g, pairs, unit, stats, best, kept, s)                   \
+           : kept.tops    ? score_logits_of<B, S, false, 1>(weight, hidden, g, pairs, unit, stats, best, kept, s)                   \
+                          : score_logits_of<B, S, false, 2>(weight, hidden, g, pairs, unit, stats, best, kept, s)
   MUON_SCORE_CASE(256, 2);
   MUON_SCORE_CASE(128, 2);
   MUON_SCORE_CASE(128, 4);
@@ -705,6 +793,16 @@ hipError_t launch_score_grad(const HeadOperand& weight, const HeadOperand& hidde
   MUON_SCORE_CASE(128, 4);
 #undef MUON_SCORE_CASE
   return hipErrorInvalidValue;
+}
+
+hipError_t launch_score_dz(const ScoreTarget& t, float unit, const ScoreKept& kept, long long blocks, const ScoreCoef& c, long long tokens, long long vocab, bool f32,
+                           uint16_t* grad, long long pitch, long long plane, hipStream_t s) {
+  const int spans = (int)((pitch + kDzSpan - 1) / kDzSpan);
+  auto go = [&](auto kernel) {
+    kernel<<<(unsigned)(tokens * spans), 256, 0, s>>>(t, unit, kept, blocks, c, vocab, spans, grad, pitch, plane);
+    return hipGetLastError();
+  };
+  return f32 ? go(score_dz_kernel<true>) : go(score_dz_kernel<false>);
 }
 
 }  // namespace muon

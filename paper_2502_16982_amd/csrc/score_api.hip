@@ -33,6 +33,13 @@ bool temperature_fits(double tau) {
 
 const void* behind(const void* p, int64_t bytes) { return p ? static_cast<const unsigned char*>(p) + bytes : nullptr; }
 
+ScoreKept kept_from(const HeadShape& s, const HeadPlan& p, void* kept, int64_t t0) {
+  if (!kept) return {nullptr, 0, nullptr};
+  unsigned char* at = static_cast<unsigned char*>(kept);
+  float* tops = s.f32 ? nullptr : reinterpret_cast<float*>(at + score_kept_values(s)) + t0 * p.blocks;
+  return {at + t0 * p.vocab_pitch * (s.f32 ? 4 : 2), p.vocab_pitch, tops};
+}
+
 struct Scale {
   float inv_tau, unit;
 };
@@ -72,19 +79,31 @@ int muon_log_probs_bytes(const muon_head* head, int32_t top, size_t max_bytes, s
   });
 }
 
+int muon_log_probs_kept_bytes(const muon_head* head, size_t* out) {
+  return guarded([&]() -> int {
+    HeadShape s;
+    if (!out) return MUON_E_INVALID_ARG;
+    if (int st = score_shape(head, false, false, &s)) return st;
+    *out = score_kept_bytes(s);
+    return MUON_OK;
+  });
+}
+
 int muon_log_probs(const muon_head* h, const void* targets, int32_t targets_bytes, int32_t top, double temperature, float* log_prob, float* entropy,
-                   float* lse, float* lse_rest, int64_t* top_index, float* top_log_prob, void* workspace, size_t workspace_bytes, void* hip_stream) {
+                   float* lse, float* lse_rest, int64_t* top_index, float* top_log_prob, void* kept, size_t kept_bytes, void* workspace,
+                   size_t workspace_bytes, void* hip_stream) {
   return guarded([&]() -> int {
     HeadShape s;
     if (int st = score_shape(h, false, false, &s)) return st;
-    if ((targets_bytes != 4 && targets_bytes != 8) || top < 0 || top > kScoreMaxTop || top > s.vocab || !temperature_fits(temperature))
+    if ((targets_bytes != 4 && targets_bytes != 8) || top < 0 || top > kScoreMaxTop || top > s.vocab || !temperature_fits(temperature) || (top && kept))
       return MUON_E_INVALID_ARG;
     if (s.tokens == 0) return MUON_OK;
     if (!h->weight || !h->hidden || !entropy || !lse || !lse_rest || (targets != nullptr) != (log_prob != nullptr) || (top && (!top_index || !top_log_prob)))
       return MUON_E_INVALID_ARG;
     if (!aligned(targets, targets_bytes) || !aligned(log_prob, 4) || !aligned(entropy, 4) || !aligned(lse, 4) || !aligned(lse_rest, 4) ||
-        !aligned(top_index, 8) || !aligned(top_log_prob, 4) || !aligned(workspace, 256))
+        !aligned(top_index, 8) || !aligned(top_log_prob, 4) || !aligned(kept, 256) || !aligned(workspace, 256))
       return MUON_E_MISALIGNED;
+    if (kept && kept_bytes < score_kept_bytes(s)) return MUON_E_WORKSPACE_TOO_SMALL;
     ScorePlan p;
     if (!workspace || !score_plan(s, top > 0, workspace_bytes, &p)) return MUON_E_WORKSPACE_TOO_SMALL;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
@@ -100,7 +119,8 @@ int muon_log_probs(const muon_head* h, const void* targets, int32_t targets_byte
       const HeadRows rows{behind(h->hidden, elem * t0 * h->hidden_stride), h->weight, h->hidden_stride, h->weight_stride, s.width, s.f32};
       HeadOperand hidden;
       if (int st = pack_rows(h, s, p.shape, rows.hidden, n, p.piece, ws + p.packed_hidden, &hidden, stream)) return st;
-      MUON_HIP(launch_score_logits(weight, hidden, p.logits[piece == p.pieces - 1], p.shape.pairs, scale.unit, stats, best, stream));
+      MUON_HIP(launch_score_logits(weight, hidden, p.logits[piece == p.pieces - 1], p.shape.pairs, scale.unit, stats, best,
+                                   kept_from(s, p.shape, kept, t0), stream));
       const ScoreTarget t{behind(targets, targets_bytes * t0), targets_bytes == 8};
       const ScoreOut out{log_prob ? log_prob + t0 : nullptr, entropy + t0, lse + t0, lse_rest + t0,
                          top ? reinterpret_cast<long long*>(top_index) + t0 * top : nullptr, top ? top_log_prob + t0 * top : nullptr};
@@ -111,8 +131,8 @@ int muon_log_probs(const muon_head* h, const void* targets, int32_t targets_byte
 }
 
 int muon_log_probs_backward(const muon_head* h, const void* targets, int32_t targets_bytes, double temperature, const float* lse, const float* lse_rest,
-                            const float* entropy, const float* d_log_prob, const float* d_entropy, void* d_hidden, void* d_weight, void* workspace,
-                            size_t workspace_bytes, void* hip_stream) {
+                            const float* entropy, const float* d_log_prob, const float* d_entropy, const void* kept, size_t kept_bytes, void* d_hidden,
+                            void* d_weight, void* workspace, size_t workspace_bytes, void* hip_stream) {
   return guarded([&]() -> int {
     HeadShape s;
     if (int st = score_shape(h, d_hidden != nullptr, d_weight != nullptr, &s)) return st;
@@ -121,8 +141,9 @@ int muon_log_probs_backward(const muon_head* h, const void* targets, int32_t tar
       return MUON_E_INVALID_ARG;
     const uintptr_t size = s.f32 ? 4 : 2;
     if (!aligned(targets, targets_bytes) || !aligned(lse, 4) || !aligned(lse_rest, 4) || !aligned(entropy, 4) || !aligned(d_log_prob, 4) ||
-        !aligned(d_entropy, 4) || !aligned(d_hidden, size) || !aligned(d_weight, size) || !aligned(workspace, 256))
+        !aligned(d_entropy, 4) || !aligned(kept, 256) || !aligned(d_hidden, size) || !aligned(d_weight, size) || !aligned(workspace, 256))
       return MUON_E_MISALIGNED;
+    if (kept && kept_bytes < score_kept_bytes(s)) return MUON_E_WORKSPACE_TOO_SMALL;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (s.tokens == 0) {
       if (d_weight) MUON_HIP(launch_fill_zero(d_weight, size * s.vocab * s.width, stream));
@@ -136,13 +157,13 @@ int muon_log_probs_backward(const muon_head* h, const void* targets, int32_t tar
     auto f32_at = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
     const Scale scale = scale_of(temperature);
     HeadOperand weight;
-    if (int st = pack(h, s, p, ws + p.packed_weight, &weight, stream)) return st;
+    weight = {};
+    if (!kept || s.d_hidden)
+      if (int st = pack(h, s, p, ws + p.packed_weight, &weight, stream)) return st;
     for (int64_t piece = 0; piece < p.pieces; ++piece) {
       const int last = piece == p.pieces - 1;
       const int64_t t0 = piece * p.piece, n = std::min(p.piece, s.tokens - t0);
       const HeadRows rows{behind(h->hidden, (int64_t)size * t0 * h->hidden_stride), h->weight, h->hidden_stride, h->weight_stride, s.width, s.f32};
-      HeadOperand hidden;
-      if (int st = pack_rows(h, s, p, rows.hidden, n, p.piece, ws + p.packed_hidden, &hidden, stream)) return st;
       const ScoreTarget t{behind(targets, targets_bytes * t0), targets_bytes == 8};
       const ScoreGrads d{lse + t0, lse_rest + t0, entropy + t0, d_log_prob ? d_log_prob + t0 : nullptr, d_entropy ? d_entropy + t0 : nullptr};
       const ScoreCoef c{f32_at(p.scale), f32_at(p.kept), f32_at(p.value), reinterpret_cast<float2*>(ws + p.lse)};
@@ -151,7 +172,14 @@ int muon_log_probs_backward(const muon_head* h, const void* targets, int32_t tar
       const int64_t masked_plane = p.piece * p.width_k, grad_plane = p.piece * p.vocab_pitch;
       MUON_HIP(launch_score_peak(t, d, n, s.vocab, peak, stream));
       MUON_HIP(launch_score_prepare(t, scale.inv_tau, scale.unit, d, peak, rows, n, s.vocab, c, masked, p.width_k, masked_plane, stream));
-      MUON_HIP(launch_score_grad(weight, hidden, p.logits[last], p.pairs, scale.unit, t, c, s.f32, u16_at(p.grad), p.vocab_pitch, grad_plane, stream));
+      if (kept) {
+        MUON_HIP(launch_score_dz(t, scale.unit, kept_from(s, p, const_cast<void*>(kept), t0), p.blocks, c, n, s.vocab, s.f32, u16_at(p.grad), p.vocab_pitch,
+                                 grad_plane, stream));
+      } else {
+        HeadOperand hidden;
+        if (int st = pack_rows(h, s, p, rows.hidden, n, p.piece, ws + p.packed_hidden, &hidden, stream)) return st;
+        MUON_HIP(launch_score_grad(weight, hidden, p.logits[last], p.pairs, scale.unit, t, c, s.f32, u16_at(p.grad), p.vocab_pitch, grad_plane, stream));
+      }
       if (s.d_hidden) {
         const HeadOut o{static_cast<unsigned char*>(d_hidden) + size * t0 * s.width, s.f32, f32_at(p.partial), nullptr, 0, 0, scale.inv_tau, peak};
         const HeadOperand l{weight.p, weight.ld, weight.plane, s.width}, r{u16_at(p.grad), p.vocab_pitch, grad_plane, n};

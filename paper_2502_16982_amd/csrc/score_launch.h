@@ -22,8 +22,15 @@ struct ScoreBest {
   float z;
   unsigned second;
 };
+// What a forward call keeps for the backward one, [tokens, pitch]: powers 2^(y - top) in f16, up to 2^15 in a block, with each block's top per
+// token; or, tops null, z in fp32.  values null: nothing.  Not together with `best`.
+struct ScoreKept {
+  void* values;
+  long long pitch;
+  float* tops;
+};
 hipError_t launch_score_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, ScoreStats* stats,
-                               ScoreBest* best, hipStream_t s);
+                               ScoreBest* best, const ScoreKept& kept, hipStream_t s);
 
 struct ScoreOut {
   float *log_prob, *entropy, *lse, *lse_rest;      // log_prob null where there are no targets
@@ -52,5 +59,8 @@ hipError_t launch_score_prepare(const ScoreTarget& t, float inv_tau, float unit,
 // The logits' gradient over *peak, in bf16 or three planes, from the logits' product done again.
 hipError_t launch_score_grad(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, const ScoreTarget& t,
                              const ScoreCoef& c, bool f32, uint16_t* grad, long long pitch, long long plane, hipStream_t s);
+// The same from what the forward call kept.
+hipError_t launch_score_dz(const ScoreTarget& t, float unit, const ScoreKept& kept, long long blocks, const ScoreCoef& c, long long tokens, long long vocab, bool f32,
+                           uint16_t* grad, long long pitch, long long plane, hipStream_t s);
 
 }  // namespace muon

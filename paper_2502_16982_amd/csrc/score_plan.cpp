@@ -57,6 +57,9 @@ size_t score_workspace(const HeadShape& s, bool best, size_t max_bytes) {
   return std::max(bytes_of(s, best, std::min<int64_t>(all, 256)), max_bytes / 256 * 256);
 }
 
+int64_t score_kept_values(const HeadShape& s) { return up(s.tokens * head_plan_shape(s).vocab_pitch * (s.f32 ? 4 : 2), 256); }
+size_t score_kept_bytes(const HeadShape& s) { return (size_t)(score_kept_values(s) + (s.f32 ? 0 : up(s.tokens * head_plan_shape(s).blocks * 4, 256))); }
+
 bool score_plan(const HeadShape& s, bool best, size_t bytes, ScorePlan* p) {
   *p = ScorePlan{};
   p->shape = head_plan_shape(s);

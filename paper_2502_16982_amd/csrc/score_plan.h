@@ -22,6 +22,9 @@ struct ScorePlan {
 
 // Bytes for a call: pieces of up to kHeadPieceTokens (max_bytes 0), or the largest that fit, the smallest there are at least.
 size_t score_workspace(const HeadShape& s, bool best, size_t max_bytes);
+// Bytes of what a call keeps for its backward call: values of all tokens, then (bf16) the blocks' tops.
+int64_t score_kept_values(const HeadShape& s);
+size_t score_kept_bytes(const HeadShape& s);
 // The largest pieces that fit into so many bytes; false where none do.
 bool score_plan(const HeadShape& s, bool best, size_t bytes, ScorePlan* p);
 

@@ -26,13 +26,15 @@ class HeadResult(NamedTuple):
 
 class TokenScores(NamedTuple):
     """log_prob: [tokens] in fp32, or None without targets; entropy, lse: [tokens] in fp32; lse_rest: what fp32 leaves of lse; top_index:
-    [tokens, top] in int64, top_log_prob: in fp32, or None where not asked for."""
+    [tokens, top] in int64, top_log_prob: in fp32, or None where not asked for; kept: what ``log_probs_backward`` reads instead of making the logits
+    once more, or None."""
     log_prob: Optional[torch.Tensor]
     entropy: torch.Tensor
     lse: torch.Tensor
     lse_rest: torch.Tensor
     top_index: Optional[torch.Tensor]
     top_log_prob: Optional[torch.Tensor]
+    kept: Optional[torch.Tensor] = None
 
 
 def _index_bytes(t: torch.Tensor, what: str) -> int:
@@ -61,6 +63,7 @@ class LossHead:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.max_workspace_bytes = int(max_workspace_bytes)
         self.dtype = dtype
+        self.gradients = bool(gradients)
         self.workspace = None
         self._stream = None                                # handle and object of the stream that used the workspace last
         self._last = None
@@ -193,10 +196,12 @@ class LossHead:
         return targets.data_ptr(), _index_bytes(targets, "targets")
 
     def log_probs(self, hidden: torch.Tensor, weight: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0,
-                  temperature: float = 1.0) -> TokenScores:
+                  temperature: float = 1.0, keep: Optional[bool] = None) -> TokenScores:
         """Log probabilities of ``targets`` (negative: no token, 0) under the softmax of ``hidden @ weight.T / temperature``, the entropy of
         each row's whole distribution, and its ``top`` (up to 64) most likely entries with their log probabilities, the likeliest first, equal
-        ones by index."""
+        ones by index.  keep: whether the result holds what ``log_probs_backward`` saves one of its three products by, 2 bytes per token and vocabulary
+        entry (fp32: 4); only without alternatives; None: where the LossHead is for gradients and its max_workspace_bytes, if any, is not
+        exceeded."""
         head = self._head(hidden, weight)
         self._here(hidden=hidden, weight=weight, targets=targets)
         outside_autograd("LossHead.log_probs", hidden.requires_grad or weight.requires_grad)
@@ -204,11 +209,16 @@ class LossHead:
         at, size = self._targets(targets, tokens)
         with on(self.device):
             need = self._fit(head, top, 0, scores=True)
+            kept, kept_bytes = None, 0
+            if keep or (keep is None and self.gradients and not top):
+                kept_bytes = binding.muon_log_probs_kept_bytes(head)
+                if keep or not 0 < self.max_workspace_bytes < kept_bytes:
+                    kept = torch.empty(kept_bytes, dtype=torch.uint8, device=self.device)
             values = torch.empty(4, tokens, dtype=torch.float32, device=self.device).unbind(0)
             out = TokenScores(None if targets is None else values[0], *values[1:],
                               torch.empty(tokens, top, dtype=torch.int64, device=self.device) if top else None,
-                              torch.empty(tokens, top, dtype=torch.float32, device=self.device) if top else None)
-            binding.muon_log_probs(head, at, size, top, temperature, *(0 if t is None else t.data_ptr() for t in out),
+                              torch.empty(tokens, top, dtype=torch.float32, device=self.device) if top else None, kept)
+            binding.muon_log_probs(head, at, size, top, temperature, *(0 if t is None else t.data_ptr() for t in out), kept_bytes,
                                    self.workspace.data_ptr(), need, stream_handle(self.device))
         return out
 
@@ -226,6 +236,9 @@ class LossHead:
             raise MuonError(-1, "targets and d_log_prob: both or neither")
         if d_log_prob is None and d_entropy is None:
             raise MuonError(-1, "d_log_prob or d_entropy")
+        kept = scores.kept
+        if kept is not None and (kept.device != self.device or kept.numel() != binding.muon_log_probs_kept_bytes(head)):
+            raise MuonError(-1, "scores.kept: of another call's sizes")
         given = []
         for name, t in (("lse", scores.lse), ("lse_rest", scores.lse_rest), ("entropy", scores.entropy), ("d_log_prob", d_log_prob),
                         ("d_entropy", d_entropy)):
@@ -237,6 +250,7 @@ class LossHead:
         with on(self.device):
             dh, dw = self._gradients(hidden, weight, gradients)
             need = self._fit(head, 1, (1 if dh is not None else 0) | (2 if dw is not None else 0))
-            binding.muon_log_probs_backward(head, at, size, temperature, *given, *(0 if t is None else t.data_ptr() for t in (dh, dw)),
+            binding.muon_log_probs_backward(head, at, size, temperature, *given, 0 if kept is None else kept.data_ptr(),
+                                            0 if kept is None else kept.numel(), *(0 if t is None else t.data_ptr() for t in (dh, dw)),
                                             self.workspace.data_ptr(), need, stream_handle(self.device))
         return dh, dw

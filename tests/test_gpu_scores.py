@@ -5,6 +5,7 @@ largest of the row.  lse carries d and a few roundings of its own size; log prob
 summed in double.  The entropy's derivative is -p (log p + entropy), whose magnitudes add up to 2 H at most: 2 H (d + 2^-20), 2^-20 for
 the exponentials, plus 2^-20 (1 + H + log V) for the sums.  dz = g ([v = y] - p) - h p (log p + H): p carries 2 d (its logit's error and lse's),
 log p + H that and the entropy's; bf16 rounds dz once, 2^-8 relative, and the result once more (2^-8); sums of K products add (8 + sqrt K) 2^-23 of their magnitudes.
+Kept powers in f16 add 2^-11 of p and of log p, or half of f16's smallest step, 2^-40 of the largest of their block.
 """
 import numpy as np
 import pytest
@@ -67,6 +68,10 @@ def check(s, h, w, y, top=0, tau=1.0, live=None):
     return want
 
 
+def results(s):
+    return [t for t in s[:6] if t is not None]
+
+
 def check_backward(grads, s, h, w, y, dl, de, tau=1.0, dtype="bf16"):
     h64, w64 = as64(h), as64(w)
     dl64, de64 = as64(dl), as64(de)
@@ -85,6 +90,8 @@ def check_backward(grads, s, h, w, y, dl, de, tau=1.0, dtype="bf16"):
     dz, g, e = np.abs(want["d_logits"]), np.abs(g)[:, None], np.abs(e)[:, None]
     spread = dz + 2 * g * p + 2 * e * bend                                 # where its parts cancel, their errors stay
     loose = spread * 2 * d[:, None] + e * p * (2 * d + np.nan_to_num(h_err))[:, None]
+    if s.kept is not None and dtype == "bf16":
+        loose = loose + (spread + e * p) * 2.0 ** -11 + (g + 64 * e) * 2.0 ** -39 * kept[:, None]
     h0 = np.where(kept[:, None], h64, 0.0)
     for got, ref, left, b, k in ((grads[0], want["d_hidden"], True, np.abs(w64), vocab), (grads[1], want["d_weight"], False, np.abs(h0), tokens)):
         if got is None:
@@ -114,6 +121,14 @@ def test_sizes(losses, sizes, dtype):
         s = head.log_probs(h, w, y, top=top, temperature=tau)
         check(s, h, w, y, top, tau)
         check_backward(head.log_probs_backward(h, w, y, s, dl, de, temperature=tau), s, h, w, y, dl, de, tau, dtype)
+        for keep in (True, False):
+            s = head.log_probs(h, w, y, temperature=tau, keep=keep)
+            assert (s.kept is not None) == keep
+            check(s, h, w, y, 0, tau)
+            first = head.log_probs_backward(h, w, y, s, dl, de, temperature=tau)
+            check_backward(first, s, h, w, y, dl, de, tau, dtype)
+            for a, b in zip(first, head.log_probs_backward(h, w, y, s, dl, de, temperature=tau)):       # what is kept stays
+                assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -128,9 +143,11 @@ def test_forms(losses, dtype):
     assert np.isnan(want["log_prob"][4:6]).all() and float(s.log_prob[3]) == 0.0
     small = torch.where(y > 2 ** 31 - 1, 2 ** 31 - 1, y).to(torch.int32)
     again = head.log_probs(h, w, small, top=3)
-    assert all(torch.equal(a.nan_to_num(9.0), b.nan_to_num(9.0)) for a, b in zip(s, again))
+    assert all(torch.equal(a.nan_to_num(9.0), b.nan_to_num(9.0)) for a, b in zip(results(s), results(again)))
     none = head.log_probs(h, w)
-    assert none.log_prob is None and none.top_index is None and torch.equal(none.entropy, s.entropy) and torch.equal(none.lse, s.lse)
+    assert none.log_prob is None and none.top_index is None and (none.entropy - s.entropy).abs().max() <= 1e-5 and (none.lse - s.lse).abs().max() <= 1e-5
+    bare = head.log_probs(h, w, keep=False)
+    assert torch.equal(bare.entropy, s.entropy) and torch.equal(bare.lse, s.lse)
     both = head.log_probs_backward(h, w, y, s, dl, de)
     check_backward(both, s, h, w, y, dl, de, 1.0, dtype)
     dh, nothing = head.log_probs_backward(h, w, y, s, dl, de, gradients=("hidden",))
@@ -204,7 +221,7 @@ def test_values_that_are_not_finite(losses, dtype):
     head = losses.LossHead(50, 900, 72, DT[dtype])
     s, clean = head.log_probs(bad, w, y, top=5), head.log_probs(h, w, y, top=5)
     check(s, bad, w, y, 5, live=keep)
-    for a, b in zip(s, clean):
+    for a, b in zip(results(s), results(clean)):
         assert torch.equal(a[torch.from_numpy(keep).cuda()], b[torch.from_numpy(keep).cuda()])
     assert s.lse[11].isnan() and s.log_prob[11].isnan() and s.entropy[11].isnan()
     assert ((s.top_index >= 0) & (s.top_index < 900)).all()
@@ -213,6 +230,10 @@ def test_values_that_are_not_finite(losses, dtype):
     dh, dw = head.log_probs_backward(bad, w, y, s, dl, de)
     want = head.log_probs_backward(h, w, y, clean, dl, de)
     assert torch.equal(dw, want[1]) and torch.equal(dh, want[0]) and (dh[rows] == 0).all()
+    s, clean = head.log_probs(bad, w, y), head.log_probs(h, w, y)
+    dh, dw = head.log_probs_backward(bad, w, y, s, dl, de)
+    want = head.log_probs_backward(h, w, y, clean, dl, de)
+    assert s.kept is not None and torch.equal(dw, want[1]) and torch.equal(dh, want[0]) and (dh[rows] == 0).all()
 
 
 def test_logits_of_minus_infinity(losses):
@@ -232,10 +253,11 @@ def test_logits_of_minus_infinity(losses):
     assert (s.entropy.double().cpu() - torch.special.entr(logp.exp()).sum(1)).abs().max() <= 1e-4
     assert torch.equal(s.top_index.cpu(), logp.topk(64).indices)
     y[0] = 3
-    s = head.log_probs(h, w, y)
     de = torch.ones(20, device="cuda")
-    dh, dw = head.log_probs_backward(h[:, :], w, y, s, de, de)
-    assert not dw.isnan().any() and (dw[128:512] == 0).all()
+    for keep in (True, False):
+        s = head.log_probs(h, w, y, keep=keep)
+        dh, dw = head.log_probs_backward(h, w, y, s, de, de)
+        assert not dw.isnan().any() and (dw[128:512] == 0).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -247,16 +269,21 @@ def test_every_form_of_launch(losses, tokens, vocab, width, dtype):
     head = losses.LossHead(tokens, vocab, width, DT[dtype])
     s = head.log_probs(h, w, y, top=4, temperature=1.3)
     dh, dw = head.log_probs_backward(h, w, y, s, dl, de, temperature=1.3)
+    k = head.log_probs(h, w, y, temperature=1.3)
+    dh2, dw2 = head.log_probs_backward(h, w, y, k, dl, de, temperature=1.3)
+    assert k.kept is not None
     logp = torch.log_softmax(h.double() @ w.double().T.contiguous() / 1.3, 1)
     entropy = torch.special.entr(logp.exp()).sum(1)
     best = logp.topk(4)
     assert torch.equal(s.top_index, best.indices)
-    for got, want in ((s.log_prob, logp.gather(1, y[:, None])[:, 0]), (s.entropy, entropy), (s.top_log_prob, best.values)):
+    for got, want in ((s.log_prob, logp.gather(1, y[:, None])[:, 0]), (s.entropy, entropy), (s.top_log_prob, best.values), (k.log_prob, logp.gather(1, y[:, None])[:, 0]),
+                      (k.entropy, entropy)):
         assert (got.double() - want).norm() <= 2e-6 * want.norm()
     p = logp.exp()
     dz = -p * (dl.double()[:, None] + de.double()[:, None] * (logp + entropy[:, None]))
     dz[torch.arange(tokens), y] += dl.double()
-    for got, want in ((dh, dz @ w.double() / 1.3), (dw, dz.T.contiguous() @ h.double() / 1.3)):
+    dh64, dw64 = dz @ w.double() / 1.3, dz.T.contiguous() @ h.double() / 1.3
+    for got, want in ((dh, dh64), (dw, dw64), (dh2, dh64), (dw2, dw64)):
         assert (got.double() - want).norm() <= (5e-3 if dtype == "bf16" else 1e-5) * want.norm()
 
 
@@ -272,6 +299,11 @@ def test_pieces(losses, dtype):
     dl, de = torch.randn(1000, generator=g).cuda(), torch.randn(1000, generator=g).cuda()
     check_backward(few.log_probs_backward(h, w, y, b, dl, de), b, h, w, y, dl, de, 1.0, dtype)
     assert few.workspace.numel() < whole.workspace.numel()
+    b = few.log_probs(h, w, y)
+    assert b.kept is None
+    b = few.log_probs(h, w, y, keep=True)
+    check(b, h, w, y)
+    check_backward(few.log_probs_backward(h, w, y, b, dl, de), b, h, w, y, dl, de, 1.0, dtype)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -282,7 +314,7 @@ def test_strides_and_alignment(losses, dtype):
     head = losses.LossHead(60, 500, 64, DT[dtype])
     dl = torch.randn(60, generator=g).cuda()
     a, b = head.log_probs(h, w, y, top=4), head.log_probs(wide[:, 3:67], tall[:, 1:65], y, top=4)
-    assert all(torch.equal(x, z) for x, z in zip(a, b))
+    assert all(torch.equal(x, z) for x, z in zip(results(a), results(b)))
     for x, z in zip(head.log_probs_backward(h, w, y, a, dl, dl), head.log_probs_backward(wide[:, 3:67], tall[:, 1:65], y, b, dl, dl)):
         assert torch.equal(x, z)
 
@@ -309,8 +341,8 @@ def test_streams_and_capture(losses):
     head = losses.LossHead(90, 2100, 96)
 
     def both(h, y):
-        s = head.log_probs(h, w, y, top=5)
-        return [*s, *head.log_probs_backward(h, w, y, s, dl, de)]
+        s, k = head.log_probs(h, w, y, top=5), head.log_probs(h, w, y)
+        return [*results(s), *results(k), *head.log_probs_backward(h, w, y, s, dl, de), *head.log_probs_backward(h, w, y, k, dl, de)]
 
     want = both(h, y)
     side = torch.cuda.Stream()
@@ -340,5 +372,6 @@ def test_no_tokens(losses):
     head = losses.LossHead(4, 300, 32)
     s = head.log_probs(h[:0], w, y[:0], top=3)
     assert s.log_prob.shape == (0,) and s.top_index.shape == (0, 3)
-    dh, dw = head.log_probs_backward(h[:0], w, y[:0], s, s.log_prob)
-    assert dh.shape == (0, 32) and (dw == 0).all()
+    for s in (s, head.log_probs(h[:0], w, y[:0])):
+        dh, dw = head.log_probs_backward(h[:0], w, y[:0], s, s.log_prob)
+        assert dh.shape == (0, 32) and (dw == 0).all()

@@ -86,28 +86,34 @@ def test_refusals():
     L = binding.lib()
     need = binding.muon_log_probs_bytes(head(), 5)
 
-    def call(h, targets=FAKE, size=8, top=5, tau=1.0, log_prob=FAKE, entropy=FAKE, lse=FAKE, rest=FAKE, index=FAKE, best=FAKE, ws=FAKE, nbytes=need):
-        return L.muon_log_probs(C.byref(h), targets, size, top, tau, log_prob, entropy, lse, rest, index, best, ws, nbytes, None)
+    def call(h, targets=FAKE, size=8, top=5, tau=1.0, log_prob=FAKE, entropy=FAKE, lse=FAKE, rest=FAKE, index=FAKE, best=FAKE, kept=None, kept_bytes=0, ws=FAKE, nbytes=need):
+        return L.muon_log_probs(C.byref(h), targets, size, top, tau, log_prob, entropy, lse, rest, index, best, kept, kept_bytes, ws, nbytes, None)
 
     h = head()
     for bad in (dict(size=2), dict(top=-1), dict(top=65), dict(tau=0.0), dict(tau=-1.0), dict(tau=float("nan")), dict(tau=float("inf")), dict(tau=1e-60),
-                dict(log_prob=None), dict(targets=None), dict(entropy=None), dict(lse=None), dict(rest=None), dict(index=None), dict(best=None)):
+                dict(log_prob=None), dict(targets=None), dict(entropy=None), dict(lse=None), dict(rest=None), dict(index=None), dict(best=None), dict(kept=FAKE, kept_bytes=1 << 30)):
         assert call(h, **bad) == -1, bad
     assert call(head(hidden=None)) == call(head(weight=None)) == -1
     assert call(h, ws=None) == call(h, nbytes=0) == call(h, nbytes=255) == -4
     for bad in (dict(targets=FAKE + 4), dict(log_prob=FAKE + 2), dict(entropy=FAKE + 2), dict(lse=FAKE + 2), dict(rest=FAKE + 2), dict(index=FAKE + 4),
-                dict(best=FAKE + 2), dict(ws=FAKE + 128)):
+                dict(best=FAKE + 2), dict(ws=FAKE + 128), dict(top=0, kept=FAKE + 128, kept_bytes=1 << 30)):
         assert call(h, **bad) == -7, bad
+    room = binding.muon_log_probs_kept_bytes(h)
+    assert room >= 4 * 256 * 2 and binding.muon_log_probs_kept_bytes(head(dtype=0)) >= 4 * 256 * 4
+    assert L.muon_log_probs_kept_bytes(C.byref(h), None) == L.muon_log_probs_kept_bytes(None, C.byref(C.c_size_t())) == -1
+    assert call(h, top=0, kept=FAKE, kept_bytes=room - 1) == -4
     assert call(head(tokens=0), ws=None) == 0
 
     back = binding.muon_head_workspace_bytes(head(), 1, 3)
 
-    def backward(h, targets=FAKE, size=8, tau=1.0, lse=FAKE, rest=FAKE, entropy=FAKE, dl=FAKE, de=FAKE, dh=FAKE, dw=FAKE, ws=FAKE, nbytes=back):
-        return L.muon_log_probs_backward(C.byref(h), targets, size, tau, lse, rest, entropy, dl, de, dh, dw, ws, nbytes, None)
+    def backward(h, targets=FAKE, size=8, tau=1.0, lse=FAKE, rest=FAKE, entropy=FAKE, dl=FAKE, de=FAKE, kept=None, kept_bytes=0, dh=FAKE, dw=FAKE, ws=FAKE,
+                 nbytes=back):
+        return L.muon_log_probs_backward(C.byref(h), targets, size, tau, lse, rest, entropy, dl, de, kept, kept_bytes, dh, dw, ws, nbytes, None)
 
     for bad in (dict(size=1), dict(tau=0.0), dict(lse=None), dict(rest=None), dict(entropy=None), dict(dl=None), dict(targets=None), dict(targets=None, dl=None, de=None)):
         assert backward(h, **bad) == -1, bad
-    assert backward(h, ws=None) == backward(h, nbytes=256) == -4
+    assert backward(h, ws=None) == backward(h, nbytes=256) == backward(h, kept=FAKE, kept_bytes=room - 1) == -4
+    assert backward(h, kept=FAKE + 128, kept_bytes=room) == -7
     for bad in (dict(targets=FAKE + 4), dict(lse=FAKE + 2), dict(rest=FAKE + 2), dict(entropy=FAKE + 2), dict(dl=FAKE + 2), dict(de=FAKE + 2), dict(dh=FAKE + 1),
                 dict(dw=FAKE + 1), dict(ws=FAKE + 128)):
         assert backward(h, **bad) == -7, bad
@@ -136,6 +142,11 @@ def test_loss_head(loss_head):
     assert calls[-1][3:5] == (3, 0.5)
     bare = head.log_probs(h, w)
     assert bare.log_prob is None and bare.top_index is None and bare.entropy.shape == (4,) and calls[-1][1] == 0
+    assert s.kept is None and bare.kept.numel() == binding.muon_log_probs_kept_bytes(calls[-1][0])       # alternatives, or what a backward call reads
+    assert head.log_probs(h, w, keep=False).kept is None
+    few = type(head)(4, 100, 16, device="cpu", max_workspace_bytes=600)
+    assert few.log_probs(h, w).kept is None and few.log_probs(h, w, keep=True).kept is not None
+    assert type(head)(4, 100, 16, device="cpu", gradients=False).log_probs(h, w).kept is None
     d = torch.ones(4)
     dh, dw = head.log_probs_backward(h, w, y, s, d, gradients=("weight",))
     assert dh is None and dw.shape == (100, 16)
@@ -143,7 +154,8 @@ def test_loss_head(loss_head):
     for call in (lambda: head.log_probs(h, w, y[:3]), lambda: head.log_probs(h, w, y.float()), lambda: head.log_probs(h, w, top=65),
                  lambda: head.log_probs(h, w, top=-1), lambda: head.log_probs_backward(h, w, y, s, None, d), lambda: head.log_probs_backward(h, w, None, s, d),
                  lambda: head.log_probs_backward(h, w, None, s, None), lambda: head.log_probs_backward(h, w, y, s, d[:3]),
-                 lambda: head.log_probs_backward(h, w, y, s, d.double()), lambda: head.log_probs_backward(h[:3], w, y[:3], s, d[:3])):
+                 lambda: head.log_probs_backward(h, w, y, s, d.double()), lambda: head.log_probs_backward(h[:3], w, y[:3], s, d[:3]),
+                 lambda: head.log_probs_backward(h, w, y, s._replace(kept=bare.kept[:-1]), d)):
         with pytest.raises(binding.MuonError):
             call()
     with pytest.warns(UserWarning, match="not recorded by autograd"):
