@@ -257,6 +257,177 @@ __global__ __launch_bounds__(256, B == 128 && S == 2 ? 2 : 1) void score_logits_
 #endif
 }
 
+// ---- forward, few tokens: the same statistics straight from the rows ----
+// 16 rows of W or H and 64 (fp32 32) columns, as the matrix instruction of 16 x 16 takes them: lane l holds row l % 16 and, of its group l / 16, 32
+// neighbouring bytes, so that four lanes take whole lines; which columns a step is made of is free as long as both operands agree.
+template <bool F32>
+struct FewPart {
+  static constexpr int COLS = F32 ? 32 : 64, OWN = COLS / 4, SIZE = F32 ? 4 : 2;
+  u32x4 v[2];
+  __device__ __forceinline__ void load(const unsigned char* p) {
+    v[0] = *reinterpret_cast<const u32x4_any*>(p);
+    v[1] = *reinterpret_cast<const u32x4_any*>(p + 16);
+  }
+  // its first `count` elements, zeros behind them
+  __device__ __forceinline__ void load_some(const unsigned char* p, int count) {
+    v[0] = v[1] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int e = 0; e < OWN; ++e) {
+      if (e >= count) continue;
+      if constexpr (F32) v[e / 4][e % 4] = reinterpret_cast<const unsigned*>(p)[e];
+      else v[e / 8][e / 2 % 4] |= (unsigned)reinterpret_cast<const u16*>(p)[e] << 16 * (e & 1);
+    }
+  }
+};
+typedef float few_acc __attribute__((ext_vector_type(4)));
+template <bool F32>
+__device__ __forceinline__ few_acc few_multiply(const FewPart<F32>& w, const FewPart<F32>& h, few_acc acc) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const unsigned a = w.v[u][e], b = h.v[u][e];
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a), __uint_as_float(b), acc, 0, 0, 0);
+      }
+    } else {
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w.v[u]), __builtin_bit_cast(bf16x8, h.v[u]), acc, 0, 0, 0);
+    }
+  }
+  return acc;
+}
+
+// Block: 128 vocabulary entries x up to 16 NT tokens, 32 entries per wave.  fp32 rows as they are, on the fp32 matrix instructions.  Bound by W's
+// rows: fp32 100003 x 2048, 819 MB, with one token 200 us with the finish (4.1 TB/s), with 64 by the matrix instructions, 481.
+template <bool F32, int NT, bool BEST>
+__global__ __launch_bounds__(256) void score_few_kernel(HeadRows rows, long long tokens, long long vocab, float unit, ScoreStats* __restrict__ stats,
+                                                        ScoreBest* __restrict__ best) {
+  using P = FewPart<F32>;
+  constexpr int kAhead = NT == 1 ? 4 : NT == 2 ? 2 : 1, kPitch = kHeadGrain + 4;
+  __shared__ float zs[16 * kPitch];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const long long block = blockIdx.x, v0 = block * kHeadGrain;
+  const unsigned char *w[2], *h[NT];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const long long row = v0 + 32 * wave + 16 * u + r;
+    w[u] = static_cast<const unsigned char*>(rows.weight) + ((row < vocab ? row : vocab - 1) * rows.weight_stride + P::OWN * g) * P::SIZE;
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const long long token = 16 * t + r;
+    h[t] = static_cast<const unsigned char*>(rows.hidden) + ((token < tokens ? token : tokens - 1) * rows.hidden_stride + P::OWN * g) * P::SIZE;
+  }
+  few_acc acc[2][NT];
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[u][t] = few_acc{0.f, 0.f, 0.f, 0.f};
+  struct Batch {
+    P w[kAhead][2], h[kAhead][NT];
+  };
+  const long long batch = (long long)kAhead * P::COLS, whole = rows.width / batch * batch;
+  const auto load = [&](long long k, Batch& b) {
+#pragma unroll
+    for (int c = 0; c < kAhead; ++c) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) b.w[c][u].load(w[u] + (k + c * P::COLS) * P::SIZE);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) b.h[c][t].load(h[t] + (k + c * P::COLS) * P::SIZE);
+    }
+  };
+  const auto take = [&](const Batch& b) {
+#pragma unroll
+    for (int c = 0; c < kAhead; ++c)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[u][t] = few_multiply<F32>(b.w[c][u], b.h[c][t], acc[u][t]);
+  };
+  // a batch is multiplied while the next one is on its way
+  if (whole) {
+    Batch b0, b1;
+    load(0, b0);
+    for (long long k = 0;;) {
+      k += batch;
+      const bool more = k < whole;
+      if (more) load(k, b1);
+      take(b0);
+      if (!more) break;
+      k += batch;
+      const bool again = k < whole;
+      if (again) load(k, b0);
+      take(b1);
+      if (!again) break;
+    }
+  }
+  for (long long k = whole; k < rows.width; k += P::COLS) {           // the rest of the rows
+    const long long left = rows.width - k - P::OWN * g;
+    const int count = left < 0 ? 0 : left < P::OWN ? (int)left : P::OWN;
+    P a[2], b[NT];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) a[u].load_some(w[u] + k * P::SIZE, count);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) b[t].load_some(h[t] + k * P::SIZE, count);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[u][t] = few_multiply<F32>(a[u], b[t], acc[u][t]);
+  }
+  // 16 tokens at a time through LDS; then 16 threads to a token, four to a group, eight entries each
+  const int mine = threadIdx.x >> 4, c = threadIdx.x & 15, group = c >> 2, half = group & 1;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (t) __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = 32 * wave + 16 * u + 4 * g + e;
+        zs[r * kPitch + row] = v0 + row < vocab ? acc[u][t][e] : -INFINITY;
+      }
+    __syncthreads();
+    float z[8], first = -INFINITY, second = -INFINITY;
+    int place = 8 * (c & 3);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int at = 8 * (c & 3) + e;
+      z[e] = zs[mine * kPitch + 64 * (group >> 1) + place_row(at, half)];
+      second = __builtin_amdgcn_fmed3f(first, second, z[e]);
+      place = z[e] > first ? at : place;
+      first = fmaxf(first, z[e]);
+    }
+#pragma unroll
+    for (int off = 1; off < 4; off *= 2) {
+      const float f = __shfl_xor(first, off, 64), s = __shfl_xor(second, off, 64);
+      const int p = __shfl_xor(place, off, 64);
+      second = fmaxf(fmaxf(second, s), fminf(first, f));
+      place = f > first || (f == first && p < place) ? p : place;
+      first = fmaxf(first, f);
+    }
+    float top = fmaxf(first, __shfl_xor(first, 4, 64));
+    top = fmaxf(top, __shfl_xor(top, 8, 64));
+    top = top == -INFINITY ? 0.f : unit * top;
+    float sum = 0.f, slope = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float y = fmaf(unit, z[e], -top), x = __builtin_amdgcn_exp2f(y);
+      sum += x;
+      slope = fmaf(x, fmaxf(y, kFarBelow), slope);
+    }
+#pragma unroll
+    for (int off = 1; off < 16; off *= 2) {
+      sum += __shfl_xor(sum, off, 64);
+      slope += __shfl_xor(slope, off, 64);
+    }
+    const long long token = 16 * t + mine, blocks = (vocab + kHeadGrain - 1) / kHeadGrain;
+    if (token >= tokens) continue;
+    if (BEST && (c & 3) == 0)
+      best[(token * blocks + block) * (kHeadGrain / kScoreGroup) + group] = ScoreBest{first, (__float_as_uint(second) & ~31u) | (unsigned)place};
+    if (c == 0) stats[token * blocks + block] = ScoreStats{top, sum, slope, 0.f};
+  }
+}
+
 // ---- forward: one block per token joins the blocks and picks the alternatives ----
 typedef unsigned long long u64;
 
@@ -741,6 +912,18 @@ hipError_t launch_score_logits(const HeadOperand& weight, const HeadOperand& hid
   MUON_SCORE_CASE(128, 4);
 #undef MUON_SCORE_CASE
   return hipErrorInvalidValue;
+}
+
+hipError_t launch_score_few(const HeadRows& rows, long long tokens, long long vocab, float unit, ScoreStats* stats, ScoreBest* best, hipStream_t s) {
+  const long long blocks = (vocab + kHeadGrain - 1) / kHeadGrain;
+  auto go = [&](auto kernel) {
+    kernel<<<(unsigned)blocks, 256, 0, s>>>(rows, tokens, vocab, unit, stats, best);
+    return hipGetLastError();
+  };
+  if (!rows.f32) return best ? go(score_few_kernel<false, 1, true>) : go(score_few_kernel<false, 1, false>);
+  if (tokens <= 16) return best ? go(score_few_kernel<true, 1, true>) : go(score_few_kernel<true, 1, false>);
+  if (tokens <= 32) return best ? go(score_few_kernel<true, 2, true>) : go(score_few_kernel<true, 2, false>);
+  return best ? go(score_few_kernel<true, 4, true>) : go(score_few_kernel<true, 4, false>);
 }
 
 hipError_t launch_score_finish(const ScoreTarget& t, float inv_tau, float unit, const ScoreStats* stats, long long blocks,

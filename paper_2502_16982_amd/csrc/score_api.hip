@@ -105,22 +105,27 @@ int muon_log_probs(const muon_head* h, const void* targets, int32_t targets_byte
       return MUON_E_MISALIGNED;
     if (kept && kept_bytes < score_kept_bytes(s)) return MUON_E_WORKSPACE_TOO_SMALL;
     ScorePlan p;
-    if (!workspace || !score_plan(s, top > 0, workspace_bytes, &p)) return MUON_E_WORKSPACE_TOO_SMALL;
+    if (!workspace || !score_plan(s, top > 0, kept != nullptr, workspace_bytes, &p)) return MUON_E_WORKSPACE_TOO_SMALL;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const Scale scale = scale_of(temperature);
     const int64_t elem = s.f32 ? 4 : 2;
-    HeadOperand weight;
-    if (int st = pack(h, s, p.shape, ws + p.packed_weight, &weight, stream)) return st;
+    HeadOperand weight{};
+    if (!p.few)
+      if (int st = pack(h, s, p.shape, ws + p.packed_weight, &weight, stream)) return st;
     ScoreStats* stats = reinterpret_cast<ScoreStats*>(ws + p.stats);
     ScoreBest* best = top ? reinterpret_cast<ScoreBest*>(ws + p.best) : nullptr;
     for (int64_t piece = 0; piece < p.pieces; ++piece) {
       const int64_t t0 = piece * p.piece, n = std::min(p.piece, s.tokens - t0);
       const HeadRows rows{behind(h->hidden, elem * t0 * h->hidden_stride), h->weight, h->hidden_stride, h->weight_stride, s.width, s.f32};
-      HeadOperand hidden;
-      if (int st = pack_rows(h, s, p.shape, rows.hidden, n, p.piece, ws + p.packed_hidden, &hidden, stream)) return st;
-      MUON_HIP(launch_score_logits(weight, hidden, p.logits[piece == p.pieces - 1], p.shape.pairs, scale.unit, stats, best,
-                                   kept_from(s, p.shape, kept, t0), stream));
+      if (p.few) {
+        MUON_HIP(launch_score_few(rows, n, s.vocab, scale.unit, stats, best, stream));
+      } else {
+        HeadOperand hidden;
+        if (int st = pack_rows(h, s, p.shape, rows.hidden, n, p.piece, ws + p.packed_hidden, &hidden, stream)) return st;
+        MUON_HIP(launch_score_logits(weight, hidden, p.logits[piece == p.pieces - 1], p.shape.pairs, scale.unit, stats, best,
+                                     kept_from(s, p.shape, kept, t0), stream));
+      }
       const ScoreTarget t{behind(targets, targets_bytes * t0), targets_bytes == 8};
       const ScoreOut out{log_prob ? log_prob + t0 : nullptr, entropy + t0, lse + t0, lse_rest + t0,
                          top ? reinterpret_cast<long long*>(top_index) + t0 * top : nullptr, top ? top_log_prob + t0 * top : nullptr};

@@ -32,6 +32,9 @@ struct ScoreKept {
 hipError_t launch_score_logits(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, ScoreStats* stats,
                                ScoreBest* best, const ScoreKept& kept, hipStream_t s);
 
+// The same statistics for few tokens (16, fp32 64 at most), from the rows themselves.
+hipError_t launch_score_few(const HeadRows& rows, long long tokens, long long vocab, float unit, ScoreStats* stats, ScoreBest* best, hipStream_t s);
+
 struct ScoreOut {
   float *log_prob, *entropy, *lse, *lse_rest;      // log_prob null where there are no targets
   long long* top_index;

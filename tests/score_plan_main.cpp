@@ -20,7 +20,9 @@ static void walk(const HeadShape& s, bool best, size_t limit) {
   const size_t need = score_workspace(s, best, limit);
   CHECK(need % 256 == 0 && need > 0);
   ScorePlan p;
-  CHECK(score_plan(s, best, need, &p));
+  const bool keep = !best && s.width % 2;
+  CHECK(score_plan(s, best, keep, need, &p));
+  CHECK(p.few == (!keep && p.shape.pack_weight && s.tokens <= (s.f32 ? 64 : 16)) && (!p.few || p.pieces == 1));
   CHECK(p.total <= need && p.piece >= 1 && p.piece <= kHeadPieceTokens);
   CHECK(p.pieces == (s.tokens ? (s.tokens + p.piece - 1) / p.piece : 1));
   CHECK(p.pieces == 1 || p.piece % 256 == 0);
@@ -43,7 +45,7 @@ static void walk(const HeadShape& s, bool best, size_t limit) {
     CHECK(p.logits[i].blocks() < (int64_t{1} << 24));
   }
   ScorePlan none;
-  CHECK(!score_plan(s, best, 0, &none));
+  CHECK(!score_plan(s, best, false, 0, &none));
   if (limit) {
     CHECK(score_workspace(s, best, limit) <= std::max(limit, score_workspace(s, best, 1)));
     CHECK(score_workspace(s, best, limit) <= score_workspace(s, best, 0));

@@ -287,6 +287,24 @@ def test_every_form_of_launch(losses, tokens, vocab, width, dtype):
         assert (got.double() - want).norm() <= (5e-3 if dtype == "bf16" else 1e-5) * want.norm()
 
 
+@pytest.mark.parametrize("dtype,tokens", [("bf16", 1), ("bf16", 16), ("bf16", 17), ("f32", 1), ("f32", 16), ("f32", 17), ("f32", 33), ("f32", 64), ("f32", 65)])
+@pytest.mark.parametrize("vocab,width", [(1, 1), (127, 3), (129, 31), (1000, 65), (700, 515), (4100, 129)])
+def test_few_tokens(losses, dtype, tokens, vocab, width):
+    """Rows as they are, of odd widths and, in a wider buffer, at odd addresses; on both sides of the limits."""
+    h, w, y, g = make(tokens, vocab, width, dtype, seed=tokens)
+    y = torch.where(torch.rand(tokens, generator=g).cuda() < 0.2, -1, y)
+    head = losses.LossHead(tokens, vocab, width, DT[dtype], gradients=False)
+    top = min(vocab, 9)
+    s = head.log_probs(h, w, y, top=top, temperature=0.8)
+    check(s, h, w, y, top, 0.8)
+    bare = head.log_probs(h, w, y, temperature=0.8)
+    assert all(torch.equal(a, b) for a, b in zip(results(s)[:4], results(bare)))
+    rows, tall = torch.full((tokens, width + 5), 9.0, dtype=DT[dtype], device="cuda"), torch.full((vocab, width + 7), 9.0, dtype=DT[dtype], device="cuda")
+    rows[:, 1:1 + width], tall[:, 3:3 + width] = h, w
+    for a, b in zip(results(s), results(head.log_probs(rows[:, 1:1 + width], tall[:, 3:3 + width], y, top=top, temperature=0.8))):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_pieces(losses, dtype):
     """A limited workspace gives the same scores, in pieces of tokens; the weight's gradient is summed over them in fp32."""
