@@ -54,10 +54,10 @@ struct ScoreGrads {
   const float *lse, *lse_rest, *entropy;           // of the forward call
   const float *d_log_prob, *d_entropy;             // d_entropy null: 0
 };
-// *peak = the largest finite |gradient| of the piece, or 1.
+// *peak = the largest finite |gradient| of the piece, or 1: by a launch of its own, or, for few tokens, by the preparation.
 hipError_t launch_score_peak(const ScoreTarget& t, const ScoreGrads& d, long long tokens, long long vocab, float* peak, hipStream_t s);
 // The coefficients, and, with `masked`, hidden states as operand planes, zeros where the token has no gradient.
-hipError_t launch_score_prepare(const ScoreTarget& t, float inv_tau, float unit, const ScoreGrads& d, const float* peak, const HeadRows& rows,
+hipError_t launch_score_prepare(const ScoreTarget& t, float inv_tau, float unit, const ScoreGrads& d, float* peak, const HeadRows& rows,
                                 long long tokens, long long vocab, const ScoreCoef& c, uint16_t* masked, long long ld, long long plane, hipStream_t s);
 // The logits' gradient over *peak, in bf16 or three planes, from the logits' product done again.
 hipError_t launch_score_grad(const HeadOperand& weight, const HeadOperand& hidden, const HeadProduct& g, int pairs, float unit, const ScoreTarget& t,
