@@ -380,6 +380,7 @@ int muon_distill(const muon_head* head, const void* index, int32_t index_bytes, 
  * double, dz is rounded to bf16 once.  lse_rest is what fp32 leaves of lse.
  * kept: device memory of the caller's (256-byte aligned, muon_log_probs_kept_bytes: 2 bytes per token and vocabulary entry, fp32 4) in which a forward
  * call without alternatives leaves what the backward call reads instead of making the logits once more, as often as it is called; null for none.
+ * Of few tokens whose rows a longer call would copy first nothing is kept (0 bytes).
  */
 int muon_log_probs_kept_bytes(const muon_head* head, size_t* out);
 /* Bytes of workspace (256-byte aligned) of muon_log_probs; top: 0 (no alternatives) .. min(64, vocab); max_bytes as above.

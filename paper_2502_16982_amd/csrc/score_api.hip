@@ -104,6 +104,7 @@ int muon_log_probs(const muon_head* h, const void* targets, int32_t targets_byte
         !aligned(top_index, 8) || !aligned(top_log_prob, 4) || !aligned(kept, 256) || !aligned(workspace, 256))
       return MUON_E_MISALIGNED;
     if (kept && kept_bytes < score_kept_bytes(s)) return MUON_E_WORKSPACE_TOO_SMALL;
+    if (score_kept_bytes(s) == 0) kept = nullptr;
     ScorePlan p;
     if (!workspace || !score_plan(s, top > 0, kept != nullptr, workspace_bytes, &p)) return MUON_E_WORKSPACE_TOO_SMALL;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
@@ -149,6 +150,7 @@ int muon_log_probs_backward(const muon_head* h, const void* targets, int32_t tar
         !aligned(d_entropy, 4) || !aligned(kept, 256) || !aligned(d_hidden, size) || !aligned(d_weight, size) || !aligned(workspace, 256))
       return MUON_E_MISALIGNED;
     if (kept && kept_bytes < score_kept_bytes(s)) return MUON_E_WORKSPACE_TOO_SMALL;
+    if (score_kept_bytes(s) == 0) kept = nullptr;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (s.tokens == 0) {
       if (d_weight) MUON_HIP(launch_fill_zero(d_weight, size * s.vocab * s.width, stream));

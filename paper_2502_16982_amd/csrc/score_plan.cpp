@@ -58,12 +58,17 @@ size_t score_workspace(const HeadShape& s, bool best, size_t max_bytes) {
 }
 
 int64_t score_kept_values(const HeadShape& s) { return up(s.tokens * head_plan_shape(s).vocab_pitch * (s.f32 ? 4 : 2), 256); }
-size_t score_kept_bytes(const HeadShape& s) { return (size_t)(score_kept_values(s) + (s.f32 ? 0 : up(s.tokens * head_plan_shape(s).blocks * 4, 256))); }
+bool score_few(const HeadShape& s) { return head_plan_shape(s).pack_weight && s.tokens <= (s.f32 ? kScoreFewF32 : kScoreFew); }
+
+size_t score_kept_bytes(const HeadShape& s) {
+  if (score_few(s)) return 0;
+  return (size_t)(score_kept_values(s) + (s.f32 ? 0 : up(s.tokens * head_plan_shape(s).blocks * 4, 256)));
+}
 
 bool score_plan(const HeadShape& s, bool best, bool keep, size_t bytes, ScorePlan* p) {
   *p = ScorePlan{};
   p->shape = head_plan_shape(s);
-  p->few = !keep && p->shape.pack_weight && s.tokens <= (s.f32 ? kScoreFewF32 : kScoreFew);
+  p->few = !keep && score_few(s);
   const int64_t piece = piece_of(s, best, bytes, kHeadPieceTokens);
   if (piece == 0) return false;
   lay_out(s, best, piece, p);

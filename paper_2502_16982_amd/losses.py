@@ -200,7 +200,7 @@ class LossHead:
         """Log probabilities of ``targets`` (negative: no token, 0) under the softmax of ``hidden @ weight.T / temperature``, the entropy of
         each row's whole distribution, and its ``top`` (up to 64) most likely entries with their log probabilities, the likeliest first, equal
         ones by index.  keep: whether the result holds what ``log_probs_backward`` saves one of its three products by, 2 bytes per token and vocabulary
-        entry (fp32: 4); only without alternatives; None: where the LossHead is for gradients and its max_workspace_bytes, if any, is not
+        entry (fp32: 4); only without alternatives, and not for few tokens where it saves nothing; None: where the LossHead is for gradients and its max_workspace_bytes, if any, is not
         exceeded."""
         head = self._head(hidden, weight)
         self._here(hidden=hidden, weight=weight, targets=targets)
@@ -212,7 +212,7 @@ class LossHead:
             kept, kept_bytes = None, 0
             if keep or (keep is None and self.gradients and not top):
                 kept_bytes = binding.muon_log_probs_kept_bytes(head)
-                if keep or not 0 < self.max_workspace_bytes < kept_bytes:
+                if kept_bytes and (keep or not 0 < self.max_workspace_bytes < kept_bytes):
                     kept = torch.empty(kept_bytes, dtype=torch.uint8, device=self.device)
             values = torch.empty(4, tokens, dtype=torch.float32, device=self.device).unbind(0)
             out = TokenScores(None if targets is None else values[0], *values[1:],

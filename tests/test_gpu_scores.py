@@ -123,7 +123,7 @@ def test_sizes(losses, sizes, dtype):
         check_backward(head.log_probs_backward(h, w, y, s, dl, de, temperature=tau), s, h, w, y, dl, de, tau, dtype)
         for keep in (True, False):
             s = head.log_probs(h, w, y, temperature=tau, keep=keep)
-            assert (s.kept is not None) == keep
+            assert (s.kept is not None) == (keep and (tokens > 64 or (dtype == "bf16" and (tokens > 16 or width % 8 == 0))))
             check(s, h, w, y, 0, tau)
             first = head.log_probs_backward(h, w, y, s, dl, de, temperature=tau)
             check_backward(first, s, h, w, y, dl, de, tau, dtype)
@@ -233,7 +233,7 @@ def test_values_that_are_not_finite(losses, dtype):
     s, clean = head.log_probs(bad, w, y), head.log_probs(h, w, y)
     dh, dw = head.log_probs_backward(bad, w, y, s, dl, de)
     want = head.log_probs_backward(h, w, y, clean, dl, de)
-    assert s.kept is not None and torch.equal(dw, want[1]) and torch.equal(dh, want[0]) and (dh[rows] == 0).all()
+    assert (s.kept is not None) == (dtype == "bf16") and torch.equal(dw, want[1]) and torch.equal(dh, want[0]) and (dh[rows] == 0).all()
 
 
 def test_logits_of_minus_infinity(losses):
@@ -271,7 +271,7 @@ def test_every_form_of_launch(losses, tokens, vocab, width, dtype):
     dh, dw = head.log_probs_backward(h, w, y, s, dl, de, temperature=1.3)
     k = head.log_probs(h, w, y, temperature=1.3)
     dh2, dw2 = head.log_probs_backward(h, w, y, k, dl, de, temperature=1.3)
-    assert k.kept is not None
+    assert k.kept is not None or (tokens <= 64 and (dtype == "f32" or width % 8))
     logp = torch.log_softmax(h.double() @ w.double().T.contiguous() / 1.3, 1)
     entropy = torch.special.entr(logp.exp()).sum(1)
     best = logp.topk(4)

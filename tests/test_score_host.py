@@ -99,7 +99,8 @@ def test_refusals():
                 dict(best=FAKE + 2), dict(ws=FAKE + 128), dict(top=0, kept=FAKE + 128, kept_bytes=1 << 30)):
         assert call(h, **bad) == -7, bad
     room = binding.muon_log_probs_kept_bytes(h)
-    assert room >= 4 * 256 * 2 and binding.muon_log_probs_kept_bytes(head(dtype=0)) >= 4 * 256 * 4
+    assert room >= 4 * 256 * 2 and binding.muon_log_probs_kept_bytes(head(tokens=100, dtype=0)) >= 100 * 256 * 4
+    assert binding.muon_log_probs_kept_bytes(head(dtype=0)) == binding.muon_log_probs_kept_bytes(head(width=15)) == 0
     assert L.muon_log_probs_kept_bytes(C.byref(h), None) == L.muon_log_probs_kept_bytes(None, C.byref(C.c_size_t())) == -1
     assert call(h, top=0, kept=FAKE, kept_bytes=room - 1) == -4
     assert call(head(tokens=0), ws=None) == 0
