@@ -393,3 +393,47 @@ def test_no_tokens(losses):
     for s in (s, head.log_probs(h[:0], w, y[:0])):
         dh, dw = head.log_probs_backward(h[:0], w, y[:0], s, s.log_prob)
         assert dh.shape == (0, 32) and (dw == 0).all()
+
+
+@pytest.mark.parametrize("dtype,tokens,vocab,width", [("f32", 3, 70001, 32768), ("bf16", 24, 140001, 32768), ("bf16", 5, 280001, 16385)])
+def test_weights_beyond_32_bits(losses, dtype, tokens, vocab, width):
+    """The weight's last rows, the only ones that are not zero, start beyond 2^31 elements (fp32: 2^32 bytes)."""
+    last = 300
+    g = torch.Generator().manual_seed(3)
+    few = (torch.randn(last, width, generator=g) * 0.02).to(DT[dtype]).cuda()
+    w = torch.zeros(vocab, width, dtype=DT[dtype], device="cuda")
+    w[-last:] = few
+    h = torch.randn(tokens, width, generator=g).to(DT[dtype]).cuda()
+    y = torch.randint(vocab - last, vocab, (tokens,), generator=g).cuda()
+    head = losses.LossHead(tokens, vocab, width, DT[dtype], gradients=False)
+    s = head.log_probs(h, w, y, top=2)
+    h64, w64 = as64(h), as64(few)
+    z = h64 @ w64.T
+    lse = np.log(vocab - last + np.exp(z).sum(axis=1))
+    entropy = lse - (np.exp(z - lse[:, None]) * z).sum(axis=1)
+    _, lse_err, h_err = errors(h64, w64, 1.0, lse, entropy)
+    h_err = h_err + 2.0 ** -20 * np.log(vocab)
+    order = np.argsort(-z, axis=1)[:, :2]
+    assert (np.abs(as64(s.lse) - lse) <= lse_err).all()
+    assert (np.abs(as64(s.entropy) - entropy) <= h_err).all()
+    assert np.array_equal(s.top_index.cpu().numpy(), order + vocab - last)
+    for got, at in ((s.log_prob[:, None], (y.cpu().numpy() - vocab + last)[:, None]), (s.top_log_prob, order)):
+        want = np.take_along_axis(z, at, 1) - lse[:, None]
+        assert (np.abs(as64(got) - want) <= lse_err[:, None] + 2.0 ** -22 * np.abs(want)).all()
+
+
+def test_kept_powers_beyond_32_bits(losses):
+    """17000 x 131072 kept powers; the last tokens are the only ones with gradients."""
+    tokens, vocab, width, last = 17000, 131072, 64, 48
+    h, w, y, g = make(tokens, vocab, width, "bf16")
+    dl, de = torch.zeros(tokens), torch.zeros(tokens)
+    dl[-last:], de[-last:] = torch.randn(last, generator=g), torch.randn(last, generator=g) * 0.3
+    dl, de = dl.cuda(), de.cuda()
+    head = losses.LossHead(tokens, vocab, width)
+    s = head.log_probs(h, w, y)
+    assert s.kept.numel() > 2 ** 32
+    dh, dw = head.log_probs_backward(h, w, y, s, dl, de)
+    assert (dh[:-last] == 0).all()
+    part = losses.TokenScores(*(None if t is None else t[-last:] for t in s[:6]), s.kept)
+    check(part, h[-last:], w, y[-last:])
+    check_backward((dh[-last:], dw), part, h[-last:], w, y[-last:], dl[-last:], de[-last:])
