@@ -773,14 +773,14 @@ __global__ __launch_bounds__(256) void score_dz_kernel(ScoreTarget t, float unit
       float y[8], p[8];
       if constexpr (F32) {
         const f32x4* z = reinterpret_cast<const f32x4*>(static_cast<const float*>(kept.values) + row + v);
-        const f32x4 two[2] = {z[0], z[1]};
+        const f32x4 two[2] = {__builtin_nontemporal_load(z), __builtin_nontemporal_load(z + 1)};
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           y[e] = fmaxf(fmaf(unit, two[e / 4][e % 4], -l2.x) - l2.y, kFarBelow);
           p[e] = __builtin_amdgcn_exp2f(y[e]);
         }
       } else {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const u16*>(kept.values) + row + v);
+        const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const u16*>(kept.values) + row + v));
         const float shift = (kept.tops[token * blocks + v / kHeadGrain] - l2.x) - l2.y, f = __builtin_amdgcn_exp2f(shift);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
