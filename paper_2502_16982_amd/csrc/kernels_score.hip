@@ -72,15 +72,46 @@ struct Add {
   }
 };
 
+// Elements [c, c + 8) of a row that has them, as they lie there.  (load_row8 decides for each row anew and waits for it there: the finish of
+// 300 x 8191 x 512 fp32, top 20, 35 us so, 22 with these.)
+template <bool F32>
+struct Raw8 {
+  u32x4 w[F32 ? 2 : 1];
+};
+template <bool F32>
+__device__ __forceinline__ Raw8<F32> load_raw8(const void* base, long long row_at, long long c) {
+  const char* p = static_cast<const char*>(base) + (row_at + c) * (F32 ? 4 : 2);
+  Raw8<F32> r;
+#pragma unroll
+  for (int q = 0; q < (F32 ? 2 : 1); ++q) {
+    if constexpr (F32) r.w[q] = __builtin_bit_cast(u32x4, (f32x4)*reinterpret_cast<const f32x4_any*>(p + 16 * q));
+    else r.w[q] = *reinterpret_cast<const u32x4_any*>(p);
+  }
+  return r;
+}
+template <bool F32>
+__device__ __forceinline__ double raw_value(const Raw8<F32>& r, int e) {
+  if constexpr (F32) return (double)__uint_as_float(r.w[e / 4][e % 4]);
+  else return (double)(e % 2 ? bf16_hi(r.w[0][e / 2]) : bf16_lo(r.w[0][e / 2]));
+}
+template <bool F32>
+__device__ __forceinline__ float load_one(const void* base, long long at) {
+  if constexpr (F32) return static_cast<const float*>(base)[at];
+  else return bf16_value(static_cast<const u16*>(base)[at]);
+}
+
 // <a, b> over `width` elements by a whole wave, in double.
 template <bool F32>
 __device__ __forceinline__ double row_dot64(const void* a, long long a_at, const void* b, long long b_at, long long width) {
   double sum = 0.0;
-  for (long long c = (threadIdx.x & 63) * 8; c < width; c += 512) {
-    const Row8 x = load_row8<F32>(a, a_at, c, width), y = load_row8<F32>(b, b_at, c, width);
+  const int lane = threadIdx.x & 63;
+  for (long long c = lane * 8; c + 8 <= width; c += 512) {
+    const Raw8<F32> x = load_raw8<F32>(a, a_at, c), y = load_raw8<F32>(b, b_at, c);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fma((double)x.v[e], (double)y.v[e], sum);
+    for (int e = 0; e < 8; ++e) sum = fma(raw_value(x, e), raw_value(y, e), sum);
   }
+  const long long c = width / 8 * 8 + lane;              // the last elements, one per lane
+  if (c < width) sum = fma((double)load_one<F32>(a, a_at + c), (double)load_one<F32>(b, b_at + c), sum);
   return wave_all(sum, Add{});
 }
 
@@ -431,6 +462,29 @@ __global__ __launch_bounds__(256) void score_few_kernel(HeadRows rows, long long
 // ---- forward: one block per token joins the blocks and picks the alternatives ----
 typedef unsigned long long u64;
 
+// A value that a wave's lanes agree on, in scalar registers.
+template <typename X>
+__device__ __forceinline__ X same_in_all(X x) {
+  static_assert(sizeof(X) == 8, "two words");
+  u32x2 w = __builtin_bit_cast(u32x2, x);
+  w.x = __builtin_amdgcn_readfirstlane(w.x);
+  w.y = __builtin_amdgcn_readfirstlane(w.y);
+  return __builtin_bit_cast(X, w);
+}
+
+// Threads, neighbours, that share one of n items: as many as there are, a power of two.
+template <int NT>
+__device__ __forceinline__ int sharers(int n) {
+  int s = 1;
+  while (s < 64 && 2 * s * n <= NT) s *= 2;
+  return s;
+}
+// Sum over the `s` neighbours.
+__device__ __forceinline__ int shared_sum(int x, int s) {
+  for (int d = 1; d < s; d *= 2) x += __shfl_xor(x, d, 64);
+  return x;
+}
+
 // Larger keys are larger values, then lower rows; 0 is none.
 __device__ __forceinline__ unsigned rising(unsigned bits) { return bits ^ ((unsigned)((int)bits >> 31) | 0x80000000u); }
 __device__ __forceinline__ u64 key_of(float z, unsigned row) { return (u64)rising(__float_as_uint(z)) << 32 | (0xffffffffu - row); }
@@ -440,9 +494,11 @@ __device__ __forceinline__ float second_bound(unsigned w) { return __uint_as_flo
 constexpr int kPickGroups = 4096;                // groups whose keys stay in registers: all, up to 131072 vocabulary entries
 constexpr int kPickList = 256;
 
-// Bound by the chain of its memory accesses for a few tokens, by the rows whose logits are summed again for many.
+// Bound by the chain of its memory accesses for a few tokens (8 x 32768 x 1024, top 5: 10 us), by the rows whose logits are summed again and the
+// operations of the choice for many: 4096 x 100003 x 2048, top 8, 94 us, of which the statistics 16, the choice 36; 2048 x 32768 x 1024, top 64, 184.
+// Blocks of 256 threads are held to registers for five waves: with four 138 and 249, with six, which spill, 169 and 284 us.
 template <bool F32, bool PICK, int NT>
-__global__ __launch_bounds__(NT) void score_finish_kernel(ScoreTarget t, float inv_tau, float unit, const ScoreStats* __restrict__ stats, long long blocks,
+__global__ __launch_bounds__(NT, NT == 256 ? 5 : 1) void score_finish_kernel(ScoreTarget t, float inv_tau, float unit, const ScoreStats* __restrict__ stats, long long blocks,
                                                            const ScoreBest* __restrict__ best, long long groups, int top, HeadRows rows,
                                                            long long vocab, ScoreOut out) {
   constexpr int NW = NT / 64, kPickKeys = kPickGroups / NT;
@@ -488,7 +544,7 @@ __global__ __launch_bounds__(NT) void score_finish_kernel(ScoreTarget t, float i
     }
   }
   // the given token's logit: here, or, with picks, beside theirs
-  const long long y = out.log_prob ? target_at(t, token) : -1;
+  const long long y = same_in_all(out.log_prob ? target_at(t, token) : -1);
   const bool there = y >= 0 && y < vocab;
   double given = 0.0;
   if (!PICK && there && wave == NW - 1)
@@ -507,7 +563,7 @@ __global__ __launch_bounds__(NT) void score_finish_kernel(ScoreTarget t, float i
   double mass = 0.0, tilt = 0.0;
 #pragma unroll
   for (int w = 0; w < NW; ++w) mass += sums[w], tilt += sums[NW + w];
-  const double per = (double)inv_tau / (double)unit, l2 = log2(mass), lse = per * ((double)all + l2);
+  const double per = (double)inv_tau / (double)unit, l2 = log2(mass), lse = same_in_all(per * ((double)all + l2));
   if (tid == 0) {
     const double h = per * (l2 - tilt / mass);
     out.entropy[token] = h < 0.0 ? 0.f : (float)h;       // (what rounding leaves below 0; NaN stays)
@@ -553,11 +609,13 @@ __global__ __launch_bounds__(NT) void score_finish_kernel(ScoreTarget t, float i
     const int shares = coarse ? 64 : 256;
     if (own) atomicMax(&bins[tid % shares], own);
     __syncthreads();
-    if (tid < shares) {
-      const u64 share = bins[tid];
+    {
+      const int s = NT / shares, i = tid / s;
+      const u64 share = bins[i];
       int rank = 0;
 #pragma unroll 8
-      for (int i = 0; i < shares; ++i) rank += bins[i] > share;
+      for (int k = tid % s; k < shares; k += s) rank += bins[k] > share;
+      rank = shared_sum(rank, s);
       if (share && rank == pick - 1) bound = share;
     }
     __syncthreads();
@@ -595,19 +653,22 @@ __global__ __launch_bounds__(NT) void score_finish_kernel(ScoreTarget t, float i
     // the picks, by the threads that hold them: their rows, and all rows of a group whose second may be among the largest as well
     u64 key = 0;
     int rank = 0;
-    if (tid < n) {
-      key = list[tid];
+    const int s = sharers<NT>(n), item = tid / s;
+    const bool holds = item < n && tid % s == 0;
+    if (item < n) {
+      key = list[item];
 #pragma unroll 8
-      for (int k = 0; k < n; ++k) rank += list[k] > key;
+      for (int k = tid % s; k < n; k += s) rank += list[k] > key;
+      rank = shared_sum(rank, s);
       if (rank == pick - 1) bound = key;
     }
     if (tid == 0 && n < pick) bound = 0;
     const int have = n < pick ? n : pick;
     __syncthreads();
-    if (tid < n && rank < pick) {
+    if (holds && rank < pick) {
       const unsigned row = key_row(key);
       row_of[rank] = (int)row;
-      if (((u64)rising(__float_as_uint(second_bound(seconds[tid]))) << 32 | 0xffffffffu) >= bound) open[atomicAdd(&counts[1], 1)] = (int)row;
+      if (((u64)rising(__float_as_uint(second_bound(seconds[item]))) << 32 | 0xffffffffu) >= bound) open[atomicAdd(&counts[1], 1)] = (int)row;
     }
     __syncthreads();
     const int c = have + 32 * counts[1];
@@ -629,15 +690,23 @@ __global__ __launch_bounds__(NT) void score_finish_kernel(ScoreTarget t, float i
           z[u] = 0.0;
           at[u] = (row < 0 ? 0 : row) * rows.weight_stride;
         }
-        for (long long k = lane * 8; k < rows.width; k += 512) {
-          const Row8 x = load_row8<F32>(rows.hidden, token * rows.hidden_stride, k, rows.width);
-          Row8 w[U];
+        for (long long k = lane * 8; k + 8 <= rows.width; k += 512) {
+          const Raw8<F32> x = load_raw8<F32>(rows.hidden, token * rows.hidden_stride, k);
+          Raw8<F32> w[U];
 #pragma unroll
-          for (int u = 0; u < U; ++u) w[u] = load_row8<F32>(rows.weight, at[u], k, rows.width);
+          for (int u = 0; u < U; ++u) w[u] = load_raw8<F32>(rows.weight, at[u], k);
 #pragma unroll
-          for (int u = 0; u < U; ++u)
+          for (int u = 0; u < U; ++u) {
+            __builtin_amdgcn_sched_barrier(0);           // a row after the other: doubles of all would not fit the registers
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[u] = fma((double)x.v[e], (double)w[u].v[e], z[u]);
+            for (int e = 0; e < 8; ++e) z[u] = fma(raw_value(x, e), raw_value(w[u], e), z[u]);
+          }
+        }
+        if (lane < (int)(rows.width & 7)) {              // the last elements, one per lane
+          const long long k = rows.width / 8 * 8 + lane;
+          const double x = load_one<F32>(rows.hidden, token * rows.hidden_stride + k);
+#pragma unroll
+          for (int u = 0; u < U; ++u) z[u] = fma(x, (double)load_one<F32>(rows.weight, at[u] + k), z[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -657,17 +726,19 @@ __global__ __launch_bounds__(NT) void score_finish_kernel(ScoreTarget t, float i
     if (all_rows <= NW) sum_rows(std::integral_constant<int, 1>{});
     else sum_rows(std::integral_constant<int, 4>{});
     __syncthreads();
-    for (int i = tid; i < c; i += NT) {
+    const int s2 = sharers<NT>(c);
+    for (int i = tid / s2; i < c; i += NT / s2) {
       const int row = row_of[i];
       const u64 mine_is = rank_of[i];
       int ahead = 0;
 #pragma unroll 8
-      for (int k = 0; k < c; ++k) {
-        const int other = row_of[k];
+      for (int k = tid % s2; k < c; k += s2) {             // (no row, -1, is the largest)
+        const unsigned other = row_of[k];
         const u64 is = rank_of[k];
-        ahead += is > mine_is || (is == mine_is && other >= 0 && other < row);
+        ahead += (int)(is > mine_is) | ((int)(is == mine_is) & (int)(other < (unsigned)row));
       }
-      if (row >= 0 && ahead < top) {
+      ahead = shared_sum(ahead, s2);
+      if (row >= 0 && ahead < top && tid % s2 == 0) {
         out.top_index[token * top + ahead] = row;
         out.top_log_prob[token * top + ahead] = log_prob(value[i]);
       }
