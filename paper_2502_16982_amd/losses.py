@@ -200,8 +200,8 @@ class LossHead:
         """Log probabilities of ``targets`` (negative: no token, 0) under the softmax of ``hidden @ weight.T / temperature``, the entropy of
         each row's whole distribution, and its ``top`` (up to 64) most likely entries with their log probabilities, the likeliest first, equal
         ones by index.  keep: whether the result holds what ``log_probs_backward`` saves one of its three products by, 2 bytes per token and vocabulary
-        entry (fp32: 4); only without alternatives, and not for few tokens where it saves nothing; None: where the LossHead is for gradients and its max_workspace_bytes, if any, is not
-        exceeded."""
+        entry (fp32: 4); only without alternatives, and not for few tokens where it saves nothing; None: where the LossHead is for gradients and
+        its max_workspace_bytes, if any, is not exceeded."""
         head = self._head(hidden, weight)
         self._here(hidden=hidden, weight=weight, targets=targets)
         outside_autograd("LossHead.log_probs", hidden.requires_grad or weight.requires_grad)
