@@ -237,8 +237,8 @@ class LossHead:
         if d_log_prob is None and d_entropy is None:
             raise MuonError(-1, "d_log_prob or d_entropy")
         kept = scores.kept
-        if kept is not None and (kept.device != self.device or kept.numel() != binding.muon_log_probs_kept_bytes(head)):
-            raise MuonError(-1, "scores.kept: of another call's sizes")
+        if kept is not None and (kept.device != self.device or kept.numel() != (binding.muon_log_probs_kept_bytes(head) or kept.numel())):
+            raise MuonError(-1, "scores.kept: of another call's sizes")         # (0: a call whose own rows would be copied; it makes the logits again)
         given = []
         for name, t in (("lse", scores.lse), ("lse_rest", scores.lse_rest), ("entropy", scores.entropy), ("d_log_prob", d_log_prob),
                         ("d_entropy", d_entropy)):

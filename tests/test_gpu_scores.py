@@ -395,6 +395,18 @@ def test_no_tokens(losses):
         assert dh.shape == (0, 32) and (dw == 0).all()
 
 
+def test_gradients_from_rows_of_another_alignment(losses):
+    """Scores that kept their powers, gradients by the same values in rows that would be copied: the logits are made again."""
+    h, w, y, g = make(5, 700, 64, "bf16")
+    head = losses.LossHead(5, 700, 64)
+    s = head.log_probs(h, w, y)
+    assert s.kept is not None
+    dl, de = torch.randn(5, generator=g).cuda(), torch.randn(5, generator=g).cuda()
+    other = torch.empty(700 * 64 + 1, dtype=w.dtype, device="cuda")[1:].view(700, 64).copy_(w)
+    check_backward(head.log_probs_backward(h, other, y, s, dl, de), s, h, w, y, dl, de)
+    check_backward(head.log_probs_backward(h, w, y, head.log_probs(h, other, y), dl, de), s, h, w, y, dl, de)
+
+
 @pytest.mark.parametrize("dtype,tokens,vocab,width", [("f32", 3, 70001, 32768), ("bf16", 24, 140001, 32768), ("bf16", 5, 280001, 16385)])
 def test_weights_beyond_32_bits(losses, dtype, tokens, vocab, width):
     """The weight's last rows, the only ones that are not zero, start beyond 2^31 elements (fp32: 2^32 bytes)."""
