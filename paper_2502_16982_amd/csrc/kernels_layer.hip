@@ -72,7 +72,8 @@ __device__ __forceinline__ int find_pairs(const LayerPairs& p, int e, int base, 
   return seen;
 }
 
-__device__ __forceinline__ float activate(int act, float z) { return act == 0 ? z / (1.f + expf(-z)) : fmaxf(z, 0.f); }
+// (a comparison, not the maximum instruction, which would make a NaN 0)
+__device__ __forceinline__ float activate(int act, float z) { return act == 0 ? z / (1.f + expf(-z)) : z < 0.f ? 0.f : z; }
 
 template <bool F32>
 struct Elem {

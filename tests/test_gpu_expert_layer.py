@@ -189,3 +189,30 @@ def test_refusals(experts):
         a.update(over)
         with pytest.raises(MuonError):
             experts.layer(**a)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("activation", ["silu", "relu"])
+@pytest.mark.parametrize("tokens,width,inner,n,top", [(4, 70, 90, 5, 2), (2, 700, 300, 4, 2), (1, 4096, 1408, 8, 8)])
+def test_activations_of_nan_are_nan(experts, tokens, width, inner, n, top, activation, dtype):
+    """NaN in a hidden state, and in one element of an expert's Gate or Up, reaches every element of the rows it is part of, wherever the activation is
+    made: beside the first product, in the second one's operand or by a launch of its own."""
+    x, up, down, expert, weights, gate = make(tokens, width, inner, n, top, dtype)
+    expert[0] = torch.arange(top)
+    nan = float("nan")
+    for g in (gate, None):
+        want = experts.layer(x, up, down, expert, weights, gate=g, activation=activation)
+        check(want, x, up, down, expert, weights, g, activation)
+        bad_x = x.clone()
+        bad_x[0, width - 1] = nan
+        got = experts.layer(bad_x, up, down, expert, weights, gate=g, activation=activation)
+        assert got[0].isnan().all() and torch.equal(got[1:], want[1:])
+        reached = (expert == 0).any(1)
+        for which in ("up", "gate"):
+            m = {"up": up, "gate": g}[which]
+            if m is None:
+                continue
+            m = m.clone()
+            m[0, 0, inner - 1] = nan
+            got = experts.layer(x, m if which == "up" else up, down, expert, weights, gate=m if which == "gate" else g, activation=activation)
+            assert got[reached].isnan().all() and torch.equal(got[~reached], want[~reached]), which
