@@ -116,6 +116,7 @@ __device__ __forceinline__ double row_dot64(const void* a, long long a_at, const
 }
 
 // ---- forward: the product's epilogue ----
+constexpr float kProbScale = (float)(1 << (int)kProbTop);
 constexpr float kFarBelow = -1e4f;               // 2^this is 0: an infinite exponent times its power of 0 has to be 0
 
 // Groups of a token in order of (64 vocabulary entries, half): a lane's 32 accumulators of a column, in two MFMA tiles.
@@ -202,7 +203,7 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
   auto take_powers = [&](auto masked) {
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
-      top[j] = (top[j] == -INFINITY ? 0.f : unit * top[j]) - (KEEP == 1 ? kProbTop : 0.f);
+      top[j] = top[j] == -INFINITY ? 0.f : unit * top[j];
       float sum = 0.f, slope = 0.f;
 #pragma unroll
       for (int i = 0; i < T::FM; ++i)
@@ -217,7 +218,9 @@ __device__ __forceinline__ void score_tile(const HeadOperand& weight, const Head
             sum += x[e];
             slope = fmaf(x[e], fmaxf(y, kFarBelow), slope);
           }
-          if constexpr (KEEP == 1) tile.put(smem, i, j, q, u32x2{pack_f16(x[0], x[1]), pack_f16(x[2], x[3])});
+          // (only what is kept is times 2^kProbTop: in the sums, exponents 15 from 0 would carry the rounding steps of 15, and the entropy is their difference)
+          if constexpr (KEEP == 1)
+            tile.put(smem, i, j, q, u32x2{pack_f16(kProbScale * x[0], kProbScale * x[1]), pack_f16(kProbScale * x[2], kProbScale * x[3])});
           __builtin_amdgcn_sched_barrier(0);
         }
       sums[j] = sum + __shfl_xor(sum, 32, 64);
@@ -855,7 +858,7 @@ __global__ __launch_bounds__(256) void score_dz_kernel(ScoreTarget t, float unit
         }
       } else {
         const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const u16*>(kept.values) + row + v));
-        const float shift = (kept.tops[token * blocks + v / kHeadGrain] - l2.x) - l2.y, f = __builtin_amdgcn_exp2f(shift);
+        const float shift = ((kept.tops[token * blocks + v / kHeadGrain] - l2.x) - l2.y) - kProbTop, f = __builtin_amdgcn_exp2f(shift);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const unsigned pair = w[e / 2];                // (a bit cast of the vector's element itself would take its first)

@@ -22,7 +22,7 @@ struct ScoreBest {
   float z;
   unsigned second;
 };
-// What a forward call keeps for the backward one, [tokens, pitch]: powers 2^(y - top) in f16, up to 2^15 in a block, with each block's top per
+// What a forward call keeps for the backward one, [tokens, pitch]: powers 2^(15 + y - top) in f16, up to 2^15 in a block, with each block's top per
 // token; or, tops null, z in fp32.  values null: nothing.  Not together with `best`.
 struct ScoreKept {
   void* values;

@@ -449,3 +449,37 @@ def test_kept_powers_beyond_32_bits(losses):
     part = losses.TokenScores(*(None if t is None else t[-last:] for t in s[:6]), s.kept)
     check(part, h[-last:], w, y[-last:])
     check_backward((dh[-last:], dw), part, h[-last:], w, y[-last:], dl[-last:], de[-last:])
+
+
+@pytest.mark.parametrize("tokens,vocab,width", [(64, 1024, 64), (171, 36393, 72)])
+def test_entropy_of_peaked_rows(losses, tokens, vocab, width):
+    """A token's likeliest entry and n others in one block, everything else without weight, logits exact (hidden states pick a column of the weight).
+
+    With a_i = z_top - z_i, q the probabilities, A = sum q a, rounding steps u = 2^-24: sums of n + 1 powers and of their products with exponents, and
+    two joins of waves, are off by (n + 2) u of themselves, a power by 2 u (the instruction's last bit) and by a_i u (its exponent's rounding), the products by u, the
+    exponents' unit by u.  entropy = log S + A takes an error e of a power i with q_i e (1 + a_i + A) and one of S with (1 + A); the result is rounded once more.
+    Exponents relative to anything but the largest would carry steps of their own size."""
+    g = torch.Generator().manual_seed(0)
+    z = torch.full((vocab, width), -200.0)
+    top = (torch.rand(width, generator=g) * 16 - 8).bfloat16().float()
+    for c in range(width):
+        n = 1 + c % 4
+        at = int(torch.randint(vocab // 128, (1,), generator=g)) * 128 + torch.randperm(128, generator=g)[:n + 1]
+        z[at[0], c] = top[c]
+        z[at[1:], c] = (top[c] - 0.5 - c // 4 * 0.85 - torch.rand(n, generator=g)).bfloat16().float()
+    h = torch.eye(width)[torch.arange(tokens) % width].bfloat16().cuda()
+    head = losses.LossHead(tokens, vocab, width)
+    z64 = z.double().numpy().T[np.arange(tokens) % width]
+    a = z64.max(1, keepdims=True) - z64
+    p = np.where(a < 100, np.exp(-a), 0.0)
+    lse = z64.max(1) + np.log(p.sum(1))
+    q, n = p / p.sum(1, keepdims=True), (p > 0).sum(1) - 1
+    a = np.where(p > 0, a, 0.0)
+    mean = (q * a).sum(1)
+    entropy = np.log(p.sum(1)) + mean
+    others = np.where(a > 0, q, 0.0) * (2 + a)
+    err = 2.0 ** -24 * ((n + 2) * (1 + 2 * mean) + 2 * (1 + mean) + mean + (others * (1 + a + mean[:, None])).sum(1) + (q * a * a).sum(1))
+    lse_err = 2.0 ** -24 * (n + 4 + others.sum(1) + mean)
+    for s in (head.log_probs(h, z.bfloat16().cuda(), keep=True), head.log_probs(h, z.bfloat16().cuda(), keep=False), head.log_probs(h, z.bfloat16().cuda(), top=3)):
+        assert (np.abs(as64(s.entropy) - entropy) <= err + 2.0 ** -24 * entropy).all(), np.max(np.abs(as64(s.entropy) - entropy) / err)
+        assert (np.abs(as64(s.lse) + as64(s.lse_rest) - lse) <= lse_err + 2.0 ** -48 * np.abs(lse)).all()
