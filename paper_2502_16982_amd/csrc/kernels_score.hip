@@ -816,6 +816,9 @@ __global__ __launch_bounds__(256) void score_prepare_kernel(ScoreTarget t, float
         const double d0 = (double)inv_tau * z - lse, lp = d0 > 0.0 ? 0.0 : d0, p = exp(lp);
         value = (float)(-g * expm1(lp) - (x.h != 0.f && p > 0.0 ? h * p * (lp + entropy) : 0.0));
       }
+      // logits that are NaN or infinite: no gradient of the token is a number.  (The powers alone would not say so: a NaN exponent is cut off at
+      // kFarBelow; and an infinite sum stands for a token without gradients.)
+      if (!(fabsf(l2.x) < INFINITY)) a = value = l2.x = __builtin_nanf("");
     }
     if (threadIdx.x == 0) {
       c.a[token] = a;

@@ -483,3 +483,22 @@ def test_entropy_of_peaked_rows(losses, tokens, vocab, width):
     for s in (head.log_probs(h, z.bfloat16().cuda(), keep=True), head.log_probs(h, z.bfloat16().cuda(), keep=False), head.log_probs(h, z.bfloat16().cuda(), top=3)):
         assert (np.abs(as64(s.entropy) - entropy) <= err + 2.0 ** -24 * entropy).all(), np.max(np.abs(as64(s.entropy) - entropy) / err)
         assert (np.abs(as64(s.lse) + as64(s.lse_rest) - lse) <= lse_err + 2.0 ** -48 * np.abs(lse)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_of_logits_that_are_not_finite(losses, dtype):
+    """A token with gradients whose logits are NaN or infinite: no gradient of its own and none of the weight is finite; the other tokens' rows stay."""
+    h, w, y, g = make(90, 900, 72, dtype)
+    dl, de = torch.randn(90, generator=g).cuda(), torch.randn(90, generator=g).cuda()
+    head = losses.LossHead(90, 900, 72, DT[dtype])
+    for value in (float("nan"), float("inf")):
+        bad = h.clone()
+        bad[11, 5] = value
+        rest = [t for t in range(90) if t != 11]
+        for keep in (True, False):
+            s, clean = head.log_probs(bad, w, y, keep=keep), head.log_probs(h, w, y, keep=keep)
+            for a, b, to in ((dl, None, y), (dl, de, y), (None, de, None)):
+                dh, dw = head.log_probs_backward(bad, w, to, s, a, b)
+                want, _ = head.log_probs_backward(h, w, to, clean, a, b)
+                assert dh[11].isnan().all() and torch.equal(dh[rest], want[rest])
+                assert dw.isnan().all(), (value, keep, a is None, b is None, int(dw.isnan().all(1).sum()))
