@@ -228,7 +228,8 @@ class LossHead:
         """(d_hidden, d_weight) of ``(d_log_prob * log_prob + d_entropy * entropy).sum()`` with the ``scores`` that ``log_probs`` gave for the
         same hidden states, weight, targets and temperature.  ``d_log_prob`` is None without targets, ``d_entropy`` None for 0."""
         head = self._head(hidden, weight)
-        self._here(hidden=hidden, weight=weight, targets=targets, d_log_prob=d_log_prob, d_entropy=d_entropy, lse=scores.lse)
+        self._here(hidden=hidden, weight=weight, targets=targets, d_log_prob=d_log_prob, d_entropy=d_entropy, lse=scores.lse, lse_rest=scores.lse_rest,
+                   entropy=scores.entropy, kept=scores.kept)
         outside_autograd("LossHead.log_probs_backward", hidden.requires_grad or weight.requires_grad)
         tokens = hidden.shape[0]
         at, size = self._targets(targets, tokens)
@@ -237,7 +238,7 @@ class LossHead:
         if d_log_prob is None and d_entropy is None:
             raise MuonError(-1, "d_log_prob or d_entropy")
         kept = scores.kept
-        if kept is not None and (kept.device != self.device or kept.numel() != (binding.muon_log_probs_kept_bytes(head) or kept.numel())):
+        if kept is not None and kept.numel() != (binding.muon_log_probs_kept_bytes(head) or kept.numel()):
             raise MuonError(-1, "scores.kept: of another call's sizes")         # (0: a call whose own rows would be copied; it makes the logits again)
         given = []
         for name, t in (("lse", scores.lse), ("lse_rest", scores.lse_rest), ("entropy", scores.entropy), ("d_log_prob", d_log_prob),

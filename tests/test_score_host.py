@@ -170,3 +170,16 @@ def test_plans(tmp_path):
                    check=True)
     out = subprocess.run([exe], capture_output=True, text=True)
     assert out.returncode == 0 and "ok" in out.stdout, out.stdout + out.stderr
+
+
+def test_scores_of_another_device_are_refused(loss_head):
+    """Each tensor of the scores whose address goes to the library has to be where the workspace is."""
+    head, calls = loss_head
+    h, w, y = torch.zeros(4, 16, dtype=torch.bfloat16), torch.zeros(100, 16, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int64)
+    s, d = head.log_probs(h, w, y), torch.ones(4)
+    head.log_probs_backward(h, w, y, s, d, d)
+    count = len(calls)
+    for name in ("lse", "lse_rest", "entropy", "kept"):
+        with pytest.raises(binding.MuonError, match="is on meta|another call"):
+            head.log_probs_backward(h, w, y, s._replace(**{name: getattr(s, name).to("meta")}), d, d)
+    assert len(calls) == count
