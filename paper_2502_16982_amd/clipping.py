@@ -46,9 +46,12 @@ class GradClipper:
         need = binding.muon_grad_norm_bytes(array, len(grads))
         self.grads, self.device, self._array, self._need = grads, device, array, need
 
-    def _call(self, entry, max_norm: float) -> ClipScale:
+    def _on_gpu(self) -> None:
         if self.device.type != "cuda":
             raise MuonError(-1, f"gradients on a GPU, not on {self.device}")
+
+    def _call(self, entry, max_norm: float) -> ClipScale:
+        self._on_gpu()
         with on(self.device):
             norm = torch.empty((), dtype=torch.float64, device=self.device)
             scale = torch.empty((), dtype=torch.float32, device=self.device)
@@ -68,5 +71,6 @@ class GradClipper:
 
     def scale_(self, scale: torch.Tensor) -> None:
         """The gradients times one fp32 element on their device, such as a scale from the norm over several processes, in place."""
+        self._on_gpu()
         with on(self.device):
             binding.muon_grad_scale(self._array, len(self.grads), binding.grad_scale_ptr(scale, self.device), stream_handle(self.device))

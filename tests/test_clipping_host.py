@@ -92,3 +92,9 @@ def test_lists_are_cut_into_whole_spans(tmp_path):
     out = subprocess.run([exe], capture_output=True, text=True)
     assert out.returncode == 0, out.stdout + out.stderr
     assert "ok" in out.stdout
+
+
+def test_scaling_refuses_gradients_that_are_not_on_a_gpu():
+    on_cpu = clipping.GradClipper([torch.zeros(4), torch.zeros(0)])
+    with pytest.raises(binding.MuonError, match="on a GPU"):
+        on_cpu.scale_(torch.ones(1))
