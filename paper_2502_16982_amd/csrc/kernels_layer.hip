@@ -346,7 +346,7 @@ __device__ __forceinline__ void stage(const LayerPairs& p, const LayerSums& from
   __syncthreads();
 }
 
-// Block: (matrix, run of the summed axis, tile of columns, slot); four waves to a matrix, MATS matrices to a block.  NT: tiles of pairs that there may
+// Block: (matrix, run of the summed axis, tile of columns) and slot; four waves to a matrix, MATS matrices to a block.  NT: tiles of pairs that there may
 // be at a time.
 template <bool F32, int MATS, int NT, bool STAGED>
 __global__ __launch_bounds__(256 * MATS, 2) void layer_product_kernel(LayerPairs p, LayerProduct g, LayerRows rows, LayerMatrix w, LayerMatrix gate, LayerSums from,
@@ -361,9 +361,7 @@ __global__ __launch_bounds__(256 * MATS, 2) void layer_product_kernel(LayerPairs
   int b = blockIdx.x;
   const int apart = MATS == 1 ? g.mats : 1, matrix = MATS == 1 ? b % apart : wave / kLayerWaves;
   b /= apart;
-  const int run = b % g.runs;
-  b /= g.runs;
-  const int tile = b % g.tiles, slot = b / g.tiles;
+  const int run = b % g.runs, tile = b / g.runs, slot = blockIdx.y;
   const int e = __builtin_amdgcn_readfirstlane(p.slot_is_pair ? expert_of(p, slot) : slot);
   if (e < 0) return;
   const long long col0 = (long long)tile * (16 * E::COLS);
@@ -409,7 +407,7 @@ __global__ __launch_bounds__(256 * MATS, 2) void layer_product_kernel(LayerPairs
 template <bool F32>
 __global__ __launch_bounds__(256) void layer_act_kernel(LayerPairs p, int runs, long long n, int gated, int act, const float* __restrict__ part,
                                                         void* __restrict__ inner) {
-  const long long spans = (n + 255) / 256, pair = blockIdx.x / spans, c = blockIdx.x % spans * 256 + threadIdx.x;
+  const long long pair = blockIdx.y, c = blockIdx.x * 256ll + threadIdx.x;
   if (c >= n || expert_of(p, (int)pair) < 0) return;
   const int mats = gated ? 2 : 1;
   float up = 0.f, lead = 0.f;
@@ -423,15 +421,14 @@ __global__ __launch_bounds__(256) void layer_act_kernel(LayerPairs p, int runs, 
   else static_cast<u16*>(inner)[pair * n + c] = (u16)(pack_bf16(h, 0.f) & 0xffffu);
 }
 
-// 128 columns of a token per block: four neighbouring ones per thread, the token's terms over eight groups of threads, joined in LDS.
-constexpr int kJoinColumns = 128;
+// kJoinColumns columns of a token per block: four neighbouring ones per thread, the token's terms over eight groups of threads, joined in LDS.
 template <bool F32>
 __global__ __launch_bounds__(256) void layer_join_kernel(LayerPairs p, int runs, long long n, const float* __restrict__ rows, const float* __restrict__ weights,
                                                          void* __restrict__ out) {
   __shared__ f32x4 parts[8][32];
-  const long long spans = (n + kJoinColumns - 1) / kJoinColumns, token = blockIdx.x / spans;
+  const long long token = blockIdx.y;
   const int quad = threadIdx.x & 31, group = threadIdx.x >> 5, terms = p.top * runs;
-  const long long c = blockIdx.x % spans * kJoinColumns + 4 * quad;
+  const long long c = blockIdx.x * (long long)kJoinColumns + 4 * quad;
   const int count = c >= n ? 0 : n - c < 4 ? (int)(n - c) : 4;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -456,7 +453,7 @@ __global__ __launch_bounds__(256) void layer_join_kernel(LayerPairs p, int runs,
   parts[group][quad] = sum;
   __syncthreads();
   if (threadIdx.x >= kJoinColumns) return;
-  const long long at = blockIdx.x % spans * kJoinColumns + threadIdx.x;
+  const long long at = blockIdx.x * (long long)kJoinColumns + threadIdx.x;
   if (at >= n) return;
   const float* of = reinterpret_cast<const float*>(parts) + threadIdx.x;
   float x = of[0];
@@ -466,16 +463,18 @@ __global__ __launch_bounds__(256) void layer_join_kernel(LayerPairs p, int runs,
   else static_cast<u16*>(out)[token * n + at] = (u16)(pack_bf16(x, 0.f) & 0xffffu);
 }
 
+dim3 blocks_of(const LayerGrid& g) { return dim3((unsigned)g.x, (unsigned)g.y); }
+
 }  // namespace
 
 hipError_t launch_layer_product(const LayerPairs& p, const LayerProduct& g, const LayerRows& x, const LayerMatrix& w, const LayerMatrix* gate,
                                 const LayerSums* from, bool f32, int act, void* out, hipStream_t s) {
   const bool together = gate && g.mats == 1;
-  const unsigned blocks = (unsigned)((long long)p.slots * g.tiles * g.runs * g.mats);
+  const LayerGrid grid = layer_product_grid(g, p.slots, together);
   const LayerMatrix none{};
   const LayerSums rows{};
   auto go = [&](auto kernel) {
-    kernel<<<blocks, together ? 512 : 256, 0, s>>>(p, g, x, w, gate ? *gate : none, from ? *from : rows, act, out);
+    kernel<<<blocks_of(grid), grid.threads, 0, s>>>(p, g, x, w, gate ? *gate : none, from ? *from : rows, act, out);
     return hipGetLastError();
   };
 #define MUON_LAYER_CASE(NT)                                                                                            \
@@ -490,16 +489,16 @@ hipError_t launch_layer_product(const LayerPairs& p, const LayerProduct& g, cons
 }
 
 hipError_t launch_layer_act(const LayerPairs& p, int runs, long long n, bool gated, bool f32, int act, const float* part, void* inner, hipStream_t s) {
-  const unsigned blocks = (unsigned)((n + 255) / 256 * p.pairs);
-  if (f32) layer_act_kernel<true><<<blocks, 256, 0, s>>>(p, runs, n, gated, act, part, inner);
-  else layer_act_kernel<false><<<blocks, 256, 0, s>>>(p, runs, n, gated, act, part, inner);
+  const LayerGrid grid = layer_act_grid(n, p.pairs);
+  if (f32) layer_act_kernel<true><<<blocks_of(grid), grid.threads, 0, s>>>(p, runs, n, gated, act, part, inner);
+  else layer_act_kernel<false><<<blocks_of(grid), grid.threads, 0, s>>>(p, runs, n, gated, act, part, inner);
   return hipGetLastError();
 }
 
 hipError_t launch_layer_join(const LayerPairs& p, int runs, long long n, bool f32, const float* rows, const float* weights, void* out, hipStream_t s) {
-  const unsigned blocks = (unsigned)((n + kJoinColumns - 1) / kJoinColumns * (p.pairs / p.top));
-  if (f32) layer_join_kernel<true><<<blocks, 256, 0, s>>>(p, runs, n, rows, weights, out);
-  else layer_join_kernel<false><<<blocks, 256, 0, s>>>(p, runs, n, rows, weights, out);
+  const LayerGrid grid = layer_join_grid(n, p.pairs / p.top);
+  if (f32) layer_join_kernel<true><<<blocks_of(grid), grid.threads, 0, s>>>(p, runs, n, rows, weights, out);
+  else layer_join_kernel<false><<<blocks_of(grid), grid.threads, 0, s>>>(p, runs, n, rows, weights, out);
   return hipGetLastError();
 }
 

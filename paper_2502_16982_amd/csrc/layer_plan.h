@@ -82,4 +82,20 @@ inline LayerPlan layer_plan(const LayerShape& s) {
   return p;
 }
 
+// A launch: blocks along two axes, the first one fastest, and threads per block.  An axis holds less than 2^32 threads, the second one 2^16 blocks; the largest
+// calls have 2^32 in all, so that slots, tokens and pairs have an axis of their own.
+struct LayerGrid {
+  int64_t x, y;
+  int threads;
+};
+
+constexpr int kJoinColumns = 128;                // of a block of the join
+
+// together: gate and up by one block.
+inline LayerGrid layer_product_grid(const LayerProduct& p, int slots, bool together) {
+  return {(int64_t)p.tiles * p.runs * p.mats, slots, 64 * kLayerWaves * (together ? 2 : 1)};
+}
+inline LayerGrid layer_act_grid(int64_t n, int64_t pairs) { return {(n + 255) / 256, pairs, 256}; }
+inline LayerGrid layer_join_grid(int64_t n, int64_t tokens) { return {(n + kJoinColumns - 1) / kJoinColumns, tokens, 256}; }
+
 }  // namespace muon

@@ -96,3 +96,12 @@ def test_oracle():
     assert np.allclose(layer_oracle.act("silu", t.numpy()), torch.nn.functional.silu(t).numpy(), rtol=1e-14)
     out, _ = layer_oracle.layer(x, up, down, expert, None, None, "relu")
     assert np.allclose(out[0], sum(np.maximum(x[0] @ up[e], 0) @ down[e] for e in (0, 1)), rtol=1e-14)
+
+
+def test_launches(tmp_path):
+    """No axis of a launch holds 2^32 threads, at the largest sizes that are taken either."""
+    exe = str(tmp_path / "layer_grid")
+    subprocess.run(["g++", "-O1", "-g", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                    os.path.join(ROOT, "tests", "layer_grid_main.cpp"), "-o", exe], check=True)
+    out = subprocess.run([exe], capture_output=True, text=True)
+    assert out.returncode == 0 and "ok" in out.stdout, out.stdout + out.stderr

@@ -216,3 +216,46 @@ def test_activations_of_nan_are_nan(experts, tokens, width, inner, n, top, activ
             m[0, 0, inner - 1] = nan
             got = experts.layer(x, m if which == "up" else up, down, expert, weights, gate=m if which == "gate" else g, activation=activation)
             assert got[reached].isnan().all() and torch.equal(got[~reached], want[~reached]), which
+
+
+def silu64(z):
+    return z / (1 + (-z).exp())
+
+
+def test_most_blocks_of_the_products(experts):
+    """As many experts, as many columns as there may be, both matrices by one block: 2^32 threads.  Experts share matrices of one row; bounds as the oracle's."""
+    n, inner, g = 4096, 1 << 17, torch.Generator().manual_seed(8)
+    up, gate, down = (torch.randn(inner, generator=g).cuda() for _ in range(3))
+    x = torch.randn(n, 1, generator=g).cuda()
+    weights = torch.rand(n, 1, generator=g).cuda()
+    expert = torch.randperm(n, generator=g)[:, None].cuda()
+    out = experts.layer(x, up.view(1, 1, inner).expand(n, 1, inner), down.view(1, inner, 1).expand(n, inner, 1), expert, weights,
+                        gate=gate.view(1, 1, inner).expand(n, 1, inner))
+    step = 2.0 ** -23
+    for at in range(0, n, 256):
+        x64, w64 = x[at:at + 256].double(), weights[at:at + 256, 0].double()
+        u, z = x64 * up.double(), x64 * gate.double()
+        lead = silu64(z)
+        h = lead * u
+        h_err = 1.1 * 5 * step * z.abs() * u.abs() * (1 + 5 * step) + lead.abs() * 5 * step * u.abs() + h.abs() * 2.0 ** -21
+        y = h @ down.double()
+        bound = w64 * (h_err @ down.double().abs() + (4 + inner ** 0.5) * step * (h.abs() @ down.double().abs()) + 2.0 ** -20 * y.abs()) + step * (w64 * y).abs()
+        assert ((out[at:at + 256, 0].double() - w64 * y).abs() <= bound).all()
+
+
+def test_most_blocks_of_the_join(experts):
+    """As many tokens as there may be, of the largest width: 2^32 threads."""
+    tokens, width, g = 1 << 14, 1 << 17, torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn(tokens, width, generator=g, device="cuda", dtype=torch.bfloat16)
+    up = (torch.randn(width, generator=g, device="cuda") * width ** -0.5).bfloat16()
+    down = torch.randn(width, generator=g, device="cuda").bfloat16()
+    out = experts.layer(x, up.view(1, width, 1), down.view(1, 1, width), torch.zeros(tokens, 1, dtype=torch.int32, device="cuda"))
+    step = 2.0 ** -23
+    for at in range(0, tokens, 1024):
+        x64 = x[at:at + 1024].double()
+        u = x64 @ up.double()
+        h = silu64(u)
+        h_err = 1.1 * (4 + width ** 0.5) * step * (x64.abs() @ up.double().abs()) + h.abs() * (2.0 ** -8 + 2.0 ** -21)
+        scale = h_err + h.abs() * (5 * step + 2.0 ** -20 + 2.0 ** -8 * 1.01)             # bound of row t: scale_t |down|
+        err = (out[at:at + 1024].double() - h[:, None] * down.double()).abs_()
+        assert (err <= scale[:, None] * down.double().abs() + 1e-37).all()
