@@ -1,5 +1,5 @@
 // Log probabilities of given tokens with the entropy of the whole distribution and its top alternatives, and their gradients, from hidden states
-// H [T, D] and the head's weight W [V, D], logits never kept whole.
+// H [T, D] and the head's weight W [V, D].  Logits are not kept, but where the caller gives memory for their powers (fp32: for themselves).
 //
 //   z = H W^T / tau    lse = log sum_v exp z_v    log p_v = z_v - lse    entropy = -sum_v p_v log p_v
 //   d log p_y / d z_v = [v = y] - p_v             d entropy / d z_v = -p_v (log p_v + entropy)

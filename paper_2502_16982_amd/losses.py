@@ -1,6 +1,6 @@
 """Losses of a language model's head with their gradients: softmax cross entropy over a large vocabulary and distillation
 from a teacher's top logits, from hidden states and the head's weight, without keeping the logits; and log probabilities of given tokens
-with entropies and top alternatives, from the same, with a backward call of their own.
+with entropies and top alternatives, from the same, with a backward call of their own, for which the first one may keep the logits' powers.
 
 Argument checks and memory only; the arithmetic is in the HIP library (``muon_cross_entropy``, ``muon_distill``, ``muon_log_probs``).
 autograd does not see these calls: the losses' gradients are in their results, for the token_scale given.
@@ -14,6 +14,10 @@ import torch
 from . import binding
 from ._device import capturing, current_stream, on, outside_autograd, stream_handle
 from .binding import MuonError
+
+
+# What ``log_probs`` keeps unasked for at most: what 32768 tokens of a vocabulary of 131072 take in bf16, a thirty-sixth of the card's memory.
+KEEP_BYTES = 8 << 30
 
 
 class HeadResult(NamedTuple):
@@ -200,8 +204,8 @@ class LossHead:
         """Log probabilities of ``targets`` (negative: no token, 0) under the softmax of ``hidden @ weight.T / temperature``, the entropy of
         each row's whole distribution, and its ``top`` (up to 64) most likely entries with their log probabilities, the likeliest first, equal
         ones by index.  keep: whether the result holds what ``log_probs_backward`` saves one of its three products by, 2 bytes per token and vocabulary
-        entry (fp32: 4); only without alternatives, and not for few tokens where it saves nothing; None: where the LossHead is for gradients and
-        its max_workspace_bytes, if any, is not exceeded."""
+        entry (fp32: 4) beside the workspace, as long as the result lives; only without alternatives, and not for few tokens where it saves nothing;
+        None: where the LossHead is for gradients and that is no more than its max_workspace_bytes or, without such a limit, 8 GiB."""
         head = self._head(hidden, weight)
         self._here(hidden=hidden, weight=weight, targets=targets)
         outside_autograd("LossHead.log_probs", hidden.requires_grad or weight.requires_grad)
@@ -212,7 +216,7 @@ class LossHead:
             kept, kept_bytes = None, 0
             if keep or (keep is None and self.gradients and not top):
                 kept_bytes = binding.muon_log_probs_kept_bytes(head)
-                if kept_bytes and (keep or not 0 < self.max_workspace_bytes < kept_bytes):
+                if kept_bytes and (keep or kept_bytes <= (self.max_workspace_bytes or KEEP_BYTES)):
                     kept = torch.empty(kept_bytes, dtype=torch.uint8, device=self.device)
             values = torch.empty(4, tokens, dtype=torch.float32, device=self.device).unbind(0)
             out = TokenScores(None if targets is None else values[0], *values[1:],

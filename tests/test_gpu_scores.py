@@ -502,3 +502,22 @@ def test_gradients_of_logits_that_are_not_finite(losses, dtype):
                 want, _ = head.log_probs_backward(h, w, to, clean, a, b)
                 assert dh[11].isnan().all() and torch.equal(dh[rest], want[rest])
                 assert dw.isnan().all(), (value, keep, a is None, b is None, int(dw.isnan().all(1).sum()))
+
+
+def test_long_batches_keep_nothing_by_default(losses):
+    """36000 x 131072: powers would take more than is kept unasked for; the logits are made again."""
+    tokens, vocab, width, last = 36000, 131072, 64, 48
+    h, w, y, g = make(tokens, vocab, width, "bf16")
+    dl, de = torch.zeros(tokens), torch.zeros(tokens)
+    dl[-last:], de[-last:] = torch.randn(last, generator=g), torch.randn(last, generator=g) * 0.3
+    dl, de = dl.cuda(), de.cuda()
+    head = losses.LossHead(tokens, vocab, width)
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    s = head.log_probs(h, w, y)
+    assert s.kept is None and torch.cuda.max_memory_allocated() - before < 2 ** 24
+    dh, dw = head.log_probs_backward(h, w, y, s, dl, de)
+    assert (dh[:-last] == 0).all()
+    part = losses.TokenScores(*(None if t is None else t[-last:] for t in s[:6]))
+    check(part, h[-last:], w, y[-last:])
+    check_backward((dh[-last:], dw), part, h[-last:], w, y[-last:], dl[-last:], de[-last:])

@@ -183,3 +183,23 @@ def test_scores_of_another_device_are_refused(loss_head):
         with pytest.raises(binding.MuonError, match="is on meta|another call"):
             head.log_probs_backward(h, w, y, s._replace(**{name: getattr(s, name).to("meta")}), d, d)
     assert len(calls) == count
+
+
+def test_what_is_kept_by_default_is_bounded(loss_head, monkeypatch):
+    """Without a limit of the LossHead's own the kept powers of a long batch would outgrow everything else."""
+    from paper_2502_16982_amd import losses
+    head, calls = loss_head
+    assert losses.KEEP_BYTES == 8 << 30
+    h, w = torch.zeros(40000, 8, dtype=torch.bfloat16), torch.zeros(131072, 8, dtype=torch.bfloat16)
+    assert 40000 * 131072 * 2 > losses.KEEP_BYTES
+    assert head.log_probs(h, w).kept is None and calls[-1][11] == 0
+    h, w = h[:20], w[:1000]
+    need = 20 * 1024 * 2 + (20 * 8 * 4 + 255) // 256 * 256
+    monkeypatch.setattr(losses, "KEEP_BYTES", need - 1)
+    assert head.log_probs(h, w).kept is None and calls[-1][11] == 0
+    kept = head.log_probs(h, w, keep=True).kept
+    assert kept.numel() == need and calls[-1][11:13] == (kept.data_ptr(), need)
+    assert losses.LossHead(20, 1000, 8, device="cpu", max_workspace_bytes=1 << 24).log_probs(h, w).kept.numel() == need      # the limit given counts instead
+    assert losses.LossHead(20, 1000, 8, device="cpu", max_workspace_bytes=need - 1).log_probs(h, w).kept is None
+    monkeypatch.setattr(losses, "KEEP_BYTES", need)
+    assert head.log_probs(h, w).kept.numel() == need
