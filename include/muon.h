@@ -381,6 +381,7 @@ int muon_distill(const muon_head* head, const void* index, int32_t index_bytes, 
  * kept: device memory of the caller's (256-byte aligned, muon_log_probs_kept_bytes: 2 bytes per token and vocabulary entry, fp32 4) in which a forward
  * call without alternatives leaves what the backward call reads instead of making the logits once more, as often as it is called; null for none.
  * Of few tokens whose rows a longer call would copy first nothing is kept (0 bytes).
+ * A token with gradients whose logits are NaN or infinite makes them NaN.
  */
 int muon_log_probs_kept_bytes(const muon_head* head, size_t* out);
 /* Bytes of workspace (256-byte aligned) of muon_log_probs; top: 0 (no alternatives) .. min(64, vocab); max_bytes as above.
@@ -434,7 +435,7 @@ int muon_expert_combine_backward(const muon_routing* routing, const void* d_out,
 
 /*
  * A mixture's layer for few tokens, where reading the chosen experts' matrices is all the time there is: no sort, no rows in the experts'
- * order, every chosen expert's matrices read once for all of its tokens.
+ * order, every chosen expert's matrices read once for each 32 of its pairs.
  *   out[t] = sum_j weights[t, j] h(t, j) Down_e,  h(t, j) = act(x[t] Gate_e) * (x[t] Up_e),  e = expert[t, j];  without a gate act(x[t] Up_e)
  * over the pairs whose expert is in [0, experts); the others are dropped, whatever their weight; a token without any gets zero; an expert that a
  * token names twice counts twice.  weights null: all 1.

@@ -836,6 +836,9 @@ __global__ __launch_bounds__(256) void score_prepare_kernel(ScoreTarget t, float
   }
 }
 
+// dz is rounded to bf16 (fp32: to three planes of it) as the operand of two products on the matrix cores.  That and their own rounding, 1.7e-3 of the norm
+// each, are what bf16 gradients are off by, 2.4e-3.
+//
 // The logits' gradient from what the forward call kept, by spans of a token's row.  Bound by memory: 2 bytes in and 2 out, fp32 4 and 6.
 // What is kept is read with the streaming hint, which leaves the memory-side cache to the gradient that two products read next (scores and gradients of
 // 2048 x 32768 x 1024: 507 us without, 477 with; of 8192 x 100003 x 2048 the same).  6.2 TB/s at the latter.
@@ -1027,7 +1030,9 @@ hipError_t launch_score_finish(const ScoreTarget& t, float inv_tau, float unit, 
     return hipGetLastError();
   };
   if (!top) return rows.f32 ? go(score_finish_kernel<true, false, 256>, 256) : go(score_finish_kernel<false, false, 256>, 256);
-  // few tokens: threads enough to fill the chip with one block or two per compute unit
+  // Few tokens: threads enough to fill the chip with one block or two per compute unit.  Calls with 8 alternatives in graphs, us, with 256, 512 and 1024
+  // threads: 32768 x 1024 with 8 tokens 28.2, 25.4, 25.7, 192 38.7, 33.0, 31.9, 256 35.2, 32.5, 32.6, 320 46.7, 45.2, 50.9, 512 54.6, 50.3, 57.2, 1024 94.4,
+  // 94.6, 110.4; 100003 x 2048 with 64 123.2, 119.0, 118.2, 256 167.1, 160.8, 161.3, 512 226.2, 225.0, 229.5, 1024 409.5, 408.3, 419.7.
   if (tokens <= 256) return rows.f32 ? go(score_finish_kernel<true, true, 1024>, 1024) : go(score_finish_kernel<false, true, 1024>, 1024);
   if (tokens <= 512) return rows.f32 ? go(score_finish_kernel<true, true, 512>, 512) : go(score_finish_kernel<false, true, 512>, 512);
   return rows.f32 ? go(score_finish_kernel<true, true, 256>, 256) : go(score_finish_kernel<false, true, 256>, 256);

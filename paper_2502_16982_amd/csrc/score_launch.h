@@ -23,7 +23,8 @@ struct ScoreBest {
   unsigned second;
 };
 // What a forward call keeps for the backward one, [tokens, pitch]: powers 2^(15 + y - top) in f16, up to 2^15 in a block, with each block's top per
-// token; or, tops null, z in fp32.  values null: nothing.  Not together with `best`.
+// token; or, tops null, z in fp32.  values null: nothing.  Not together with `best`.  (f16: its step is an eighth of the one that dz is rounded by;
+// fp32 would double what both calls move most of.)
 struct ScoreKept {
   void* values;
   long long pitch;

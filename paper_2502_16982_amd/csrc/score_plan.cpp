@@ -73,6 +73,10 @@ bool score_plan(const HeadShape& s, bool best, bool keep, size_t bytes, ScorePla
   if (piece == 0) return false;
   lay_out(s, best, piece, p);
   const int64_t sizes[2] = {piece, s.tokens - (p->pieces - 1) * piece};
+  // The losses' choice of tiles, from times with their shorter epilogue, holds for these.  All tiles of 128 and all of 256, us, without and with 8
+  // alternatives: 2048 x 32768 x 1024 140 and 134, 177 and 170; 4096 x 32768 x 1024 273 and 261, 347 and 329; 1024 x 50257 x 768 90 and 105, 118 and 132 (128 is
+  // taken: 92, 117); 4096 x 100003 x 2048 1667 and 1408, 1770 and 1511; 512 x 100003 x 2048 249 and 230, 269 and 252 (256 with quarters: 204, 223).  With powers kept 2048 x 32768 x
+  // 512 would be faster in 128 (104.5 against 112); 161 and 155, 362 and 324, 110 and 123 at the first three.
   for (int i = 0; i < 2; ++i) p->logits[i] = head_product(s.vocab, std::max<int64_t>(1, sizes[i]), p->shape.width_k, p->shape.pairs, 0);
   return true;
 }

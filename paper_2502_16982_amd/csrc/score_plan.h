@@ -5,7 +5,8 @@
 namespace muon {
 
 constexpr int kScoreMaxTop = 64;
-// Alternatives are picked among so many more than are asked for: fp32 sums may order logits otherwise that are nearly alike.
+// Alternatives are picked among so many more than are asked for: fp32 sums may order logits otherwise that are nearly alike.  With none, 4 and 12 more: 4096 x
+// 100003 x 2048, top 8, 1495, 1507, 1530 us; 8 x 32768 x 1024, top 5, 23.3, 25.0, 25.9.
 constexpr int kScoreMargin = 4;
 // Vocabulary entries of a group, of which the largest logit is kept.
 constexpr int kScoreGroup = 32;

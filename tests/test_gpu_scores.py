@@ -521,3 +521,28 @@ def test_long_batches_keep_nothing_by_default(losses):
     part = losses.TokenScores(*(None if t is None else t[-last:] for t in s[:6]))
     check(part, h[-last:], w, y[-last:])
     check_backward((dh[-last:], dw), part, h[-last:], w, y[-last:], dl[-last:], de[-last:])
+
+
+@pytest.mark.parametrize("dtype,tokens", [("bf16", 16), ("bf16", 17), ("f32", 64), ("f32", 65)])
+def test_alternatives_that_fp32_cannot_tell_apart(losses, dtype, tokens):
+    """Twelve entries in groups of their own whose logits differ by less than fp32 sums resolve, more than are picked beside the asked for, on both sides of
+    the limits of few tokens: what comes back is within the sums' error of the largest, and in the order of sums in double."""
+    vocab, width, top = 3000, 515, 3
+    h, w, y, g = make(tokens, vocab, width, dtype, pull=0.0)
+    row, at = torch.randn(width, generator=g).to(DT[dtype]).cuda() * 0.5, torch.arange(12, device="cuda") * 224 + 5
+    h = (h.float() * 0.1 + row.float()).to(DT[dtype])
+    w[at] = row
+    h[:, 0], w[:, 0] = 2.0 ** -20, 0.0
+    w[at, 0] = torch.randperm(12, generator=g).to(DT[dtype]).cuda() + 1
+    head = losses.LossHead(tokens, vocab, width, DT[dtype], gradients=False)
+    s = head.log_probs(h, w, top=top)
+    h64, w64 = as64(h), as64(w)
+    want = so.scores(h64, w64, None, 12)
+    d, lse_err, _ = errors(h64, w64, 1.0, want["lse"], want["entropy"])
+    z, index = h64 @ w64.T, s.top_index.cpu().numpy()
+    got = np.take_along_axis(z, index, 1)
+    assert np.isin(index, at.cpu().numpy()).all() and all(len(set(i)) == top for i in index)
+    assert (np.sort(z, axis=1)[:, -12] - np.sort(z, axis=1)[:, -13] > 2 * d).all() and (np.ptp(np.sort(z, axis=1)[:, -12:], axis=1) < d).all()
+    assert (got >= want["top_log_prob"][:, top - 1:top] + want["lse"][:, None] - 2 * d[:, None]).all()
+    assert (np.diff(got, axis=1) < 0).all()
+    assert (np.abs(as64(s.top_log_prob) - (got - want["lse"][:, None])) <= lse_err[:, None] + 2.0 ** -22 * np.abs(got - want["lse"][:, None])).all()
